@@ -353,3 +353,10 @@ def gconv_bwd_filter(d: GroupDesc, x, dy, dw, workspace, stream=None):
     if rc != 0:
         raise DwconvError(rc, "gconv_bwd_filter")
     return dw
+
+
+# ---- operators over token sequences (layer norm, causal convolution, selective scan) -------------------
+
+from .sequence import (SEQ_EXPORTS, CconvDesc, LnormDesc, SscanDesc, cconv_bwd, cconv_bwd_workspace_bytes, cconv_desc, cconv_fwd,  # noqa: E402,F401
+                       cconv_step, lnorm_bwd, lnorm_bwd_workspace_bytes, lnorm_desc, lnorm_fwd, sscan_bwd, sscan_bwd_workspace_bytes,
+                       sscan_desc, sscan_fwd, sscan_fwd_workspace_bytes, sscan_kept_bytes, sscan_step)

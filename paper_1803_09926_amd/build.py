@@ -12,7 +12,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdwconv.so")
-BINDING = os.path.join(HERE, "_binding.so")
+BINDINGS = {"binding.cpp": os.path.join(HERE, "_binding.so"), "seq_binding.cpp": os.path.join(HERE, "_seq_binding.so")}
 OBJDIR = os.path.join(HERE, "_build")
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
@@ -33,30 +33,31 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _binding() -> None:
-    """The Python binding's call path, a CPython extension against torch's own headers and libraries (host code only)."""
+def _binding(source: str, to: str) -> None:
+    """A part of the Python binding's call path, a CPython extension against torch's own headers and libraries (host code only)."""
     import torch
     from torch.utils import cpp_extension
     inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(HIPCC))), "include")]
-    tmp = BINDING + ".tmp.%d" % os.getpid()
+    tmp = to + ".tmp.%d" % os.getpid()
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-isystem" + i for i in inc]
-    cmd += [os.path.join(CSRC, "binding.cpp"), "-o", tmp, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
+    cmd += [os.path.join(CSRC, source), "-o", tmp, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
             "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("g++ failed for binding.cpp:\n%s" % r.stderr)
-    os.replace(tmp, BINDING)
+        raise RuntimeError("g++ failed for %s:\n%s" % (source, r.stderr))
+    os.replace(tmp, to)
 
 
 def build(verbose: bool = True) -> str:
-    """Compile every .hip file and the binding (always, even if built ones are already there) and link."""
+    """Compile every .hip file and the binding's parts (always, even if built ones are already there) and link."""
     os.makedirs(OBJDIR, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
-        native = ex.submit(_binding)
+        native = [ex.submit(_binding, source, to) for source, to in BINDINGS.items()]
         objs = list(ex.map(_compile, srcs))
-        native.result()
+        for n in native:
+            n.result()
     tmp = LIB + ".tmp.%d" % os.getpid()
     subprocess.check_call([HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp] + objs)
     os.replace(tmp, LIB)

@@ -9,12 +9,7 @@
 // package's types, tensors and parameters in device memory of the expected type, size and contiguity, a stream whose handle is a
 // number, no function mode active): the
 // caller then checks argument by argument, raises, or takes the general way.  The library is not linked: bind() hands over its entry points.
-#include <Python.h>
-#include <ATen/ATen.h>
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
+#include "binding.hpp"
 
 #include "../../include/dwconv.h"
 
@@ -49,24 +44,7 @@ constexpr int NENTRIES = sizeof ENTRIES / sizeof ENTRIES[0];
 // set once by bind(), under the interpreter's lock
 void *entry_points[NENTRIES];
 dims_fn dims[2];                             // dwconv_out_dims, gconv_out_dims
-PyObject *desc_type[2], *tensor_type, *parameter_type;
-
-// wrappers without memory of their own, or whose memory is not theirs to hand out
-const c10::DispatchKeySet WRAPPERS({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
-                                    c10::DispatchKey::Functionalize});
-
-const at::Tensor *plain(PyObject *o)
-{
-    if ((PyObject *)Py_TYPE(o) != tensor_type && (PyObject *)Py_TYPE(o) != parameter_type) return nullptr;
-    const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.key_set().has_any(WRAPPERS) || !t.has_storage()) return nullptr;
-    return &t;
-}
-
-struct DescView {                            // a descriptor's bytes while the call lasts
-    Py_buffer view = {};
-    ~DescView() { if (view.obj) PyBuffer_Release(&view); }
-};
+PyObject *desc_type[2];
 
 template <int E>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
@@ -109,16 +87,10 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         bytes = (size_t)t->numel() * t->itemsize();
     }
     void *stream;
-    PyObject *const given = args[nargs - 1];
-    if (given == Py_None) stream = c10::hip::getCurrentHIPStream().stream();
-    else {
-        PyObject *handle = PyObject_GetAttrString(given, "cuda_stream");
-        if (!handle) return nullptr;
-        bool taken = PyLong_Check(handle);   // (the foreign call also takes None, a c_void_p and what else stands for a pointer)
-        stream = taken ? PyLong_AsVoidPtr(handle) : nullptr;
-        Py_DECREF(handle);
-        if (PyErr_Occurred()) { PyErr_Clear(); taken = false; }
-        if (!taken) Py_RETURN_NONE;
+    switch (stream_of(args[nargs - 1], &stream)) {
+    case STREAM_ERROR: return nullptr;
+    case STREAM_OTHER: Py_RETURN_NONE;
+    case STREAM_TAKEN: break;
     }
     int rc;
     void *const fn = entry_points[E];
