@@ -34,7 +34,7 @@ extern "C" {
 /* What a descriptor may ask for at most; more is DWCONV_ERR_TOO_LARGE. */
 #define SEQOPS_MAX_T 0x7fff0000      /* tokens, sequences, slots                    */
 #define SEQOPS_MAX_C (1 << 24)       /* channels of cconv and sscan                 */
-#define SEQOPS_MAX_STRIDE 0x7fffffff /* elements from one row to the next           */
+#define SEQOPS_MAX_STRIDE (1 << 25)  /* elements from one row to the next           */
 
 /* ---- layer norm --------------------------------------------------------------------------------
  *

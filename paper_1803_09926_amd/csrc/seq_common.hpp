@@ -104,6 +104,88 @@ template <> struct Some<bf16_t, 1> {
     __device__ __forceinline__ void store(bf16_t *p, int n) const { if (n >= 1) *p = w; }
 };
 
+// An element `off` bytes from a base that all lanes share: one scalar address and a 32-bit register a lane, where 64-bit addresses take two registers
+// and several additions each.
+template <typename T> __device__ __forceinline__ const T *from(const T *base, uint32_t off) { return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + off); }
+template <typename T> __device__ __forceinline__ T *from(T *base, uint32_t off) { return reinterpret_cast<T *>(reinterpret_cast<char *>(base) + off); }
+
+// V consecutive elements that are asked for early and used late.  The loads go through a view of the rows, in which a lane that is to have zeros asks for what
+// lies outside: no branch, and so nothing that waits for them before they are used.  WHOLE: V elements are all there or none of them, and aligned to their
+// bytes; otherwise the first n are there, and each is a load of its own.
+template <typename T, int V, bool WHOLE> struct Ahead {
+    static constexpr int BYTES = V * (int)sizeof(T), WORDS = WHOLE ? (BYTES + 3) / 4 : V;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const BufView &rows, uint32_t off, int n)
+    {
+        if constexpr (WHOLE) {
+            const uint32_t at = n > 0 ? off : BufView::OUTSIDE;
+            if constexpr (BYTES == 2) w[0] = rows.b16(at, 0);
+            else if constexpr (BYTES == 4) w[0] = rows.b32(at, 0);
+            else if constexpr (BYTES == 8) { const u2raw_t v = rows.b64(at, 0); w[0] = v.x; w[1] = v.y; }
+            else {
+                static_assert(BYTES % 16 == 0, "vectors of 2, 4, 8 and 16 bytes");
+#pragma unroll
+                for (int i = 0; i < BYTES / 16; ++i) {
+                    const u4raw_t v = rows.b128(n > i * (16 / (int)sizeof(T)) ? off + 16 * i : BufView::OUTSIDE, 0);
+                    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t at = n > i ? off + i * (uint32_t)sizeof(T) : BufView::OUTSIDE;
+                if constexpr (sizeof(T) == 2) w[i] = rows.b16(at, 0);
+                else w[i] = rows.b32(at, 0);
+            }
+        }
+    }
+    // one element `row` bytes (the same in every lane) and `off` bytes into the view
+    __device__ __forceinline__ void load_row(const BufView &rows, uint32_t off, uint32_t row)
+    {
+        static_assert(V == 1, "one element");
+        if constexpr (sizeof(T) == 2) w[0] = rows.b16(off, row);
+        else w[0] = rows.b32(off, row);
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (!WHOLE || V == 1) return __uint_as_float(w[i] << 16);
+        else return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+// The counterpart for stores, rounded where T is bf16: what is not there is stored outside the view, which does nothing.  No branch here either: the loads
+// behind it would have to wait for all stores, and not for those only that come before them.
+template <typename T, int V, bool WHOLE> __device__ __forceinline__ void store_late(const BufView &rows, uint32_t off, int n, const float (&r)[V])
+{
+    constexpr int BYTES = V * (int)sizeof(T);
+    if constexpr (WHOLE && BYTES >= 4) {
+        const uint32_t at = n > 0 ? off : BufView::OUTSIDE;
+        uint32_t w[BYTES / 4];
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(r[i]);
+            else w[i] = pack2_bf16(r[2 * i], r[2 * i + 1]);
+        }
+        if constexpr (BYTES == 4) rows.st32<false>(w[0], at, 0);
+        else if constexpr (BYTES == 8) { const u2raw_t v = {w[0], w[1]}; rows.st64<false>(v, at, 0); }
+        else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const u4raw_t v = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+                rows.st128<false>(v, n > i * (16 / (int)sizeof(T)) ? off + 16 * i : BufView::OUTSIDE, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t at = n > i ? off + i * (uint32_t)sizeof(T) : BufView::OUTSIDE;
+            if constexpr (sizeof(T) == 4) rows.st32<false>(__float_as_uint(r[i]), at, 0);
+            else __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(r[i]), rows.rsrc, (int)at, 0, 0);
+        }
+    }
+}
+constexpr uint32_t VIEW_BYTES = 0x7fffffffu;   // of a view whose lanes ask for nothing that is not there, or for BufView::OUTSIDE
+
 // ---- sums over lanes -------------------------------------------------------------------------------
 // Data moves inside the vector registers (lane permutations as operand modifiers, row swaps of gfx950), not through LDS.
 template <int CTRL> __device__ __forceinline__ float lane_move(float v)

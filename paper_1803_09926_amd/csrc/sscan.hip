@@ -1,5 +1,7 @@
 // Entry points of the selective state space scan: checks of arguments, how a launch is split, workspaces.
 #include "sscan.hpp"
+#include "tune.hpp"
+#include <stdlib.h>
 
 namespace dwc {
 
@@ -27,8 +29,14 @@ int validate(const sscan_desc *d)
 // 16-byte multiples, so that what follows is aligned
 size_t floats(size_t n) { return (n + 3) / 4 * 4; }
 
-constexpr int MOST_PARTS = 64;   // a block of the last part reads the states of all before it
-constexpr int PART_UNIT = 32;    // a part is a whole number of every kernel's tiles
+constexpr int MOST_PARTS = 96;   // a block of the last part reads the states of all before it
+constexpr int PART_UNIT = KEPT_EVERY;   // a part is a whole number of tiles
+
+int tuned(const char *name, int otherwise)
+{
+    const char *v = tune_env(name);
+    return v ? atoi(v) : otherwise;
+}
 
 // `want` blocks fill the card.  Where whole sequences of equal lengths give at least half of them, a part is one or more of these, and nothing has to be
 // carried from part to part; otherwise the tokens are split wherever it may be.
@@ -49,12 +57,11 @@ ScanPlan plan(const sscan_desc *d, bool packed, int want)
         return p;
     }
     int parts = cdiv(want, p.channel_blocks);
-    if (parts > MOST_PARTS) parts = MOST_PARTS;
-    if (parts > 1 && d->T > 2 * PART_UNIT) {
-        int each = cdiv(cdiv(d->T, parts), PART_UNIT) * PART_UNIT;
-        if (each < 2 * PART_UNIT) each = 2 * PART_UNIT;
-        p.part = each;
-        p.parts = cdiv(d->T, each);
+    const int most = tuned("DWCONV_TUNE_SSCAN_MOST_PARTS", MOST_PARTS);
+    if (parts > most) parts = most;
+    if (parts > 1) {
+        p.part = cdiv(cdiv(d->T > 0 ? d->T : 1, parts), PART_UNIT) * PART_UNIT;
+        p.parts = d->T > 0 ? cdiv(d->T, p.part) : 1;
         p.carry = p.parts > 1;
     }
     return p;
@@ -62,8 +69,14 @@ ScanPlan plan(const sscan_desc *d, bool packed, int want)
 
 }  // namespace
 
-ScanPlan plan_sscan_fwd(const sscan_desc *d, bool packed) { return plan(d, packed, 768); }
-ScanPlan plan_sscan_bwd(const sscan_desc *d, bool packed) { return plan(d, packed, 512); }
+ScanPlan plan_sscan_fwd(const sscan_desc *d, bool packed)
+{
+    return plan(d, packed, tuned("DWCONV_TUNE_SSCAN_FWD_BLOCKS", 1280));
+}
+ScanPlan plan_sscan_bwd(const sscan_desc *d, bool packed)
+{
+    return plan(d, packed, tuned("DWCONV_TUNE_SSCAN_BWD_BLOCKS", 1536));
+}
 
 Scan sscan_geometry(const sscan_desc *d, const ScanPlan &p, const void *starts)
 {

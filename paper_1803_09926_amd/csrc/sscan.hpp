@@ -7,6 +7,7 @@
 // a tile by lanes that take neighbouring channels of a token, in vectors; the recurrence reads it from LDS.
 #pragma once
 #include "seq_common.hpp"
+#include <initializer_list>
 
 namespace dwc {
 
@@ -27,29 +28,27 @@ __device__ __forceinline__ ScanBlock scan_block(const Scan &g)
     return {(int)(rest % (unsigned)g.groups), (int)(id % per), (int)(rest / (unsigned)g.groups)};
 }
 
-// log(1 + e) for 0 <= e <= 1 as 2 atanh(s), s = e / (2 + e) <= 1/3: the odd series in s (its first nine terms leave 3^-19 / 19 at s = 1/3) keeps its relative
-// accuracy down to e = 0, where log of the rounded 1 + e has none.
+// log(1 + e) for 0 <= e <= 1: the logarithm of the rounded sum, one instruction, and to first order what the rounding took, which is most of the result where
+// e is small.  Within 2e-7 of the result over 2^-30 <= e <= 1, measured; a series in e / (2 + e) of that accuracy takes twice the instructions.
 __device__ __forceinline__ float log1p_unit(float e)
 {
-    const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-    float p = 1.f / 17.f;
-    p = fmaf(p, q, 1.f / 15.f);
-    p = fmaf(p, q, 1.f / 13.f);
-    p = fmaf(p, q, 1.f / 11.f);
-    p = fmaf(p, q, 1.f / 9.f);
-    p = fmaf(p, q, 1.f / 7.f);
-    p = fmaf(p, q, 1.f / 5.f);
-    p = fmaf(p, q, 1.f / 3.f);
-    p = fmaf(p, q, 1.f);
-    return 2.f * s * p;
+    const float u = 1.f + e;
+    return fmaf(__builtin_amdgcn_logf(u), LN2, e - (u - 1.f));
 }
-// max(v, 0) + log(1 + exp(-|v|)); NaN stays NaN, by way of the exponential
+// max(v, 0), in one instruction, + log(1 + exp(-|v|)); NaN stays NaN, by way of the exponential
 __device__ __forceinline__ float softplus_of(float v)
 {
     const float e = exp2_fast(-LOG2E * fabsf(v));
-    return fmaxf(v, 0.f) + log1p_unit(e);
+    return __builtin_amdgcn_fmed3f(v, 0.f, __builtin_inff()) + log1p_unit(e);
 }
-__device__ __forceinline__ float step_size(const Scan &g, float raw) { return g.softplus ? softplus_of(raw) : raw; }
+// the step sizes of V elements
+template <int V> __device__ __forceinline__ void step_sizes(const Scan &g, float (&v)[V])
+{
+    if (g.softplus) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = softplus_of(v[i]);
+    }
+}
 
 // Of L neighbouring lanes, lane q gets the sum over all of them of v[q].  L - 1 moves of one register each: at each step a lane keeps one half of its values
 // and adds its partner's of the same half (the partner of a step differs in that step's bit of the lane number).
@@ -71,6 +70,16 @@ template <int L> __device__ __forceinline__ float transpose_sum(float (&v)[L], i
     return keep + lane_move<DPP_XOR1>(give);
 }
 
+// The sum over a channel's L lanes, in each of them.
+template <int L> __device__ __forceinline__ float states_sum(float v)
+{
+    v += lane_move<DPP_XOR1>(v);
+    if constexpr (L >= 4) v += lane_move<DPP_XOR2>(v);
+    if constexpr (L >= 8) v += lane_move<DPP_HALF_MIRROR>(v);
+    if constexpr (L >= 16) v += lane_move<DPP_MIRROR>(v);
+    return v;
+}
+
 // The tokens of t0 .. t0 + n - 1 (n <= 32) that are the first of their sequence, a bit each; the same in every lane.
 __device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, int n, int end)
 {
@@ -79,6 +88,37 @@ __device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, i
     return (uint32_t)__ballot(first);
 }
 __device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of(t)) == t; }
+
+// What `count` parts from `first` on (in the direction of `step`) leave at the end of a row of them: v = e[first] + decay(first) * (e[next] + ...), with the
+// decay over a part exp(A * its sum of step sizes).  Four parts are asked for at a time: eight took registers that the kernel behind it wants.
+template <int LPC>
+__device__ __forceinline__ void gather_parts(float (&v)[4], const float (&a2)[4], const float *ends, const float *sums, int C, int chan, int q, bool valid,
+                                             int first, int step, int count)
+{
+    constexpr int AHEAD = 4;
+    float decay[4] = {1.f, 1.f, 1.f, 1.f};
+    for (int k = 0; k < count; k += AHEAD) {
+        float4 e[AHEAD];
+        float sum[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const long long at = (long long)(first + step * (k + i)) * C + chan;
+            const bool there = valid && k + i < count;
+            e[i] = there ? *reinterpret_cast<const float4 *>(ends + at * (4 * LPC) + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
+            sum[i] = there ? sums[at] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (k + i >= count) break;
+            const float u[4] = {e[i].x, e[i].y, e[i].z, e[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = fmaf(decay[j], u[j], v[j]);
+                decay[j] *= exp2_fast(a2[j] * sum[i]);
+            }
+        }
+    }
+}
 
 // ---- host (sscan.hip) ----------------------------------------------------------------------------
 // The parts that the tokens are split into: few channel blocks alone do not fill the card.  `carry`: whether a pass over the parts comes first, which
@@ -98,6 +138,19 @@ struct FwdSpace { size_t ends, sums, total; };                              // s
 FwdSpace sscan_fwd_space(const sscan_desc *d, const ScanPlan &p);
 struct BwdSpace { size_t ends, sums, dA, shared, total; };                  // as above; [parts][C * N + 2 C]; [channel blocks][T][8 LPC]
 BwdSpace sscan_bwd_space(const sscan_desc *d, const ScanPlan &p);
+
+// Whether lanes that take `each` neighbouring channels of a group find these, or 16 bytes of them where they are more, all there or none of them, in rows
+// aligned to that.
+template <typename T> bool whole_vectors(int each, int per_group, std::initializer_list<const void *> rows, std::initializer_list<long long> strides)
+{
+    const int most = 16 / (int)sizeof(T), unit = each < most ? each : most;
+    if (per_group % unit) return false;
+    for (const void *p : rows)
+        if (reinterpret_cast<uintptr_t>(p) % (unit * sizeof(T))) return false;
+    for (const long long s : strides)
+        if (s % unit) return false;
+    return true;
+}
 
 // f(the number of lanes of a channel) for the states of d
 template <typename F> hipError_t with_state_lanes(int lanes, F f)

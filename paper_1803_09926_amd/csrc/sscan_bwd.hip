@@ -30,12 +30,12 @@ struct BackOut {
 };
 
 // The first pass over the parts: from the last token of a part back to its first, the gradient that leaves the part, from zero, and the sum of step sizes.
-template <typename T, int LPC>
+template <typename T, int LPC, bool WHOLE>
 __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, BackOut out)
 {
-    constexpr int CHANNELS = 256 / LPC, TOKENS = LPC == 2 ? 16 : 32, EACH = TOKENS * CHANNELS / 256, STATES = 4 * LPC, LANES = 256 / TOKENS;
-    constexpr int SHARED = (TOKENS * STATES + 255) / 256;
-    __shared__ float2 du[TOKENS][CHANNELS];                          // step size, dv
+    typedef BackTile<LPC> S;
+    constexpr int CHANNELS = S::CHANNELS, TOKENS = S::TOKENS, EACH = S::EACH, STATES = S::STATES, LANES = S::LANES, SHARED = S::SHARED;
+    __shared__ __attribute__((aligned(16))) float steps[TOKENS][CHANNELS], dvs[TOKENS][CHANNELS];
     __shared__ float4 Cs[TOKENS][LPC];
     const ScanBlock at = scan_block(g);
     const int part = at.part + 1;                                    // (nothing comes before part 0)
@@ -44,8 +44,12 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
     const bool valid = in_group < g.per_group;
     const int row = threadIdx.x / LANES, col = threadIdx.x % LANES * EACH;
     const int first_chan = at.group * g.per_group + at.block * CHANNELS + col, n = g.per_group - at.block * CHANNELS - col;
-    const int t0 = (int)((long long)part * g.part), t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
-    if (t1 <= t0) return;
+    const int t0 = (int)((long long)part * g.part);
+    int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
+    // only the sequence that the part before ends in hands anything back
+    const int s0 = g.seq.of(t0), behind = g.seq.start(s0 + 1);
+    if (t1 <= t0 || g.seq.start(s0) == t0) return;
+    if (behind > t0 && behind < t1) t1 = behind;
 
     float a2[4], gr[4] = {0.f, 0.f, 0.f, 0.f}, bias[EACH];
 #pragma unroll
@@ -53,52 +57,77 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
 #pragma unroll
     for (int i = 0; i < EACH; ++i) bias[i] = in.dt_bias && i < n ? in.dt_bias[first_chan + i] : 0.f;
 
-    Some<T, EACH> rdt, rz, rdy;
-    float rc[SHARED];
-    auto load = [&](int tile) {
-        const int t = tile + row, m = t < t1 ? n : 0;
-        rdt.load((const T *)in.dt + (long long)t * g.dts + first_chan, m);
-        rdy.load((const T *)in.dy + (long long)t * g.ys + first_chan, m);
-        if (in.z) rz.load((const T *)in.z + (long long)t * g.zs + first_chan, m);
+    // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
+    constexpr uint32_t W = sizeof(T);
+    const uint32_t odt = ((uint32_t)row * (uint32_t)g.dts + first_chan) * W, oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W;
+    const uint32_t oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
+    const int last = t0 + (t1 - t0 - 1) / TOKENS * TOKENS;             // the tile that comes first
+    Ahead<T, EACH, WHOLE> rdt, rz, rdy;
+    Ahead<T, 1, true> rc[SHARED];
+    // the rows of the tile that is loaded next
+    const T *pdt = (const T *)in.dt + (long long)last * g.dts, *pdy = (const T *)in.dy + (long long)last * g.ys;
+    const T *pz = in.z ? (const T *)in.z + (long long)last * g.zs : pdy, *pc = (const T *)in.C + (long long)last * g.cs + (long long)at.group * g.N;
+    uint32_t oc[SHARED];
+    int rows[SHARED];                                                // of C, or one that is never there
 #pragma unroll
-        for (int i = 0; i < SHARED; ++i) {
-            const int e = threadIdx.x + 256 * i, tb = tile + e / STATES, k = e % STATES;
-            rc[i] = e < TOKENS * STATES && tb < t1 && k < g.N ? ldf((const T *)in.C + (long long)tb * g.cs + (long long)at.group * g.N + k) : 0.f;
-        }
+    for (int i = 0; i < SHARED; ++i) {
+        const int e = threadIdx.x + 256 * i, r = e / STATES, k = e % STATES;
+        rows[i] = e < TOKENS * STATES && k < g.N ? r : TOKENS;
+        oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+    }
+    auto load = [&](int tile) {
+        const int left = t1 - tile, m = row < left ? n : 0;
+        rdt.load(BufView(pdt, VIEW_BYTES), odt, m);
+        rdy.load(BufView(pdy, VIEW_BYTES), oy, m);
+        rz.load(BufView(pz, VIEW_BYTES), oz, in.z ? m : 0);
+        const BufView c(pc, VIEW_BYTES);
+#pragma unroll
+        for (int i = 0; i < SHARED; ++i) rc[i].load(c, oc[i], rows[i] < (left < TOKENS ? left : TOKENS));
+        pdt -= TOKENS * g.dts;
+        pdy -= TOKENS * g.ys;
+        pz -= TOKENS * g.zs;
+        pc -= TOKENS * g.cs;
     };
+    // the sequence of the tile's first token, looked for again where a tile lies before it
+    int s = g.seq.of(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
     float total = 0.f;
-    int tile = t0 + (t1 - t0 - 1) / TOKENS * TOKENS;
-    load(tile);
-    for (; tile >= t0; tile -= TOKENS) {
+    load(last);
+    for (int tile = last; tile >= t0; tile -= TOKENS) {
+        float d[EACH], dv[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const float d = tile + row < t1 ? step_size(g, rdt.at(i) + bias[i]) : 0.f;
-            float dv = rdy.at(i);
-            if (in.z) { const float zv = rz.at(i); dv *= zv * sigmoid(zv); }
-            du[row][col + i] = make_float2(d, dv);
+            d[i] = rdt.at(i) + bias[i];
+            dv[i] = rdy.at(i);
         }
+        step_sizes(g, d);
+        if (in.z) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) { const float zv = rz.at(i); dv[i] *= zv * sigmoid(zv); }
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) { steps[row][col + i] = d[i]; dvs[row][col + i] = dv[i]; }
 #pragma unroll
         for (int i = 0; i < SHARED; ++i) {
             const int e = threadIdx.x + 256 * i;
-            if (e < TOKENS * STATES) reinterpret_cast<float *>(Cs)[e] = rc[i];
+            if (e < TOKENS * STATES) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
         }
+        if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
+        const bool any = head >= tile || behind_it < tile + TOKENS;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, TOKENS, t1) : 0u;
         if (tile > t0) load(tile - TOKENS);
         __syncthreads();
-        const int s = g.seq.of(tile);
-        const bool any = g.seq.start(s) == tile || g.seq.start(s + 1) < tile + TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, TOKENS, t1) : 0u;
         auto walk = [&](auto special) {
 #pragma unroll 4
             for (int t = TOKENS - 1; t >= 0; --t) {
                 if constexpr (decltype(special)::value) {
                     if (tile + t >= t1) continue;
                 }
-                const float2 d = du[t][mine];
+                const float d = steps[t][mine], dv = dvs[t][mine];
                 const float4 c = Cs[t][q];
                 const float cv[4] = {c.x, c.y, c.z, c.w};
-                total += d.x;
+                total += d;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) gr[i] = fmaf(d.y, cv[i], gr[i]) * exp2_fast(d.x * a2[i]);
+                for (int i = 0; i < 4; ++i) gr[i] = fmaf(dv, cv[i], gr[i]) * exp2_fast(d * a2[i]);
                 if constexpr (decltype(special)::value) {
                     if (firsts >> t & 1) {
 #pragma unroll
@@ -117,13 +146,15 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
     }
 }
 
-template <typename T, int LPC>
-__global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut out)
+template <typename T, int LPC, bool WHOLE>
+__global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut out)
 {
     typedef BackTile<LPC> S;
-    __shared__ float4 slot[S::TOKENS][S::CHANNELS];                  // step size, step size * x, dv; then sum g B, sum r A, -, sum C h
+    // step sizes, these times x, dv, and sum C h; sum g B and sum r A take the places of the first two
+    __shared__ __attribute__((aligned(16))) float steps[S::TOKENS][S::CHANNELS], gains[S::TOKENS][S::CHANNELS], dvs[S::TOKENS][S::CHANNELS],
+        ys[S::TOKENS][S::CHANNELS];
     __shared__ float4 Bs[S::TOKENS][LPC], Cs[S::TOKENS][LPC];
-    __shared__ float red[4][S::TOKENS][2 * S::STATES];               // dB and dC of each wavefront's channels
+    __shared__ float red[5][S::TOKENS][2 * S::STATES];               // dB and dC of each wavefront's channels; what lanes without a sum write
     const ScanBlock at = scan_block(g);
     const int lane = threadIdx.x & 63, q = lane % LPC, wv = threadIdx.x >> 6;
     const int mine = wv * (64 / LPC) + lane / LPC, in_group = at.block * S::CHANNELS + mine, chan = at.group * g.per_group + in_group;
@@ -146,79 +177,122 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
 
     if (out.ends && t1 < g.seq.T) {                                  // what the parts behind hand back to the sequence that goes on there
         const int end = g.seq.start(g.seq.of(t1 - 1) + 1);
-        float decay[4] = {1.f, 1.f, 1.f, 1.f};
-        for (int p = at.part + 1; p < g.parts && (long long)p * g.part < end; ++p) {
-            if (!valid) continue;
-            const float4 e = *reinterpret_cast<const float4 *>(out.ends + ((long long)p * g.C + chan) * S::STATES + 4 * q);
-            const float sum = out.sums[(long long)p * g.C + chan];
-            const float v[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                gr[i] = fmaf(decay[i], v[i], gr[i]);
-                decay[i] *= exp2_fast(a2[i] * sum);
-            }
-        }
+        // (parts whose first token that sequence still has)
+        const long long reach = ((long long)(end < g.seq.T ? end : g.seq.T) - 1) / g.part - at.part;
+        const int most = g.parts - 1 - at.part;
+        gather_parts<LPC>(gr, a2, out.ends, out.sums, g.C, chan, q, valid, at.part + 1, 1, reach < most ? (int)reach : most);
     }
 
+    // Where a lane's sum of dB or dC goes: state 4 q and the next for even and odd rows, two further for the upper eight lanes of a row.  A lane that is left
+    // without one writes where nothing reads: no branch, across which the compiler would move work and hold more in registers.
+    float *const sum_to = LPC == 16 || (lane & 7) < LPC
+                              ? &red[wv][0][(lane >> 5) * S::STATES + 4 * q + (lane >> 4 & 1) + (LPC < 16 && lane & 8 ? 2 : 0)]
+                              : &red[4][0][lane % (2 * S::STATES)];
+
     auto init_of = [&](int s, float (&h)[4]) {
-        const float *p = in.init + ((long long)s * g.C + chan) * g.N + 4 * q;
+        int c = chan;                                                // rare: its address is not to be held in registers meanwhile
+        asm volatile("" : "+v"(c));
+        const float *p = in.init + ((long long)s * g.C + c) * g.N + 4 * q;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = in.init && valid && 4 * q + i < g.N ? p[i] : 0.f;
     };
 
-    Some<T, S::EACH> rx, rdt, rz, rdy;
-    float rb[S::SHARED], rc[S::SHARED];
-    float4 rh = make_float4(0.f, 0.f, 0.f, 0.f);
+    // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
+    constexpr uint32_t W = sizeof(T);
+    const uint32_t ox = ((uint32_t)row * (uint32_t)g.xs + first_chan) * W, odt = ((uint32_t)row * (uint32_t)g.dts + first_chan) * W;
+    const uint32_t oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W, oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
+    const uint32_t oh = (uint32_t)(mine * S::STATES + 4 * q) * 4;    // from the block's first channel
+    const int last = t0 + (t1 - t0 - 1) / S::TOKENS * S::TOKENS;       // the tile that comes first
+    Ahead<T, S::EACH, WHOLE> rx, rdt, rz, rdy;
+    Ahead<T, 1, true> rb[S::SHARED], rc[S::SHARED];
+    Ahead<float, 4, true> rh;
+    // the rows of the tile that is loaded next, and of the one that is written next
+    const T *px = (const T *)in.x + (long long)last * g.xs, *pdt = (const T *)in.dt + (long long)last * g.dts, *pdy = (const T *)in.dy + (long long)last * g.ys;
+    const T *pz = in.z ? (const T *)in.z + (long long)last * g.zs : px;
+    const T *pb = (const T *)in.B + (long long)last * g.bs + (long long)at.group * g.N, *pc = (const T *)in.C + (long long)last * g.cs + (long long)at.group * g.N;
+    const float *ph = in.kept + ((long long)(last / KEPT_EVERY) * g.C + chan - mine) * S::STATES;
+    T *pdx = (T *)out.dx + (long long)last * g.xs, *pddt = (T *)out.ddt + (long long)last * g.dts, *pdz = in.z ? (T *)out.dz + (long long)last * g.zs : pdx;
+    float *pshared = out.shared + ((long long)(at.group * g.blocks_of_group + at.block) * g.seq.T + last) * (2 * S::STATES);
+    uint32_t ob[S::SHARED], oc[S::SHARED];
+    int rows[S::SHARED];                                             // of B and C, or one that is never there
+#pragma unroll
+    for (int i = 0; i < S::SHARED; ++i) {
+        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = e % S::STATES;
+        rows[i] = e < S::TOKENS * S::STATES && k < g.N ? r : S::TOKENS;
+        ob[i] = ((uint32_t)r * (uint32_t)g.bs + k) * W;
+        oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+    }
     auto load = [&](int tile) {
-        const int t = tile + row, m = t < t1 ? n : 0;
-        rx.load((const T *)in.x + (long long)t * g.xs + first_chan, m);
-        rdt.load((const T *)in.dt + (long long)t * g.dts + first_chan, m);
-        rdy.load((const T *)in.dy + (long long)t * g.ys + first_chan, m);
-        if (in.z) rz.load((const T *)in.z + (long long)t * g.zs + first_chan, m);
+        const int left = t1 - tile, m = row < left ? n : 0;
+        rx.load(BufView(px, VIEW_BYTES), ox, m);
+        rdt.load(BufView(pdt, VIEW_BYTES), odt, m);
+        rdy.load(BufView(pdy, VIEW_BYTES), oy, m);
+        rz.load(BufView(pz, VIEW_BYTES), oz, in.z ? m : 0);
+        const BufView b(pb, VIEW_BYTES), c(pc, VIEW_BYTES);
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
-            const int e = threadIdx.x + 256 * i, tb = tile + e / S::STATES, k = e % S::STATES;
-            const bool inside = e < S::TOKENS * S::STATES && tb < t1 && k < g.N;
-            rb[i] = inside ? ldf((const T *)in.B + (long long)tb * g.bs + (long long)at.group * g.N + k) : 0.f;
-            rc[i] = inside ? ldf((const T *)in.C + (long long)tb * g.cs + (long long)at.group * g.N + k) : 0.f;
+            const int there = rows[i] < (left < S::TOKENS ? left : S::TOKENS);
+            rb[i].load(b, ob[i], there);
+            rc[i].load(c, oc[i], there);
         }
-        if (valid) rh = *reinterpret_cast<const float4 *>(in.kept + ((long long)(tile / KEPT_EVERY) * g.C + chan) * S::STATES + 4 * q);
+        rh.load(BufView(ph, VIEW_BYTES), oh, valid);
+        px -= S::TOKENS * g.xs;
+        pdt -= S::TOKENS * g.dts;
+        pdy -= S::TOKENS * g.ys;
+        pz -= S::TOKENS * g.zs;
+        pb -= S::TOKENS * g.bs;
+        pc -= S::TOKENS * g.cs;
+        ph -= (long long)g.C * S::STATES;
     };
+    // the sequence of the tile's first token, looked for again where a tile lies before it
+    int s = g.seq.of(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
 
-    int tile = t0 + (t1 - t0 - 1) / S::TOKENS * S::TOKENS;
-    load(tile);
-    for (; tile >= t0; tile -= S::TOKENS) {
-        const Some<T, S::EACH> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
-        const float hin[4] = {rh.x, rh.y, rh.z, rh.w};
+    load(last);
+    for (int tile = last; tile >= t0; tile -= S::TOKENS) {
+        const Ahead<T, S::EACH, WHOLE> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
+        const float hin[4] = {rh.at(0), rh.at(1), rh.at(2), rh.at(3)};
         const int m = tile + row < t1 ? n : 0;
         float delta[S::EACH];
+        {
+            float dv[S::EACH];
 #pragma unroll
-        for (int i = 0; i < S::EACH; ++i) {
-            delta[i] = m > 0 ? step_size(g, kdt.at(i) + bias[i]) : 0.f;
-            float dv = kdy.at(i);
-            if (in.z) { const float zv = kz.at(i); dv *= zv * sigmoid(zv); }
-            slot[row][col + i] = make_float4(delta[i], delta[i] * kx.at(i), dv, 0.f);
+            for (int i = 0; i < S::EACH; ++i) {
+                delta[i] = kdt.at(i) + bias[i];
+                dv[i] = kdy.at(i);
+            }
+            step_sizes(g, delta);
+            if (in.z) {
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) { const float zv = kz.at(i); dv[i] *= zv * sigmoid(zv); }
+            }
+#pragma unroll
+            for (int i = 0; i < S::EACH; ++i) {
+                steps[row][col + i] = delta[i];
+                gains[row][col + i] = delta[i] * kx.at(i);
+                dvs[row][col + i] = dv[i];
+            }
         }
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
             const int e = threadIdx.x + 256 * i;
             if (e < S::TOKENS * S::STATES) {
-                reinterpret_cast<float *>(Bs)[e] = rb[i];
-                reinterpret_cast<float *>(Cs)[e] = rc[i];
+                reinterpret_cast<float *>(Bs)[e] = rb[i].at(0);
+                reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
             }
         }
+        if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
+        const bool any = head >= tile || behind_it < tile + S::TOKENS;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
         if (tile > t0) load(tile - S::TOKENS);
         __syncthreads();
-        const int s = g.seq.of(tile);
-        const bool any = g.seq.start(s) == tile || g.seq.start(s + 1) < tile + S::TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
 
         auto walk = [&](auto special) {
             constexpr bool SPECIAL = decltype(special)::value;
-            float decay[S::TOKENS][4], h[S::TOKENS][4], sums[LPC], more[LPC];
+            float h[S::TOKENS][4], sums[LPC], more[LPC];
 #pragma unroll
             for (int t = 0; t < S::TOKENS; ++t) {
-                const float4 v = slot[t][mine], b = Bs[t][q], c = Cs[t][q];
+                const float d = steps[t][mine], gain = gains[t][mine];
+                const float4 b = Bs[t][q], c = Cs[t][q];
                 const float bv[4] = {b.x, b.y, b.z, b.w}, cv[4] = {c.x, c.y, c.z, c.w};
                 float before[4], sum = 0.f;
 #pragma unroll
@@ -228,19 +302,22 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    decay[t][i] = exp2_fast(v.x * a2[i]);
-                    h[t][i] = fmaf(decay[t][i], before[i], v.y * bv[i]);
+                    h[t][i] = fmaf(exp2_fast(d * a2[i]), before[i], gain * bv[i]);
                     sum = fmaf(cv[i], h[t][i], sum);
                 }
                 sums[t % LPC] = sum;
-                if (t % LPC == LPC - 1 && in.z) slot[t - (LPC - 1) + q][mine].w = transpose_sum<LPC>(sums, q);
+                if (t % LPC == LPC - 1) ys[t - (LPC - 1) + q][mine] = transpose_sum<LPC>(sums, q);
             }
+            // Read LDS again on the way back: without these the compiler keeps what it read on the way there, 11 values a token, in registers, and spills.
+            int mine2 = mine, q2 = q;
+            asm volatile("" : "+v"(mine2), "+v"(q2));
 #pragma unroll
             for (int t = S::TOKENS - 1; t >= 0; --t) {
                 if (SPECIAL && tile + t >= t1) {                     // behind the last token
                     sums[t % LPC] = more[t % LPC] = 0.f;
                 } else {
-                    const float4 v = slot[t][mine], b = Bs[t][q], c = Cs[t][q];
+                    const float d = steps[t][mine2], gain = gains[t][mine2], dv = dvs[t][mine2];
+                    const float4 b = Bs[t][q2], c = Cs[t][q2];
                     const float bv[4] = {b.x, b.y, b.z, b.w}, cv[4] = {c.x, c.y, c.z, c.w};
                     float before[4], db[4], dc[4], sg = 0.f, sa = 0.f;
 #pragma unroll
@@ -250,14 +327,14 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        gr[i] = fmaf(v.z, cv[i], gr[i]);
-                        db[i] = gr[i] * v.y;
-                        dc[i] = v.z * h[t][i];
+                        gr[i] = fmaf(dv, cv[i], gr[i]);
+                        db[i] = gr[i] * gain;
+                        dc[i] = dv * h[t][i];
                         sg = fmaf(gr[i], bv[i], sg);
-                        const float r = gr[i] * (decay[t][i] * before[i]);
+                        gr[i] *= exp2_fast(d * a2[i]);
+                        const float r = gr[i] * before[i];
                         sa = fmaf(r, a2[i], sa);
-                        dA[i] = fmaf(r, v.x, dA[i]);
-                        gr[i] *= decay[t][i];
+                        dA[i] = fmaf(r, d, dA[i]);
                     }
                     if constexpr (SPECIAL) {
                         if (firsts >> t & 1) {
@@ -270,7 +347,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
                     // over the wavefront's channels: after the halves (dB below, dC above) and the rows (state 2j below 2j + 1) a lane has two states' sums
                     const float w0 = rows_join(halves_join(db[0], dc[0]), halves_join(db[1], dc[1]));
                     const float w1 = rows_join(halves_join(db[2], dc[2]), halves_join(db[3], dc[3]));
-                    float *const to = &red[wv][t][(lane >> 5) * S::STATES + 4 * q + (lane >> 4 & 1)];
+                    float *const to = sum_to + t * 2 * S::STATES;
                     if constexpr (LPC == 16) {
                         to[0] = w0;
                         to[2] = w1;
@@ -279,13 +356,13 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
                         float w = lane & 8 ? u1 : u0;
                         if constexpr (LPC <= 4) w += lane_move<0x104>(w);        // four lanes further up; used in the lower four of eight
                         if constexpr (LPC == 2) w += lane_move<DPP_XOR2>(w);
-                        if ((lane & 7) < LPC) to[lane & 8 ? 2 : 0] = w;
+                        *to = w;
                     }
                 }
                 if (t % LPC == 0) {
                     const float a = transpose_sum<LPC>(sums, q), b2 = transpose_sum<LPC>(more, q);
-                    slot[t + q][mine].x = a;
-                    slot[t + q][mine].y = b2 * LN2;
+                    steps[t + q][mine] = a;
+                    gains[t + q][mine] = b2 * LN2;
                 }
             }
         };
@@ -294,39 +371,41 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
         __syncthreads();
 
         {
-            float dx[S::EACH], dd[S::EACH], dz[S::EACH];
+            float dx[S::EACH], dd[S::EACH], dz[S::EACH] = {};
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
-                const float4 v = slot[row][col + i];
+                const float gb = steps[row][col + i], ra = gains[row][col + i];
                 const float xv = kx.at(i), dout = kdy.at(i);
                 float dv = dout;
                 if (in.z) {
                     const float zv = kz.at(i), sz = sigmoid(zv);
                     dv *= zv * sz;
-                    dz[i] = dout * fmaf(skip[i], xv, v.w) * (sz + zv * sz * (1.f - sz));
+                    dz[i] = dout * fmaf(skip[i], xv, ys[row][col + i]) * (sz + zv * sz * (1.f - sz));
                 }
-                dx[i] = fmaf(skip[i], dv, delta[i] * v.x);
-                dd[i] = fmaf(xv, v.x, v.y);
+                dx[i] = fmaf(skip[i], dv, delta[i] * gb);
+                dd[i] = fmaf(xv, gb, ra);
                 if (g.softplus) dd[i] *= sigmoid(kdt.at(i) + bias[i]);
                 if (m > 0) {
                     dskip[i] = fmaf(dv, xv, dskip[i]);
                     dbias[i] += dd[i];
                 }
             }
-            Some<T, S::EACH> o;
-            o.set(dx);
-            o.store((T *)out.dx + (long long)(tile + row) * g.xs + first_chan, m);
-            o.set(dd);
-            o.store((T *)out.ddt + (long long)(tile + row) * g.dts + first_chan, m);
-            if (in.z) {
-                o.set(dz);
-                o.store((T *)out.dz + (long long)(tile + row) * g.zs + first_chan, m);
-            }
-            float *const to = out.shared + ((long long)(at.group * g.blocks_of_group + at.block) * g.seq.T + tile) * (2 * S::STATES);
-            for (int e = threadIdx.x; e < S::TOKENS * 2 * S::STATES; e += 256) {
+            store_late<T, S::EACH, WHOLE>(BufView(pdx, VIEW_BYTES), ox, m, dx);
+            store_late<T, S::EACH, WHOLE>(BufView(pddt, VIEW_BYTES), odt, m, dd);
+            store_late<T, S::EACH, WHOLE>(BufView(pdz, VIEW_BYTES), oz, in.z ? m : 0, dz);
+            const BufView to(pshared, VIEW_BYTES);
+            const int there = (t1 - tile) * 2 * S::STATES;
+#pragma unroll
+            for (int e = threadIdx.x, i = 0; i < (S::TOKENS * 2 * S::STATES + 255) / 256; ++i, e += 256) {
                 const int t = e / (2 * S::STATES), k = e % (2 * S::STATES);
-                if (tile + t < t1) to[e] = (red[0][t][k] + red[1][t][k]) + (red[2][t][k] + red[3][t][k]);
+                if constexpr (S::TOKENS * 2 * S::STATES % 256 != 0) { if (e >= S::TOKENS * 2 * S::STATES) break; }
+                const float sum[1] = {(red[0][t][k] + red[1][t][k]) + (red[2][t][k] + red[3][t][k])};
+                store_late<float, 1, true>(to, (uint32_t)e * 4, e < there, sum);
             }
+            pdx -= S::TOKENS * g.xs;
+            pddt -= S::TOKENS * g.dts;
+            pdz -= S::TOKENS * g.zs;
+            pshared -= S::TOKENS * 2 * S::STATES;
         }
     }
 
@@ -337,16 +416,15 @@ __global__ __launch_bounds__(256) void k_sscan_bwd(Scan g, BackIn in, BackOut ou
         for (int i = 0; i < 4; ++i)
             if (4 * q + i < g.N) to[(long long)chan * g.N + 4 * q + i] = dA[i];
     }
-    float2 *const sums = reinterpret_cast<float2 *>(&slot[0][0]);    // (a lane's own places: the ones that it has read)
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < S::EACH; ++i) sums[row * S::CHANNELS + col + i] = make_float2(dskip[i], dbias[i]);
+    for (int i = 0; i < S::EACH; ++i) { steps[row][col + i] = dskip[i]; gains[row][col + i] = dbias[i]; }
     __syncthreads();
     for (int c = threadIdx.x; c < S::CHANNELS; c += 256) {
         const int k = at.block * S::CHANNELS + c;
         if (k >= g.per_group) continue;
         float a = 0.f, b = 0.f;
-        for (int r = 0; r < S::TOKENS; ++r) { a += sums[r * S::CHANNELS + c].x; b += sums[r * S::CHANNELS + c].y; }
+        for (int r = 0; r < S::TOKENS; ++r) { a += steps[r][c]; b += gains[r][c]; }
         to[(long long)g.C * g.N + at.group * g.per_group + k] = a;
         to[(long long)g.C * g.N + g.C + at.group * g.per_group + k] = b;
     }
@@ -385,8 +463,14 @@ template <typename T> hipError_t launch(const sscan_desc *d, const sscan_tensors
         if (!launchable(blocks, 256) || !launchable(last, 256)) return hipErrorInvalidValue;
         const hipError_t e = with_state_lanes(p.lanes, [&](auto lanes) {
             constexpr int LPC = decltype(lanes)::value;
-            if (p.carry) hipLaunchKernelGGL((k_sscan_bwd_carry<T, LPC>), dim3((unsigned)(blocks - p.channel_blocks)), dim3(256), 0, stream, g, in, out);
-            hipLaunchKernelGGL((k_sscan_bwd<T, LPC>), dim3((unsigned)blocks), dim3(256), 0, stream, g, in, out);
+            auto both = [&](auto whole) {
+                constexpr bool WHOLE = decltype(whole)::value;
+                if (p.carry) hipLaunchKernelGGL((k_sscan_bwd_carry<T, LPC, WHOLE>), dim3((unsigned)(blocks - p.channel_blocks)), dim3(256), 0, stream, g, in, out);
+                hipLaunchKernelGGL((k_sscan_bwd<T, LPC, WHOLE>), dim3((unsigned)blocks), dim3(256), 0, stream, g, in, out);
+            };
+            const bool whole = whole_vectors<T>(BackTile<LPC>::EACH, g.per_group, {t->x, t->dt, t->z, t->dy, t->dx, t->ddt, t->dz}, {g.xs, g.dts, g.zs, g.ys});
+            if (whole) both(std::true_type());
+            else both(std::false_type());
             hipLaunchKernelGGL(k_sscan_bwd_shared<T>, dim3((unsigned)last), dim3(256), 0, stream, g, 4 * LPC, workspace + space.shared, (T *)t->dB, (T *)t->dC);
         });
         if (e != hipSuccess) return e;

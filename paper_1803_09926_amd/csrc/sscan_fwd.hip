@@ -12,23 +12,31 @@ namespace dwc {
 
 namespace {
 
+// A tile of the tokens: those between two states that are kept.
 template <int LPC> struct Tile {
-    static constexpr int CHANNELS = 256 / LPC, TOKENS = LPC == 2 ? 16 : 32, EACH = TOKENS * CHANNELS / 256, STATES = 4 * LPC;
+    static constexpr int CHANNELS = 256 / LPC, TOKENS = KEPT_EVERY, EACH = TOKENS * CHANNELS / 256, STATES = 4 * LPC;
     static constexpr int LANES = 256 / TOKENS;                        // that share a token's channels, EACH of them a lane
     static constexpr int SHARED = (TOKENS * STATES + 255) / 256;      // values of B, and of C, that a lane brings
+    static constexpr int PLANE = CHANNELS + 64 / LPC;
+    static constexpr int WAVES = LPC == 2 ? 3 : 5;                    // a SIMD: what the registers and 31 KB of LDS allow; 6 and 8 spill, and take 3 and 20 % longer
 };
 
+// WHOLE: a lane's channels are all there or none of them, in rows that are aligned to them.
 // ENDS: the first pass, which leaves the states at the parts' ends; otherwise the pass that writes y.
-template <typename T, int LPC, bool ENDS>
-__global__ __launch_bounds__(256) void k_sscan_fwd(Scan g, const T *__restrict__ x, const T *__restrict__ dt, const float *__restrict__ A,
+template <typename T, int LPC, bool ENDS, bool WHOLE>
+__global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, const T *__restrict__ x, const T *__restrict__ dt, const float *__restrict__ A,
                                                    const T *__restrict__ B, const T *__restrict__ Cm, const float *__restrict__ D,
                                                    const T *__restrict__ z, const float *__restrict__ dt_bias, const float *__restrict__ init,
                                                    T *__restrict__ y, float *__restrict__ final, float *__restrict__ kept, float *__restrict__ ends,
                                                    float *__restrict__ sums)
 {
     typedef Tile<LPC> S;
-    __shared__ float2 du[S::TOKENS][S::CHANNELS];                     // step size, step size * x; y takes the first's place
+    // step sizes, and these times x.  Lanes write EACH neighbours, 16 bytes for 16 states: no two on one bank
+    __shared__ __attribute__((aligned(16))) float steps[S::TOKENS][S::CHANNELS], gains[S::TOKENS][S::CHANNELS];
     __shared__ float4 Bs[S::TOKENS][LPC], Cs[ENDS ? 1 : S::TOKENS][LPC];
+    // a token's and channel's y, a share from each of its lanes: added up by the lane that rounds and stores, in 3 additions for 16 states, where moves between
+    // the lanes took 9 instructions for 4 tokens.  A plane of channels for each lane, 64 / LPC further on than the banks' turn
+    __shared__ __attribute__((aligned(16))) float shares[ENDS ? 1 : S::TOKENS][LPC][ENDS ? 4 : S::PLANE];
     const ScanBlock at = scan_block(g);
     const int lane = threadIdx.x & 63, q = lane % LPC, wv = threadIdx.x >> 6;
     // the lane's channel in the recurrence
@@ -37,7 +45,13 @@ __global__ __launch_bounds__(256) void k_sscan_fwd(Scan g, const T *__restrict__
     // the lane's token and channels in what is elementwise
     const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * S::EACH;
     const int first_chan = at.group * g.per_group + at.block * S::CHANNELS + col, n = g.per_group - at.block * S::CHANNELS - col;
-    const int t0 = (int)((long long)at.part * g.part), t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
+    int t0 = (int)((long long)at.part * g.part);
+    const int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
+    if (ENDS) {                                                       // only what the next part goes on from is asked for
+        if (first_token(g.seq, t1)) return;
+        const int f = g.seq.start(g.seq.of(t1 - 1));
+        if (f > t0 && f < t1) t0 += (f - t0) / S::TOKENS * S::TOKENS;
+    }
 
     float a2[4], h[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -49,17 +63,27 @@ __global__ __launch_bounds__(256) void k_sscan_fwd(Scan g, const T *__restrict__
         skip[i] = !ENDS && D && i < n ? D[first_chan + i] : 0.f;
     }
 
-    auto put_state = [&](float *to, int s) {                          // a sequence's row of [sequences,C,N]
+    // a sequence's row of [sequences,C,N]; rare, so that its address is not to be held in registers meanwhile
+    auto put_state = [&](float *to, int s) {
         if (!valid) return;
-        float *p = to + ((long long)s * g.C + chan) * g.N + 4 * q;
+        int c = chan;
+        asm volatile("" : "+v"(c));
+        float *p = to + ((long long)s * g.C + c) * g.N + 4 * q;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (4 * q + i < g.N) p[i] = h[i];
     };
     auto get_state = [&](int s) {
-        const float *p = init + ((long long)s * g.C + chan) * g.N + 4 * q;
+        int c = chan;
+        asm volatile("" : "+v"(c));
+        const float *p = init + ((long long)s * g.C + c) * g.N + 4 * q;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = init && valid && 4 * q + i < g.N ? p[i] : 0.f;
+    };
+
+    auto keep_state = [&](int tile) {
+        if (valid)
+            *reinterpret_cast<float4 *>(kept + ((long long)(tile / KEPT_EVERY) * g.C + chan) * S::STATES + 4 * q) = make_float4(h[0], h[1], h[2], h[3]);
     };
 
     // an empty sequence hands on what it was given; 64 sequences are looked at together
@@ -81,112 +105,105 @@ __global__ __launch_bounds__(256) void k_sscan_fwd(Scan g, const T *__restrict__
         const int f = g.seq.start(g.seq.of(t0));
         if (f < t0) {
             const int least = (f < 0 ? 0 : f) / g.part;
-            float decay[4] = {1.f, 1.f, 1.f, 1.f};
-            for (int p = at.part - 1; p >= least; --p) {
-                if (!valid) continue;
-                const float4 e = *reinterpret_cast<const float4 *>(ends + ((long long)p * g.C + chan) * S::STATES + 4 * q);
-                const float sum = sums[(long long)p * g.C + chan];
-                const float v[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    h[i] = fmaf(decay[i], v[i], h[i]);
-                    decay[i] *= exp2_fast(a2[i] * sum);
-                }
-            }
+            gather_parts<LPC>(h, a2, ends, sums, g.C, chan, q, valid, at.part - 1, -1, at.part - least);
         }
     }
 
-    Some<T, S::EACH> rx, rdt, rz;
-    float rb[S::SHARED], rc[S::SHARED];
+    // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
+    constexpr uint32_t W = sizeof(T);
+    const uint32_t ox = ((uint32_t)row * (uint32_t)g.xs + first_chan) * W, odt = ((uint32_t)row * (uint32_t)g.dts + first_chan) * W;
+    const uint32_t oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W, oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
+    Ahead<T, S::EACH, WHOLE> rx, rdt, rz;
+    Ahead<T, 1, true> rb[S::SHARED], rc[S::SHARED];
+    // the rows of the tile that is loaded next, moved on by additions: a product of 64 bits for each of them and tile took 60 scalar instructions
+    const T *px = x + (long long)t0 * g.xs, *pdt = dt + (long long)t0 * g.dts, *pz = !ENDS && z ? z + (long long)t0 * g.zs : x;
+    const T *pb = B + (long long)t0 * g.bs + (long long)at.group * g.N, *pc = ENDS ? pb : Cm + (long long)t0 * g.cs + (long long)at.group * g.N;
+    T *py = ENDS ? nullptr : y + (long long)t0 * g.ys;
+    uint32_t ob[S::SHARED], oc[S::SHARED];
+    int rows[S::SHARED];                                              // of B and C, or one that is never there
+#pragma unroll
+    for (int i = 0; i < S::SHARED; ++i) {
+        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = e % S::STATES;
+        rows[i] = e < S::TOKENS * S::STATES && k < g.N ? r : S::TOKENS;
+        ob[i] = ((uint32_t)r * (uint32_t)g.bs + k) * W;
+        oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+    }
     auto load = [&](int tile) {
-        const int t = tile + row, m = t < t1 ? n : 0;
-        rx.load(x + (long long)t * g.xs + first_chan, m);
-        rdt.load(dt + (long long)t * g.dts + first_chan, m);
-        if (!ENDS && z) rz.load(z + (long long)t * g.zs + first_chan, m);
+        const int left = t1 - tile, m = row < left ? n : 0;
+        rx.load(BufView(px, VIEW_BYTES), ox, m);
+        rdt.load(BufView(pdt, VIEW_BYTES), odt, m);
+        if (!ENDS) rz.load(BufView(pz, VIEW_BYTES), oz, z ? m : 0);
+        const BufView b(pb, VIEW_BYTES), c(pc, VIEW_BYTES);
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
-            const int e = threadIdx.x + 256 * i, tb = tile + e / S::STATES, k = e % S::STATES;
-            const bool in = e < S::TOKENS * S::STATES && tb < t1 && k < g.N;
-            rb[i] = in ? ldf(B + (long long)tb * g.bs + (long long)at.group * g.N + k) : 0.f;
-            if (!ENDS) rc[i] = in ? ldf(Cm + (long long)tb * g.cs + (long long)at.group * g.N + k) : 0.f;
+            const int in = rows[i] < (left < S::TOKENS ? left : S::TOKENS);
+            rb[i].load(b, ob[i], in);
+            if (!ENDS) rc[i].load(c, oc[i], in);
         }
+        px += S::TOKENS * g.xs;
+        pdt += S::TOKENS * g.dts;
+        pz += S::TOKENS * g.zs;
+        pb += S::TOKENS * g.bs;
+        pc += S::TOKENS * g.cs;
     };
     load(t0);
 
-    int s = g.seq.of(t0), next = g.seq.start(s + 1);
+    int s = g.seq.of(t0), head = g.seq.start(s), next = g.seq.start(s + 1);    // the sequence of the tile's first token
     float total = 0.f;
     for (int tile = t0; tile < t1; tile += S::TOKENS) {
-        const Some<T, S::EACH> kx = rx, kz = rz;
+        const Ahead<T, S::EACH, WHOLE> kx = rx, kz = rz;
         {
-            float2 o[S::EACH];
+            float d[S::EACH];
 #pragma unroll
-            for (int i = 0; i < S::EACH; ++i) {
-                // beyond the last token the step size is zero: the state stays
-                const float d = tile + row < t1 ? step_size(g, rdt.at(i) + bias[i]) : 0.f;
-                o[i] = make_float2(d, d * rx.at(i));
-            }
+            for (int i = 0; i < S::EACH; ++i) d[i] = rdt.at(i) + bias[i];
+            step_sizes(g, d);
 #pragma unroll
-            for (int i = 0; i < S::EACH; ++i) du[row][col + i] = o[i];
+            for (int i = 0; i < S::EACH; ++i) { steps[row][col + i] = d[i]; gains[row][col + i] = d[i] * rx.at(i); }
 #pragma unroll
             for (int i = 0; i < S::SHARED; ++i) {
                 const int e = threadIdx.x + 256 * i;
                 if (e < S::TOKENS * S::STATES) {
-                    reinterpret_cast<float *>(Bs)[e] = rb[i];
-                    if (!ENDS) reinterpret_cast<float *>(Cs)[e] = rc[i];
+                    reinterpret_cast<float *>(Bs)[e] = rb[i].at(0);
+                    if (!ENDS) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
                 }
             }
         }
+        if (tile >= next) { s = g.seq.of(tile); head = g.seq.start(s); next = g.seq.start(s + 1); }
+        const bool any = head == tile || next < tile + S::TOKENS;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
+        if (!ENDS && kept && !(firsts & 1)) keep_state(tile);
         if (tile + S::TOKENS < t1) load(tile + S::TOKENS);
         __syncthreads();
 
-        if (tile >= next) { s = g.seq.of(tile); next = g.seq.start(s + 1); }
-        const bool any = g.seq.start(s) == tile || next < tile + S::TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
-
-        auto walk = [&](auto special) {           // special: a sequence starts here, or the tokens end
-            constexpr int GROUP = LPC < 4 ? 4 : LPC;
-            for (int t = 0; t < S::TOKENS; t += GROUP) {
-                float part[GROUP];
+        auto token = [&](int t) {                                     // the state at token t; its share of y
+            const float d = steps[t][mine], gain = gains[t][mine];
+            const float4 b = Bs[t][q];
+            const float bv[4] = {b.x, b.y, b.z, b.w};
+            if (ENDS) total += d;
 #pragma unroll
-                for (int u = 0; u < GROUP; ++u) {
-                    const int tt = t + u;
-                    part[u] = 0.f;
-                    if constexpr (decltype(special)::value) {
-                        if (tile + tt >= t1) continue;
-                        if (firsts >> tt & 1) {
-                            if (!ENDS && final && tile + tt > t0) put_state(final, g.seq.of(tile + tt - 1));
-                            get_state(g.seq.of(tile + tt));
-                        }
-                    }
-                    if (!ENDS && kept && (tt % KEPT_EVERY) == 0 && valid) {
-                        const float4 v = make_float4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<float4 *>(kept + ((long long)((tile + tt) / KEPT_EVERY) * g.C + chan) * S::STATES + 4 * q) = v;
-                    }
-                    const float2 d = du[tt][mine];
-                    const float4 b = Bs[tt][q];
-                    const float bv[4] = {b.x, b.y, b.z, b.w};
-                    if (ENDS) total += d.x;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) h[i] = fmaf(exp2_fast(d.x * a2[i]), h[i], d.y * bv[i]);
-                    if (!ENDS) {
-                        const float4 c = Cs[tt][q];
-                        part[u] = fmaf(c.x, h[0], fmaf(c.y, h[1], fmaf(c.z, h[2], c.w * h[3])));
-                    }
-                }
-                if (!ENDS) {
-#pragma unroll
-                    for (int u = 0; u < GROUP; u += LPC) {
-                        float v[LPC];
-#pragma unroll
-                        for (int j = 0; j < LPC; ++j) v[j] = part[u + j];
-                        // (only this wavefront reads the place, and it has)
-                        du[t + u + q][mine].x = transpose_sum<LPC>(v, q);
-                    }
-                }
-            }
+            for (int i = 0; i < 4; ++i) h[i] = fmaf(exp2_fast(d * a2[i]), h[i], gain * bv[i]);
+            if (ENDS) return 0.f;
+            const float4 c = Cs[t][q];
+            return fmaf(c.x, h[0], fmaf(c.y, h[1], fmaf(c.z, h[2], c.w * h[3])));
         };
-        if (firsts || tile + S::TOKENS > t1) walk(std::true_type());
-        else walk(std::false_type());
+        if (firsts || tile + S::TOKENS > t1) {                        // sequences start here, or the tokens end
+#pragma unroll 1
+            for (int t = 0; t < S::TOKENS && tile + t < t1; ++t) {
+                if (firsts >> t & 1) {
+                    if (!ENDS && final && tile + t > t0) put_state(final, g.seq.of(tile + t - 1));
+                    get_state(g.seq.of(tile + t));
+                    if (!ENDS && kept && t == 0) keep_state(tile);
+                }
+                const float share = token(t);
+                if (!ENDS) shares[ENDS ? 0 : t][q][ENDS ? 0 : mine] = share;
+            }
+        } else {
+#pragma unroll 8
+            for (int t = 0; t < S::TOKENS; ++t) {
+                const float share = token(t);
+                if (!ENDS) shares[ENDS ? 0 : t][q][ENDS ? 0 : mine] = share;
+            }
+        }
         __syncthreads();
 
         if (!ENDS) {
@@ -194,12 +211,14 @@ __global__ __launch_bounds__(256) void k_sscan_fwd(Scan g, const T *__restrict__
             const int m = tile + row < t1 ? n : 0;
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
-                o[i] = fmaf(skip[i], kx.at(i), du[row][col + i].x);
+                o[i] = shares[ENDS ? 0 : row][0][ENDS ? 0 : col + i];
+#pragma unroll
+                for (int j = 1; j < LPC; ++j) o[i] += shares[ENDS ? 0 : row][j][ENDS ? 0 : col + i];
+                o[i] = fmaf(skip[i], kx.at(i), o[i]);
                 if (z) { const float v = kz.at(i); o[i] *= v * sigmoid(v); }
             }
-            Some<T, S::EACH> out;
-            out.set(o);
-            out.store(y + (long long)(tile + row) * g.ys + first_chan, m);
+            store_late<T, S::EACH, WHOLE>(BufView(py, VIEW_BYTES), oy, m, o);
+            py += S::TOKENS * g.ys;
         }
     }
     if (ENDS) {
@@ -234,7 +253,10 @@ __global__ __launch_bounds__(256) void k_sscan_step(Scan g, const T *__restrict_
     a.load(A + (long long)c * g.N + 4 * q, n);
     b.load(B + (long long)t * g.bs + shared, n);
     cc.load(Cm + (long long)t * g.cs + shared, n);
-    const float xv = ldf(x + (long long)t * g.xs + c), d = step_size(g, ldf(dt + (long long)t * g.dts + c) + (dt_bias ? dt_bias[c] : 0.f));
+    const float xv = ldf(x + (long long)t * g.xs + c);
+    float step[1] = {ldf(dt + (long long)t * g.dts + c) + (dt_bias ? dt_bias[c] : 0.f)};
+    step_sizes(g, step);
+    const float d = step[0];
     float hv[4], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -243,10 +265,7 @@ __global__ __launch_bounds__(256) void k_sscan_step(Scan g, const T *__restrict_
     }
     h.set(hv);
     h.store(st, n);
-    sum += lane_move<DPP_XOR1>(sum);
-    if constexpr (LPC >= 4) sum += lane_move<DPP_XOR2>(sum);
-    if constexpr (LPC >= 8) sum += lane_move<DPP_HALF_MIRROR>(sum);
-    if constexpr (LPC >= 16) sum += lane_move<DPP_MIRROR>(sum);
+    sum = states_sum<LPC>(sum);
     if (q) return;
     if (D) sum = fmaf(D[c], xv, sum);
     if (z) { const float v = ldf(z + (long long)t * g.zs + c); sum *= v * sigmoid(v); }
@@ -268,8 +287,15 @@ template <typename T> hipError_t launch(const sscan_desc *d, const sscan_tensors
                                (const T *)t->C, (const float *)t->D, (const T *)t->z, (const float *)t->dt_bias, (const float *)t->init, (T *)t->y,
                                (float *)t->final, (float *)t->kept, ends, sums);
         };
-        if (p.carry) run(k_sscan_fwd<T, LPC, true>, blocks - (unsigned)p.channel_blocks);   // (nothing follows the last part)
-        run(k_sscan_fwd<T, LPC, false>, blocks);
+        auto both = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            if (p.carry) run(k_sscan_fwd<T, LPC, true, WHOLE>, blocks - (unsigned)p.channel_blocks);   // (nothing follows the last part)
+            run(k_sscan_fwd<T, LPC, false, WHOLE>, blocks);
+        };
+        constexpr int EACH = Tile<LPC>::EACH;
+        const bool whole = whole_vectors<T>(EACH, g.per_group, {t->x, t->dt, t->z, t->y}, {g.xs, g.dts, g.zs, g.ys});
+        if (whole) both(std::true_type());
+        else both(std::false_type());
     });
 }
 
