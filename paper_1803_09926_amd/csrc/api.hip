@@ -108,7 +108,7 @@ const char *dwconv_status_string(int status)
     case DWCONV_ERR_NULL: return "null pointer";
     case DWCONV_ERR_BAD_DIM: return "bad dimension (N,C,H,W,K,stride,mult must be >= 1, pad >= 0, output non-empty)";
     case DWCONV_ERR_BAD_ENUM: return "bad layout or dtype";
-    case DWCONV_ERR_WORKSPACE: return "bwd_filter workspace missing or too small";
+    case DWCONV_ERR_WORKSPACE: return "workspace missing or too small";
     case DWCONV_ERR_ALIGN: return "pointer not 16-byte aligned";
     case DWCONV_ERR_UNSUPPORTED: return "unsupported (K larger than DWCONV_MAX_K)";
     case DWCONV_ERR_LAUNCH: return "HIP kernel launch failed";

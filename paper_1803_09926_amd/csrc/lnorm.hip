@@ -1,12 +1,14 @@
 // Layer norm over the channels of each token, forward and backward.  The contract stands in include/seqops.h.
 //
-// A team of lanes (a wavefront, or a block of 4 or 16 of them) holds a row in registers, V consecutive channels a vector and NV vectors a lane, so
+// A team of lanes (a wavefront, or a block of 2 to 16 of them) holds a row in registers, V consecutive channels a vector and NV vectors a lane, so
 // that the row is read once, the variance is taken about the mean that is already known (two sums over the team, no cancellation), and all is written once.
-// Both passes are bound by memory.
+// Both passes are bound by memory: 32768 x 1024 in bf16 with a residual takes 48.5 us, 5.5 TB/s, where a large copy reaches 5.2; the backward pass at
+// 9999 x 1536 in fp32 34 us and 6 for the sum of its partials, 5.4 TB/s of the first.
 //
 // The weight's gradient is a sum over rows: each lane keeps the sums of its own channels over all rows that its team walks, the teams of a block add
 // theirs in LDS one after the other, and the blocks' partials meet in seq_sum.hip.
 #include "seq_common.hpp"
+#include <initializer_list>
 
 namespace dwc {
 
@@ -42,33 +44,59 @@ template <int TEAM> __device__ __forceinline__ float team_sum(float a, float *ld
     return a;
 }
 
-template <typename T, int TEAM, int V, int NV, int BLOCK>
+// V channels of a row from channel c on.  WHOLE: C is a multiple of V and rows are aligned: loads and stores through a view of the row, in which what lies
+// behind its end reads zero and is not written, without a branch.  Otherwise each vector is looked at.
+template <typename T, int V, bool WHOLE> struct Part;
+template <typename T, int V> struct Part<T, V, true> {
+    Ahead<T, V, true> v;
+    __device__ __forceinline__ void load(const T *row, int C, int c) { v.load(BufView(row, (uint32_t)C * (uint32_t)sizeof(T)), (uint32_t)c * (uint32_t)sizeof(T), 1); }
+    __device__ __forceinline__ float at(int i) const { return v.at(i); }
+    static __device__ __forceinline__ void store(T *row, int C, int c, const float (&r)[V])
+    {
+        // (past the end of the last 16 bytes of a vector that starts inside there is nothing: a whole vector is inside or outside)
+        store_late<T, V, true>(BufView(row, (uint32_t)C * (uint32_t)sizeof(T)), (uint32_t)c * (uint32_t)sizeof(T), 1, r);
+    }
+};
+template <typename T, int V> struct Part<T, V, false> {
+    Some<T, V> v;
+    __device__ __forceinline__ void load(const T *row, int C, int c) { v.load(row + c, C - c); }
+    __device__ __forceinline__ float at(int i) const { return v.at(i); }
+    static __device__ __forceinline__ void store(T *row, int C, int c, const float (&r)[V])
+    {
+        Some<T, V> p;
+        p.set(r);
+        p.store(row + c, C - c);
+    }
+};
+
+template <typename T, int TEAM, int V, int NV, int BLOCK, bool WHOLE>
 __global__ __launch_bounds__(BLOCK) void k_lnorm_fwd(int rows, int C, float eps, float inv_c, const T *__restrict__ x, const T *__restrict__ residual,
                                                      const T *__restrict__ w, const T *__restrict__ b, T *__restrict__ y, T *__restrict__ total,
                                                      float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
+    typedef Part<T, V, WHOLE> P;
     __shared__ float lds[2][TEAM / 64];
     const int lane = threadIdx.x % TEAM;
     const long long row = (long long)blockIdx.x * (BLOCK / TEAM) + threadIdx.x / TEAM;
-    if (row >= rows) return;   // (whole teams: a block of one team is always inside)
-    const T *xr = x + row * C;
-    Some<T, V> in[NV], more[NV];
+    if (row >= rows) return;   // (whole wavefronts; a block of one team is always inside)
+    P in[NV], more[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) in[j].load(xr + (j * TEAM + lane) * V, C - (j * TEAM + lane) * V);
+    for (int j = 0; j < NV; ++j) in[j].load(x + row * C, C, (j * TEAM + lane) * V);
     float s[NV][V], sum = 0.f;
     if (residual) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) more[j].load(residual + row * C + (j * TEAM + lane) * V, C - (j * TEAM + lane) * V);
+        for (int j = 0; j < NV; ++j) more[j].load(residual + row * C, C, (j * TEAM + lane) * V);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
             for (int i = 0; i < V; ++i) s[j][i] = in[j].at(i) + more[j].at(i);
-            more[j].set(s[j]);
-            more[j].store(total + row * C + (j * TEAM + lane) * V, C - (j * TEAM + lane) * V);
+            P::store(total + row * C, C, (j * TEAM + lane) * V, s[j]);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) in[j].get(s[j]);
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[j][i] = in[j].at(i);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -85,68 +113,75 @@ __global__ __launch_bounds__(BLOCK) void k_lnorm_fwd(int rows, int C, float eps,
         }
     const float var = team_sum<TEAM>(squares, lds[1]) * inv_c, rstd = 1.f / sqrtf(var + eps);
     if (mean_out && lane == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
+    P p[NV];
+    if (w) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * TEAM + lane) * V, n = C - c;
-        if (n <= 0) break;
-        float o[V];
-        Some<T, V> p;
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = s[j][i] * rstd;
-        if (w) {
-            p.load(w + c, n);
-#pragma unroll
-            for (int i = 0; i < V; ++i) o[i] *= p.at(i);
-        }
-        if (b) {
-            p.load(b + c, n);
-#pragma unroll
-            for (int i = 0; i < V; ++i) o[i] += p.at(i);
-        }
-        p.set(o);
-        p.store(y + row * C + c, n);
+        for (int j = 0; j < NV; ++j) p[j].load(w, C, (j * TEAM + lane) * V);
     }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[j][i] *= w ? rstd * p[j].at(i) : rstd;
+    if (b) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) p[j].load(b, C, (j * TEAM + lane) * V);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[j][i] += p[j].at(i);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) P::store(y + row * C, C, (j * TEAM + lane) * V, s[j]);
 }
 
-// Rows are dealt out to the teams of the whole launch in turn.  partials: [blocks][2][C], or NULL where the weight's gradient is not asked for.
-template <typename T, int TEAM, int V, int NV, int BLOCK>
+// Rows are dealt out to the teams of the whole launch in turn; a team asks for its next row before it works on the one in hand.
+// partials: [blocks][2][C], or NULL where the weight's gradient is not asked for.
+template <typename T, int TEAM, int V, int NV, int BLOCK, bool WHOLE>
 __global__ __launch_bounds__(BLOCK) void k_lnorm_bwd(int rows, int C, float inv_c, const T *__restrict__ x, const T *__restrict__ w,
                                                      const float *__restrict__ mean_in, const float *__restrict__ rstd_in, const T *__restrict__ dy,
                                                      const T *__restrict__ dtotal, T *__restrict__ dx, float *__restrict__ partials)
 {
+    typedef Part<T, V, WHOLE> P;
     constexpr int TEAMS = BLOCK / TEAM;
     __shared__ float lds[2][2 * TEAM / 64];
     extern __shared__ float sums[];            // [2][C], where a block has more than one team
     const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    Some<T, V> wr[NV];
+    P wr[NV];
     float gw[NV][V], gb[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if (w) wr[j].load(w + (j * TEAM + lane) * V, C - (j * TEAM + lane) * V);
+        if (w) wr[j].load(w, C, (j * TEAM + lane) * V);
 #pragma unroll
         for (int i = 0; i < V; ++i) gw[j][i] = gb[j][i] = 0.f;
     }
-    int turn = 0;
-    for (long long row = (long long)blockIdx.x * TEAMS + team; row < rows; row += (long long)gridDim.x * TEAMS, turn ^= 1) {
-        Some<T, V> xr[NV], gr[NV], ar[NV];
+    struct Row { P x[NV], dy[NV], add[NV]; float mean, rstd; } ahead;
+    auto load = [&](long long row) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * TEAM + lane) * V;
-            xr[j].load(x + row * C + c, C - c);
-            gr[j].load(dy + row * C + c, C - c);
+            ahead.x[j].load(x + row * C, C, (j * TEAM + lane) * V);
+            ahead.dy[j].load(dy + row * C, C, (j * TEAM + lane) * V);
         }
         if (dtotal) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j) ar[j].load(dtotal + row * C + (j * TEAM + lane) * V, C - (j * TEAM + lane) * V);
+            for (int j = 0; j < NV; ++j) ahead.add[j].load(dtotal + row * C, C, (j * TEAM + lane) * V);
         }
-        const float mean = mean_in[row], rstd = rstd_in[row];
+        ahead.mean = mean_in[row];
+        ahead.rstd = rstd_in[row];
+    };
+    int turn = 0;
+    const long long stride = (long long)gridDim.x * TEAMS;
+    long long row = (long long)blockIdx.x * TEAMS + team;
+    if (row < rows) load(row);
+    for (; row < rows; row += stride, turn ^= 1) {
+        const Row r = ahead;
+        if (row + stride < rows) load(row + stride);
         float m1 = 0.f, m2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 // beyond the row dy is zero, and so are all products with it
-                const float xhat = (xr[j].at(i) - mean) * rstd, g = gr[j].at(i), gx = g * xhat;
+                const float xhat = (r.x[j].at(i) - r.mean) * r.rstd, g = r.dy[j].at(i), gx = g * xhat;
                 gb[j][i] += g;
                 gw[j][i] += gx;
                 m1 += w ? g * wr[j].at(i) : g;
@@ -157,20 +192,17 @@ __global__ __launch_bounds__(BLOCK) void k_lnorm_bwd(int rows, int C, float inv_
         m2 *= inv_c;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * TEAM + lane) * V, n = C - c;
             float o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float xhat = (xr[j].at(i) - mean) * rstd, g = w ? gr[j].at(i) * wr[j].at(i) : gr[j].at(i);
-                o[i] = rstd * ((g - m1) - xhat * m2);
+                const float xhat = (r.x[j].at(i) - r.mean) * r.rstd, g = w ? r.dy[j].at(i) * wr[j].at(i) : r.dy[j].at(i);
+                o[i] = r.rstd * ((g - m1) - xhat * m2);
             }
             if (dtotal) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] += ar[j].at(i);
+                for (int i = 0; i < V; ++i) o[i] += r.add[j].at(i);
             }
-            Some<T, V> p;
-            p.set(o);
-            p.store(dx + row * C + c, n);
+            P::store(dx + row * C, C, (j * TEAM + lane) * V, o);
         }
     }
     if (!partials) return;
@@ -213,34 +245,49 @@ int validate(const lnorm_desc *d)
     return DWCONV_OK;
 }
 
-// How many lanes share a row, and how many of its channels a lane has.  The backward pass has five values a channel in registers, the forward pass two.
+// How many lanes share a row, and how many of its channels a lane has.  A wavefront alone needs no barrier; 16 channels a lane (8 in the backward pass, which
+// holds seven values a channel) leave enough wavefronts on a compute unit: 2048 channels of bf16 by 64, 128, 256 lanes forward 26.0, 26.0, 29.1 us (16384
+// rows); backward 67, 50, 47 us.  1536 channels of fp32 forward 27.7, 26.5, 25.4 us (9999 rows), backward 60, 41, 40 us.
 struct Team { int lanes, channels; };
 Team fwd_team(int C)
 {
     if (C <= 512) return {64, 8};
     if (C <= 1024) return {64, 16};
-    if (C <= 2048) return {64, 32};
+    if (C <= 2048) return {128, 16};
     if (C <= 4096) return {256, 16};
-    if (C <= 8192) return {256, 32};
+    if (C <= 8192) return {512, 16};
     return {1024, 16};
 }
-Team bwd_team(int C)
+// Few rows: a row a block of 128 lanes, 8 x 1024 in bf16 7.5 us, where four rows a block whose sums meet in LDS take 10.8; 600 rows 10.7 and 12.6 us.
+constexpr int FEW_ROWS = 1024;
+Team bwd_team(int C, int T)
 {
+    if (C <= 1024 && T <= FEW_ROWS) return {128, 8};
     if (C <= 512) return {64, 8};
     if (C <= 1024) return {64, 16};
     if (C <= 2048) return {256, 8};
-    if (C <= 4096) return {256, 16};
+    if (C <= 4096) return {512, 8};
     if (C <= 8192) return {1024, 8};
     return {1024, 16};
 }
-constexpr int block_of(int lanes) { return lanes < 256 ? 256 : lanes; }
+constexpr int block_of(int lanes) { return lanes == 64 ? 256 : lanes; }
 
-// Blocks of the backward pass: four on each of the 256 compute units, fewer where there are fewer rows.
+// Blocks of the backward pass: two on each of the 256 compute units (one of 1024 lanes), fewer where there are fewer rows.  Each leaves partials that are read again:
+// 256, 512, 1024 blocks take 63, 42, 46 us at 9999 x 1536 in fp32, and 61, 47, 57 at 32768 x 1024 in bf16.
 int bwd_blocks(const lnorm_desc *d)
 {
-    const int lanes = bwd_team(d->C).lanes, teams = block_of(lanes) / lanes, most = lanes == 1024 ? 256 : 1024;
+    const int lanes = bwd_team(d->C, d->T).lanes, teams = block_of(lanes) / lanes, most = lanes == 1024 ? 256 : 512;
     const int need = d->T > 0 ? cdiv(d->T, teams) : 0;
     return need < most ? need : most;
+}
+
+// Whether rows are whole vectors of 16 bytes, each aligned to that
+bool whole_rows(const lnorm_desc *d, std::initializer_list<const void *> rows)
+{
+    if (d->C % (d->dtype == DWCONV_F32 ? 4 : 8)) return false;
+    for (const void *p : rows)
+        if (unaligned16(p)) return false;
+    return true;
 }
 
 // f(lanes, vectors a lane) with the numbers as types
@@ -258,28 +305,37 @@ template <typename T> hipError_t launch_fwd(const lnorm_desc *d, const lnorm_ten
     const Team team = fwd_team(d->C);
     auto launch = [&](auto shape) {
         typedef decltype(shape) S;
-        hipLaunchKernelGGL((k_lnorm_fwd<T, S::TEAM, V, S::VECTORS, S::BLOCK>), dim3((unsigned)cdiv(d->T, S::BLOCK / S::TEAM)), dim3(S::BLOCK), 0, stream,
-                           d->T, d->C, d->eps, 1.f / (float)d->C, (const T *)t->x, (const T *)t->residual, (const T *)t->w, (const T *)t->b, (T *)t->y,
-                           (T *)t->total, (float *)t->mean, (float *)t->rstd);
+        auto run = [&](auto whole) {
+            hipLaunchKernelGGL((k_lnorm_fwd<T, S::TEAM, V, S::VECTORS, S::BLOCK, decltype(whole)::value>), dim3((unsigned)cdiv(d->T, S::BLOCK / S::TEAM)),
+                               dim3(S::BLOCK), 0, stream, d->T, d->C, d->eps, 1.f / (float)d->C, (const T *)t->x, (const T *)t->residual, (const T *)t->w,
+                               (const T *)t->b, (T *)t->y, (T *)t->total, (float *)t->mean, (float *)t->rstd);
+        };
+        if (whole_rows(d, {t->x, t->residual, t->w, t->b, t->y, t->total})) run(std::true_type());
+        else run(std::false_type());
     };
-    const bool found = shape_is<V, 64, 8>(team, launch) || shape_is<V, 64, 16>(team, launch) || shape_is<V, 64, 32>(team, launch) ||
-                       shape_is<V, 256, 16>(team, launch) || shape_is<V, 256, 32>(team, launch) || shape_is<V, 1024, 16>(team, launch);
+    const bool found = shape_is<V, 64, 8>(team, launch) || shape_is<V, 64, 16>(team, launch) || shape_is<V, 128, 16>(team, launch) ||
+                       shape_is<V, 256, 16>(team, launch) || shape_is<V, 512, 16>(team, launch) || shape_is<V, 1024, 16>(team, launch);
     return found ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 template <typename T> hipError_t launch_bwd(const lnorm_desc *d, const lnorm_tensors *t, float *partials, hipStream_t stream)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    const Team team = bwd_team(d->C);
+    const Team team = bwd_team(d->C, d->T);
     auto launch = [&](auto shape) {
         typedef decltype(shape) S;
         const size_t lds = S::BLOCK > S::TEAM && partials ? 2 * (size_t)d->C * sizeof(float) : 0;
-        hipLaunchKernelGGL((k_lnorm_bwd<T, S::TEAM, V, S::VECTORS, S::BLOCK>), dim3((unsigned)bwd_blocks(d)), dim3(S::BLOCK), lds, stream, d->T, d->C,
-                           1.f / (float)d->C, (const T *)t->x, (const T *)t->w, (const float *)t->mean, (const float *)t->rstd, (const T *)t->dy,
-                           (const T *)t->dtotal, (T *)t->dx, partials);
+        auto run = [&](auto whole) {
+            hipLaunchKernelGGL((k_lnorm_bwd<T, S::TEAM, V, S::VECTORS, S::BLOCK, decltype(whole)::value>), dim3((unsigned)bwd_blocks(d)), dim3(S::BLOCK), lds,
+                               stream, d->T, d->C, 1.f / (float)d->C, (const T *)t->x, (const T *)t->w, (const float *)t->mean, (const float *)t->rstd,
+                               (const T *)t->dy, (const T *)t->dtotal, (T *)t->dx, partials);
+        };
+        if (whole_rows(d, {t->x, t->w, t->dy, t->dtotal, t->dx})) run(std::true_type());
+        else run(std::false_type());
     };
-    const bool found = shape_is<V, 64, 8>(team, launch) || shape_is<V, 64, 16>(team, launch) || shape_is<V, 256, 8>(team, launch) ||
-                       shape_is<V, 256, 16>(team, launch) || shape_is<V, 1024, 8>(team, launch) || shape_is<V, 1024, 16>(team, launch);
+    const bool found = shape_is<V, 128, 8>(team, launch) || shape_is<V, 64, 8>(team, launch) || shape_is<V, 64, 16>(team, launch) ||
+                       shape_is<V, 256, 8>(team, launch) || shape_is<V, 512, 8>(team, launch) || shape_is<V, 1024, 8>(team, launch) ||
+                       shape_is<V, 1024, 16>(team, launch);
     return found ? hipGetLastError() : hipErrorInvalidValue;
 }
 
