@@ -302,13 +302,13 @@ __global__ __launch_bounds__(256, K <= 4 ? 3 : 2) void k_cconv_bwd(Conv g, const
     }
 }
 
+// A block of 64 lanes takes neighbouring channels of one row, `across` of them the row: its slot is a scalar.
 template <typename T, int K, int V>
-__global__ __launch_bounds__(256) void k_cconv_step(Conv g, int nv, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ b,
-                                                    const int32_t *__restrict__ slots, T *__restrict__ state, T *__restrict__ y)
+__global__ __launch_bounds__(64) void k_cconv_step(Conv g, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ b,
+                                                   const int32_t *__restrict__ slots, T *__restrict__ state, T *__restrict__ y)
 {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int t = (int)(id / nv), c = (int)(id % nv) * V, n = g.C - c;
-    if (t >= g.seq.T) return;
+    const int t = (int)(blockIdx.x / g.across), c = ((int)(blockIdx.x % g.across) * 64 + threadIdx.x) * V, n = g.C - c;
+    if (n <= 0) return;
     const int slot = slots ? slots[t] : t;
     T *const yr = y + (long long)t * g.y_stride + c;
     Some<T, V> out;
@@ -441,14 +441,12 @@ template <typename T> hipError_t launch_bwd(const cconv_desc *d, const cconv_ten
 
 template <typename T> hipError_t launch_step(const cconv_desc *d, const cconv_tensors *t, hipStream_t stream)
 {
-    constexpr int V = CHANNELS;
-    const int nv = cdiv(d->C, V);
-    const long long blocks = ((long long)d->T * nv + 255) / 256;
-    if (!launchable(blocks, 256)) return hipErrorInvalidValue;
-    const Launch l = {nv, 1, 1, 1, 1};
+    const int vectors = cdiv(d->C, CHANNELS);
+    const Launch l = {vectors, 64, 1, d->T, (unsigned)cdiv(vectors, 64)};
+    if (!launchable(l.down * l.across, 64)) return hipErrorInvalidValue;
     return with_taps(d->K, [&](auto k) {
-        hipLaunchKernelGGL((k_cconv_step<T, decltype(k)::value, V>), dim3((unsigned)blocks), dim3(256), 0, stream, geometry(d, l, nullptr), nv,
-                           (const T *)t->x, (const T *)t->w, (const T *)t->b, (const int32_t *)t->slots, (T *)t->state, (T *)t->y);
+        hipLaunchKernelGGL((k_cconv_step<T, decltype(k)::value, CHANNELS>), dim3((unsigned)(l.down * l.across)), dim3(64), 0, stream,
+                           geometry(d, l, nullptr), (const T *)t->x, (const T *)t->w, (const T *)t->b, (const int32_t *)t->slots, (T *)t->state, (T *)t->y);
     });
 }
 

@@ -29,7 +29,7 @@ int validate(const sscan_desc *d)
 // 16-byte multiples, so that what follows is aligned
 size_t floats(size_t n) { return (n + 3) / 4 * 4; }
 
-constexpr int MOST_PARTS = 96;   // a block of the last part reads the states of all before it
+constexpr int MOST_PARTS = 80;   // a block of the last part reads the states of all before it
 constexpr int PART_UNIT = KEPT_EVERY;   // a part is a whole number of tiles
 
 int tuned(const char *name, int otherwise)

@@ -90,12 +90,12 @@ __device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, i
 __device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of(t)) == t; }
 
 // What `count` parts from `first` on (in the direction of `step`) leave at the end of a row of them: v = e[first] + decay(first) * (e[next] + ...), with the
-// decay over a part exp(A * its sum of step sizes).  Four parts are asked for at a time: eight took registers that the kernel behind it wants.
+// decay over a part exp(A * its sum of step sizes).  Six parts are asked for at a time: eight take registers that the kernel behind it wants.
 template <int LPC>
 __device__ __forceinline__ void gather_parts(float (&v)[4], const float (&a2)[4], const float *ends, const float *sums, int C, int chan, int q, bool valid,
                                              int first, int step, int count)
 {
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 6;
     float decay[4] = {1.f, 1.f, 1.f, 1.f};
     for (int k = 0; k < count; k += AHEAD) {
         float4 e[AHEAD];

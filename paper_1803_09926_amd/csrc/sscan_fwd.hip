@@ -237,9 +237,10 @@ __global__ __launch_bounds__(256) void k_sscan_step(Scan g, const T *__restrict_
                                                     const T *__restrict__ z, const float *__restrict__ dt_bias, const int32_t *__restrict__ slots,
                                                     float *__restrict__ state, T *__restrict__ y)
 {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, which = id / LPC;
-    const int q = (int)(id % LPC), t = (int)(which / g.C), c = (int)(which % g.C), n = g.N - 4 * q;
-    if (t >= g.seq.T) return;                                          // (all lanes of a channel)
+    // a block takes neighbouring channels of one row: its slot is a scalar, and no lane divides
+    const int t = (int)(blockIdx.x / (unsigned)g.blocks_of_group), q = threadIdx.x % LPC;
+    const int c = (int)(blockIdx.x % (unsigned)g.blocks_of_group) * (256 / LPC) + threadIdx.x / LPC, n = g.N - 4 * q;
+    if (c >= g.C) return;                                              // (all lanes of a channel)
     const int slot = slots ? slots[t] : t;
     if (slot < 0 || slot >= g.seq.n) {
         if (q == 0) stf(y + (long long)t * g.ys + c, 0.f);
@@ -302,8 +303,9 @@ template <typename T> hipError_t launch(const sscan_desc *d, const sscan_tensors
 template <typename T> hipError_t launch_one(const sscan_desc *d, const sscan_tensors *t, hipStream_t stream)
 {
     ScanPlan p = {state_lanes(d->N), 1, 1, 1, false};
-    const Scan g = sscan_geometry(d, p, nullptr);
-    const long long blocks = ((long long)d->T * d->C * p.lanes + 255) / 256;
+    Scan g = sscan_geometry(d, p, nullptr);
+    g.blocks_of_group = cdiv(d->C, 256 / p.lanes);                     // here: of a row
+    const long long blocks = (long long)d->T * g.blocks_of_group;
     if (!launchable(blocks, 256)) return hipErrorInvalidValue;
     return with_state_lanes(p.lanes, [&](auto lanes) {
         hipLaunchKernelGGL((k_sscan_step<T, decltype(lanes)::value>), dim3((unsigned)blocks), dim3(256), 0, stream, g, (const T *)t->x, (const T *)t->dt,
