@@ -331,6 +331,17 @@ def test_scan_of_whole_sequences_a_part(gpu_lib):
         _scan_case("f32", 704, 16, 1, EVEN(32 * 40, 40), packed, True, seed=11)
 
 
+@pytest.mark.parametrize("blocks,most", [(1, 80), (2, 2), (12, 80), (60, 7), (4096, 80), (4096, 300)])
+@pytest.mark.parametrize("N", [8, 16, 33])
+def test_scan_however_it_is_split(gpu_lib, blocks, most, N):
+    """One part, parts of one tile, more parts than one look back takes, whole sequences a part and several of them: the plans of other sizes, forced on a small one."""
+    knobs = {"DWCONV_TUNE_SSCAN_FWD_BLOCKS": blocks, "DWCONV_TUNE_SSCAN_BWD_BLOCKS": blocks, "DWCONV_TUNE_SSCAN_MOST_PARTS": most}
+    with dw.tuning_overrides(knobs):
+        _scan_case("f32", 70, N, 1, RAGGED, True, True, seed=N)
+        _scan_case("f32", 70, N, 1, EVEN(288, 6), False, True, seed=N + 1)
+        _scan_case("bf16", 70, N, 2, EVEN(290, 1), False, False, seed=N + 2)
+
+
 def test_scan_states_and_gradients_that_hardly_decay_and_that_vanish(gpu_lib):
     """Decays next to 1 and far below the smallest number, step sizes from 1e-6 to 20: the parts' products and the kept states hold either way."""
     m = Made(3, "f32")
