@@ -151,12 +151,20 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     int s = g.seq.of(t0), head = g.seq.start(s), next = g.seq.start(s + 1);    // the sequence of the tile's first token
     float total = 0.f;
     for (int tile = t0; tile < t1; tile += S::TOKENS) {
-        const Ahead<T, S::EACH, WHOLE> kx = rx, kz = rz;
+        float direct[ENDS ? 1 : S::EACH], gate[ENDS ? 1 : S::EACH];    // D * x, and what the gate lets through
         {
             float d[S::EACH];
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) d[i] = rdt.at(i) + bias[i];
             step_sizes(g, d);
+            if (!ENDS) {
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) { direct[ENDS ? 0 : i] = skip[i] * rx.at(i); gate[ENDS ? 0 : i] = 1.f; }
+                if (z) {
+#pragma unroll
+                    for (int i = 0; i < S::EACH; ++i) { const float v = rz.at(i); gate[ENDS ? 0 : i] = v * sigmoid(v); }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) { steps[row][col + i] = d[i]; gains[row][col + i] = d[i] * rx.at(i); }
 #pragma unroll
@@ -210,13 +218,13 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
             float o[S::EACH];
             const int m = tile + row < t1 ? n : 0;
 #pragma unroll
-            for (int i = 0; i < S::EACH; ++i) {
-                o[i] = shares[ENDS ? 0 : row][0][ENDS ? 0 : col + i];
+            for (int i = 0; i < S::EACH; ++i) o[i] = direct[ENDS ? 0 : i];
 #pragma unroll
-                for (int j = 1; j < LPC; ++j) o[i] += shares[ENDS ? 0 : row][j][ENDS ? 0 : col + i];
-                o[i] = fmaf(skip[i], kx.at(i), o[i]);
-                if (z) { const float v = kz.at(i); o[i] *= v * sigmoid(v); }
-            }
+            for (int j = 0; j < LPC; ++j)
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) o[i] += shares[ENDS ? 0 : row][j][ENDS ? 0 : col + i];
+#pragma unroll
+            for (int i = 0; i < S::EACH; ++i) o[i] *= gate[ENDS ? 0 : i];
             store_late<T, S::EACH, WHOLE>(BufView(py, VIEW_BYTES), oy, m, o);
             py += S::TOKENS * g.ys;
         }
