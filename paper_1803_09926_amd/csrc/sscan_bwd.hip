@@ -375,24 +375,33 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         __syncthreads();
 
         {
-            float dx[S::EACH], dd[S::EACH], dz[S::EACH] = {};
+            // (a branch for all of a lane's channels, not one for each)
+            float dv[S::EACH], dx[S::EACH], dd[S::EACH], dz[S::EACH] = {};
+#pragma unroll
+            for (int i = 0; i < S::EACH; ++i) dv[i] = kdy.at(i);
+            if (in.z) {
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) {
+                    const float zv = kz.at(i), sz = sigmoid(zv);
+                    dz[i] = dv[i] * fmaf(skip[i], kx.at(i), ys[row][col + i]) * (sz + zv * sz * (1.f - sz));
+                    dv[i] *= zv * sz;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
-                const float gb = steps[row][col + i], ra = gains[row][col + i];
-                const float xv = kx.at(i), dout = kdy.at(i);
-                float dv = dout;
-                if (in.z) {
-                    const float zv = kz.at(i), sz = sigmoid(zv);
-                    dv *= zv * sz;
-                    dz[i] = dout * fmaf(skip[i], xv, ys[row][col + i]) * (sz + zv * sz * (1.f - sz));
-                }
-                dx[i] = fmaf(skip[i], dv, delta[i] * gb);
-                dd[i] = fmaf(xv, gb, ra);
-                if (g.softplus) dd[i] *= sigmoid(kdt.at(i) + bias[i]);
-                if (m > 0) {
-                    dskip[i] = fmaf(dv, xv, dskip[i]);
-                    dbias[i] += dd[i];
-                }
+                const float gb = steps[row][col + i];
+                dx[i] = fmaf(skip[i], dv[i], delta[i] * gb);
+                dd[i] = fmaf(kx.at(i), gb, gains[row][col + i]);
+            }
+            if (g.softplus) {
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) dd[i] *= sigmoid(kdt.at(i) + bias[i]);
+            }
+            const bool counts = m > 0;
+#pragma unroll
+            for (int i = 0; i < S::EACH; ++i) {
+                dskip[i] += counts ? dv[i] * kx.at(i) : 0.f;
+                dbias[i] += counts ? dd[i] : 0.f;
             }
             store_late<T, S::EACH, WHOLE>(BufView(pdx, VIEW_BYTES), ox, m, dx);
             store_late<T, S::EACH, WHOLE>(BufView(pddt, VIEW_BYTES), odt, m, dd);
