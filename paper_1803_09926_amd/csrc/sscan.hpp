@@ -80,13 +80,16 @@ template <int L> __device__ __forceinline__ float states_sum(float v)
     return v;
 }
 
-// The tokens of t0 .. t0 + n - 1 (n <= 32) that are the first of their sequence, a bit each; the same in every lane.
-__device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, int n, int end)
+// The tokens of t0 .. t0 + n - 1 (n <= 32) that are the first of their sequence, a bit each; the same in every lane.  `of` gets the token's sequence in the
+// lane of its number from t0, and that of the token before t0 in the last lane: a search in each token's turn costs a chain of loads for each.
+__device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, int n, int end, int &of)
 {
-    const int lane = threadIdx.x & 63, t = t0 + lane;
-    const bool first = lane < n && t < end && seq.start(seq.of(t)) == t;
-    return (uint32_t)__ballot(first);
+    const int lane = threadIdx.x & 63, t = lane == 63 ? t0 - 1 : t0 + lane;
+    const bool there = t >= 0 && t < end && (lane < n || lane == 63);
+    of = there ? seq.of(t) : 0;
+    return (uint32_t)__ballot(there && lane < n && seq.start(of) == t);
 }
+__device__ __forceinline__ int sequence_of(int of, int t) { return __builtin_amdgcn_readlane(of, t & 63); }   // of token t from t0, -1 the one before it
 __device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of(t)) == t; }
 
 // What `count` parts from `first` on (in the direction of `step`) leave at the end of a row of them: v = e[first] + decay(first) * (e[next] + ...), with the

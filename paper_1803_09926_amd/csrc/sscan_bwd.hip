@@ -115,7 +115,8 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
         }
         if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
         const bool any = head >= tile || behind_it < tile + TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, TOKENS, t1) : 0u;
+        int of = 0;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, TOKENS, t1, of) : 0u;
         if (tile > t0) load(tile - TOKENS);
         __syncthreads();
         auto walk = [&](auto special) {
@@ -284,7 +285,8 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         }
         if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
         const bool any = head >= tile || behind_it < tile + S::TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
+        int of = 0;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1, of) : 0u;
         if (tile > t0) load(tile - S::TOKENS);
         __syncthreads();
 
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
                 for (int i = 0; i < 4; ++i) before[i] = t ? h[t ? t - 1 : 0][i] : hin[i];
                 if constexpr (SPECIAL) {
-                    if (firsts >> t & 1) init_of(g.seq.of(tile + t), before);
+                    if (firsts >> t & 1) init_of(sequence_of(of, t), before);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
                     for (int i = 0; i < 4; ++i) before[i] = t ? h[t ? t - 1 : 0][i] : hin[i];
                     if constexpr (SPECIAL) {
-                        if (firsts >> t & 1) init_of(g.seq.of(tile + t), before);
+                        if (firsts >> t & 1) init_of(sequence_of(of, t), before);
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {

@@ -178,7 +178,8 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
         }
         if (tile >= next) { s = g.seq.of(tile); head = g.seq.start(s); next = g.seq.start(s + 1); }
         const bool any = head == tile || next < tile + S::TOKENS;
-        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1) : 0u;
+        int of = 0;
+        const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1, of) : 0u;
         if (!ENDS && kept && !(firsts & 1)) keep_state(tile);
         if (tile + S::TOKENS < t1) load(tile + S::TOKENS);
         __syncthreads();
@@ -198,8 +199,8 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
 #pragma unroll 1
             for (int t = 0; t < S::TOKENS && tile + t < t1; ++t) {
                 if (firsts >> t & 1) {
-                    if (!ENDS && final && tile + t > t0) put_state(final, g.seq.of(tile + t - 1));
-                    get_state(g.seq.of(tile + t));
+                    if (!ENDS && final && tile + t > t0) put_state(final, sequence_of(of, t - 1));
+                    get_state(sequence_of(of, t));
                     if (!ENDS && kept && t == 0) keep_state(tile);
                 }
                 const float share = token(t);
