@@ -238,6 +238,19 @@ struct Sequences {
         }
         return lo;
     }
+    // the same for a t that is the same in a wavefront's 64 lanes, all of which are here: one load for 64 sequences, two for 4096
+    __device__ __forceinline__ int of_one(int t) const
+    {
+        if (!starts) return of(t);
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64;
+            const long long at = lo + (long long)step * ((threadIdx.x & 63) + 1);
+            lo += step * __popcll(__ballot(at < hi && starts[at < hi ? at : lo] <= t));
+            hi = hi - lo > step ? lo + step : hi;
+        }
+        return lo;
+    }
 };
 
 // ---- elementwise -----------------------------------------------------------------------------------

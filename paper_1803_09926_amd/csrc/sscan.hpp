@@ -90,7 +90,7 @@ __device__ __forceinline__ uint32_t first_tokens(const Sequences &seq, int t0, i
     return (uint32_t)__ballot(there && lane < n && seq.start(of) == t);
 }
 __device__ __forceinline__ int sequence_of(int of, int t) { return __builtin_amdgcn_readlane(of, t & 63); }   // of token t from t0, -1 the one before it
-__device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of(t)) == t; }
+__device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of_one(t)) == t; }
 
 // What `count` parts from `first` on (in the direction of `step`) leave at the end of a row of them: v = e[first] + decay(first) * (e[next] + ...), with the
 // decay over a part exp(A * its sum of step sizes).  Six parts are asked for at a time: eight take registers that the kernel behind it wants.

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
     const int t0 = (int)((long long)part * g.part);
     int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
     // only the sequence that the part before ends in hands anything back
-    const int s0 = g.seq.of(t0), behind = g.seq.start(s0 + 1);
+    const int s0 = g.seq.of_one(t0), behind = g.seq.start(s0 + 1);
     if (t1 <= t0 || g.seq.start(s0) == t0) return;
     if (behind > t0 && behind < t1) t1 = behind;
 
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
         pc -= TOKENS * g.cs;
     };
     // the sequence of the tile's first token, looked for again where a tile lies before it
-    int s = g.seq.of(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
+    int s = g.seq.of_one(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
     float total = 0.f;
     load(last);
     for (int tile = last; tile >= t0; tile -= TOKENS) {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
             const int e = threadIdx.x + 256 * i;
             if (e < TOKENS * STATES) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
         }
-        if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
+        if (tile < head) { s = g.seq.of_one(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
         const bool any = head >= tile || behind_it < tile + TOKENS;
         int of = 0;
         const uint32_t firsts = any ? first_tokens(g.seq, tile, TOKENS, t1, of) : 0u;
@@ -178,10 +178,11 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         dskip[i] = dbias[i] = 0.f;
     }
 
+    // the sequence of the tile's first token, looked for again where a tile lies before it
+    int s = g.seq.of_one(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
     if (out.ends && t1 < g.seq.T) {                                  // what the parts behind hand back to the sequence that goes on there
-        const int end = g.seq.start(g.seq.of(t1 - 1) + 1);
         // (parts whose first token that sequence still has)
-        const long long reach = ((long long)(end < g.seq.T ? end : g.seq.T) - 1) / g.part - at.part;
+        const long long reach = ((long long)(behind_it < g.seq.T ? behind_it : g.seq.T) - 1) / g.part - at.part;
         const int most = g.parts - 1 - at.part;
         gather_parts<LPC>(gr, a2, out.ends, out.sums, g.C, chan, q, valid, at.part + 1, 1, reach < most ? (int)reach : most);
     }
@@ -247,9 +248,6 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         pc -= S::TOKENS * g.cs;
         ph -= (long long)g.C * S::STATES;
     };
-    // the sequence of the tile's first token, looked for again where a tile lies before it
-    int s = g.seq.of(t1 - 1), head = g.seq.start(s), behind_it = g.seq.start(s + 1);
-
     load(last);
     for (int tile = last; tile >= t0; tile -= S::TOKENS) {
         const Ahead<T, S::EACH, WHOLE> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
@@ -283,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
                 reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
             }
         }
-        if (tile < head) { s = g.seq.of(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
+        if (tile < head) { s = g.seq.of_one(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
         const bool any = head >= tile || behind_it < tile + S::TOKENS;
         int of = 0;
         const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1, of) : 0u;

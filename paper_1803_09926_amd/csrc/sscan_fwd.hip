@@ -48,8 +48,8 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     int t0 = (int)((long long)at.part * g.part);
     const int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
     if (ENDS) {                                                       // only what the next part goes on from is asked for
-        if (first_token(g.seq, t1)) return;
-        const int f = g.seq.start(g.seq.of(t1 - 1));
+        const int f = g.seq.start(g.seq.of_one(t1));
+        if (f == t1) return;
         if (f > t0 && f < t1) t0 += (f - t0) / S::TOKENS * S::TOKENS;
     }
 
@@ -101,12 +101,10 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = 0.f;
 
-    if (!ENDS && ends) {                                              // the state that the parts before leave
-        const int f = g.seq.start(g.seq.of(t0));
-        if (f < t0) {
-            const int least = (f < 0 ? 0 : f) / g.part;
-            gather_parts<LPC>(h, a2, ends, sums, g.C, chan, q, valid, at.part - 1, -1, at.part - least);
-        }
+    int s = g.seq.of_one(t0), head = g.seq.start(s), next = g.seq.start(s + 1);    // the sequence of the tile's first token
+    if (!ENDS && ends && head < t0) {                                 // the state that the parts before leave
+        const int least = (head < 0 ? 0 : head) / g.part;
+        gather_parts<LPC>(h, a2, ends, sums, g.C, chan, q, valid, at.part - 1, -1, at.part - least);
     }
 
     // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
@@ -148,7 +146,6 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     };
     load(t0);
 
-    int s = g.seq.of(t0), head = g.seq.start(s), next = g.seq.start(s + 1);    // the sequence of the tile's first token
     float total = 0.f;
     for (int tile = t0; tile < t1; tile += S::TOKENS) {
         float direct[ENDS ? 1 : S::EACH], gate[ENDS ? 1 : S::EACH];    // D * x, and what the gate lets through
@@ -176,7 +173,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
                 }
             }
         }
-        if (tile >= next) { s = g.seq.of(tile); head = g.seq.start(s); next = g.seq.start(s + 1); }
+        if (tile >= next) { s = g.seq.of_one(tile); head = g.seq.start(s); next = g.seq.start(s + 1); }
         const bool any = head == tile || next < tile + S::TOKENS;
         int of = 0;
         const uint32_t firsts = any ? first_tokens(g.seq, tile, S::TOKENS, t1, of) : 0u;
@@ -236,7 +233,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
             if (q == 0) sums[(long long)at.part * g.C + chan] = total;
         }
     } else if (final && (t1 == g.seq.T || first_token(g.seq, t1))) {
-        put_state(final, g.seq.of(t1 - 1));
+        put_state(final, g.seq.of_one(t1 - 1));
     }
 }
 
