@@ -153,6 +153,8 @@ template <typename T, int LPC, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut out)
 {
     typedef BackTile<LPC> S;
+    // Rows that take more than 4 registers each are read twice, before and behind the walk: held meanwhile, they spill.
+    constexpr bool AGAIN = Ahead<T, S::EACH, WHOLE>::WORDS > 4;
     // step sizes, these times x, dv, and sum C h; sum g B and sum r A take the places of the first two
     __shared__ __attribute__((aligned(16))) float steps[S::TOKENS][S::CHANNELS], gains[S::TOKENS][S::CHANNELS], dvs[S::TOKENS][S::CHANNELS],
         ys[S::TOKENS][S::CHANNELS];
@@ -250,7 +252,9 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     };
     load(last);
     for (int tile = last; tile >= t0; tile -= S::TOKENS) {
-        const Ahead<T, S::EACH, WHOLE> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
+        Ahead<T, S::EACH, WHOLE> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
+        const T *const hx = px + S::TOKENS * g.xs, *const hdt = pdt + S::TOKENS * g.dts, *const hdy = pdy + S::TOKENS * g.ys;   // this tile's rows
+        const T *const hz = pz + S::TOKENS * g.zs;
         const float hin[4] = {rh.at(0), rh.at(1), rh.at(2), rh.at(3)};
         const int m = tile + row < t1 ? n : 0;
         float delta[S::EACH];
@@ -372,6 +376,12 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         };
         if (firsts || tile + S::TOKENS > t1) walk(std::true_type());
         else walk(std::false_type());
+        if constexpr (AGAIN) {
+            kx.load(BufView(hx, VIEW_BYTES), ox, m);
+            kdt.load(BufView(hdt, VIEW_BYTES), odt, m);
+            kdy.load(BufView(hdy, VIEW_BYTES), oy, m);
+            kz.load(BufView(hz, VIEW_BYTES), oz, in.z ? m : 0);
+        }
         __syncthreads();
 
         {
