@@ -111,8 +111,9 @@ template <typename T> __device__ __forceinline__ T *from(T *base, uint32_t off) 
 
 // V consecutive elements that are asked for early and used late.  The loads go through a view of the rows, in which a lane that is to have zeros asks for what
 // lies outside: no branch, and so nothing that waits for them before they are used.  WHOLE: V elements are all there or none of them, and aligned to their
-// bytes; otherwise the first n are there, and each is a load of its own.
-template <typename T, int V, bool WHOLE> struct Ahead {
+// bytes; otherwise each is a load of its own, STEP elements from the one before, and those less than n from the first are there.
+template <typename T, int V, bool WHOLE, int STEP = 1> struct Ahead {
+    static_assert(STEP == 1 || !WHOLE, "vectors are of neighbours");
     static constexpr int BYTES = V * (int)sizeof(T), WORDS = WHOLE ? (BYTES + 3) / 4 : V;
     uint32_t w[WORDS];
     __device__ __forceinline__ void load(const BufView &rows, uint32_t off, int n)
@@ -133,7 +134,7 @@ template <typename T, int V, bool WHOLE> struct Ahead {
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const uint32_t at = n > i ? off + i * (uint32_t)sizeof(T) : BufView::OUTSIDE;
+                const uint32_t at = n > i * STEP ? off + i * STEP * (uint32_t)sizeof(T) : BufView::OUTSIDE;
                 if constexpr (sizeof(T) == 2) w[i] = rows.b16(at, 0);
                 else w[i] = rows.b32(at, 0);
             }
@@ -155,7 +156,8 @@ template <typename T, int V, bool WHOLE> struct Ahead {
 };
 // The counterpart for stores, rounded where T is bf16: what is not there is stored outside the view, which does nothing.  No branch here either: the loads
 // behind it would have to wait for all stores, and not for those only that come before them.
-template <typename T, int V, bool WHOLE> __device__ __forceinline__ void store_late(const BufView &rows, uint32_t off, int n, const float (&r)[V])
+template <typename T, int V, bool WHOLE, int STEP = 1>
+__device__ __forceinline__ void store_late(const BufView &rows, uint32_t off, int n, const float (&r)[V])
 {
     constexpr int BYTES = V * (int)sizeof(T);
     if constexpr (WHOLE && BYTES >= 4) {
@@ -178,7 +180,7 @@ template <typename T, int V, bool WHOLE> __device__ __forceinline__ void store_l
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t at = n > i ? off + i * (uint32_t)sizeof(T) : BufView::OUTSIDE;
+            const uint32_t at = n > i * STEP ? off + i * STEP * (uint32_t)sizeof(T) : BufView::OUTSIDE;
             if constexpr (sizeof(T) == 4) rows.st32<false>(__float_as_uint(r[i]), at, 0);
             else __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(r[i]), rows.rsrc, (int)at, 0, 0);
         }

@@ -44,7 +44,8 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
     const int lane = threadIdx.x & 63, q = lane % LPC, wv = threadIdx.x >> 6;
     const int mine = wv * (64 / LPC) + lane / LPC, in_group = at.block * CHANNELS + mine, chan = at.group * g.per_group + in_group;
     const bool valid = in_group < g.per_group;
-    const int row = threadIdx.x / LANES, col = threadIdx.x % LANES * EACH;
+    constexpr int STEP = WHOLE ? 1 : LANES;                         // between a lane's channels: alone they are loads of their own, next to other lanes'
+    const int row = threadIdx.x / LANES, col = threadIdx.x % LANES * (WHOLE ? EACH : 1);
     const int first_chan = at.group * g.per_group + at.block * CHANNELS + col, n = g.per_group - at.block * CHANNELS - col;
     const int t0 = (int)((long long)part * g.part);
     int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
@@ -57,14 +58,14 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
 #pragma unroll
     for (int i = 0; i < 4; ++i) a2[i] = valid && 4 * q + i < g.N ? in.A[(long long)chan * g.N + 4 * q + i] * LOG2E : 0.f;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) bias[i] = in.dt_bias && i < n ? in.dt_bias[first_chan + i] : 0.f;
+    for (int i = 0; i < EACH; ++i) bias[i] = in.dt_bias && i * STEP < n ? in.dt_bias[first_chan + i * STEP] : 0.f;
 
     // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
     constexpr uint32_t W = sizeof(T);
     const uint32_t odt = ((uint32_t)row * (uint32_t)g.dts + first_chan) * W, oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W;
     const uint32_t oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
     const int last = t0 + (t1 - t0 - 1) / TOKENS * TOKENS;             // the tile that comes first
-    Ahead<T, EACH, WHOLE> rdt, rz, rdy;
+    Ahead<T, EACH, WHOLE, STEP> rdt, rz, rdy;
     Ahead<T, 1, true> rc[SHARED];
     // the rows of the tile that is loaded next
     const T *pdt = (const T *)in.dt + (long long)last * g.dts, *pdy = (const T *)in.dy + (long long)last * g.ys;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
             for (int i = 0; i < EACH; ++i) { const float zv = rz.at(i); dv[i] *= zv * sigmoid(zv); }
         }
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) { steps[row][col + i] = d[i]; dvs[row][col + i] = dv[i]; }
+        for (int i = 0; i < EACH; ++i) { steps[row][col + i * STEP] = d[i]; dvs[row][col + i * STEP] = dv[i]; }
 #pragma unroll
         for (int i = 0; i < SHARED; ++i) {
             const int e = threadIdx.x + 256 * i;
@@ -153,8 +154,6 @@ template <typename T, int LPC, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut out)
 {
     typedef BackTile<LPC> S;
-    // Rows that take more than 4 registers each are read twice, before and behind the walk: held meanwhile, they spill.
-    constexpr bool AGAIN = Ahead<T, S::EACH, WHOLE>::WORDS > 4;
     // step sizes, these times x, dv, and sum C h; sum g B and sum r A take the places of the first two
     __shared__ __attribute__((aligned(16))) float steps[S::TOKENS][S::CHANNELS], gains[S::TOKENS][S::CHANNELS], dvs[S::TOKENS][S::CHANNELS],
         ys[S::TOKENS][S::CHANNELS];
@@ -164,7 +163,10 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     const int lane = threadIdx.x & 63, q = lane % LPC, wv = threadIdx.x >> 6;
     const int mine = wv * (64 / LPC) + lane / LPC, in_group = at.block * S::CHANNELS + mine, chan = at.group * g.per_group + in_group;
     const bool valid = in_group < g.per_group;
-    const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * S::EACH;
+    constexpr int STEP = WHOLE ? 1 : S::LANES;                         // between a lane's channels: alone they are loads of their own, next to other lanes'
+    const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * (WHOLE ? S::EACH : 1);
+    // Rows that take more than 4 registers each are read twice, before and behind the walk: held meanwhile, they spill.
+    constexpr bool AGAIN = Ahead<T, S::EACH, WHOLE, STEP>::WORDS > 4;
     const int first_chan = at.group * g.per_group + at.block * S::CHANNELS + col, n = g.per_group - at.block * S::CHANNELS - col;
     const int t0 = (int)((long long)at.part * g.part), t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
     if (t1 <= t0) return;
@@ -175,8 +177,8 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     float bias[S::EACH], skip[S::EACH], dskip[S::EACH], dbias[S::EACH];
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) {
-        bias[i] = in.dt_bias && i < n ? in.dt_bias[first_chan + i] : 0.f;
-        skip[i] = in.D && i < n ? in.D[first_chan + i] : 0.f;
+        bias[i] = in.dt_bias && i * STEP < n ? in.dt_bias[first_chan + i * STEP] : 0.f;
+        skip[i] = in.D && i * STEP < n ? in.D[first_chan + i * STEP] : 0.f;
         dskip[i] = dbias[i] = 0.f;
     }
 
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     const uint32_t oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W, oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
     const uint32_t oh = (uint32_t)(mine * S::STATES + 4 * q) * 4;    // from the block's first channel
     const int last = t0 + (t1 - t0 - 1) / S::TOKENS * S::TOKENS;       // the tile that comes first
-    Ahead<T, S::EACH, WHOLE> rx, rdt, rz, rdy;
+    Ahead<T, S::EACH, WHOLE, STEP> rx, rdt, rz, rdy;
     Ahead<T, 1, true> rb[S::SHARED], rc[S::SHARED];
     Ahead<float, 4, true> rh;
     // the rows of the tile that is loaded next, and of the one that is written next
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     };
     load(last);
     for (int tile = last; tile >= t0; tile -= S::TOKENS) {
-        Ahead<T, S::EACH, WHOLE> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
+        Ahead<T, S::EACH, WHOLE, STEP> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
         const T *const hx = px + S::TOKENS * g.xs, *const hdt = pdt + S::TOKENS * g.dts, *const hdy = pdy + S::TOKENS * g.ys;   // this tile's rows
         const T *const hz = pz + S::TOKENS * g.zs;
         const float hin[4] = {rh.at(0), rh.at(1), rh.at(2), rh.at(3)};
@@ -272,9 +274,9 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
             }
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
-                steps[row][col + i] = delta[i];
-                gains[row][col + i] = delta[i] * kx.at(i);
-                dvs[row][col + i] = dv[i];
+                steps[row][col + i * STEP] = delta[i];
+                gains[row][col + i * STEP] = delta[i] * kx.at(i);
+                dvs[row][col + i * STEP] = dv[i];
             }
         }
 #pragma unroll
@@ -393,15 +395,15 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
                 for (int i = 0; i < S::EACH; ++i) {
                     const float zv = kz.at(i), sz = sigmoid(zv);
-                    dz[i] = dv[i] * fmaf(skip[i], kx.at(i), ys[row][col + i]) * (sz + zv * sz * (1.f - sz));
+                    dz[i] = dv[i] * fmaf(skip[i], kx.at(i), ys[row][col + i * STEP]) * (sz + zv * sz * (1.f - sz));
                     dv[i] *= zv * sz;
                 }
             }
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
-                const float gb = steps[row][col + i];
+                const float gb = steps[row][col + i * STEP];
                 dx[i] = fmaf(skip[i], dv[i], delta[i] * gb);
-                dd[i] = fmaf(kx.at(i), gb, gains[row][col + i]);
+                dd[i] = fmaf(kx.at(i), gb, gains[row][col + i * STEP]);
             }
             if (g.softplus) {
 #pragma unroll
@@ -413,9 +415,9 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
                 dskip[i] += counts ? dv[i] * kx.at(i) : 0.f;
                 dbias[i] += counts ? dd[i] : 0.f;
             }
-            store_late<T, S::EACH, WHOLE>(BufView(pdx, VIEW_BYTES), ox, m, dx);
-            store_late<T, S::EACH, WHOLE>(BufView(pddt, VIEW_BYTES), odt, m, dd);
-            store_late<T, S::EACH, WHOLE>(BufView(pdz, VIEW_BYTES), oz, in.z ? m : 0, dz);
+            store_late<T, S::EACH, WHOLE, STEP>(BufView(pdx, VIEW_BYTES), ox, m, dx);
+            store_late<T, S::EACH, WHOLE, STEP>(BufView(pddt, VIEW_BYTES), odt, m, dd);
+            store_late<T, S::EACH, WHOLE, STEP>(BufView(pdz, VIEW_BYTES), oz, in.z ? m : 0, dz);
             const BufView to(pshared, VIEW_BYTES);
             const int there = (t1 - tile) * 2 * S::STATES;
 #pragma unroll
@@ -441,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < S::EACH; ++i) { steps[row][col + i] = dskip[i]; gains[row][col + i] = dbias[i]; }
+    for (int i = 0; i < S::EACH; ++i) { steps[row][col + i * STEP] = dskip[i]; gains[row][col + i * STEP] = dbias[i]; }
     __syncthreads();
     for (int c = threadIdx.x; c < S::CHANNELS; c += 256) {
         const int k = at.block * S::CHANNELS + c;

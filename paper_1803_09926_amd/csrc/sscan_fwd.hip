@@ -43,7 +43,8 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     const int mine = wv * (64 / LPC) + lane / LPC, in_group = at.block * S::CHANNELS + mine, chan = at.group * g.per_group + in_group;
     const bool valid = in_group < g.per_group;
     // the lane's token and channels in what is elementwise
-    const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * S::EACH;
+    constexpr int STEP = WHOLE ? 1 : S::LANES;                         // between a lane's channels: alone they are loads of their own, next to other lanes'
+    const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * (WHOLE ? S::EACH : 1);
     const int first_chan = at.group * g.per_group + at.block * S::CHANNELS + col, n = g.per_group - at.block * S::CHANNELS - col;
     int t0 = (int)((long long)at.part * g.part);
     const int t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
@@ -59,8 +60,8 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     float bias[S::EACH], skip[S::EACH];
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) {
-        bias[i] = dt_bias && i < n ? dt_bias[first_chan + i] : 0.f;
-        skip[i] = !ENDS && D && i < n ? D[first_chan + i] : 0.f;
+        bias[i] = dt_bias && i * STEP < n ? dt_bias[first_chan + i * STEP] : 0.f;
+        skip[i] = !ENDS && D && i * STEP < n ? D[first_chan + i * STEP] : 0.f;
     }
 
     // a sequence's row of [sequences,C,N]; rare, so that its address is not to be held in registers meanwhile
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     constexpr uint32_t W = sizeof(T);
     const uint32_t ox = ((uint32_t)row * (uint32_t)g.xs + first_chan) * W, odt = ((uint32_t)row * (uint32_t)g.dts + first_chan) * W;
     const uint32_t oz = ((uint32_t)row * (uint32_t)g.zs + first_chan) * W, oy = ((uint32_t)row * (uint32_t)g.ys + first_chan) * W;
-    Ahead<T, S::EACH, WHOLE> rx, rdt, rz;
+    Ahead<T, S::EACH, WHOLE, STEP> rx, rdt, rz;
     Ahead<T, 1, true> rb[S::SHARED], rc[S::SHARED];
     // the rows of the tile that is loaded next, moved on by additions: a product of 64 bits for each of them and tile took 60 scalar instructions
     const T *px = x + (long long)t0 * g.xs, *pdt = dt + (long long)t0 * g.dts, *pz = !ENDS && z ? z + (long long)t0 * g.zs : x;
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
                 }
             }
 #pragma unroll
-            for (int i = 0; i < S::EACH; ++i) { steps[row][col + i] = d[i]; gains[row][col + i] = d[i] * rx.at(i); }
+            for (int i = 0; i < S::EACH; ++i) { steps[row][col + i * STEP] = d[i]; gains[row][col + i * STEP] = d[i] * rx.at(i); }
 #pragma unroll
             for (int i = 0; i < S::SHARED; ++i) {
                 const int e = threadIdx.x + 256 * i;
@@ -220,10 +221,10 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
 #pragma unroll
             for (int j = 0; j < LPC; ++j)
 #pragma unroll
-                for (int i = 0; i < S::EACH; ++i) o[i] += shares[ENDS ? 0 : row][j][ENDS ? 0 : col + i];
+                for (int i = 0; i < S::EACH; ++i) o[i] += shares[ENDS ? 0 : row][j][ENDS ? 0 : col + i * STEP];
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) o[i] *= gate[ENDS ? 0 : i];
-            store_late<T, S::EACH, WHOLE>(BufView(py, VIEW_BYTES), oy, m, o);
+            store_late<T, S::EACH, WHOLE, STEP>(BufView(py, VIEW_BYTES), oy, m, o);
             py += S::TOKENS * g.ys;
         }
     }
