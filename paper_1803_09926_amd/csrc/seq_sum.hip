@@ -6,8 +6,8 @@ namespace dwc {
 namespace {
 
 // A block adds COLUMNS neighbouring columns; 64 / COLUMNS * WAVES rows of lanes take every so many partials each, and their sums are added in LDS in turn.
-// Bound by the latency of the reads, which are a few per cent of what the first stage reads: many partials take many lanes a column (1024 partials
-// of 3072 columns: 13.8 us with four lanes a column, 6.2 with 64).
+// Bound by the latency of the reads, which are a few per cent of what the first stage reads: many partials take many lanes a column (the
+// 1024 of a norm of 1536 channels: 13.8 us with four lanes a column, 6.2 with 64; its 512 now 4.7).
 template <int COLUMNS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_sum_partials(const float *__restrict__ partials, int parts, long long n0, long long n1, long long n,
                                                              float *out0, float *out1, float *out2)
