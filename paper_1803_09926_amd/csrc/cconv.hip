@@ -2,7 +2,7 @@
 //
 // A lane owns V neighbouring channels and walks down a strip of tokens with the last K - 1 rows in registers, so that each row is read once a strip (and
 // K - 1 rows more at its head).  All three passes are bound by memory: forward 8191 x 1536 in bf16 takes 13 us, 3.9 TB/s, where a copy of these rows takes
-// 10.5 (strips are short there, and a third of the rows come twice); backward 16384 x 1024 in fp32 47 us, 4.3 TB/s, and 4.7 for the sum of the partials,
+// 10.5 (strips are 16 tokens there, and three rows of each come twice); backward 16384 x 1024 in fp32 47 us, 4.3 TB/s, and 4.7 for the sum of the partials,
 // where an addition of tensors of that size takes 35.  At a sequence's first token the rows in registers are replaced by the sequence's
 // rows of init, or zeros: what an earlier sequence holds, infinities and NaN among it, is never multiplied by anything of a later one.
 //

@@ -342,6 +342,16 @@ def test_scan_however_it_is_split(gpu_lib, blocks, most, N):
         _scan_case("bf16", 70, N, 2, EVEN(290, 1), False, False, seed=N + 2)
 
 
+@pytest.mark.parametrize("S,T", [(60, 64), (65, 150), (130, 40), (4200, 150)])
+@pytest.mark.parametrize("C,N", [(24, 16), (75, 5)])
+def test_scan_of_more_sequences_than_lanes(gpu_lib, S, T, C, N):
+    """Sequences of any lengths, most of them empty where they are many; both with one part and with a tile a part."""
+    bounds = [0] + sorted(np.random.default_rng(S).integers(0, T + 1, S - 1).tolist()) + [T]
+    for blocks in (1, 4096):
+        with dw.tuning_overrides({"DWCONV_TUNE_SSCAN_FWD_BLOCKS": blocks, "DWCONV_TUNE_SSCAN_BWD_BLOCKS": blocks}):
+            _scan_case("f32", C, N, 1, bounds, True, True, seed=S)
+
+
 def test_scan_states_and_gradients_that_hardly_decay_and_that_vanish(gpu_lib):
     """Decays next to 1 and far below the smallest number, step sizes from 1e-6 to 20: the parts' products and the kept states hold either way."""
     m = Made(3, "f32")
