@@ -20,9 +20,6 @@ namespace {
 template <int LPC> struct BackTile {
     static constexpr int CHANNELS = 256 / LPC, TOKENS = KEPT_EVERY, EACH = TOKENS / LPC, STATES = 4 * LPC, LANES = 256 / TOKENS;
     static constexpr int SHARED = (TOKENS * STATES + 255) / 256;
-    // of the last tokens the decays stay in registers for the way back, as many as 256 registers hold in both types: of none, 6 and 12 tokens 206, 197,
-    // 192 us (8192 x 1536 in bf16; 12 of fp32 spill, and so do any of 8 states)
-    static constexpr int HELD = LPC == 4 || LPC == 8 ? 10 : 0;
 };
 
 struct BackIn {
@@ -170,6 +167,10 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     const int row = threadIdx.x / S::LANES, col = threadIdx.x % S::LANES * (WHOLE ? S::EACH : 1);
     // Rows that take more than 4 registers each are read twice, before and behind the walk: held meanwhile, they spill.
     constexpr bool AGAIN = Ahead<T, S::EACH, WHOLE, STEP>::WORDS > 4;
+    // Of the tile's last tokens the decays stay in registers for the way back, as many as 256 registers hold: of none, 6 and 12 tokens 206, 197, 192 us (8192 x
+    // 1536 x 16 in bf16).  What spills is slower: 12 in fp32 331 us both ways for 10's 330; 12 of 32 states 304 for 11's 302 (bf16), 318 for 10's 308 (fp32); 10
+    // where channels are read one by one 364 for 6's 346 (1533 of them).
+    constexpr int HELD = LPC == 4 ? (!WHOLE ? 6 : sizeof(T) == 4 ? 10 : 12) : LPC == 8 ? (WHOLE && sizeof(T) == 2 ? 11 : 10) : 0;
     const int first_chan = at.group * g.per_group + at.block * S::CHANNELS + col, n = g.per_group - at.block * S::CHANNELS - col;
     const int t0 = (int)((long long)at.part * g.part), t1 = g.seq.T - t0 < g.part ? g.seq.T : t0 + g.part;
     if (t1 <= t0) return;
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 
         auto walk = [&](auto special) {
             constexpr bool SPECIAL = decltype(special)::value;
-            float h[S::TOKENS][4], decays[S::HELD > 0 ? S::HELD : 1][4], sums[LPC], more[LPC];
+            float h[S::TOKENS][4], decays[HELD > 0 ? HELD : 1][4], sums[LPC], more[LPC];
 #pragma unroll
             for (int t = 0; t < S::TOKENS; ++t) {
                 const float d = steps[t][mine], gain = gains[t][mine];
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float decay = exp2_fast(d * a2[i]);
-                    if (t >= S::TOKENS - S::HELD) decays[t >= S::TOKENS - S::HELD ? t - (S::TOKENS - S::HELD) : 0][i] = decay;
+                    if (t >= S::TOKENS - HELD) decays[t >= S::TOKENS - HELD ? t - (S::TOKENS - HELD) : 0][i] = decay;
                     h[t][i] = fmaf(decay, before[i], gain * bv[i]);
                     sum = fmaf(cv[i], h[t][i], sum);
                 }
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
                         db[i] = gr[i] * gain;
                         dc[i] = dv * h[t][i];
                         sg = fmaf(gr[i], bv[i], sg);
-                        gr[i] *= t >= S::TOKENS - S::HELD ? decays[t >= S::TOKENS - S::HELD ? t - (S::TOKENS - S::HELD) : 0][i] : exp2_fast(d * a2[i]);
+                        gr[i] *= t >= S::TOKENS - HELD ? decays[t >= S::TOKENS - HELD ? t - (S::TOKENS - HELD) : 0][i] : exp2_fast(d * a2[i]);
                         const float r = gr[i] * before[i];
                         sa = fmaf(r, a2[i], sa);
                         dA[i] = fmaf(r, d, dA[i]);
