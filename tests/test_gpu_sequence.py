@@ -400,6 +400,39 @@ def test_scan_carries_nothing_across_sequences(gpu_lib):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scan_offsets_beyond_32_bits(gpu_lib, dtype):
+    """Rows as far apart as they may be, which the passes read and write as they do dense ones."""
+    T, C, N, far = 75, 24, 16, 1 << 25
+    m = Made(9, dtype)
+    on = {k: m.dev(a, k in ("x", "dt", "z", "B", "C")) for k, a in _scan_made(m, T, C, N, 1).items()}
+    on["dy"] = m.dev(m.host((T, C)))
+    read, written = (torch.empty((T - 1) * far + 256, dtype=TORCH[dtype], device="cuda") for _ in range(2))
+    results = []
+    for stride in (None, far):
+        d = dw.sscan_desc(T, C, N, 1, 1, DTYPE[dtype], True, *[stride] * 6)
+        rows, column = dict(on), 0
+        if stride:
+            for k in ("x", "dt", "z", "B", "C", "dy"):
+                width = on[k].numel() // T
+                rows[k] = read.as_strided((T, width), (far, 1), column).copy_(on[k].reshape(T, width))
+                column += width
+        outs, column = {}, 0
+        for k, width in (("y", C), ("dx", C), ("ddt", C), ("dz", C), ("dB", N), ("dC", N)):
+            outs[k] = written.as_strided((T, width), (far, 1), column) if stride else torch.empty(T, width, dtype=TORCH[dtype], device="cuda")
+            column += width
+        sums = {k: torch.empty_like(on[a]) for k, a in (("dA", "A"), ("dD", "D"), ("ddt_bias", "dt_bias"))}
+        call = (d, rows["x"], rows["dt"], on["A"], rows["B"], rows["C"])
+        more = {"D": on["D"], "z": rows["z"], "dt_bias": on["dt_bias"]}
+        kept = torch.empty(dw.sscan_kept_bytes(d) // 4, device="cuda")
+        dw.sscan_fwd(*call, outs["y"], _space(dw.sscan_fwd_workspace_bytes(d)), kept=kept, **more)
+        dw.sscan_bwd(*call, kept, rows["dy"], outs["dx"], outs["ddt"], sums["dA"], outs["dB"], outs["dC"], _space(dw.sscan_bwd_workspace_bytes(d)),
+                     dD=sums["dD"], dz=outs["dz"], ddt_bias=sums["ddt_bias"], **more)
+        results.append({k: t.contiguous() for k, t in {**outs, **sums}.items()})
+    for k, dense in results[0].items():
+        assert torch.isfinite(dense).all() and torch.equal(dense, results[1][k]), k
+
+
 def test_scan_of_no_tokens(gpu_lib):
     m = Made(2, "f32")
     C, N = 20, 5
