@@ -446,10 +446,17 @@ template <typename T> hipError_t launch_step(const cconv_desc *d, const cconv_te
 {
     const int vectors = cdiv(d->C, CHANNELS);
     const Launch l = {vectors, 64, 1, d->T, (unsigned)cdiv(vectors, 64)};
-    if (!launchable(l.down * l.across, 64)) return hipErrorInvalidValue;
+    const long long most = most_blocks(64) / l.across;                // rows of one launch
     return with_taps(d->K, [&](auto k) {
-        hipLaunchKernelGGL((k_cconv_step<T, decltype(k)::value, CHANNELS>), dim3((unsigned)(l.down * l.across)), dim3(64), 0, stream,
-                           geometry(d, l, nullptr), (const T *)t->x, (const T *)t->w, (const T *)t->b, (const int32_t *)t->slots, (T *)t->state, (T *)t->y);
+        constexpr int K = decltype(k)::value;
+        for (long long row = 0; row < d->T; row += most) {
+            const long long rows = d->T - row < most ? d->T - row : most, own = t->slots ? 0 : row;     // the first slot, where rows have their own number
+            Conv g = geometry(d, l, nullptr);
+            g.seq.n -= (int)own;
+            hipLaunchKernelGGL((k_cconv_step<T, K, CHANNELS>), dim3((unsigned)(rows * l.across)), dim3(64), 0, stream, g, (const T *)t->x + row * d->x_stride,
+                               (const T *)t->w, (const T *)t->b, t->slots ? (const int32_t *)t->slots + row : nullptr,
+                               (T *)t->state + own * (K - 1) * d->C, (T *)t->y + row * d->y_stride);
+        }
     });
 }
 

@@ -242,6 +242,7 @@ int validate(const lnorm_desc *d)
     if (d->dtype != DWCONV_F32 && d->dtype != DWCONV_BF16) return DWCONV_ERR_BAD_ENUM;
     if (d->T < 0 || d->C < 1 || !(d->eps >= 0.f)) return DWCONV_ERR_BAD_DIM;
     if (d->C > LNORM_MAX_C) return DWCONV_ERR_UNSUPPORTED;
+    if (d->T > SEQOPS_MAX_T) return DWCONV_ERR_TOO_LARGE;
     return DWCONV_OK;
 }
 
@@ -305,10 +306,16 @@ template <typename T> hipError_t launch_fwd(const lnorm_desc *d, const lnorm_ten
     const Team team = fwd_team(d->C);
     auto launch = [&](auto shape) {
         typedef decltype(shape) S;
+        constexpr int TEAMS = S::BLOCK / S::TEAM;
+        constexpr long long MOST = most_blocks(S::BLOCK) * TEAMS;      // rows
         auto run = [&](auto whole) {
-            hipLaunchKernelGGL((k_lnorm_fwd<T, S::TEAM, V, S::VECTORS, S::BLOCK, decltype(whole)::value>), dim3((unsigned)cdiv(d->T, S::BLOCK / S::TEAM)),
-                               dim3(S::BLOCK), 0, stream, d->T, d->C, d->eps, 1.f / (float)d->C, (const T *)t->x, (const T *)t->residual, (const T *)t->w,
-                               (const T *)t->b, (T *)t->y, (T *)t->total, (float *)t->mean, (float *)t->rstd);
+            for (long long row = 0; row < d->T; row += MOST) {
+                const int rows = (int)(d->T - row < MOST ? d->T - row : MOST);
+                auto at = [&](const void *p) { return p ? (const T *)p + row * d->C : nullptr; };
+                hipLaunchKernelGGL((k_lnorm_fwd<T, S::TEAM, V, S::VECTORS, S::BLOCK, decltype(whole)::value>), dim3((unsigned)cdiv(rows, TEAMS)), dim3(S::BLOCK),
+                                   0, stream, rows, d->C, d->eps, 1.f / (float)d->C, at(t->x), at(t->residual), (const T *)t->w, (const T *)t->b,
+                                   (T *)at(t->y), (T *)at(t->total), t->mean ? (float *)t->mean + row : nullptr, t->rstd ? (float *)t->rstd + row : nullptr);
+            }
         };
         if (whole_rows(d, {t->x, t->residual, t->w, t->b, t->y, t->total})) run(std::true_type());
         else run(std::false_type());

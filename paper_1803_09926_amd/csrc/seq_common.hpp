@@ -267,6 +267,8 @@ hipError_t launch_sum_partials(const float *partials, int parts, long long n0, l
                                hipStream_t stream);
 
 // ---- host ------------------------------------------------------------------------------------------
+// The most blocks of one launch, which has fewer than 2^32 lanes.  What takes more of them goes in several launches.
+constexpr long long most_blocks(int threads) { return ((1ll << 32) - 1) / threads; }
 inline bool unaligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline bool unaligned_to(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DWCONV_F32 ? 3u : 1u)) != 0; }
 inline bool unaligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }

@@ -5,17 +5,17 @@ namespace dwc {
 
 namespace {
 
-// A block adds COLUMNS neighbouring columns; 64 / COLUMNS * WAVES rows of lanes take every so many partials each, and their sums are added in LDS in turn.
+// A block adds COLUMNS neighbouring columns, block 0 those from column `first` on; 64 / COLUMNS * WAVES rows of lanes take every so many partials each, and their sums are added in LDS in turn.
 // Bound by the latency of the reads, which are a few per cent of what the first stage reads: many partials take many lanes a column (the
 // 1024 of a norm of 1536 channels: 13.8 us with four lanes a column, 6.2 with 64; its 512 now 4.7).
 template <int COLUMNS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_sum_partials(const float *__restrict__ partials, int parts, long long n0, long long n1, long long n,
-                                                             float *out0, float *out1, float *out2)
+__global__ __launch_bounds__(64 * WAVES) void k_sum_partials(const float *__restrict__ partials, int parts, long long first, long long n0, long long n1,
+                                                             long long n, float *out0, float *out1, float *out2)
 {
     constexpr int ROWS = 64 / COLUMNS * WAVES;
     __shared__ double sums[ROWS][COLUMNS];
     const int row = threadIdx.x / COLUMNS, col = threadIdx.x % COLUMNS;
-    const long long i = (long long)blockIdx.x * COLUMNS + col;
+    const long long i = first + (long long)blockIdx.x * COLUMNS + col;
     double s = 0.0;
     if (i < n) {
         const float *p = partials + i;
@@ -48,10 +48,14 @@ hipError_t launch_sum_partials(const float *partials, int parts, long long n0, l
 {
     if (n == 0) return hipSuccess;
     const bool many = parts >= 128;
-    const long long blocks = (n + (many ? 15 : 63)) / (many ? 16 : 64);
-    if (!launchable(blocks, many ? 1024 : 256)) return hipErrorInvalidValue;
-    if (many) hipLaunchKernelGGL((k_sum_partials<16, 16>), dim3((unsigned)blocks), dim3(1024), 0, stream, partials, parts, n0, n1, n, out0, out1, out2);
-    else hipLaunchKernelGGL((k_sum_partials<64, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, partials, parts, n0, n1, n, out0, out1, out2);
+    const int columns = many ? 16 : 64, threads = many ? 1024 : 256;
+    const long long blocks = (n + columns - 1) / columns, most = most_blocks(threads);
+    for (long long b = 0; b < blocks; b += most) {
+        const unsigned now = (unsigned)(blocks - b < most ? blocks - b : most);
+        const long long first = b * columns;
+        if (many) hipLaunchKernelGGL((k_sum_partials<16, 16>), dim3(now), dim3(threads), 0, stream, partials, parts, first, n0, n1, n, out0, out1, out2);
+        else hipLaunchKernelGGL((k_sum_partials<64, 4>), dim3(now), dim3(threads), 0, stream, partials, parts, first, n0, n1, n, out0, out1, out2);
+    }
     return hipGetLastError();
 }
 

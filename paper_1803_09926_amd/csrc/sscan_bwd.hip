@@ -459,11 +459,12 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     }
 }
 
-// dB and dC: the sum over a group's channel blocks, a lane a value, neighbours at neighbouring states.
+// dB and dC: the sum over a group's channel blocks, a lane a value, neighbours at neighbouring states; from value `first` on.
 template <typename T>
-__global__ __launch_bounds__(256) void k_sscan_bwd_shared(Scan g, int states, const float *__restrict__ shared, T *__restrict__ dB, T *__restrict__ dC)
+__global__ __launch_bounds__(256) void k_sscan_bwd_shared(Scan g, int states, long long first, const float *__restrict__ shared, T *__restrict__ dB,
+                                                          T *__restrict__ dC)
 {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long id = first + (long long)blockIdx.x * 256 + threadIdx.x;
     const int k = (int)(id % (2 * g.N)), n = k % g.N, is_c = k / g.N;
     const long long rest = id / (2 * g.N), t = rest / g.groups;
     const int group = (int)(rest % g.groups);
@@ -488,8 +489,8 @@ template <typename T> hipError_t launch(const sscan_desc *d, const sscan_tensors
                            (const float *)t->init, (const float *)t->kept};
         const BackOut out = {t->dx, t->ddt, t->dz, p.carry ? workspace + space.ends : nullptr, p.carry ? workspace + space.sums : nullptr,
                              workspace + space.dA, workspace + space.shared};
-        const long long blocks = (long long)p.channel_blocks * p.parts, last = ((long long)d->T * d->groups * 2 * d->N + 255) / 256;
-        if (!launchable(blocks, 256) || !launchable(last, 256)) return hipErrorInvalidValue;
+        const long long blocks = (long long)p.channel_blocks * p.parts, sums = ((long long)d->T * d->groups * 2 * d->N + 255) / 256;
+        if (!launchable(blocks, 256)) return hipErrorInvalidValue;
         const hipError_t e = with_state_lanes(p.lanes, [&](auto lanes) {
             constexpr int LPC = decltype(lanes)::value;
             auto both = [&](auto whole) {
@@ -500,7 +501,11 @@ template <typename T> hipError_t launch(const sscan_desc *d, const sscan_tensors
             const bool whole = whole_vectors<T>(BackTile<LPC>::EACH, g.per_group, {t->x, t->dt, t->z, t->dy, t->dx, t->ddt, t->dz}, {g.xs, g.dts, g.zs, g.ys});
             if (whole) both(std::true_type());
             else both(std::false_type());
-            hipLaunchKernelGGL(k_sscan_bwd_shared<T>, dim3((unsigned)last), dim3(256), 0, stream, g, 4 * LPC, workspace + space.shared, (T *)t->dB, (T *)t->dC);
+            for (long long b = 0; b < sums; b += most_blocks(256)) {
+                const long long n = sums - b < most_blocks(256) ? sums - b : most_blocks(256);
+                hipLaunchKernelGGL(k_sscan_bwd_shared<T>, dim3((unsigned)n), dim3(256), 0, stream, g, 4 * LPC, b * 256, workspace + space.shared, (T *)t->dB,
+                                   (T *)t->dC);
+            }
         });
         if (e != hipSuccess) return e;
     }

@@ -314,12 +314,16 @@ template <typename T> hipError_t launch_one(const sscan_desc *d, const sscan_ten
     ScanPlan p = {state_lanes(d->N), 1, 1, 1, false};
     Scan g = sscan_geometry(d, p, nullptr);
     g.blocks_of_group = cdiv(d->C, 256 / p.lanes);                     // here: of a row
-    const long long blocks = (long long)d->T * g.blocks_of_group;
-    if (!launchable(blocks, 256)) return hipErrorInvalidValue;
+    const long long most = most_blocks(256) / g.blocks_of_group;       // rows of one launch
     return with_state_lanes(p.lanes, [&](auto lanes) {
-        hipLaunchKernelGGL((k_sscan_step<T, decltype(lanes)::value>), dim3((unsigned)blocks), dim3(256), 0, stream, g, (const T *)t->x, (const T *)t->dt,
-                           (const float *)t->A, (const T *)t->B, (const T *)t->C, (const float *)t->D, (const T *)t->z, (const float *)t->dt_bias,
-                           (const int32_t *)t->slots, (float *)t->state, (T *)t->y);
+        for (long long row = 0; row < d->T; row += most) {
+            const long long rows = d->T - row < most ? d->T - row : most, own = t->slots ? 0 : row;     // the first slot, where rows have their own number
+            g.seq.n = d->sequences - (int)own;
+            hipLaunchKernelGGL((k_sscan_step<T, decltype(lanes)::value>), dim3((unsigned)(rows * g.blocks_of_group)), dim3(256), 0, stream, g,
+                               (const T *)t->x + row * g.xs, (const T *)t->dt + row * g.dts, (const float *)t->A, (const T *)t->B + row * g.bs,
+                               (const T *)t->C + row * g.cs, (const float *)t->D, t->z ? (const T *)t->z + row * g.zs : nullptr, (const float *)t->dt_bias,
+                               t->slots ? (const int32_t *)t->slots + row : nullptr, (float *)t->state + own * d->C * d->N, (T *)t->y + row * g.ys);
+        }
     });
 }
 

@@ -161,3 +161,9 @@ def test_rows_are_recognised_whatever_the_dimensions():
     assert sq._is_rows(torch.zeros(1, 16)[:, :8], 1, 8, 16) and sq._is_rows(torch.zeros(6, 4)[:, :1], 6, 1, 4)
     assert not sq._is_rows(torch.zeros(8, 6).t(), 6, 8, 8) and not sq._is_rows(torch.zeros(6, 7), 6, 8, 8)
     assert not sq._is_rows(torch.zeros(2, 5, 8)[:, :3], 6, 8, 8)
+
+
+def test_more_rows_than_a_norm_takes():
+    assert _call("lnorm_fwd", DESCS["lnorm"](T=0x7fff0001)) == E_LARGE
+    assert _call("lnorm_bwd", DESCS["lnorm"](T=0x7fffffff)) == E_LARGE and dw.lnorm_bwd_workspace_bytes(DESCS["lnorm"](T=0x7fffffff)) == 0
+    assert dw.lnorm_bwd_workspace_bytes(DESCS["lnorm"](T=0x7fff0000)) > 0
