@@ -71,7 +71,8 @@ class TokenMixer:
         return p, p[:, :R] @ self.p["w_dt"], p[:, R:R + N], p[:, R + N:]
 
     def forward(self, hidden, residual=None, starts=None, sequences=1, states=None, keep=False):
-        """(hidden, residual) after the block, for T packed tokens.  states: continues these sequences, and moves them on.  keep: for `backward`."""
+        """(hidden, residual) after the block, for T packed tokens.  states: continues these sequences, and moves them on.  keep: for `backward`, to which
+        the states that the sequences began with are constants."""
         p, T, C = self.p, hidden.shape[0], self.C
         nd, cd, sd = self._descs(T, sequences)
         normed, total = self._new(T, self.M), hidden if residual is None else self._new(T, self.M)
@@ -86,17 +87,18 @@ class TokenMixer:
         kept = torch.empty(max(dw.sscan_kept_bytes(sd), 16), device=u.device, dtype=torch.uint8) if keep else None
         dw.sscan_fwd(sd, u, dt, self._decay(), B, Cm, y, self._space("fwd", dw.sscan_fwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"],
                      starts=starts, init=h, final=new_h, kept=kept)
+        began = (rows.clone(), h.clone()) if keep and states is not None else (None, None)
         if states is not None:
             rows.copy_(new_rows)
             h.copy_(new_h)
         if keep:
-            self.kept = (total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences)
+            self.kept = (total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences, began)
         return y @ p["w_out"], total
 
     def backward(self, dhidden, dresidual=None):
         """From the gradients of what `forward` gave to (the gradient of hidden and residual alike, the gradients by parameter)."""
         p, C, R, N = self.p, self.C, self.R, self.N
-        total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences = self.kept
+        total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences, (rows, h) = self.kept
         T = total.shape[0]
         nd, cd, sd = self._descs(T, sequences)
         g = {k: torch.empty(v.shape, device=v.device) for k, v in p.items() if not k.startswith("w_")}
@@ -105,7 +107,7 @@ class TokenMixer:
         du, ddt, dproj, dxz = self._new(T, C), self._new(T, C), torch.empty_like(proj), torch.empty_like(xz)
         A = self._decay()
         dw.sscan_bwd(sd, u, dt, A, proj[:, R:R + N], proj[:, R + N:], kept, dy, du, ddt, g["A_log"], dproj[:, R:R + N], dproj[:, R + N:],
-                     self._space("bwd", dw.sscan_bwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"], starts=starts, dD=g["D"],
+                     self._space("bwd", dw.sscan_bwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"], starts=starts, init=h, dD=g["D"],
                      dz=dxz[:, C:], ddt_bias=g["dt_bias"])
         g["A_log"].mul_(A)
         g["w_dt"] = proj[:, :R].t() @ ddt
@@ -113,7 +115,7 @@ class TokenMixer:
         g["w_x"] = u.t() @ dproj
         du.addmm_(dproj, p["w_x"].t())
         dw.cconv_bwd(cd, xz[:, :C], p["conv_w"], p["conv_b"], du, dxz[:, :C], g["conv_w"], g["conv_b"],
-                     self._space("conv", dw.cconv_bwd_workspace_bytes(cd)), starts=starts)
+                     self._space("conv", dw.cconv_bwd_workspace_bytes(cd)), starts=starts, init=rows)
         g["w_in"] = normed.t() @ dxz
         dnormed, dx = dxz @ p["w_in"].t(), self._new(T, self.M)
         dw.lnorm_bwd(nd, total, p["norm_w"], mean, rstd, dnormed, dx, g["norm_w"], g["norm_b"], self._space("norm", dw.lnorm_bwd_workspace_bytes(nd)),

@@ -1,0 +1,57 @@
+"""The block of the sequence operators over sequences that continue earlier ones: its gradients, to which the states that they began with are constants, against automatic
+differentiation of plain operations in 64 bits, and the states that it hands on."""
+import pytest
+import torch
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+
+
+def _plain(p, x, residual, bounds, rows, h0):
+    """The block in 64 bits, its sequences behind the rows of the convolution and the states of the scan that they are given: (hidden, residual, rows, states)."""
+    R = p["w_dt"].shape[0]
+    C, N = p["A_log"].shape
+    K = p["conv_w"].shape[0]
+    s = x + residual
+    xz = torch.nn.functional.layer_norm(s, s.shape[1:], p["norm_w"], p["norm_b"], 1e-5) @ p["w_in"]
+    xi, z = xz[:, :C], xz[:, C:]
+    outs, new_rows, new_h = [], [], []
+    for i, (lo, hi) in enumerate(zip(bounds[:-1], bounds[1:])):
+        line = torch.cat([rows[i], xi[lo:hi]])
+        u = torch.nn.functional.silu(sum(p["conv_w"][k] * line[k:k + hi - lo] for k in range(K)) + p["conv_b"])
+        proj = u @ p["w_x"]
+        delta = torch.nn.functional.softplus(proj[:, :R] @ p["w_dt"] + p["dt_bias"])
+        B, Cm = proj[:, R:R + N], proj[:, R + N:]
+        h = h0[i]
+        for t in range(hi - lo):
+            h = torch.exp(delta[t][:, None] * -torch.exp(p["A_log"])) * h + (delta[t] * u[t])[:, None] * B[t]
+            outs.append((h @ Cm[t] + p["D"] * u[t]) * torch.nn.functional.silu(z[lo + t]))
+        new_rows.append(line[hi - lo:])
+        new_h.append(h)
+    return torch.stack(outs) @ p["w_out"], s, torch.stack(new_rows), torch.stack(new_h)
+
+
+@pytest.mark.parametrize("bounds,packed", [([0, 9, 9, 41], True), ([0, 18, 36], False)])
+def test_gradients_of_a_block_that_continues(gpu_lib, bounds, packed):
+    from paper_1803_09926_amd.token_mixer import TokenMixer
+    torch.manual_seed(8)
+    M, S, T = 32, len(bounds) - 1, bounds[-1]
+    block = TokenMixer(M, states=5, dtype=torch.float32, seed=6)
+    x, residual, dh, dr = (torch.randn(T, M) for _ in range(4))
+    rows, h = torch.randn(S, block.K - 1, block.C), torch.randn(S, block.C, block.N)
+    states = (rows.cuda(), h.cuda())
+    starts = torch.tensor(bounds, dtype=torch.int32, device="cuda") if packed else None
+    hidden, total = block.forward(x.cuda(), residual.cuda(), starts, S, states=states, keep=True)
+    dx, grads = block.backward(dh.cuda(), dr.cuda())
+    p = {k: v.detach().cpu().double().requires_grad_() for k, v in block.p.items()}
+    x64 = x.double().requires_grad_()
+    want, s, new_rows, new_h = _plain(p, x64, residual.double(), bounds, rows.double(), h.double())
+    ((want * dh).sum() + (s * dr).sum()).backward()
+    # fp32 products of up to 64 terms in a row of four, each within about 1e-6 of its size: 2e-5 for the chain, 5e-5 for sums over tokens behind it
+    gu.assert_close(gu.to_host(hidden), want.detach().numpy(), 2e-5, "hidden")
+    gu.assert_close(gu.to_host(states[0]), new_rows.detach().numpy(), 2e-5, "the convolution's rows")
+    gu.assert_close(gu.to_host(states[1]), new_h.detach().numpy(), 2e-5, "the scan's states")
+    gu.assert_close(gu.to_host(dx), x64.grad.numpy(), 2e-5, "dx")
+    for k in p:
+        gu.assert_close(gu.to_host(grads[k]), p[k].grad.numpy(), 5e-5, k)
