@@ -88,6 +88,12 @@ Scan sscan_geometry(const sscan_desc *d, const ScanPlan &p, const void *starts)
     Scan g;
     g.C = d->C; g.N = d->N; g.groups = d->groups; g.per_group = d->C / d->groups;
     g.blocks_of_group = p.channel_blocks / d->groups;
+    g.copies = 1;
+    while (2 * g.copies * d->N <= 4 * p.lanes) g.copies *= 2;
+    g.twice = 4 * p.lanes / g.copies - d->N;
+    g.share = 1.f / (float)g.copies;
+    g.by_n = cdiv(1 << 16, d->N);
+    g.by_twice = g.twice ? cdiv(1 << 16, g.twice) : 0;
     g.softplus = d->softplus; g.part = p.part; g.parts = p.parts;
     g.xs = d->x_stride; g.dts = d->dt_stride; g.zs = d->z_stride; g.bs = d->b_stride; g.cs = d->c_stride; g.ys = d->y_stride;
     g.seq = {(const int32_t *)starts, d->sequences, d->T / d->sequences, d->T};

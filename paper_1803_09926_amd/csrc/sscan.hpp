@@ -15,6 +15,8 @@ constexpr int KEPT_EVERY = 16;   // tokens between two states that the forward p
 
 struct Scan {
     int C, N, groups, per_group, blocks_of_group;   // per_group: channels of a group
+    int copies, twice, by_n, by_twice;              // of a channel's states, see state_of; 2^16 / N and 2^16 / twice, rounded up
+    float share;                                    // 1 / copies
     int softplus, part, parts;                      // tokens of a part; parts of the launch
     long long xs, dts, zs, bs, cs, ys;              // row strides
     Sequences seq;
@@ -27,6 +29,19 @@ __device__ __forceinline__ ScanBlock scan_block(const Scan &g)
     const unsigned id = blockIdx.x, per = (unsigned)g.blocks_of_group, rest = id / per;
     return {(int)(rest % (unsigned)g.groups), (int)(id % per), (int)(rest / (unsigned)g.groups)};
 }
+
+// Which state a channel's slot k < 4 * LPC has.  Where N is less than the slots, those behind the first N have states once more: each state is there `copies` times,
+// the largest power of two for which there is room, and the first `twice` of them two times that.  Zeros in these slots would make NaN of an infinite x or step size
+// beside them; a copy has what its state has.  A copy's C is divided by the number of copies, which is exact, and so the sums over slots are those over states.
+// (k % N, and behind the N * copies slots that this reaches, what is left % twice; exact for numbers below 2^8.  Products of 24 bits are one instruction, and as
+// many states as slots are a scalar branch: these lines stand before the first load)
+__device__ __forceinline__ int state_of(const Scan &g, int k)
+{
+    if (g.N * g.copies + g.twice == g.N) return k;
+    const int left = k - g.N * g.copies;
+    return left < 0 ? k - __mul24(__mul24(k, g.by_n) >> 16, g.N) : left - __mul24(__mul24(left, g.by_twice) >> 16, g.twice);
+}
+__device__ __forceinline__ float share_of(const Scan &g, int state) { return state < g.twice ? 0.5f * g.share : g.share; }   // of C, in each of its slots
 
 // log(1 + e) for 0 <= e <= 1: the logarithm of the rounded sum, one instruction, and to first order what the rounding took, which is most of the result where
 // e is small.  Within 2e-7 of the result over 2^-30 <= e <= 1, measured; a series in e / (2 + e) of that accuracy takes twice the instructions.

@@ -22,6 +22,14 @@ template <int LPC> struct BackTile {
     static constexpr int SHARED = (TOKENS * STATES + 255) / 256;
 };
 
+// f(k) for the slots that state n has beside slot n, of `states` of them.
+template <typename F> __device__ __forceinline__ void each_copy(const Scan &g, int states, int n, F f)
+{
+    for (int k = n + g.N; k < g.N * g.copies; k += g.N) f(k);
+    if (n < g.twice)
+        for (int k = n + g.N * g.copies; k < states; k += g.twice) f(k);
+}
+
 struct BackIn {
     const void *x, *dt, *B, *C, *z, *dy;
     const float *A, *D, *dt_bias, *init, *kept;
@@ -56,7 +64,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
 
     float a2[4], gr[4] = {0.f, 0.f, 0.f, 0.f}, bias[EACH];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a2[i] = valid && 4 * q + i < g.N ? in.A[(long long)chan * g.N + 4 * q + i] * LOG2E : 0.f;
+    for (int i = 0; i < 4; ++i) a2[i] = valid ? in.A[(long long)chan * g.N + state_of(g, 4 * q + i)] * LOG2E : 0.f;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) bias[i] = in.dt_bias && i * STEP < n ? in.dt_bias[first_chan + i * STEP] : 0.f;
 
@@ -71,12 +79,12 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
     const T *pdt = (const T *)in.dt + (long long)last * g.dts, *pdy = (const T *)in.dy + (long long)last * g.ys;
     const T *pz = in.z ? (const T *)in.z + (long long)last * g.zs : pdy, *pc = (const T *)in.C + (long long)last * g.cs + (long long)at.group * g.N;
     uint32_t oc[SHARED];
-    int rows[SHARED];                                                // of C, or one that is never there
+    float share[SHARED];                                             // of C that a slot has
 #pragma unroll
     for (int i = 0; i < SHARED; ++i) {
-        const int e = threadIdx.x + 256 * i, r = e / STATES, k = e % STATES;
-        rows[i] = e < TOKENS * STATES && k < g.N ? r : TOKENS;
+        const int e = threadIdx.x + 256 * i, r = e / STATES, k = state_of(g, e % STATES);
         oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+        share[i] = share_of(g, k);
     }
     auto load = [&](int tile) {
         const int left = t1 - tile, m = row < left ? n : 0;
@@ -85,7 +93,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
         rz.load(BufView(pz, VIEW_BYTES), oz, in.z ? m : 0);
         const BufView c(pc, VIEW_BYTES);
 #pragma unroll
-        for (int i = 0; i < SHARED; ++i) rc[i].load(c, oc[i], rows[i] < (left < TOKENS ? left : TOKENS));
+        for (int i = 0; i < SHARED; ++i) rc[i].load(c, oc[i], (int)(threadIdx.x + 256 * i) / STATES < (left < TOKENS ? left : TOKENS));   // (a lane without a value: a row behind the tile)
         pdt -= TOKENS * g.dts;
         pdy -= TOKENS * g.ys;
         pz -= TOKENS * g.zs;
@@ -112,7 +120,7 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_carry(Scan g, BackIn in, Back
 #pragma unroll
         for (int i = 0; i < SHARED; ++i) {
             const int e = threadIdx.x + 256 * i;
-            if (e < TOKENS * STATES) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
+            if (e < TOKENS * STATES) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0) * share[i];
         }
         if (tile < head) { s = g.seq.of_one(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
         const bool any = head >= tile || behind_it < tile + TOKENS;
@@ -157,7 +165,9 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     // step sizes, these times x, dv, and sum C h; sum g B and sum r A take the places of the first two
     __shared__ __attribute__((aligned(16))) float steps[S::TOKENS][S::CHANNELS], gains[S::TOKENS][S::CHANNELS], dvs[S::TOKENS][S::CHANNELS],
         ys[S::TOKENS][S::CHANNELS];
-    __shared__ float4 Bs[S::TOKENS][LPC], Cs[S::TOKENS][LPC];
+    // B, C, and zeros that lanes without a channel have in their place: an infinity there would be NaN in the sums over channels
+    __shared__ float4 shared_rows[4][S::TOKENS][LPC];
+    __shared__ uint32_t states[LPC];                                 // offsets of a lane's four states, 8 bits each: worked out where init is read, 32 times a walk, it is code
     __shared__ float red[5][S::TOKENS][2 * S::STATES];               // dB and dC of each wavefront's channels; what lanes without a sum write
     const ScanBlock at = scan_block(g);
     const int lane = threadIdx.x & 63, q = lane % LPC, wv = threadIdx.x >> 6;
@@ -177,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 
     float a2[4], gr[4] = {0.f, 0.f, 0.f, 0.f}, dA[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a2[i] = valid && 4 * q + i < g.N ? in.A[(long long)chan * g.N + 4 * q + i] * LOG2E : 0.f;
+    for (int i = 0; i < 4; ++i) a2[i] = valid ? in.A[(long long)chan * g.N + state_of(g, 4 * q + i)] * LOG2E : 0.f;
     float bias[S::EACH], skip[S::EACH], dskip[S::EACH], dbias[S::EACH];
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) {
@@ -202,11 +212,12 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
                               : &red[4][0][lane % (2 * S::STATES)];
 
     auto init_of = [&](int s, float (&h)[4]) {
-        int c = chan;                                                // rare: its address is not to be held in registers meanwhile
-        asm volatile("" : "+v"(c));
-        const float *p = in.init + ((long long)s * g.C + c) * g.N + 4 * q;
+        int own = threadIdx.x;                                       // rare: its addresses are not to be held in registers meanwhile
+        asm volatile("" : "+v"(own));
+        const BufView rows(in.init + ((long long)s * g.C + at.group * g.per_group + at.block * S::CHANNELS) * g.N, VIEW_BYTES);
+        const uint32_t four = states[own % LPC], off = in.init && valid ? (uint32_t)(own / LPC * g.N) * 4 : BufView::OUTSIDE;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = in.init && valid && 4 * q + i < g.N ? p[i] : 0.f;
+        for (int i = 0; i < 4; ++i) h[i] = __uint_as_float(rows.b32(off + (four >> 8 * i & 0xff), 0));
     };
 
     // offsets in bytes from a tile's first row: at most 16 rows of SEQOPS_MAX_STRIDE
@@ -226,13 +237,13 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
     T *pdx = (T *)out.dx + (long long)last * g.xs, *pddt = (T *)out.ddt + (long long)last * g.dts, *pdz = in.z ? (T *)out.dz + (long long)last * g.zs : pdx;
     float *pshared = out.shared + ((long long)(at.group * g.blocks_of_group + at.block) * g.seq.T + last) * (2 * S::STATES);
     uint32_t ob[S::SHARED], oc[S::SHARED];
-    int rows[S::SHARED];                                             // of B and C, or one that is never there
+    float share[S::SHARED];                                          // of C that a slot has
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
-        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = e % S::STATES;
-        rows[i] = e < S::TOKENS * S::STATES && k < g.N ? r : S::TOKENS;
+        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = state_of(g, e % S::STATES);
         ob[i] = ((uint32_t)r * (uint32_t)g.bs + k) * W;
         oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+        share[i] = share_of(g, k);
     }
     auto load = [&](int tile) {
         const int left = t1 - tile, m = row < left ? n : 0;
@@ -243,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         const BufView b(pb, VIEW_BYTES), c(pc, VIEW_BYTES);
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
-            const int there = rows[i] < (left < S::TOKENS ? left : S::TOKENS);
+            const int there = (int)(threadIdx.x + 256 * i) / S::STATES < (left < S::TOKENS ? left : S::TOKENS);     // (a lane without a value: a row behind the tile)
             rb[i].load(b, ob[i], there);
             rc[i].load(c, oc[i], there);
         }
@@ -256,6 +267,14 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         pc -= S::TOKENS * g.cs;
         ph -= (long long)g.C * S::STATES;
     };
+    if (threadIdx.x < LPC) {
+        uint32_t four = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) four |= (uint32_t)state_of(g, 4 * threadIdx.x + i) * 4 << 8 * i;
+        states[threadIdx.x] = four;
+    }
+    for (int e = threadIdx.x; e < 2 * S::TOKENS * LPC; e += 256) shared_rows[2][0][e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 *const own_rows = &shared_rows[valid ? 0 : 2][0][q];
     load(last);
     for (int tile = last; tile >= t0; tile -= S::TOKENS) {
         Ahead<T, S::EACH, WHOLE, STEP> kx = rx, kdt = rdt, kz = rz, kdy = rdy;
@@ -287,8 +306,8 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
         for (int i = 0; i < S::SHARED; ++i) {
             const int e = threadIdx.x + 256 * i;
             if (e < S::TOKENS * S::STATES) {
-                reinterpret_cast<float *>(Bs)[e] = rb[i].at(0);
-                reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
+                reinterpret_cast<float *>(shared_rows[0])[e] = rb[i].at(0);
+                reinterpret_cast<float *>(shared_rows[1])[e] = rc[i].at(0) * share[i];
             }
         }
         if (tile < head) { s = g.seq.of_one(tile); head = g.seq.start(s); behind_it = g.seq.start(s + 1); }
@@ -304,7 +323,7 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
             for (int t = 0; t < S::TOKENS; ++t) {
                 const float d = steps[t][mine], gain = gains[t][mine];
-                const float4 b = Bs[t][q], c = Cs[t][q];
+                const float4 b = own_rows[t * LPC], c = own_rows[(S::TOKENS + t) * LPC];
                 const float bv[4] = {b.x, b.y, b.z, b.w}, cv[4] = {c.x, c.y, c.z, c.w};
                 float before[4], sum = 0.f;
 #pragma unroll
@@ -323,15 +342,16 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
                 if (t % LPC == LPC - 1) ys[t - (LPC - 1) + q][mine] = transpose_sum<LPC>(sums, q);
             }
             // Read LDS again on the way back: without these the compiler keeps what it read on the way there, 11 values a token, in registers, and spills.
-            int mine2 = mine, q2 = q;
-            asm volatile("" : "+v"(mine2), "+v"(q2));
+            int mine2 = mine, skipped = 0;
+            asm volatile("" : "+v"(mine2), "+v"(skipped));
+            const float4 *const again = own_rows + skipped;
 #pragma unroll
             for (int t = S::TOKENS - 1; t >= 0; --t) {
                 if (SPECIAL && tile + t >= t1) {                     // behind the last token
                     sums[t % LPC] = more[t % LPC] = 0.f;
                 } else {
                     const float d = steps[t][mine2], gain = gains[t][mine2], dv = dvs[t][mine2];
-                    const float4 b = Bs[t][q2], c = Cs[t][q2];
+                    const float4 b = again[t * LPC], c = again[(S::TOKENS + t) * LPC];
                     const float bv[4] = {b.x, b.y, b.z, b.w}, cv[4] = {c.x, c.y, c.z, c.w};
                     float before[4], db[4], dc[4], sg = 0.f, sa = 0.f;
 #pragma unroll
@@ -396,18 +416,31 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) dv[i] = kdy.at(i);
             if (in.z) {
+                float y[S::EACH];
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) y[i] = ys[row][col + i * STEP];
+                if (in.D) {
+                    asm volatile("");                                // (a branch, not a choice for each)
+#pragma unroll
+                    for (int i = 0; i < S::EACH; ++i) y[i] = fmaf(skip[i], kx.at(i), y[i]);
+                }
 #pragma unroll
                 for (int i = 0; i < S::EACH; ++i) {
                     const float zv = kz.at(i), sz = sigmoid(zv);
-                    dz[i] = dv[i] * fmaf(skip[i], kx.at(i), ys[row][col + i * STEP]) * (sz + zv * sz * (1.f - sz));
+                    dz[i] = dv[i] * y[i] * (sz + zv * sz * (1.f - sz));
                     dv[i] *= zv * sz;
                 }
             }
 #pragma unroll
             for (int i = 0; i < S::EACH; ++i) {
                 const float gb = steps[row][col + i * STEP];
-                dx[i] = fmaf(skip[i], dv[i], delta[i] * gb);
+                dx[i] = delta[i] * gb;
                 dd[i] = fmaf(kx.at(i), gb, gains[row][col + i * STEP]);
+            }
+            if (in.D) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < S::EACH; ++i) dx[i] = fmaf(skip[i], dv[i], dx[i]);
             }
             if (g.softplus) {
 #pragma unroll
@@ -440,15 +473,23 @@ __global__ __launch_bounds__(256, 2) void k_sscan_bwd(Scan g, BackIn in, BackOut
 
     // the part's sums over tokens: [C,N] of A, then [C] of D and [C] of dt_bias
     float *const to = out.dA + (long long)at.part * ((long long)g.C * g.N + 2ll * g.C);
-    if (valid) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * q + i < g.N) to[(long long)chan * g.N + 4 * q + i] = dA[i];
-    }
+    float *const slots = &red[0][0][0];
+    static_assert(S::CHANNELS * S::STATES <= (int)(sizeof red / sizeof(float)), "room for a value of each slot");
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) slots[mine * S::STATES + 4 * q + i] = dA[i];
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) { steps[row][col + i * STEP] = dskip[i]; gains[row][col + i * STEP] = dbias[i]; }
     __syncthreads();
+    if (valid) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = 4 * q + i;
+            if (k >= g.N) continue;
+            each_copy(g, S::STATES, k, [&](int copy) { dA[i] += slots[mine * S::STATES + copy]; });     // (which have their shares of it)
+            to[(long long)chan * g.N + k] = dA[i];
+        }
+    }
     for (int c = threadIdx.x; c < S::CHANNELS; c += 256) {
         const int k = at.block * S::CHANNELS + c;
         if (k >= g.per_group) continue;
@@ -472,8 +513,12 @@ __global__ __launch_bounds__(256) void k_sscan_bwd_shared(Scan g, int states, lo
     const long long step = (long long)g.seq.T * 2 * states;
     const float *p = shared + (long long)group * g.blocks_of_group * step + t * 2 * states + is_c * states + n;
     float sum = 0.f;
+    auto add = [&](int k) {
 #pragma unroll 4
-    for (int b = 0; b < g.blocks_of_group; ++b) sum += p[b * step];
+        for (int b = 0; b < g.blocks_of_group; ++b) sum += p[b * step + k - n];
+    };
+    add(n);
+    if (!is_c) each_copy(g, states, n, add);                         // (dC is the same in all of them)
     if (is_c) stf(dC + t * g.cs + (long long)group * g.N + n, sum);
     else stf(dB + t * g.bs + (long long)group * g.N + n, sum);
 }

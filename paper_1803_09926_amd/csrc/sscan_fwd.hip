@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
 
     float a2[4], h[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a2[i] = valid && 4 * q + i < g.N ? A[(long long)chan * g.N + 4 * q + i] * LOG2E : 0.f;
+    for (int i = 0; i < 4; ++i) a2[i] = valid ? A[(long long)chan * g.N + state_of(g, 4 * q + i)] * LOG2E : 0.f;
     float bias[S::EACH], skip[S::EACH];
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) {
@@ -77,11 +77,11 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
             if (4 * q + i < g.N) p[i] = h[i];
     };
     auto get_state = [&](int s) {
-        int c = chan;
-        asm volatile("" : "+v"(c));
-        const float *p = init + ((long long)s * g.C + c) * g.N + 4 * q;
+        int c = chan, k = 4 * q;
+        asm volatile("" : "+v"(c), "+v"(k));
+        const float *p = init + ((long long)s * g.C + c) * g.N;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = init && valid && 4 * q + i < g.N ? p[i] : 0.f;
+        for (int i = 0; i < 4; ++i) h[i] = init && valid ? p[state_of(g, k + i)] : 0.f;
     };
 
     auto keep_state = [&](int tile) {
@@ -121,13 +121,13 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
     const T *pb = B + (long long)t0 * g.bs + (long long)at.group * g.N, *pc = ENDS ? pb : Cm + (long long)t0 * g.cs + (long long)at.group * g.N;
     T *py = ENDS ? nullptr : y + (long long)t0 * g.ys;
     uint32_t ob[S::SHARED], oc[S::SHARED];
-    int rows[S::SHARED];                                              // of B and C, or one that is never there
+    float share[S::SHARED];                                           // of C that a slot has
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
-        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = e % S::STATES;
-        rows[i] = e < S::TOKENS * S::STATES && k < g.N ? r : S::TOKENS;
+        const int e = threadIdx.x + 256 * i, r = e / S::STATES, k = state_of(g, e % S::STATES);
         ob[i] = ((uint32_t)r * (uint32_t)g.bs + k) * W;
         oc[i] = ((uint32_t)r * (uint32_t)g.cs + k) * W;
+        share[i] = share_of(g, k);
     }
     auto load = [&](int tile) {
         const int left = t1 - tile, m = row < left ? n : 0;
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
         const BufView b(pb, VIEW_BYTES), c(pc, VIEW_BYTES);
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
-            const int in = rows[i] < (left < S::TOKENS ? left : S::TOKENS);
+            const int in = (int)(threadIdx.x + 256 * i) / S::STATES < (left < S::TOKENS ? left : S::TOKENS);    // (a lane without a value: a row behind the tile)
             rb[i].load(b, ob[i], in);
             if (!ENDS) rc[i].load(c, oc[i], in);
         }
@@ -159,7 +159,11 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
             step_sizes(g, d);
             if (!ENDS) {
 #pragma unroll
-                for (int i = 0; i < S::EACH; ++i) { direct[ENDS ? 0 : i] = skip[i] * rx.at(i); gate[ENDS ? 0 : i] = 1.f; }
+                for (int i = 0; i < S::EACH; ++i) { direct[ENDS ? 0 : i] = 0.f; gate[ENDS ? 0 : i] = 1.f; }
+                if (D) {
+#pragma unroll
+                    for (int i = 0; i < S::EACH; ++i) direct[ENDS ? 0 : i] = skip[i] * rx.at(i);
+                }
                 if (z) {
 #pragma unroll
                     for (int i = 0; i < S::EACH; ++i) { const float v = rz.at(i); gate[ENDS ? 0 : i] = v * sigmoid(v); }
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(256, Tile<LPC>::WAVES) void k_sscan_fwd(Scan g, con
                 const int e = threadIdx.x + 256 * i;
                 if (e < S::TOKENS * S::STATES) {
                     reinterpret_cast<float *>(Bs)[e] = rb[i].at(0);
-                    if (!ENDS) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0);
+                    if (!ENDS) reinterpret_cast<float *>(Cs)[e] = rc[i].at(0) * share[i];
                 }
             }
         }
