@@ -108,34 +108,50 @@ __device__ __forceinline__ int sequence_of(int of, int t) { return __builtin_amd
 __device__ __forceinline__ bool first_token(const Sequences &seq, int t) { return seq.start(seq.of_one(t)) == t; }
 
 // What `count` parts from `first` on (in the direction of `step`) leave at the end of a row of them: v = e[first] + decay(first) * (e[next] + ...), with the
-// decay over a part exp(A * its sum of step sizes).  Six parts are asked for at a time: eight take registers that the kernel behind it wants.
-template <int LPC>
-__device__ __forceinline__ void gather_parts(float (&v)[4], const float (&a2)[4], const float *ends, const float *sums, int C, int chan, int q, bool valid,
-                                             int first, int step, int count)
+// decay over a part exp(A * its sum of step sizes), from the farthest part on.
+template <int LPC, bool WIDE>
+__device__ __forceinline__ void gather_parts_as(float (&v)[4], const float (&a2)[4], const float *ends, const float *sums, int C, int chan, int q, bool valid,
+                                                int first, int step, int count)
 {
-    constexpr int AHEAD = 6;
-    float decay[4] = {1.f, 1.f, 1.f, 1.f};
-    for (int k = 0; k < count; k += AHEAD) {
+    constexpr int AHEAD = WIDE ? 1 : 6;                               // parts asked for at a time: eight take registers that the kernel behind it wants
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = 0.f;
+    for (int k = count - 1; k >= 0; k -= AHEAD) {
         float4 e[AHEAD];
         float sum[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const long long at = (long long)(first + step * (k + i)) * C + chan;
-            const bool there = valid && k + i < count;
+            const long long at = (long long)(first + step * (k - i)) * C + chan;
+            const bool there = valid && k >= i;
             e[i] = there ? *reinterpret_cast<const float4 *>(ends + at * (4 * LPC) + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
-            sum[i] = there ? sums[at] : 0.f;
+            sum[i] = there && k - i < count - 1 ? sums[at] : 0.f;     // (nothing comes through the farthest, whose first tokens may be another sequence's)
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            if (k + i >= count) break;
+            if (k < i) break;
             const float u[4] = {e[i].x, e[i].y, e[i].z, e[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = fmaf(decay[j], u[j], v[j]);
-                decay[j] *= exp2_fast(a2[j] * sum[i]);
+                if constexpr (WIDE) {
+                    const float root = exp2_fast(__builtin_amdgcn_fmed3f(0.5f * a2[j] * sum[i], -126.f, 127.f));
+                    v[j] = fmaf(v[j] * root, root, u[j]);
+                } else {
+                    v[j] = fmaf(v[j], exp2_fast(a2[j] * sum[i]), u[j]);
+                }
             }
         }
     }
+}
+// A decay over a whole part may pass the range of a float on either side where the state that it meets brings it back: a zero that grows stays zero, a small number may grow
+// to an ordinary one, an infinity that decays stays one.  Where that happens the sum comes out as no finite number, and is taken once more with each decay as the
+// square of its root, which is held inside the range.
+template <int LPC>
+__device__ __forceinline__ void gather_parts(float (&v)[4], const float (&a2)[4], const float *ends, const float *sums, int C, int chan, int q, bool valid,
+                                             int first, int step, int count)
+{
+    gather_parts_as<LPC, false>(v, a2, ends, sums, C, chan, q, valid, first, step, count);
+    if (!(fabsf(v[0]) + fabsf(v[1]) + fabsf(v[2]) + fabsf(v[3]) <= 3.4e38f))
+        gather_parts_as<LPC, true>(v, a2, ends, sums, C, chan, q, valid, first, step, count);
 }
 
 // ---- host (sscan.hip) ----------------------------------------------------------------------------
