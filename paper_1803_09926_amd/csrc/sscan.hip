@@ -35,10 +35,12 @@ constexpr int MOST_PARTS = 80;
 // 79, 79, 98, 155 us both ways at 1501 x 728.
 constexpr int PART_UNIT = KEPT_EVERY;
 
+// One at the least: launches are divided by these numbers.
 int tuned(const char *name, int otherwise)
 {
     const char *v = tune_env(name);
-    return v ? atoi(v) : otherwise;
+    const int n = v ? atoi(v) : otherwise;
+    return n > 1 ? n : 1;
 }
 
 // `want` blocks fill the card: five on each of 256 compute units forward (512, 768, 1024, 1280, 2048 of them 172, 150, 140, 140, 140 us at 16384 x 1024, and 326,

@@ -167,3 +167,14 @@ def test_more_rows_than_a_norm_takes():
     assert _call("lnorm_fwd", DESCS["lnorm"](T=0x7fff0001)) == E_LARGE
     assert _call("lnorm_bwd", DESCS["lnorm"](T=0x7fffffff)) == E_LARGE and dw.lnorm_bwd_workspace_bytes(DESCS["lnorm"](T=0x7fffffff)) == 0
     assert dw.lnorm_bwd_workspace_bytes(DESCS["lnorm"](T=0x7fff0000)) > 0
+
+
+def test_tuning_numbers_of_zero():
+    """Plans are divided by them: zero counts as one, and no size or query ends in an arithmetic fault."""
+    d = DESCS["sscan"](T=4096, C=256, sequences=64)
+    queries = [dw.sscan_fwd_workspace_bytes, dw.sscan_bwd_workspace_bytes, dw.sscan_kept_bytes]
+    knobs = ["DWCONV_TUNE_SSCAN_FWD_BLOCKS", "DWCONV_TUNE_SSCAN_BWD_BLOCKS", "DWCONV_TUNE_SSCAN_MOST_PARTS"]
+    with dw.tuning_overrides({k: 1 for k in knobs}):
+        want = [q(d) for q in queries]
+    with dw.tuning_overrides({k: 0 for k in knobs}):
+        assert [q(d) for q in queries] == want
