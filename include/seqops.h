@@ -31,7 +31,8 @@
 extern "C" {
 #endif
 
-/* What a descriptor may ask for at most; more is DWCONV_ERR_TOO_LARGE. */
+/* What a descriptor may ask for at most; more is DWCONV_ERR_TOO_LARGE (more channels of lnorm, taps of cconv or states of sscan than their own maxima:
+ * DWCONV_ERR_UNSUPPORTED; numbers that do not divide, or below their least: DWCONV_ERR_BAD_DIM). */
 #define SEQOPS_MAX_T 0x7fff0000      /* tokens, sequences, slots                    */
 #define SEQOPS_MAX_C (1 << 24)       /* channels of cconv and sscan                 */
 #define SEQOPS_MAX_STRIDE (1 << 25)  /* elements from one row to the next           */

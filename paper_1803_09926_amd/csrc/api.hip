@@ -106,13 +106,13 @@ const char *dwconv_status_string(int status)
     switch (status) {
     case DWCONV_OK: return "ok";
     case DWCONV_ERR_NULL: return "null pointer";
-    case DWCONV_ERR_BAD_DIM: return "bad dimension (N,C,H,W,K,stride,mult must be >= 1, pad >= 0, output non-empty)";
-    case DWCONV_ERR_BAD_ENUM: return "bad layout or dtype";
+    case DWCONV_ERR_BAD_DIM: return "bad dimension (a size, count, stride or pad below its least, an empty output, or numbers that do not divide)";
+    case DWCONV_ERR_BAD_ENUM: return "bad layout, dtype or switch";
     case DWCONV_ERR_WORKSPACE: return "workspace missing or too small";
-    case DWCONV_ERR_ALIGN: return "pointer not 16-byte aligned";
-    case DWCONV_ERR_UNSUPPORTED: return "unsupported (K larger than DWCONV_MAX_K)";
+    case DWCONV_ERR_ALIGN: return "pointer not aligned (to 16 bytes; a tensor of the sequence operators: to its elements)";
+    case DWCONV_ERR_UNSUPPORTED: return "unsupported (more filter taps, norm channels or scan states than the operator's largest: *_MAX_K, LNORM_MAX_C, SSCAN_MAX_N)";
     case DWCONV_ERR_LAUNCH: return "HIP kernel launch failed";
-    case DWCONV_ERR_TOO_LARGE: return "tensor has 2^31 or more elements";
+    case DWCONV_ERR_TOO_LARGE: return "too large (a tensor of 2^31 or more elements; sequence operators: a size or stride above SEQOPS_MAX_*)";
     case DWCONV_ERR_SCRATCH: return "shape needs more scratch than the library's static buffer holds (use dwconv_bwd_filter with a workspace)";
     default: return "unknown status";
     }

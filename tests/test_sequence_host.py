@@ -178,3 +178,13 @@ def test_tuning_numbers_of_zero():
         want = [q(d) for q in queries]
     with dw.tuning_overrides({k: 0 for k in knobs}):
         assert [q(d) for q in queries] == want
+
+
+@pytest.mark.parametrize("call,word", [
+    (lambda: _call("lnorm_fwd", DESCS["lnorm"](C=16385)), "LNORM_MAX_C"), (lambda: _call("sscan_fwd", DESCS["sscan"](N=65)), "SSCAN_MAX_N"),
+    (lambda: _call("cconv_fwd", DESCS["cconv"](K=9)), "MAX_K"), (lambda: _call("cconv_fwd", DESCS["cconv"](), x=0x1001), "elements"),
+    (lambda: _call("cconv_fwd", DESCS["cconv"](x_stride=1 << 31)), "stride"), (lambda: _call("cconv_fwd", DESCS["cconv"](silu=2)), "switch"),
+    (lambda: _call("sscan_bwd", DESCS["sscan"](T=7)), "divide"), (lambda: _call("sscan_bwd", DESCS["sscan"](T=8), None), "workspace")])
+def test_a_refusal_says_what_was_refused(call, word):
+    rc = call()
+    assert rc != OK and word in dw.status_string(rc)
