@@ -38,14 +38,11 @@ class TokenMixer:
                   "w_x": normal(C, R + 2 * N, scale=C ** -0.5), "w_dt": normal(R, C, scale=R ** -0.5),
                   "dt_bias": (dt + torch.log(-torch.expm1(-dt))).to(device), "A_log": torch.log(torch.arange(1, N + 1, device=device, dtype=torch.float32)).repeat(C, 1),
                   "D": torch.ones(C, device=device), "w_out": normal(C, M, scale=0.5 * C ** -0.5)}
-        self._spaces = {}
 
-    def _space(self, name, nbytes):
-        """A workspace that grows to the largest size asked for."""
-        t = self._spaces.get(name)
-        if t is None or t.numel() < nbytes:
-            t = self._spaces[name] = torch.empty(max(nbytes, 16), device=self.p["D"].device, dtype=torch.uint8)
-        return t
+    def _space(self, nbytes):
+        """A workspace for one call.  torch's allocator hands it out again behind that call on the same stream; one that the block held would be written by calls on
+        two streams at once."""
+        return torch.empty(max(nbytes, 16), device=self.p["D"].device, dtype=torch.uint8)
 
     def _new(self, *shape, like=None):
         return torch.empty(*shape, device=self.p["D"].device, dtype=like or self.dtype)
@@ -85,7 +82,7 @@ class TokenMixer:
         dw.cconv_fwd(cd, xz[:, :C], p["conv_w"], p["conv_b"], u, starts=starts, init=rows, final=new_rows)
         proj, dt, B, Cm = self._projected(u)
         kept = torch.empty(max(dw.sscan_kept_bytes(sd), 16), device=u.device, dtype=torch.uint8) if keep else None
-        dw.sscan_fwd(sd, u, dt, self._decay(), B, Cm, y, self._space("fwd", dw.sscan_fwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"],
+        dw.sscan_fwd(sd, u, dt, self._decay(), B, Cm, y, self._space(dw.sscan_fwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"],
                      starts=starts, init=h, final=new_h, kept=kept)
         began = (rows.clone(), h.clone()) if keep and states is not None else (None, None)
         if states is not None:
@@ -107,7 +104,7 @@ class TokenMixer:
         du, ddt, dproj, dxz = self._new(T, C), self._new(T, C), torch.empty_like(proj), torch.empty_like(xz)
         A = self._decay()
         dw.sscan_bwd(sd, u, dt, A, proj[:, R:R + N], proj[:, R + N:], kept, dy, du, ddt, g["A_log"], dproj[:, R:R + N], dproj[:, R + N:],
-                     self._space("bwd", dw.sscan_bwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"], starts=starts, init=h, dD=g["D"],
+                     self._space(dw.sscan_bwd_workspace_bytes(sd)), D=p["D"], z=xz[:, C:], dt_bias=p["dt_bias"], starts=starts, init=h, dD=g["D"],
                      dz=dxz[:, C:], ddt_bias=g["dt_bias"])
         g["A_log"].mul_(A)
         g["w_dt"] = proj[:, :R].t() @ ddt
@@ -115,10 +112,10 @@ class TokenMixer:
         g["w_x"] = u.t() @ dproj
         du.addmm_(dproj, p["w_x"].t())
         dw.cconv_bwd(cd, xz[:, :C], p["conv_w"], p["conv_b"], du, dxz[:, :C], g["conv_w"], g["conv_b"],
-                     self._space("conv", dw.cconv_bwd_workspace_bytes(cd)), starts=starts, init=rows)
+                     self._space(dw.cconv_bwd_workspace_bytes(cd)), starts=starts, init=rows)
         g["w_in"] = normed.t() @ dxz
         dnormed, dx = dxz @ p["w_in"].t(), self._new(T, self.M)
-        dw.lnorm_bwd(nd, total, p["norm_w"], mean, rstd, dnormed, dx, g["norm_w"], g["norm_b"], self._space("norm", dw.lnorm_bwd_workspace_bytes(nd)),
+        dw.lnorm_bwd(nd, total, p["norm_w"], mean, rstd, dnormed, dx, g["norm_w"], g["norm_b"], self._space(dw.lnorm_bwd_workspace_bytes(nd)),
                      dtotal=dresidual)
         return dx, g
 

@@ -55,3 +55,28 @@ def test_gradients_of_a_block_that_continues(gpu_lib, bounds, packed):
     gu.assert_close(gu.to_host(dx), x64.grad.numpy(), 2e-5, "dx")
     for k in p:
         gu.assert_close(gu.to_host(grads[k]), p[k].grad.numpy(), 5e-5, k)
+
+
+def test_calls_on_two_streams_have_workspaces_of_their_own(gpu_lib, monkeypatch):
+    from paper_1803_09926_amd import token_mixer
+    held = []
+
+    def recorded(call):
+        def run(*args, **named):
+            held.extend(a for a in args if isinstance(a, torch.Tensor) and a.dtype == torch.uint8)
+            return call(*args, **named)
+        return run
+    for name in ("sscan_fwd", "sscan_bwd", "cconv_bwd", "lnorm_bwd"):
+        monkeypatch.setattr(token_mixer.dw, name, recorded(getattr(token_mixer.dw, name)))
+    block, T = token_mixer.TokenMixer(32, dtype=torch.float32), 400
+    x, dh = torch.randn(T, 32, device="cuda"), torch.randn(T, 32, device="cuda")
+    torch.cuda.synchronize()
+    side, counts = torch.cuda.Stream(), []
+    for stream in (torch.cuda.current_stream(), side):
+        with torch.cuda.stream(stream):
+            block.forward(x, keep=True)
+            block.backward(dh)
+        counts.append(len(held))
+    torch.cuda.synchronize()
+    first, second = ({t.data_ptr() for t in held[a:b] if t.numel() > 16} for a, b in ((0, counts[0]), (counts[0], counts[1])))
+    assert first and second and not first & second
