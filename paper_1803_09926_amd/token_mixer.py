@@ -38,6 +38,7 @@ class TokenMixer:
                   "w_x": normal(C, R + 2 * N, scale=C ** -0.5), "w_dt": normal(R, C, scale=R ** -0.5),
                   "dt_bias": (dt + torch.log(-torch.expm1(-dt))).to(device), "A_log": torch.log(torch.arange(1, N + 1, device=device, dtype=torch.float32)).repeat(C, 1),
                   "D": torch.ones(C, device=device), "w_out": normal(C, M, scale=0.5 * C ** -0.5)}
+        self.kept, self._read, self._unread = None, False, 0         # of the last forward(keep=True): whether `backward` had it, and how many it has not had
 
     def _space(self, nbytes):
         """A workspace for one call.  torch's allocator hands it out again behind that call on the same stream; one that the block held would be written by calls on
@@ -69,7 +70,7 @@ class TokenMixer:
 
     def forward(self, hidden, residual=None, starts=None, sequences=1, states=None, keep=False):
         """(hidden, residual) after the block, for T packed tokens.  states: continues these sequences, and moves them on.  keep: for `backward`, to which
-        the states that the sequences began with are constants."""
+        the states that the sequences began with are constants; what it needs is in `kept` until the next forward with keep."""
         p, T, C = self.p, hidden.shape[0], self.C
         nd, cd, sd = self._descs(T, sequences)
         normed, total = self._new(T, self.M), hidden if residual is None else self._new(T, self.M)
@@ -89,13 +90,22 @@ class TokenMixer:
             rows.copy_(new_rows)
             h.copy_(new_h)
         if keep:
+            self._read, self._unread = False, self._unread + 1
             self.kept = (total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences, began)
         return y @ p["w_out"], total
 
-    def backward(self, dhidden, dresidual=None):
-        """From the gradients of what `forward` gave to (the gradient of hidden and residual alike, the gradients by parameter)."""
+    def backward(self, dhidden, dresidual=None, kept=None):
+        """From the gradients of what `forward` gave to (the gradient of hidden and residual alike, the gradients by parameter).  kept: what the block's `kept` was
+        behind that forward, where another one with keep has come since."""
         p, C, R, N = self.p, self.C, self.R, self.N
-        total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences, (rows, h) = self.kept
+        if kept is None:
+            if self.kept is None:
+                raise RuntimeError("no forward(keep=True) came before")
+            if self._read and self._unread:
+                raise RuntimeError("an earlier forward's activations were replaced by a later one's: take `kept` behind each forward(keep=True) and hand it to backward")
+            kept = self.kept
+        self._read, self._unread = self._read or kept is self.kept, max(0, self._unread - 1)
+        total, normed, mean, rstd, xz, u, proj, dt, kept, y, starts, sequences, (rows, h) = kept
         T = total.shape[0]
         nd, cd, sd = self._descs(T, sequences)
         g = {k: torch.empty(v.shape, device=v.device) for k, v in p.items() if not k.startswith("w_")}

@@ -80,3 +80,28 @@ def test_calls_on_two_streams_have_workspaces_of_their_own(gpu_lib, monkeypatch)
     torch.cuda.synchronize()
     first, second = ({t.data_ptr() for t in held[a:b] if t.numel() > 16} for a, b in ((0, counts[0]), (counts[0], counts[1])))
     assert first and second and not first & second
+
+
+def test_two_forwards_before_a_backward(gpu_lib):
+    from paper_1803_09926_amd.token_mixer import TokenMixer
+    block = TokenMixer(32, dtype=torch.float32)
+    a, b, da, db = (torch.randn(50, 32, device="cuda") for _ in range(4))
+    with pytest.raises(RuntimeError, match="came before"):
+        block.backward(da)
+
+    def alone(x, d):
+        block.forward(x, keep=True)
+        dx, g = block.backward(d)
+        again, _ = block.backward(d)                     # (as often as one likes)
+        assert torch.equal(dx, again)
+        return dx, g
+    want_a, want_b = alone(a, da), alone(b, db)
+    block.forward(a, keep=True)
+    kept = block.kept
+    block.forward(b, keep=True)
+    got_b = block.backward(db)
+    with pytest.raises(RuntimeError, match="replaced"):  # not the second one's once more
+        block.backward(da)
+    got_a = block.backward(da, kept=kept)
+    for got, want in ((got_a, want_a), (got_b, want_b)):
+        assert torch.equal(got[0], want[0]) and all(torch.equal(got[1][k], want[1][k]) for k in want[1])
