@@ -7,8 +7,7 @@
 namespace dwc {
 
 // ---- rows ----------------------------------------------------------------------------------------
-// 4, 8 and 16 bytes that lie anywhere: one load or store each, as the alignment that the types promise is an element's.
-typedef uint32_t u1any_t __attribute__((aligned(2)));
+// 8 and 16 bytes that lie anywhere: one load or store each, as the alignment that the types promise is an element's.
 typedef uint32_t u2any_t __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u4any_t __attribute__((ext_vector_type(4), aligned(2)));
 
@@ -16,7 +15,7 @@ typedef uint32_t u4any_t __attribute__((ext_vector_type(4), aligned(2)));
 // They stay as stored until they are used: bf16 takes half the registers.
 template <typename T, int V> struct Some {
     static constexpr int WORDS = (int)(V * sizeof(T)) / 4;
-    static_assert(V * sizeof(T) % 4 == 0, "whole 32-bit words");
+    static_assert(V * sizeof(T) % 8 == 0, "whole pairs of 32-bit words");
     uint32_t w[WORDS];
     __device__ __forceinline__ void load(const T *p, int n)
     {
@@ -28,11 +27,10 @@ template <typename T, int V> struct Some {
                 const u4any_t v = *reinterpret_cast<const u4any_t *>(q + 2 * i);
                 w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
             }
-            if constexpr (WORDS % 4 >= 2) {
+            if constexpr (WORDS % 4 == 2) {
                 const u2any_t v = *reinterpret_cast<const u2any_t *>(q + 2 * W4);
                 w[W4] = v.x; w[W4 + 1] = v.y;
             }
-            if constexpr (WORDS % 2 == 1) w[WORDS - 1] = *reinterpret_cast<const u1any_t *>(q + 2 * (WORDS - 1));
         } else {
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) w[i] = 0;
@@ -78,11 +76,10 @@ template <typename T, int V> struct Some {
                 const u4any_t v = {w[i], w[i + 1], w[i + 2], w[i + 3]};
                 *reinterpret_cast<u4any_t *>(q + 2 * i) = v;
             }
-            if constexpr (WORDS % 4 >= 2) {
+            if constexpr (WORDS % 4 == 2) {
                 const u2any_t v = {w[W4], w[W4 + 1]};
                 *reinterpret_cast<u2any_t *>(q + 2 * W4) = v;
             }
-            if constexpr (WORDS % 2 == 1) *reinterpret_cast<u1any_t *>(q + 2 * (WORDS - 1)) = w[WORDS - 1];
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -93,22 +90,6 @@ template <typename T, int V> struct Some {
         }
     }
 };
-// one element of bf16 has no whole word
-template <> struct Some<bf16_t, 1> {
-    bf16_t w;
-    __device__ __forceinline__ void load(const bf16_t *p, int n) { w = n >= 1 ? *p : (bf16_t)0; }
-    __device__ __forceinline__ void zero() { w = 0; }
-    __device__ __forceinline__ float at(int) const { return bf16_to_f32(w); }
-    __device__ __forceinline__ void get(float (&r)[1]) const { r[0] = bf16_to_f32(w); }
-    __device__ __forceinline__ void set(const float (&r)[1]) { w = f32_to_bf16(r[0]); }
-    __device__ __forceinline__ void store(bf16_t *p, int n) const { if (n >= 1) *p = w; }
-};
-
-// An element `off` bytes from a base that all lanes share: one scalar address and a 32-bit register a lane, where 64-bit addresses take two registers
-// and several additions each.
-template <typename T> __device__ __forceinline__ const T *from(const T *base, uint32_t off) { return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + off); }
-template <typename T> __device__ __forceinline__ T *from(T *base, uint32_t off) { return reinterpret_cast<T *>(reinterpret_cast<char *>(base) + off); }
-
 // V consecutive elements that are asked for early and used late.  The loads go through a view of the rows, in which a lane that is to have zeros asks for what
 // lies outside: no branch, and so nothing that waits for them before they are used.  WHOLE: V elements are all there or none of them, and aligned to their
 // bytes; otherwise each is a load of its own, STEP elements from the one before, and those less than n from the first are there.
@@ -139,13 +120,6 @@ template <typename T, int V, bool WHOLE, int STEP = 1> struct Ahead {
                 else w[i] = rows.b32(at, 0);
             }
         }
-    }
-    // one element `row` bytes (the same in every lane) and `off` bytes into the view
-    __device__ __forceinline__ void load_row(const BufView &rows, uint32_t off, uint32_t row)
-    {
-        static_assert(V == 1, "one element");
-        if constexpr (sizeof(T) == 2) w[0] = rows.b16(off, row);
-        else w[0] = rows.b32(off, row);
     }
     __device__ __forceinline__ float at(int i) const
     {
