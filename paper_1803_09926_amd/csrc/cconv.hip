@@ -10,6 +10,8 @@
 // past its strip; the pre-activation is computed again from x, which is read anyway for the filter's gradient.  That gradient's sums stay in
 // registers over the strip, a block adds its strips in LDS in a fixed order, and the blocks' partials meet in seq_sum.hip.
 #include "seq_common.hpp"
+#include "tune.hpp"
+#include <stdlib.h>
 
 namespace dwc {
 
@@ -376,7 +378,8 @@ Launch plan_launch(const cconv_desc *d, int lanes, int least, int most)
     l.per_block = lanes_for(l.vectors);
     l.across = (unsigned)cdiv(l.vectors, l.per_block);
     const long long tokens = (long long)d->T * l.across * l.per_block / (256 * lanes) / 4 * 4;
-    l.strip = (int)(tokens < least ? least : tokens > most ? most : tokens);
+    const char *const forced = tune_env("DWCONV_TUNE_CCONV_STRIP");
+    l.strip = forced && atoi(forced) > 0 ? atoi(forced) : (int)(tokens < least ? least : tokens > most ? most : tokens);
     const long long per = (long long)l.strip * (256 / l.per_block);
     l.down = d->T > 0 ? (d->T + per - 1) / per : 1;
     return l;
