@@ -2,7 +2,7 @@
 //
 // A lane owns V neighbouring channels and walks down a strip of tokens with the last K - 1 rows in registers, so that each row is read once a strip (and
 // K - 1 rows more at its head).  All three passes are bound by memory: forward 8191 x 1536 in bf16 takes 13 us, 3.9 TB/s, where a copy of these rows takes
-// 10.5 (strips are 16 tokens there, and three rows of each come twice); backward 16384 x 1024 in fp32 47 us, 4.3 TB/s, and 4.7 for the sum of the partials,
+// 10.5 (strips are 12 tokens there, and three rows of each come twice); backward 16384 x 1024 in fp32 47 us, 4.3 TB/s, and 4.7 for the sum of the partials,
 // where an addition of tensors of that size takes 35.  At a sequence's first token the rows in registers are replaced by the sequence's
 // rows of init, or zeros: what an earlier sequence holds, infinities and NaN among it, is never multiplied by anything of a later one.
 //
@@ -384,9 +384,10 @@ Launch plan_launch(const cconv_desc *d, int lanes, int least, int most)
     l.down = d->T > 0 ? (d->T + per - 1) / per : 1;
     return l;
 }
-// Strips of 8, 16, 32, 64 tokens, forward, 8191 x 1536 in bf16: 15.4, 13.9, 15.7, 19.6 us.  Backward, 16384 x 1024 in fp32: 66, 62, 52, 60 us
-// (a block's partials are K + 1 rows for strip * 256 / per_block tokens).  Few tokens: the walk down a strip is a chain, so it is short: least strips of 4, 8,
-// 16 tokens, backward, 200 x 768 in either type 12.0, 13.2, 16.2 us, 4000 x 768 in fp32 19.4, 20.3, 21.3, but 1000 x 2048 15.8, 14.4, 18.1 (bf16).
+// Strips of 8, 12, 16, 20, 32, 64 tokens, forward, 8191 x 1536 in bf16 (12 by this rule): 15.4, 13.7, 13.9, 15.2, 16.1, 19.8 us.  Backward, 16384 x 1024 in
+// fp32 (32 by this rule), 8, 16, 24, 32, 48, 64: 62, 59.5, 50.3, 50.5, 59.4, 60.3 us (a block's partials are K + 1 rows for strip * 256 / per_block
+// tokens).  Few tokens: the walk down a strip is a chain, so it is short: strips of 4, 8, 16 tokens, backward, 200 x 768 in either type 12.0, 13.2, 16.1 us, 4000 x
+// 768 in fp32 19.6, 20.3, 21.4, but 1000 x 2048 15.6, 13.8, 18.0 (bf16).
 Launch plan_fwd(const cconv_desc *d) { return plan_launch(d, 768, 4, 64); }
 Launch plan_bwd(const cconv_desc *d) { return plan_launch(d, 512, 4, 128); }
 

@@ -2,8 +2,9 @@
 //
 // A team of lanes (a wavefront, or a block of 2 to 16 of them) holds a row in registers, V consecutive channels a vector and NV vectors a lane, so
 // that the row is read once, the variance is taken about the mean that is already known (two sums over the team, no cancellation), and all is written once.
-// Both passes are bound by memory: 32768 x 1024 in bf16 with a residual takes 47.4 us, 5.7 TB/s, where a large copy reaches 5.2; the backward pass at
-// 9999 x 1536 in fp32 35 us, 5.3 TB/s, and 4.7 for the sum of its partials.
+// Both passes are bound by memory: 32768 x 1024 in bf16 with a residual takes 47.1 us, 5.7 TB/s, where a large copy reaches 5.2; the backward pass at
+// 9999 x 1536 in fp32 35 us, 5.3 TB/s, and 4.7 for the sum of its partials.  Above 8192 channels the backward pass is bound by spills instead: 16 channels a lane of
+// 1024 lanes need more than the 128 registers there, and 4096 x 16384 takes 245 us in bf16 (1.6 TB/s) and 432 in fp32 (1.9).
 //
 // The weight's gradient is a sum over rows: each lane keeps the sums of its own channels over all rows that its team walks, the teams of a block add
 // theirs in LDS one after the other, and the blocks' partials meet in seq_sum.hip.

@@ -29,10 +29,13 @@ int validate(const sscan_desc *d)
 // 16-byte multiples, so that what follows is aligned
 size_t floats(size_t n) { return (n + 3) / 4 * 4; }
 
-// A block of the last part reads the states of all before it: at most 24, 32, 48, 64, 80 parts take 224, 171, 150, 138.5, 137 us forward at 16384 x 1024.
+// A block of the last part reads the states of all before it, so the parts of a launch are capped: at most 24, 32, 48, 64, 80 of them take 212, 163, 141, 132, 131 us
+// forward at 16384 x 1024, where never more than 80 are asked for.  With fewer channels the cap leaves compute units idle: 32768 tokens of 64, 256, 512 channels
+// (16 states) in one sequence take 119, 138, 168 us forward with 80 parts and 82, 105, 147 with 160, both ways 318, 394, 540 and 210, 315, 473; in 64
+// sequences 110, 131, 159 and, with 320 parts, 44, 74, 121.
 constexpr int MOST_PARTS = 80;
-// A part is a whole number of tiles, one at the least: parts of at least 16, 32, 64, 128 tokens take 16.5, 17.8, 26.3, 43.8 us forward at 301 x 1024, and
-// 79, 79, 98, 155 us both ways at 1501 x 728.
+// A part is a whole number of tiles, one at the least: parts of 16, 32, 64, 112 tokens take 15.9, 17.5, 24.2, 35.7 us forward at 301 x 1024; both ways at 1501 x 728
+// those of 32 tokens, the least that the cap allows there, 64 and 128 take 73, 88, 134 us, and of 16 with a cap of 95 78.
 constexpr int PART_UNIT = KEPT_EVERY;
 
 // One at the least: launches are divided by these numbers.
@@ -43,8 +46,8 @@ int tuned(const char *name, int otherwise)
     return n > 1 ? n : 1;
 }
 
-// `want` blocks fill the card: five on each of 256 compute units forward (512, 768, 1024, 1280, 2048 of them 172, 150, 140, 140, 140 us at 16384 x 1024, and 326,
-// 272, 255, 240, 244 at 16383 x 2048), three turns of two backward (504, 960, 1536, 1920: 344, 337, 320, 325 us both ways at 8192 x 1536).
+// `want` blocks fill the card: five on each of 256 compute units forward (512, 768, 1024, 1280 of them 162, 141, 132.5, 131.5 us at 16384 x 1024, and 512, 768, 1024,
+// 1280, 2048 303, 256, 240, 228, 223 at 16383 x 2048), three turns of two backward (504, 960, 1536, 1920: 343, 337, 320, 325 us both ways at 8192 x 1536).
 // Where whole sequences of equal lengths give at least half of them, a part is one or more of these, and nothing has to be carried from part to part; otherwise
 // the tokens are split wherever it may be.
 ScanPlan plan(const sscan_desc *d, bool packed, int want)

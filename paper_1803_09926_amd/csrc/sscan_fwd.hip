@@ -1,9 +1,10 @@
 // Selective state space scan, forward, and one token at a time.  See sscan.hpp for the layout of the work, include/seqops.h for the contract.
 //
-// Each state costs a multiply, an exponential at a quarter of the vector rate, a multiply and two multiply-adds a token: 32 cycles of a SIMD for 64 of
-// them, where the tensors move 8 bytes (bf16) for 16 states.  The kernel is bound by its vector instructions: 85 % of the cycles issue one, and 4 in 5 of
-// these are the recurrence's.  16384 tokens of 1024 channels of 16 states take 135 us (61 the first pass, 96 the second, each timed alone), 16383 of 2048
-// 230 us, 2.3 states a ns; that many states at 6 instructions each, and no first pass, would take 41 and 82.
+// Each state costs a multiply, an exponential at half the vector rate (8.1 cycles measured, 4.4 a multiply-add), a multiply and two multiply-adds a token: 24 cycles
+// of a SIMD for 64 of them, where the tensors move 8 bytes (bf16) for 16 states.  The kernel is bound by its vector instructions: they are active in 78 % of its cycles,
+// 92 % of those in which the compute units are busy, and the recurrence is three fifths of them (three quarters in the first pass).  16384 tokens of 1024
+// channels of 16 states take 132 us (62 the first pass, 95 the second, each timed alone), 16383 of 2048 228 us, 2.4 states a ns; that many states at 24
+// cycles each, and no first pass, would take 41 and 82.
 //
 // Where there are few channels the tokens are split into parts.  A first pass finds each part's state at its end from zero and the sum of its step
 // sizes (the decay over a part is exp(A * sum)); a block of the second pass then walks back over the parts before it, to the one that holds its sequence's first
