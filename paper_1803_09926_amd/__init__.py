@@ -360,3 +360,6 @@ def gconv_bwd_filter(d: GroupDesc, x, dy, dw, workspace, stream=None):
 from .sequence import (SEQ_EXPORTS, CconvDesc, LnormDesc, SscanDesc, cconv_bwd, cconv_bwd_workspace_bytes, cconv_desc, cconv_fwd,  # noqa: E402,F401
                        cconv_step, lnorm_bwd, lnorm_bwd_workspace_bytes, lnorm_desc, lnorm_fwd, sscan_bwd, sscan_bwd_workspace_bytes,
                        sscan_desc, sscan_fwd, sscan_fwd_workspace_bytes, sscan_kept_bytes, sscan_step)
+from .delta import (DELTA_EXPORTS, GdeltaDesc, HnormDesc, RnormDesc, gdelta_bwd, gdelta_bwd_workspace_bytes, gdelta_desc, gdelta_fwd,  # noqa: E402,F401
+                    gdelta_fwd_workspace_bytes, gdelta_kept_bytes, gdelta_step, hnorm_bwd, hnorm_bwd_workspace_bytes, hnorm_desc, hnorm_fwd, rnorm_bwd,
+                    rnorm_bwd_workspace_bytes, rnorm_desc, rnorm_fwd)

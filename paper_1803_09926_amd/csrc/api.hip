@@ -110,9 +110,9 @@ const char *dwconv_status_string(int status)
     case DWCONV_ERR_BAD_ENUM: return "bad layout, dtype or switch";
     case DWCONV_ERR_WORKSPACE: return "workspace missing or too small";
     case DWCONV_ERR_ALIGN: return "pointer not aligned (to 16 bytes; a tensor of the sequence operators: to its elements)";
-    case DWCONV_ERR_UNSUPPORTED: return "unsupported (more filter taps, norm channels or scan states than the operator's largest: *_MAX_K, LNORM_MAX_C, SSCAN_MAX_N)";
+    case DWCONV_ERR_UNSUPPORTED: return "unsupported (more filter taps, norm channels, scan states or columns of a head than the operator's largest: *_MAX_K, LNORM_MAX_C, SSCAN_MAX_N, GDELTA_MAX_K, GDELTA_MAX_V, HNORM_MAX_D, RNORM_MAX_C)";
     case DWCONV_ERR_LAUNCH: return "HIP kernel launch failed";
-    case DWCONV_ERR_TOO_LARGE: return "too large (a tensor of 2^31 or more elements; sequence operators: a size or stride above SEQOPS_MAX_*)";
+    case DWCONV_ERR_TOO_LARGE: return "too large (a tensor of 2^31 or more elements; sequence operators: a size or stride above SEQOPS_MAX_*, or GDELTA_MAX_H)";
     case DWCONV_ERR_SCRATCH: return "shape needs more scratch than the library's static buffer holds (use dwconv_bwd_filter with a workspace)";
     default: return "unknown status";
     }

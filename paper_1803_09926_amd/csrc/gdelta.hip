@@ -1,0 +1,186 @@
+// Entry points of the gated delta rule (include/deltaops.h): checks, sizes, and the order of its kernels.
+#include "gdelta_launch.hpp"
+#include <initializer_list>
+#include <math.h>
+
+namespace dwc {
+
+namespace {
+
+constexpr long long TOKENS = 64;                  // of a chunk
+
+int validate(const gdelta_desc *d)
+{
+    if (!d) return DWCONV_ERR_NULL;
+    if (d->dtype != DWCONV_F32 && d->dtype != DWCONV_BF16) return DWCONV_ERR_BAD_ENUM;
+    if ((d->softplus | 1) != 1 || (d->sigmoid | 1) != 1 || (d->norm | 1) != 1) return DWCONV_ERR_BAD_ENUM;
+    if (d->T < 0 || d->H < 1 || d->K < 1 || d->V < 1 || d->key_heads < 1 || d->sequences < 1 || d->H % d->key_heads) return DWCONV_ERR_BAD_DIM;
+    if (!isfinite(d->scale) || !(d->eps >= 0.f) || !isfinite(d->eps)) return DWCONV_ERR_BAD_DIM;
+    if (d->K > GDELTA_MAX_K || d->V > GDELTA_MAX_V) return DWCONV_ERR_UNSUPPORTED;
+    const long long keys = (long long)d->key_heads * d->K, values = (long long)d->H * d->V;
+    if (d->T > SEQOPS_MAX_T || d->sequences > SEQOPS_MAX_T || d->H > GDELTA_MAX_H) return DWCONV_ERR_TOO_LARGE;
+    for (const int64_t s : {d->q_stride, d->k_stride, d->v_stride, d->a_stride, d->b_stride, d->y_stride})
+        if (s > SEQOPS_MAX_STRIDE) return DWCONV_ERR_TOO_LARGE;
+    if (d->T > 1 && (d->q_stride < keys || d->k_stride < keys || d->v_stride < values || d->a_stride < d->H || d->b_stride < d->H || d->y_stride < values))
+        return DWCONV_ERR_BAD_DIM;
+    // chunks are counted in 32 bits, bytes of all states in 64
+    const long long chunks = d->T / TOKENS + d->sequences;
+    long long all;
+    if (chunks > 0x7fffffffll || __builtin_mul_overflow(chunks * d->H, 1ll << 20, &all)) return DWCONV_ERR_TOO_LARGE;
+    return DWCONV_OK;
+}
+
+constexpr size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+GdArgs args_of(const gdelta_desc *d, const gdelta_tensors *t)
+{
+    GdArgs g = {d->T, d->H, d->K, d->V, d->key_heads, d->sequences, t->starts ? 0 : d->T / d->sequences, d->softplus, d->sigmoid, d->norm, d->scale, d->eps,
+                d->q_stride, d->k_stride, d->v_stride, d->a_stride, d->b_stride, d->y_stride, t->q, t->k, t->v, t->a, t->b, (const float *)t->A,
+                (const float *)t->a_bias, (const int32_t *)t->starts};
+    return g;
+}
+
+size_t first_pass_bytes(const gdelta_desc *d, const GdLayout &l) { return (size_t)l.chunks * d->H * (size_t)(2 * l.matrix + l.vectors); }
+void place_first_pass(const gdelta_desc *d, const GdLayout &l, char *p, GdSpace *s)
+{
+    s->T = p;
+    s->P = s->T + l.chunks * d->H * l.matrix;
+    s->vec = s->P + l.chunks * d->H * l.matrix;
+}
+void place_kept(const gdelta_desc *d, const GdLayout &l, void *kept, GdSpace *s)
+{
+    place_first_pass(d, l, (char *)kept, s);
+    char *const p = (char *)kept + first_pass_bytes(d, l);
+    s->S = (float *)p;
+    s->U = (float *)(p + l.chunks * d->H * l.state);
+}
+
+}  // namespace
+
+GdLayout gdelta_layout(const gdelta_desc *d, bool packed)
+{
+    GdLayout l = {};
+    const long long length = d->T / d->sequences;
+    l.chunks = d->T == 0 ? 0 : packed ? d->T / TOKENS + d->sequences : d->sequences * ((length + TOKENS - 1) / TOKENS);
+    l.KP = d->K <= 32 ? 32 : d->K <= 64 ? 64 : d->K <= 128 ? 128 : 256;
+    l.VP = cdiv(d->V, 32) * 32;
+    l.inner = d->dtype == DWCONV_F32 ? 3 : 2;
+    l.matrix = l.inner * TOKENS * TOKENS * 2;
+    l.vectors = 9 * TOKENS * 4;
+    l.state = (long long)l.KP * l.VP * 4;
+    l.rows = TOKENS * l.VP * 4;
+    return l;
+}
+
+}  // namespace dwc
+
+using namespace dwc;
+
+extern "C" {
+
+size_t gdelta_kept_bytes(const gdelta_desc *desc)
+{
+    if (validate(desc) != DWCONV_OK) return 0;
+    const GdLayout l = gdelta_layout(desc, true);
+    return first_pass_bytes(desc, l) + (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows);
+}
+
+size_t gdelta_fwd_workspace_bytes(const gdelta_desc *desc)
+{
+    if (validate(desc) != DWCONV_OK) return 0;
+    return first_pass_bytes(desc, gdelta_layout(desc, true));
+}
+
+size_t gdelta_bwd_workspace_bytes(const gdelta_desc *desc)
+{
+    if (validate(desc) != DWCONV_OK) return 0;
+    const GdLayout l = gdelta_layout(desc, true);
+    return (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows) + round16((size_t)l.chunks * desc->H * 2 * sizeof(float));
+}
+
+static int check_tensors(const gdelta_desc *d, const gdelta_tensors *t, std::initializer_list<const void *> stored, std::initializer_list<const void *> others)
+{
+    if (!t) return DWCONV_ERR_NULL;
+    if (d->T > 0)
+        for (const void *p : stored)
+            if (!p) return DWCONV_ERR_NULL;
+    for (const void *p : stored)
+        if (unaligned_to(p, d->dtype)) return DWCONV_ERR_ALIGN;
+    for (const void *p : others)
+        if (unaligned4(p)) return DWCONV_ERR_ALIGN;
+    return DWCONV_OK;
+}
+
+int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = validate(desc);
+    if (rc != DWCONV_OK) return rc;
+    if (!t) return DWCONV_ERR_NULL;
+    rc = check_tensors(desc, t, {t->q, t->k, t->v, t->a, t->b, t->y}, {t->A, t->a_bias, t->starts, t->init, t->final});
+    if (rc != DWCONV_OK) return rc;
+    if (!t->starts && desc->T % desc->sequences) return DWCONV_ERR_BAD_DIM;
+    const GdLayout l = gdelta_layout(desc, t->starts != nullptr), most = gdelta_layout(desc, true);
+    GdSpace s = {};
+    if (t->kept) {
+        if (unaligned16(t->kept)) return DWCONV_ERR_ALIGN;
+        place_kept(desc, most, t->kept, &s);
+    } else if (most.chunks) {
+        if (!workspace || workspace_bytes < first_pass_bytes(desc, most)) return DWCONV_ERR_WORKSPACE;
+        if (unaligned16(workspace)) return DWCONV_ERR_ALIGN;
+        place_first_pass(desc, most, (char *)workspace, &s);
+    }
+    if (desc->T == 0 && !t->final) return DWCONV_OK;
+    const GdArgs g = args_of(desc, t);
+    hipError_t e = hipSuccess;
+    if (desc->T > 0) e = launch_gdelta_prep(desc->dtype, g, l, s, (hipStream_t)stream);
+    if (e == hipSuccess) e = launch_gdelta_fwd(desc->dtype, g, l, s, (const float *)t->init, t->y, (float *)t->final, (hipStream_t)stream);
+    return e == hipSuccess ? DWCONV_OK : DWCONV_ERR_LAUNCH;
+}
+
+int gdelta_bwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = validate(desc);
+    if (rc != DWCONV_OK) return rc;
+    if (!t) return DWCONV_ERR_NULL;
+    rc = check_tensors(desc, t, {t->q, t->k, t->v, t->a, t->b, t->dy, t->dq, t->dk, t->dv, t->da, t->db}, {t->A, t->a_bias, t->starts, t->dA, t->da_bias});
+    if (rc != DWCONV_OK) return rc;
+    if (desc->T > 0 && !t->kept) return DWCONV_ERR_NULL;
+    if (!t->starts && desc->T % desc->sequences) return DWCONV_ERR_BAD_DIM;
+    const GdLayout l = gdelta_layout(desc, t->starts != nullptr), most = gdelta_layout(desc, true);
+    if (most.chunks) {
+        if (!workspace || workspace_bytes < gdelta_bwd_workspace_bytes(desc)) return DWCONV_ERR_WORKSPACE;
+        if (unaligned16(workspace) || unaligned16(t->kept)) return DWCONV_ERR_ALIGN;
+    }
+    GdSpace s = {};
+    place_kept(desc, most, t->kept, &s);
+    s.dS = (float *)workspace;
+    s.X = (float *)((char *)workspace + most.chunks * desc->H * most.state);
+    s.partials = (float *)((char *)s.X + most.chunks * desc->H * most.rows);
+    const GdArgs g = args_of(desc, t);
+    hipError_t e = hipSuccess;
+    if (desc->T > 0) {
+        e = launch_gdelta_bwd_states(desc->dtype, g, l, s, t->dy, t->dv, (hipStream_t)stream);
+        if (e == hipSuccess) e = launch_gdelta_bwd_rows(desc->dtype, g, l, s, t->dy, t->dq, t->dk, t->da, t->db, (hipStream_t)stream);
+    }
+    if (e == hipSuccess && (t->dA || t->da_bias))
+        e = launch_sum_partials(s.partials, (int)l.chunks, desc->H, 2ll * desc->H, 2ll * desc->H, (float *)t->dA, (float *)t->da_bias, nullptr, (hipStream_t)stream);
+    return e == hipSuccess ? DWCONV_OK : DWCONV_ERR_LAUNCH;
+}
+
+int gdelta_step(const gdelta_desc *desc, const gdelta_tensors *t, void *stream)
+{
+    int rc = validate(desc);
+    if (rc != DWCONV_OK) return rc;
+    if (!t) return DWCONV_ERR_NULL;
+    rc = check_tensors(desc, t, {t->q, t->k, t->v, t->a, t->b, t->y}, {t->A, t->a_bias, t->slots, t->state});
+    if (rc != DWCONV_OK) return rc;
+    if (desc->T == 0) return DWCONV_OK;
+    if (!t->state) return DWCONV_ERR_NULL;
+    if (!t->slots && desc->T > desc->sequences) return DWCONV_ERR_BAD_DIM;
+    GdArgs g = args_of(desc, t);
+    g.starts = nullptr;
+    const hipError_t e = launch_gdelta_step(desc->dtype, g, (const int32_t *)t->slots, (float *)t->state, t->y, (hipStream_t)stream);
+    return e == hipSuccess ? DWCONV_OK : DWCONV_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,218 @@
+// The gated delta rule backward, the walk back over a sequence's chunks: the gradient of the state, and of what the tokens write to it.
+//
+// As the walk forward (gdelta_fwd.hip), with dS the gradient of the state behind a chunk:
+//   dU = P^T dY + (exp(G_end - G) * K) dS,  X = T^T dU,  dV = beta * X
+//   dS = exp(G_end) dS + (scale exp(G) * Q)^T dY - (exp(G) * K)^T dV
+// X and the dS behind the chunk are what the gradients of keys, queries and gates take (gdelta_bwd_rows.hip), for all chunks at once.
+#include "gdelta_states.hpp"
+
+namespace dwc {
+
+namespace {
+
+template <typename T, int KP, int NT, bool SHARE>
+__global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, unsigned first,
+                                                                  int blocks)
+{
+    typedef Walk<T, KP, SHARE> W;
+    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM;
+    extern __shared__ __align__(16) char lds[];
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
+    bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
+    float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
+    const unsigned bid = first + blockIdx.x;
+    const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const Columns<NT> cols((int)(bid % (unsigned)blocks));
+    const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
+    const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
+    const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const yp = dy + (long long)h * g.V;
+
+    v4f_t S[KP / 16][NT];
+#pragma unroll
+    for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+
+    Rows<T, KP, THREADS> rows;
+    Matrix<INNER, THREADS> matrix, second;
+    float o[4][4][NT];
+    auto load_keys = [&](long long c) {
+        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = (base + c) * g.H + h;
+        rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
+        matrix.load(s.T + where * l.matrix);
+        second.load(s.P + where * l.matrix);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) cols.load(yp + (at + row_of(mt, r)) * g.y_stride, g.V, row_of(mt, r) < len, o[mt][r]);
+    };
+    if (chunks > 0) load_keys(chunks - 1);
+    for (long long c = chunks - 1; c >= 0; --c) {
+        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = (base + c) * g.H + h;
+        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+        float *const vl = vecs + (c & 1) * 256;
+        if (SHARE && c < chunks - 1) __syncthreads();
+        rows.template put<LD>(kt);
+        matrix.put(tm);
+        second.put(pm);
+        vl[threadIdx.x] = vec[threadIdx.x];
+        rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
+        const float decay = vec[VEC_ONE * 64];
+#pragma unroll
+        for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
+                cols.store(s.dS + where * (l.state / 4) + (long long)row_of(ct, r) * l.VP, l.VP, true, x);
+            }
+        __syncthreads();
+        // dU
+        v4f_t U[4][NT];
+        Frag f[2][NT][INNER];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c0 = 0; c0 < KP / 32; ++c0) {
+            Frag p[NT][INNER];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c0][nt], S[2 * c0 + 1][nt], p[nt]);
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+                Frag a[RAW];
+                frags_rows<RAW, LD>(a, kt, PLANE, mt * 16, c0 * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(U[mt][nt], a, p[nt]);
+            }
+        }
+        {
+            v4f_t d[4][NT];
+            Frag b[2][NT][RAW];
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) d[mt][nt] = v4f_t{o[mt][0][nt], o[mt][1][nt], o[mt][2][nt], o[mt][3][nt]};
+            split_rows<RAW, NT>(d, b);
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+                const float4 write = four(vl + VEC_WRITE * 64, mt);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) U[mt][nt] = times(U[mt][nt], write);
+#pragma unroll
+                for (int ks = mt / 2; ks < 2; ++ks) {
+                    Frag a[INNER];
+                    frags_cols<INNER, LDM>(a, pm, PLANE_M, ks * 32, mt * 16);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<INNER, RAW>(U[mt][nt], a, b[ks][nt]);
+                }
+            }
+        }
+        // X
+        split_rows<INNER, NT>(U, f);
+        v4f_t X[4][NT];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = mt / 2; ks < 2; ++ks) {
+                Frag a[INNER];
+                frags_cols<INNER, LDM>(a, tm, PLANE_M, ks * 32, mt * 16);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(X[mt][nt], a, f[ks][nt]);
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            const float4 beta = four(vl + VEC_BETA * 64, mt), read = four(vl + VEC_READ * 64, mt);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x[NT], y[NT];
+                const int row = row_of(mt, r);
+                const float b = r == 0 ? beta.x : r == 1 ? beta.y : r == 2 ? beta.z : beta.w;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    x[nt] = X[mt][nt][r];
+                    y[nt] = x[nt] * b;
+                }
+                cols.store(s.X + where * (l.rows / 4) + (long long)row * l.VP, l.VP, true, x);
+                cols.store(dv + (at + row) * g.v_stride + (long long)h * g.V, g.V, row < len, y);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = -times(times(X[mt][nt], beta), read);
+        }
+        // dS
+        split_rows<INNER, NT>(X, f);
+#pragma unroll
+        for (int ct = 0; ct < KP / 16; ++ct) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Frag a[RAW];
+                frags_cols<RAW, LD>(a, kt, PLANE, ks * 32, ct * 16);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            const float4 ask = four(vl + VEC_ASK * 64, mt);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = times(v4f_t{o[mt][0][nt], o[mt][1][nt], o[mt][2][nt], o[mt][3][nt]}, ask);
+        }
+        split_rows<INNER, NT>(X, f);
+        if constexpr (SHARE) __syncthreads();
+        rows.template put<LD>(qt);
+        if (c > 0) load_keys(c - 1);
+        __syncthreads();
+#pragma unroll
+        for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Frag a[RAW];
+                frags_cols<RAW, LD>(a, qt, PLANE, ks * 32, ct * 16);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
+            }
+    }
+}
+
+template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+{
+    constexpr bool SHARE = shares<T, KP>();
+    constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    const auto kernel = k_gdelta_bwd_states<T, KP, NT, SHARE>;
+    const hipError_t e = gd_lds(kernel, lds);
+    if (e != hipSuccess) return e;
+    const int blocks = cdiv(l.VP, WAVES * 16 * NT);
+    return gd_launches((long long)g.sequences * blocks, THREADS, [&](unsigned first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, (const T *)dy, (T *)dv, first, blocks);
+    });
+}
+
+template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+{
+    const bool wide = l.VP > 64;
+    switch (l.KP) {
+    case 32: return wide ? launch<T, 32, 2>(g, l, s, dy, dv, stream) : launch<T, 32, 1>(g, l, s, dy, dv, stream);
+    case 64: return wide ? launch<T, 64, 2>(g, l, s, dy, dv, stream) : launch<T, 64, 1>(g, l, s, dy, dv, stream);
+    case 128: return wide ? launch<T, 128, 2>(g, l, s, dy, dv, stream) : launch<T, 128, 1>(g, l, s, dy, dv, stream);
+    default: return launch<T, 256, 1>(g, l, s, dy, dv, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_gdelta_bwd_states(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+{
+    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, dy, dv, stream) : launch_of<bf16_t>(g, l, s, dy, dv, stream);
+}
+
+}  // namespace dwc

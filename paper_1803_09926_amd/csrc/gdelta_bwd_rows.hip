@@ -1,0 +1,468 @@
+// The gated delta rule backward: the gradients of queries, keys and gates, for all chunks of 64 tokens at once.
+//
+// With S the state before the chunk and dS its gradient behind it, U what the tokens write, X = T^T dU (gdelta_bwd.hip), E[i,j] = exp(G[i] - G[j]),
+//   F = scale E * (dY U^T) on and below the diagonal,  M = -beta E * (X U^T) below it (rows and columns times the lengths' inverses)
+//   dq = scale exp(G) * dY S^T + F K
+//   dk = F^T Q + (M + M^T) K - beta exp(G) * X S^T + exp(G_end - G) * U dS^T
+//   dbeta[i] = X[i].V[i] - exp(G[i]) k[i].(S X[i]) - sum_j E (X U^T)[i,j] k[i].k[j]
+//   the gradient of the logarithm of token t's decay: the sum of what has passed it, exp(G_end) dS.S, all that tokens i >= t read of S, all that tokens j < t write for
+//           the chunk's end, and F * QK^T + M * KK^T over i >= t > j.  No term is in it that does not carry the decay: none cancel, however small it is.
+// One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens (of 256-wide keys 128 columns).  What is contracted over V
+// is read in blocks of 32 columns.
+#include "gdelta_tile.hpp"
+#include "gdelta_launch.hpp"
+
+namespace dwc {
+
+namespace {
+
+constexpr int VB = 32, LDV = VB + PAD;
+
+template <typename T, int KP> struct Back {
+    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP + PAD;
+    static constexpr int HALVES = KP > 128 ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
+    static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
+    static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
+    static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * LDM * 2, SECOND = TILE + 2 * MATRIX;
+    static constexpr size_t REGION = FIRST > SECOND ? FIRST : SECOND;
+    // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums
+    static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8, LDS = REGION + FLOATS * 4;
+};
+
+constexpr int DPP_SHR1 = 0x111, DPP_SHR2 = 0x112, DPP_SHR4 = 0x114, DPP_SHR8 = 0x118;      // from the lane so many to the left, zero at a row's start
+// the sum over the 16 lanes of a row, in every one of them
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += lane_move<DPP_XOR1>(v);
+    v += lane_move<DPP_XOR2>(v);
+    v += lane_move<DPP_HALF_MIRROR>(v);
+    return v + lane_move<DPP_MIRROR>(v);
+}
+
+template <typename T, int KP>
+__global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
+                                                                             T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
+{
+    typedef Back<T, KP> C;
+    constexpr int RAW = C::RAW, INNER = C::INNER, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
+    constexpr int TILES = C::TILES, THREADS = C::THREADS, HALVES = C::HALVES;
+    extern __shared__ __align__(16) char lds[];
+    bf16_t *const st = reinterpret_cast<bf16_t *>(lds), *const dst = C::TURNS ? st : st + INNER * PLANE_S;
+    bf16_t *const xt = dst + INNER * PLANE_S, *const ut = xt + INNER * PLANE_V, *const yt = ut + INNER * PLANE_V;
+    bf16_t *const tile = reinterpret_cast<bf16_t *>(lds), *const fm = tile + RAW * PLANE, *const mm = fm + INNER * PLANE_M;
+    float *const row_m = reinterpret_cast<float *>(lds + C::REGION), *const xv = row_m + 64;
+    float *const passing = xv + 64, *const dot_a = passing + 8 * 64, *const dot_b = dot_a + 2 * 64, *const dot_c = dot_b + 2 * 64;
+    float *const wave_sums = dot_c + 2 * 64;
+
+    const unsigned id = first + blockIdx.x;
+    const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
+    const int wv = threadIdx.x >> 6, mt = wv & 3, half = wv >> 2, col0 = half * C::KW;
+    const bool does_f = HALVES == 1 || half == 0, does_m = HALVES == 1 || half == 1;
+    const ChunkAt at = gd_chunk(g, (int)id);
+    if (at.len == 0) {
+        for (int i = threadIdx.x; i < 2 * share; i += THREADS) s.partials[(long long)id * 2 * g.H + i / share * g.H + kh * share + i % share] = 0.f;
+        return;
+    }
+    const T *const kp = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K, *const qp = (const T *)g.q + at.first * g.q_stride + (long long)kh * g.K;
+    auto put_tile = [&](const T *p, long long stride) {
+        Rows<T, KP, THREADS> rows;
+        rows.load(p, stride, at.len, g.K);
+        rows.template put<LD>(tile);
+    };
+    auto tile_at = [&](int row, int col) {           // of a tile of keys or queries
+        float v = 0.f;
+#pragma unroll
+        for (int i = RAW - 1; i >= 0; --i) v += bf16_to_f32(tile[i * PLANE + row * LD + place(col)]);
+        return v;
+    };
+
+    // products of keys with keys and queries: rows 16 mt.., columns 16 n..
+    v4f_t kk[4], qk[4];
+    {
+        Frag qa[KP / 32][RAW];
+        const int row = mt * 16 + m;
+#pragma unroll
+        for (int c = 0; c < KP / 32; ++c) {
+            Some<T, 4> v[2];
+            uint32_t w[4][RAW];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int col = c * 32 + i * 16 + q4 * 4;
+                v[i].load(qp + row * g.q_stride + col, row < at.len ? g.K - col : 0);
+                split2<RAW>(v[i].at(0), v[i].at(1), w[2 * i]);
+                split2<RAW>(v[i].at(2), v[i].at(3), w[2 * i + 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
+        }
+        put_tile(kp, g.k_stride);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            kk[n] = qk[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+            if (n > mt) continue;
+#pragma unroll
+            for (int c = 0; c < KP / 32; ++c) {
+                Frag a[RAW], b[RAW];
+                frags_rows<RAW, LD>(b, tile, PLANE, n * 16, c * 32);
+                if (does_m) {
+                    frags_rows<RAW, LD>(a, tile, PLANE, mt * 16, c * 32);
+                    mma<RAW, RAW>(kk[n], a, b);
+                }
+                if (does_f) mma<RAW, RAW>(qk[n], qa[c], b);
+            }
+        }
+    }
+
+    v4f_t gq[TILES], gk[TILES];                          // the gradients of q and k, their lengths taken for constants
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) gq[t] = gk[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
+
+    for (int hh = 0; hh < share; ++hh) {
+        const int h = kh * share + hh;
+        const long long where = (long long)id * g.H + h;
+        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+        const float *const sp = s.S + where * (l.state / 4), *const dsp = s.dS + where * (l.state / 4);
+        const float *const xp = s.X + where * (l.rows / 4), *const up = s.U + where * (l.rows / 4);
+        const T *const yp = dy + at.first * g.y_stride + (long long)h * g.V, *const vp = (const T *)g.v + at.first * g.v_stride + (long long)h * g.V;
+        v4f_t ys[TILES], xs[TILES], us[TILES], yu[4], xu[4];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) ys[t] = xs[t] = us[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < 4; ++n) yu[n] = xu[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        float ss = 0.f, xv_part = 0.f;                   // dS.S and X.V, this lane's share
+
+        for (int v0 = 0; v0 < l.VP; v0 += VB) {
+            __syncthreads();
+            constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
+            float keep[C::TURNS ? PER : 1][8];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int n = threadIdx.x + i * THREADS, row = n / (VB / 8), col = n % (VB / 8) * 8;
+                if (ALL % THREADS && n >= ALL) break;
+                float a[8], b[8];
+                const float4 a0 = *reinterpret_cast<const float4 *>(sp + (long long)row * l.VP + v0 + col), a1 = *reinterpret_cast<const float4 *>(sp + (long long)row * l.VP + v0 + col + 4);
+                const float4 b0 = *reinterpret_cast<const float4 *>(dsp + (long long)row * l.VP + v0 + col), b1 = *reinterpret_cast<const float4 *>(dsp + (long long)row * l.VP + v0 + col + 4);
+                a[0] = a0.x; a[1] = a0.y; a[2] = a0.z; a[3] = a0.w; a[4] = a1.x; a[5] = a1.y; a[6] = a1.z; a[7] = a1.w;
+                b[0] = b0.x; b[1] = b0.y; b[2] = b0.z; b[3] = b0.w; b[4] = b1.x; b[5] = b1.y; b[6] = b1.z; b[7] = b1.w;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ss += a[j] * b[j];
+                put8<INNER>(st + row * LDV, PLANE_S, col, a);
+                if constexpr (C::TURNS) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) keep[i][j] = b[j];
+                } else put8<INNER>(dst + row * LDV, PLANE_S, col, b);
+            }
+            {
+                const int n = threadIdx.x % 256, row = n / (VB / 8), col = n % (VB / 8) * 8;
+                auto eight = [&](const float *p, float (&x)[8]) {
+                    const float4 a = *reinterpret_cast<const float4 *>(p + (long long)row * l.VP + v0 + col), b = *reinterpret_cast<const float4 *>(p + (long long)row * l.VP + v0 + col + 4);
+                    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                };
+                if (HALVES == 1 || threadIdx.x < 256) {
+                    float x[8];
+                    eight(xp, x);
+                    Some<T, 8> v;
+                    v.load(vp + row * g.v_stride + v0 + col, row < at.len ? g.V - v0 - col : 0);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) xv_part += x[j] * v.at(j);
+                    put8<INNER>(xt + row * LDV, PLANE_V, col, x);
+                }
+                if (HALVES == 1 || threadIdx.x >= 256) {
+                    float x[8];
+                    eight(up, x);
+                    put8<INNER>(ut + row * LDV, PLANE_V, col, x);
+                    Some<T, 8> v;
+                    v.load(yp + row * g.y_stride + v0 + col, row < at.len ? g.V - v0 - col : 0);
+                    put8_stored<T>(yt + row * LDV, PLANE_V, col, v);
+                }
+            }
+            __syncthreads();
+            Frag ya[RAW], xa[INNER], ua[INNER];
+            frags_rows<RAW, LDV>(ya, yt, PLANE_V, mt * 16, 0);
+            frags_rows<INNER, LDV>(xa, xt, PLANE_V, mt * 16, 0);
+            frags_rows<INNER, LDV>(ua, ut, PLANE_V, mt * 16, 0);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                if (n > mt) continue;
+                Frag b[INNER];
+                frags_rows<INNER, LDV>(b, ut, PLANE_V, n * 16, 0);
+                if (does_f) mma<RAW, INNER>(yu[n], ya, b);
+                if (does_m) mma<INNER, INNER>(xu[n], xa, b);
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                Frag b[INNER];
+                frags_rows<INNER, LDV>(b, st, PLANE_S, col0 + t * 16, 0);
+                mma<RAW, INNER>(ys[t], ya, b);
+                mma<INNER, INNER>(xs[t], xa, b);
+            }
+            if constexpr (C::TURNS) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int n = threadIdx.x + i * THREADS;
+                    put8<INNER>(dst + n / (VB / 8) * LDV, PLANE_S, n % (VB / 8) * 8, keep[i]);
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                Frag b[INNER];
+                frags_rows<INNER, LDV>(b, dst, PLANE_S, col0 + t * 16, 0);
+                mma<INNER, INNER>(us[t], ua, b);
+            }
+        }
+        __syncthreads();                                 // the first region is free
+        ss = lanes_sum(ss);
+        if (lane == 0) wave_sums[wv] = ss;
+        xv_part += lane_move<DPP_XOR1>(xv_part);
+        xv_part += lane_move<DPP_XOR2>(xv_part);
+        if (threadIdx.x < 256 && threadIdx.x % 4 == 0) xv[threadIdx.x / 4] = xv_part;
+
+        // F and M + M^T, and what of their products passes each token
+        {
+            const double *const G = reinterpret_cast<const double *>(vec + VEC_G * 64);
+            float rm[4], before[4];                      // before: the sums of the tiles to the left
+#pragma unroll
+            for (int r = 0; r < 4; ++r) rm[r] = before[r] = 0.f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int j = n * 16 + m;
+                const double gj = G[j];
+                const float kj = vec[VEC_RK * 64 + j];
+                float pass = 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = mt * 16 + 4 * q4 + r;
+                    const float e = i >= j ? expf((float)(G[i] - gj)) * kj : 0.f;
+                    float x = 0.f;
+                    uint32_t p[INNER];
+                    if (does_f) {
+                        const float f = i >= j ? g.scale * vec[VEC_RQ * 64 + i] * e * yu[n][r] : 0.f;
+                        x += f * qk[n][r];
+                        split2<INNER>(f, 0.f, p);
+#pragma unroll
+                        for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + i * LDM + place(j)] = (bf16_t)p[k];
+                    }
+                    if (does_m && i >= j) {
+                        const float b = i > j ? -vec[VEC_RK * 64 + i] * e * xu[n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
+                        rm[r] += b * kk[n][r];
+                        x += f * kk[n][r];
+                        split2<INNER>(f, 0.f, p);
+#pragma unroll
+                        for (int k = 0; k < INNER; ++k) {
+                            mm[k * PLANE_M + i * LDM + place(j)] = (bf16_t)p[k];
+                            mm[k * PLANE_M + j * LDM + place(i)] = (bf16_t)p[k];
+                        }
+                    }
+                    // the sum over the columns before j, of the rows from j on
+                    float left = lane_move<DPP_SHR1>(x);
+                    left += lane_move<DPP_SHR1>(left);
+                    left += lane_move<DPP_SHR2>(left);
+                    left += lane_move<DPP_SHR4>(left);
+                    left += lane_move<DPP_SHR8>(left);
+                    pass += i >= j ? left + before[r] : 0.f;
+                    before[r] += row_sum(x);
+                }
+                pass = rows_join(pass, pass);
+                pass = halves_join(pass, pass);
+                if (q4 == 0) passing[wv * 64 + j] = pass;
+            }
+            if (does_m) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    rm[r] = row_sum(rm[r]);
+                    if (m == 0) row_m[mt * 16 + 4 * q4 + r] = rm[r];
+                }
+            }
+        }
+        put_tile(qp, g.q_stride);
+        __syncthreads();
+        {
+            float dot[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot[r] = 0.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = mt * 16 + 4 * q4 + r;
+                    const float x = ys[t][r] * vec[VEC_ASK * 64 + i];
+                    gq[t][r] += x;
+                    dot[r] += x * tile_at(i, col0 + t * 16 + m);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { dot[r] = row_sum(dot[r]); if (m == 0) dot_a[half * 64 + mt * 16 + 4 * q4 + r] = dot[r]; }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if (ks < mt / 2) continue;
+                Frag a[INNER];
+                frags_cols<INNER, LDM>(a, fm, PLANE_M, ks * 32, mt * 16);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    Frag b[RAW];
+                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16);
+                    mma<INNER, RAW>(gk[t], a, b);
+                }
+            }
+        }
+        __syncthreads();
+        put_tile(kp, g.k_stride);
+        __syncthreads();
+        {
+            float db_[4], dc_[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) db_[r] = dc_[r] = 0.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = mt * 16 + 4 * q4 + r;
+                    const float k = tile_at(i, col0 + t * 16 + m);
+                    const float x = xs[t][r] * vec[VEC_READ * 64 + i], u = us[t][r] * vec[VEC_WRITE * 64 + i];
+                    gk[t][r] += u - vec[VEC_BETA * 64 + i] * x;
+                    db_[r] += x * k;
+                    dc_[r] += u * k;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                db_[r] = row_sum(db_[r]);
+                dc_[r] = row_sum(dc_[r]);
+                if (m == 0) {
+                    dot_b[half * 64 + mt * 16 + 4 * q4 + r] = db_[r];
+                    dot_c[half * 64 + mt * 16 + 4 * q4 + r] = dc_[r];
+                }
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Frag a[INNER], b2[INNER];
+                frags_rows<INNER, LDM>(a, fm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, LDM>(b2, mm, PLANE_M, mt * 16, ks * 32);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    Frag b[RAW];
+                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16);
+                    if (ks <= mt / 2) mma<INNER, RAW>(gq[t], a, b);
+                    mma<INNER, RAW>(gk[t], b2, b);
+                }
+            }
+        }
+        __syncthreads();
+        if (wv == 0) {                                   // gates: a lane a token
+            const float beta = vec[VEC_BETA * 64 + lane];
+            float a = dot_a[lane], b = dot_b[lane], c = dot_c[lane];
+            if constexpr (HALVES == 2) { a += dot_a[64 + lane]; b += dot_b[64 + lane]; c += dot_c[64 + lane]; }
+            float pass = 0.f, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < THREADS / 64; ++i) {
+                pass += passing[i * 64 + lane];
+                sum += wave_sums[i];
+            }
+            // what is read from the token on, and what was written before it
+            const float left = __shfl_up(c, 1, 64);      // (by all lanes: one that is not here hands out nothing)
+            double d = (double)(a - beta * b), w = lane ? (double)left : 0.0;
+#pragma unroll
+            for (int off = 1; off < 64; off *= 2) {
+                const double down = __shfl_down(d, off, 64), up = __shfl_up(w, off, 64);
+                if (lane + off < 64) d += down;
+                if (lane >= off) w += up;
+            }
+            const float dbeta = xv[lane] - b + row_m[lane];
+            float dg = (float)(d + w + (double)(pass + vec[VEC_ONE * 64] * sum)), for_a = 0.f, for_A = 0.f;
+            if (lane < at.len) {
+                const float raw = gd_raw(g, ldf((const T *)g.a + (at.first + lane) * g.a_stride + h), h), soft = gd_soft(g, raw), A = g.A ? g.A[h] : -1.f;
+                if (A * soft < GD_LEAST) dg = 0.f;
+                for_A = dg * soft;
+                for_a = dg * A * (g.softplus ? 1.f / (1.f + expf(-raw)) : 1.f);
+                const float rate = gd_rate(g, ldf((const T *)g.b + (at.first + lane) * g.b_stride + h));
+                stf(da + (at.first + lane) * g.a_stride + h, for_a);
+                stf(db + (at.first + lane) * g.b_stride + h, g.sigmoid ? dbeta * rate * (1.f - rate) : dbeta);
+            }
+            for_A = lanes_sum(for_A);
+            for_a = lanes_sum(for_a);
+            if (lane == 0) {
+                s.partials[(long long)id * 2 * g.H + h] = for_A;
+                s.partials[(long long)id * 2 * g.H + g.H + h] = for_a;
+            }
+        }
+    }
+
+    // The lengths: of n = r x the gradient r (dn - n (n.dn)), where the factor r is in already.  The tile holds the keys.
+    const float *const vec = reinterpret_cast<const float *>(s.vec + ((long long)id * g.H + kh * share) * l.vectors);
+    auto finish = [&](v4f_t (&grad)[TILES], int which, T *out, long long stride) {
+        float dot[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) dot[r] = 0.f;
+        if (g.norm) {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dot[r] += grad[t][r] * tile_at(mt * 16 + 4 * q4 + r, col0 + t * 16 + m);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot[r] = row_sum(dot[r]);
+            if constexpr (HALVES == 2) {
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (m == 0) dot_a[half * 64 + mt * 16 + 4 * q4 + r] = dot[r];
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dot[r] = dot_a[mt * 16 + 4 * q4 + r] + dot_a[64 + mt * 16 + 4 * q4 + r];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = mt * 16 + 4 * q4 + r;
+            const float inv = vec[which * 64 + i], f = g.norm ? inv * inv * dot[r] : 0.f;
+            if (i >= at.len) continue;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const int col = col0 + t * 16 + m;
+                if (col < g.K) stf(out + i * stride + col, g.norm ? grad[t][r] - f * tile_at(i, col) : grad[t][r]);
+            }
+        }
+    };
+    finish(gk, VEC_RK, dk + at.first * g.k_stride + (long long)kh * g.K, g.k_stride);
+    __syncthreads();
+    put_tile(qp, g.q_stride);
+    __syncthreads();
+    finish(gq, VEC_RQ, dq + at.first * g.q_stride + (long long)kh * g.K, g.q_stride);
+}
+
+template <typename T, int KP>
+hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dq, void *dk, void *da, void *db, hipStream_t stream)
+{
+    typedef Back<T, KP> C;
+    static_assert(C::LDS <= 160 * 1024, "LDS of a compute unit");
+    const auto kernel = k_gdelta_bwd_rows<T, KP>;
+    const hipError_t e = gd_lds(kernel, C::LDS);
+    if (e != hipSuccess) return e;
+    return gd_launches(l.chunks, C::THREADS, [&](unsigned first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(C::THREADS), C::LDS, stream, g, l, s, (const T *)dy, (T *)dq, (T *)dk, (T *)da, (T *)db, first);
+    });
+}
+
+template <typename T>
+hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dq, void *dk, void *da, void *db, hipStream_t stream)
+{
+    switch (l.KP) {
+    case 32: return launch<T, 32>(g, l, s, dy, dq, dk, da, db, stream);
+    case 64: return launch<T, 64>(g, l, s, dy, dq, dk, da, db, stream);
+    case 128: return launch<T, 128>(g, l, s, dy, dq, dk, da, db, stream);
+    default: return launch<T, 256>(g, l, s, dy, dq, dk, da, db, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_gdelta_bwd_rows(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dq, void *dk, void *da, void *db,
+                                  hipStream_t stream)
+{
+    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, dy, dq, dk, da, db, stream) : launch_of<bf16_t>(g, l, s, dy, dq, dk, da, db, stream);
+}
+
+}  // namespace dwc

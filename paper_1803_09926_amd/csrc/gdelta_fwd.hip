@@ -1,0 +1,292 @@
+// The gated delta rule, the walk over a sequence's chunks: what they answer, and the state behind them.
+//
+// A block of four wavefronts has 16 or 32 columns of a head's state a wavefront in registers, from the sequence's first chunk to its last; the columns are independent.
+// Of each chunk, with the first pass's T and P and the state S before it,
+//   U = T (beta * (V - exp(G) * K S)),  Y = scale exp(G) * Q S + P U,  S = exp(G_end) S + (exp(G_end - G) * K)^T U
+// all as products on the matrix cores: S, V, U and Y never leave the registers, as a result tile is an operand as it lies; K, Q, T and P go through LDS, and the next ones
+// are on their way from memory meanwhile.
+#include "gdelta_states.hpp"
+
+namespace dwc {
+
+namespace {
+
+template <typename T, int KP, int NT, bool SHARE>
+__global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
+                                                           float *__restrict__ final, unsigned first, int blocks)
+{
+    typedef Walk<T, KP, SHARE> W;
+    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM;
+    extern __shared__ __align__(16) char lds[];
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
+    bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
+    float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
+    const unsigned bid = first + blockIdx.x;
+    const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const Columns<NT> cols((int)(bid % (unsigned)blocks));
+    const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
+    const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
+    const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const vp = (const T *)g.v + (long long)h * g.V;
+
+    v4f_t S[KP / 16][NT];
+    const long long state = ((long long)seq * g.H + h) * g.K * g.V;
+#pragma unroll
+    for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float x[NT];
+            const int row = row_of(ct, r);
+            cols.load(init + state + (long long)row * g.V, g.V, init && row < g.K, x);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt][r] = x[nt];
+        }
+    Frag Sp[KP / 32][NT][INNER];
+    auto split_state = [&] {
+#pragma unroll
+        for (int c = 0; c < KP / 32; ++c)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c][nt], S[2 * c + 1][nt], Sp[c][nt]);
+    };
+    split_state();
+
+    Rows<T, KP, THREADS> rows;
+    Matrix<INNER, THREADS> matrix;
+    float v[4][4][NT];
+    auto load_keys = [&](long long c) {
+        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
+        rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
+        matrix.load(s.T + ((base + c) * g.H + h) * l.matrix);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) cols.load(vp + (at + row_of(mt, r)) * g.v_stride, g.V, row_of(mt, r) < len, v[mt][r]);
+    };
+    if (chunks > 0) load_keys(0);
+    for (long long c = 0; c < chunks; ++c) {
+        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = (base + c) * g.H + h;
+        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+        float *const vl = vecs + (c & 1) * 256;
+        if (SHARE && c) __syncthreads();
+        rows.template put<LD>(kt);
+        matrix.put(tm);
+        vl[threadIdx.x] = vec[threadIdx.x];
+        rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
+        matrix.load(s.P + where * l.matrix);
+        const float decay = vec[VEC_ONE * 64];
+        const int bad = reinterpret_cast<const int *>(vec + VEC_ONE * 64)[1];
+        __syncthreads();
+        if (s.S) {
+#pragma unroll
+            for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
+                    cols.store(s.S + where * (l.state / 4) + (long long)row_of(ct, r) * l.VP, l.VP, true, x);
+                }
+        }
+        // What is not finite in v, or the first key or gate that is not: from there on the column is, and before it nothing is of it.
+        int from[NT];
+        bool odd = bad < CHUNK;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            from[nt] = bad;
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!finite(v[mt][r][nt])) { from[nt] = min(from[nt], row_of(mt, r)); odd = true; }
+        }
+        odd = __any(odd);
+        if (odd) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                from[nt] = min(from[nt], __shfl_xor(from[nt], 16, 64));
+                from[nt] = min(from[nt], __shfl_xor(from[nt], 32, 64));
+            }
+        }
+        v4f_t R[4][NT];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) R[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c0 = 0; c0 < KP / 32; ++c0)
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+                Frag a[RAW];
+                frags_rows<RAW, LD>(a, kt, PLANE, mt * 16, c0 * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(R[mt][nt], a, Sp[c0][nt]);
+            }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            const float4 read = four(vl + VEC_READ * 64, mt), beta = four(vl + VEC_BETA * 64, mt);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const v4f_t x = {v[mt][0][nt], v[mt][1][nt], v[mt][2][nt], v[mt][3][nt]};
+                R[mt][nt] = times(x - times(R[mt][nt], read), beta);
+            }
+        }
+        if (odd) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (row_of(mt, r) >= from[nt]) R[mt][nt][r] = 0.f;
+        }
+        Frag f[2][NT][INNER];
+        split_rows<INNER, NT>(R, f);
+        v4f_t U[4][NT];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks <= mt / 2; ++ks) {
+                Frag a[INNER];
+                frags_rows<INNER, LDM>(a, tm, PLANE_M, mt * 16, ks * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(U[mt][nt], a, f[ks][nt]);
+            }
+        }
+        if (s.U) {
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) x[nt] = U[mt][nt][r];
+                    cols.store(s.U + where * (l.rows / 4) + (long long)row_of(mt, r) * l.VP, l.VP, true, x);
+                }
+        }
+        v4f_t w[4][NT];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            const float4 write = four(vl + VEC_WRITE * 64, mt);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) w[mt][nt] = times(U[mt][nt], write);
+        }
+        split_rows<INNER, NT>(w, f);
+#pragma unroll
+        for (int ct = 0; ct < KP / 16; ++ct) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Frag a[RAW];
+                frags_cols<RAW, LD>(a, kt, PLANE, ks * 32, ct * 16);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
+            }
+        }
+        if constexpr (SHARE) __syncthreads();
+        rows.template put<LD>(qt);
+        matrix.put(pm);
+        if (c + 1 < chunks) load_keys(c + 1);
+        __syncthreads();
+        split_rows<INNER, NT>(U, f);
+        v4f_t O[4][NT];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c0 = 0; c0 < KP / 32; ++c0)
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+                Frag a[RAW];
+                frags_rows<RAW, LD>(a, qt, PLANE, mt * 16, c0 * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(O[mt][nt], a, Sp[c0][nt]);
+            }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            const float4 ask = four(vl + VEC_ASK * 64, mt);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
+#pragma unroll
+            for (int ks = 0; ks <= mt / 2; ++ks) {
+                Frag a[INNER];
+                frags_rows<INNER, LDM>(a, pm, PLANE_M, mt * 16, ks * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(O[mt][nt], a, f[ks][nt]);
+            }
+        }
+        if (odd) {
+            const float nan = __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (row_of(mt, r) >= from[nt]) O[mt][nt][r] = nan;
+#pragma unroll
+                for (int ct = 0; ct < KP / 16; ++ct)
+                    if (from[nt] < CHUNK) S[ct][nt] = v4f_t{nan, nan, nan, nan};
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) x[nt] = O[mt][nt][r];
+                const int row = row_of(mt, r);
+                cols.store(y + (at + row) * g.y_stride + (long long)h * g.V, g.V, row < len, x);
+            }
+        split_state();
+    }
+    if (!final) return;
+#pragma unroll
+    for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float x[NT];
+            const int row = row_of(ct, r);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
+            cols.store(final + state + (long long)row * g.V, g.V, row < g.K, x);
+        }
+}
+
+template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+{
+    constexpr bool SHARE = shares<T, KP>();
+    constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    const auto kernel = k_gdelta_fwd<T, KP, NT, SHARE>;
+    const hipError_t e = gd_lds(kernel, lds);
+    if (e != hipSuccess) return e;
+    const int blocks = cdiv(l.VP, WAVES * 16 * NT);
+    return gd_launches((long long)g.sequences * blocks, THREADS, [&](unsigned first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, init, (T *)y, final, first, blocks);
+    });
+}
+
+template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+{
+    const bool wide = l.VP > 64;
+    switch (l.KP) {
+    case 32: return wide ? launch<T, 32, 2>(g, l, s, init, y, final, stream) : launch<T, 32, 1>(g, l, s, init, y, final, stream);
+    case 64: return wide ? launch<T, 64, 2>(g, l, s, init, y, final, stream) : launch<T, 64, 1>(g, l, s, init, y, final, stream);
+    case 128: return wide ? launch<T, 128, 2>(g, l, s, init, y, final, stream) : launch<T, 128, 1>(g, l, s, init, y, final, stream);
+    default: return launch<T, 256, 1>(g, l, s, init, y, final, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+{
+    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, init, y, final, stream) : launch_of<bf16_t>(g, l, s, init, y, final, stream);
+}
+
+}  // namespace dwc

@@ -1,0 +1,304 @@
+// The gated delta rule, first pass: what a chunk's keys, queries and gates give without its state, for all chunks of 64 tokens at once.
+//
+// With G the sum of the decays' logarithms from the chunk's start, and S the state before the chunk, what its tokens write is U with
+//   U = T (beta * (V - exp(G) * K S)),  T = (I + L)^-1,  L[i,j] = beta[i] exp(G[i] - G[j]) k[i].k[j] below the diagonal
+// and what they answer is exp(G) * Q S + P U with P[i,j] = scale exp(G[i] - G[j]) q[i].k[j] on and below it.  T and P are made here.
+//
+// One block of four wavefronts a chunk and key head; the products of q and k are taken once and serve all value heads.  T by blocks of 16: the four on the
+// diagonal by substitution, one a wavefront, and each column of blocks below by products with the fp32 matrix instruction, a wavefront each.
+#include "gdelta_tile.hpp"
+#include "gdelta_launch.hpp"
+
+namespace dwc {
+
+namespace {
+
+constexpr int THREADS = 256, LDF = 68;            // floats of a row of an fp32 matrix in LDS
+
+template <typename T, int KP> struct Prep {
+    static constexpr int RAW = PartsOf<T>::RAW, LD = KP + PAD;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, F32S = (size_t)CHUNK * LDF * 4;
+    static constexpr size_t LDS = TILE + 2 * F32S + 64 * 8 + 5 * 64 * 4;
+};
+
+// the parts of an fp32 matrix in LDS, into memory
+template <int N> __device__ __forceinline__ void put_matrix(const float *f, char *to)
+{
+    const int row = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
+    bf16_t *const p = reinterpret_cast<bf16_t *>(to) + row * CHUNK;
+#pragma unroll
+    for (int j = 0; j < 16; j += 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = f[row * LDF + c + j + i];
+        put8<N>(p, CHUNK * CHUNK, c + j, x);
+    }
+}
+
+template <typename T, int KP>
+__global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restrict__ t_out, char *__restrict__ p_out, char *__restrict__ vec_out, long long matrix,
+                                                         long long vectors, unsigned first)
+{
+    typedef Prep<T, KP> C;
+    constexpr int RAW = C::RAW, INNER = PartsOf<T>::INNER, LD = C::LD, PLANE = CHUNK * LD;
+    extern __shared__ __align__(16) char lds[];
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds);
+    float *const L = reinterpret_cast<float *>(lds + C::TILE), *const X = L + CHUNK * LDF;      // L, then P; the inverse
+    double *const Gs = reinterpret_cast<double *>(X + CHUNK * LDF);
+    float *const betas = reinterpret_cast<float *>(Gs + 64), *const rks = betas + 64, *const rqs = rks + 64;
+    int *const bads = reinterpret_cast<int *>(rqs + 64);          // [64] tokens whose key is not finite
+    const unsigned id = first + blockIdx.x;
+    const ChunkAt at = gd_chunk(g, (int)id);
+    if (at.len == 0) return;
+    const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, m = lane & 15, q4 = lane >> 4;
+
+    // keys into LDS; a token's key that is not finite counts as none, and the token is remembered
+    if (threadIdx.x < 64) bads[threadIdx.x] = 0;
+    __syncthreads();
+    {
+        const T *const p = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K;
+        constexpr int PER_ROW = KP / 8;
+        for (int i = threadIdx.x; i < CHUNK * PER_ROW; i += THREADS) {
+            const int row = i / PER_ROW, col = i % PER_ROW * 8;
+            Some<T, 8> v;
+            v.load(p + row * g.k_stride + col, row < at.len ? g.K - col : 0);
+            bool bad = false;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bad |= !finite(v.at(j));
+            if (bad) bads[row] = 1;
+            put8_stored<T>(kt + row * LD, PLANE, col, v);
+        }
+    }
+    __syncthreads();
+    // lengths: four lanes a key
+    {
+        const int row = threadIdx.x / 4;
+        const bool bad = bads[row] != 0;
+        float s = 0.f;
+        for (int c = threadIdx.x % 4 * 8; c < KP; c += 32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v = 0.f;
+#pragma unroll
+                for (int i = RAW - 1; i >= 0; --i) v += bf16_to_f32(kt[i * PLANE + row * LD + c + j]);
+                s += v * v;
+                if (bad) {
+#pragma unroll
+                    for (int i = 0; i < RAW; ++i) kt[i * PLANE + row * LD + c + j] = 0;
+                }
+            }
+        }
+        s += lane_move<DPP_XOR1>(s);
+        s += lane_move<DPP_XOR2>(s);
+        if (threadIdx.x % 4 == 0) {
+            const float rk = row >= at.len || bad ? 0.f : g.norm ? 1.f / sqrtf(s + g.eps) : 1.f;
+            if (!finite(rk)) bads[row] = 1;              // (a key of length zero without eps)
+            rks[row] = finite(rk) ? rk : 0.f;
+        }
+    }
+    // queries: each wavefront its 16 rows, straight from memory in the order of the operands
+    Frag qa[KP / 32][RAW];
+    {
+        const int row = wv * 16 + m;
+        const T *const p = (const T *)g.q + (at.first + row) * g.q_stride + (long long)kh * g.K;
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < KP / 32; ++c) {
+            Some<T, 4> v[2];
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int col = c * 32 + i * 16 + q4 * 4;
+                v[i].load(p + col, row < at.len ? g.K - col : 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[4 * i + j] = v[i].at(j);
+                    s += x[4 * i + j] * x[4 * i + j];
+                }
+            }
+            uint32_t w[4][RAW];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) split2<RAW>(x[2 * i], x[2 * i + 1], w[i]);
+#pragma unroll
+            for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
+        }
+        s = rows_join(s, s);
+        s = halves_join(s, s);
+        if (q4 == 0) rqs[row] = row >= at.len ? 0.f : g.norm ? 1.f / sqrtf(s + g.eps) : 1.f;
+    }
+    __syncthreads();
+    v4f_t kk[4], qk[4];                                  // rows 16 wv.., columns 16 n..
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        kk[n] = qk[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        if (n > wv) continue;
+#pragma unroll
+        for (int c = 0; c < KP / 32; ++c) {
+            Frag a[RAW], b[RAW];
+            frags_rows<RAW, LD>(a, kt, PLANE, wv * 16, c * 32);
+            frags_rows<RAW, LD>(b, kt, PLANE, n * 16, c * 32);
+            mma<RAW, RAW>(kk[n], a, b);
+            mma<RAW, RAW>(qk[n], qa[c], b);
+        }
+    }
+
+    for (int hh = 0; hh < share; ++hh) {
+        const int h = kh * share + hh;
+        const long long where = (long long)id * g.H + h;
+        float *const vec = reinterpret_cast<float *>(vec_out + where * vectors);
+        // gates, by each wavefront: a lane a token
+        const bool here = lane < at.len;
+        float d = 0.f, beta = 0.f;
+        if (here) {
+            d = gd_log_decay(g, gd_raw(g, ldf((const T *)g.a + (at.first + lane) * g.a_stride + h), h), h);
+            beta = gd_rate(g, ldf((const T *)g.b + (at.first + lane) * g.b_stride + h));
+        }
+        const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
+        const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
+        if (lane >= bad_from) d = beta = 0.f;
+        double G = d;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const double up = __shfl_up(G, off, 64);
+            if (lane >= off) G += up;
+        }
+        const double end = __shfl(G, 63, 64);
+        __syncthreads();                                 // the head before has been read
+        if (wv == 0) {
+            Gs[lane] = G;
+            betas[lane] = beta;
+            const float rk = rks[lane], rq = rqs[lane], lam = expf((float)G);
+            vec[VEC_READ * 64 + lane] = lam * rk;
+            vec[VEC_BETA * 64 + lane] = beta;
+            vec[VEC_WRITE * 64 + lane] = expf((float)(end - G)) * rk;
+            vec[VEC_ASK * 64 + lane] = g.scale * lam * rq;
+            vec[VEC_RQ * 64 + lane] = rq;
+            vec[VEC_RK * 64 + lane] = rk;
+            reinterpret_cast<double *>(vec + VEC_G * 64)[lane] = G;
+            if (lane == 0) {
+                vec[VEC_ONE * 64] = expf((float)end);
+                reinterpret_cast<int *>(vec + VEC_ONE * 64)[1] = bad_from;
+            }
+        }
+        __syncthreads();
+        v4f_t pv[4];
+        {
+            double gi[4];
+            float bi[4], ki[4], qi[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = wv * 16 + 4 * q4 + r;
+                gi[r] = Gs[i]; bi[r] = betas[i]; ki[r] = rks[i]; qi[r] = g.scale * rqs[i];
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int j = n * 16 + m;
+                const double gj = Gs[j];
+                const float kj = rks[j];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wv * 16 + 4 * q4 + r;
+                    const float e = i >= j ? expf((float)(gi[r] - gj)) * kj : 0.f;
+                    pv[n][r] = i >= j ? qi[r] * e * qk[n][r] : 0.f;
+                    L[i * LDF + j] = i > j ? bi[r] * ki[r] * e * kk[n][r] : 0.f;
+                }
+            }
+        }
+        __syncthreads();
+        // the inverse of the diagonal block wv: lane m has its column m
+        {
+            const float *const D = L + wv * 16 * LDF + wv * 16;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float s = i == m ? 1.f : 0.f;
+#pragma unroll
+                for (int j = 0; j < i; ++j) s -= D[i * LDF + j] * x[j];
+                x[i] = s;
+            }
+            if (q4 == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) X[(wv * 16 + i) * LDF + wv * 16 + m] = x[i];
+            }
+        }
+        __syncthreads();
+        // the blocks of column wv below the diagonal, and zeros above it
+        {
+            v4f_t col[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) col[0][r] = X[(wv * 16 + 4 * q4 + r) * LDF + wv * 16 + m];
+#pragma unroll
+            for (int n = 1; n < 4; ++n) {
+                const int i = wv + n;                    // block row
+                if (i > 3) break;
+                v4f_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < n; ++k) {
+                    const float4 a = *reinterpret_cast<const float4 *>(L + (i * 16 + m) * LDF + (wv + k) * 16 + 4 * q4);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, col[k][0], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, col[k][1], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, col[k][2], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, col[k][3], s, 0, 0, 0);
+                }
+                const float4 a = *reinterpret_cast<const float4 *>(X + (i * 16 + m) * LDF + i * 16 + 4 * q4);
+                v4f_t c = {0.f, 0.f, 0.f, 0.f};
+                c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, -s[0], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, -s[1], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, -s[2], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, -s[3], c, 0, 0, 0);
+                col[n] = c;
+            }
+            // (the diagonal blocks that others read are not written here)
+#pragma unroll
+            for (int n = 1; n < 4; ++n) {
+                if (wv + n < 4) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) X[((wv + n) * 16 + 4 * q4 + r) * LDF + wv * 16 + m] = col[n][r];
+                }
+                if (n <= wv) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) X[((wv - n) * 16 + 4 * q4 + r) * LDF + wv * 16 + m] = 0.f;
+                }
+            }
+        }
+        __syncthreads();
+        put_matrix<INNER>(X, t_out + where * matrix);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) L[(wv * 16 + 4 * q4 + r) * LDF + n * 16 + m] = pv[n][r];
+        __syncthreads();
+        put_matrix<INNER>(L, p_out + where * matrix);
+    }
+}
+
+template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
+{
+    const auto kernel = k_gdelta_prep<T, KP>;
+    constexpr size_t lds = Prep<T, KP>::LDS;
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    const hipError_t e = gd_lds(kernel, lds);
+    if (e != hipSuccess) return e;
+    return gd_launches(l.chunks, THREADS, [&](unsigned first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(THREADS), lds, stream, g, s.T, s.P, s.vec, l.matrix, l.vectors, first);
+    });
+}
+
+template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
+{
+    switch (l.KP) {
+    case 32: return launch<T, 32>(g, l, s, stream);
+    case 64: return launch<T, 64>(g, l, s, stream);
+    case 128: return launch<T, 128>(g, l, s, stream);
+    default: return launch<T, 256>(g, l, s, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
+{
+    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, stream) : launch_of<bf16_t>(g, l, s, stream);
+}
+
+}  // namespace dwc

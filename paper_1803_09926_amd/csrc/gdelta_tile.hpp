@@ -1,0 +1,227 @@
+// Tiles of the gated delta rule's matrix products.
+//
+// All products run on the bf16 matrix instruction of 16 x 16 x 32.  A number of 32 bits takes part as a sum of bf16 parts: what a bf16 tensor holds is one part; what
+// the kernels compute themselves (states, inverses, what tokens write) two parts of bf16 tensors' passes, 2^-17 of itself; and everything three parts of fp32
+// tensors' passes, which hold all of its 24 bits.  Of a product of parts those count whose order is below the larger number of parts (1 x 2: two instructions, 2 x 2:
+// three, 3 x 3: six).  All sums are fp32.
+//
+// Lanes: m = lane % 16, q = lane / 16.  A result tile has rows 4 q + r (r = 0..3) of column m in a lane.  Two result tiles below each other are an operand as they are: the
+// contraction runs over their 32 rows in the order 4 q + 0..3 of the first, 4 q + 0..3 of the second.  Tiles in LDS are stored so that 16 consecutive bytes of a row hold the
+// same order (within every 32 columns), and columns are read through the transposing reads of LDS.
+#pragma once
+#include "gdelta.hpp"
+
+namespace dwc {
+
+namespace {
+
+typedef float v4f_t __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b_t __attribute__((ext_vector_type(8)));
+typedef short v4h_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u4t_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2t_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// `blocks` workgroups in launches that each have fewer than 2^32 lanes: f(the first, how many)
+template <typename F> hipError_t gd_launches(long long blocks, int threads, F f)
+{
+    const long long most = most_blocks(threads);
+    for (long long first = 0; first < blocks; first += most) f((unsigned)first, (unsigned)(blocks - first < most ? blocks - first : most));
+    return hipGetLastError();
+}
+// more LDS than a launch has without being told
+template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+constexpr int CHUNK = 64;
+constexpr int PAD = 8;                            // elements behind a row of an LDS tile: rows start at other banks
+constexpr int LDM = CHUNK + PAD;                  // of a tile of CHUNK columns
+
+template <typename T> struct PartsOf;
+template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1, INNER = 2; };
+template <> struct PartsOf<float> { static constexpr int RAW = 3, INNER = 3; };
+
+struct Frag { u4t_t w; };
+
+__device__ __forceinline__ v4f_t mfma(const Frag &a, const Frag &b, v4f_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b_t, a.w), __builtin_bit_cast(v8b_t, b.w), c, 0, 0, 0);
+}
+template <int PA, int PB> __device__ __forceinline__ void mma(v4f_t &c, const Frag (&a)[PA], const Frag (&b)[PB])
+{
+    constexpr int ORDER = PA > PB ? PA : PB;
+#pragma unroll
+    for (int i = PA - 1; i >= 0; --i)             // the small ones first
+#pragma unroll
+        for (int j = PB - 1; j >= 0; --j)
+            if (i + j < ORDER) c = mfma(a[i], b[j], c);
+}
+
+// two numbers as N parts, each a pair of bf16: what is left after a part is taken is exact
+template <int N> __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p[i] = pack2_bf16(x, y);
+        if (i + 1 < N) {
+            x -= __uint_as_float(p[i] << 16);
+            y -= __uint_as_float(p[i] & 0xffff0000u);
+        }
+    }
+}
+// two result tiles, one below the other, as an operand
+template <int N> __device__ __forceinline__ void split_tiles(const v4f_t &a, const v4f_t &b, Frag (&f)[N])
+{
+    uint32_t p[4][N];
+    split2<N>(a[0], a[1], p[0]);
+    split2<N>(a[2], a[3], p[1]);
+    split2<N>(b[0], b[1], p[2]);
+    split2<N>(b[2], b[3], p[3]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i].w = u4t_t{p[0][i], p[1][i], p[2][i], p[3][i]};
+}
+
+// where in an LDS row the four columns from 4 * j4 on lie
+__device__ __forceinline__ constexpr int place4(int j4) { return (j4 >> 3) * 32 + (j4 & 3) * 8 + ((j4 >> 2) & 1) * 4; }
+__device__ __forceinline__ constexpr int place(int col) { return place4(col >> 2) + (col & 3); }
+
+// Operands out of LDS tiles of leading dimension LD.  rows: 16 of them from r0, contracted over the 32 columns from c0 on.  cols: 16 of them from c0, contracted over
+// the 32 rows from r0 on.
+template <int LD> __device__ __forceinline__ Frag frag_rows(const bf16_t *tile, int r0, int c0)
+{
+    const int lane = threadIdx.x & 63;
+    return {*reinterpret_cast<const u4t_t *>(tile + (r0 + (lane & 15)) * LD + c0 + (lane >> 4) * 8)};
+}
+typedef __attribute__((address_space(3))) v4h_t *lds_v4h_t;
+template <int LD> __device__ __forceinline__ Frag frag_cols(const bf16_t *tile, int r0, int c0)
+{
+    const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    const bf16_t *const p = tile + (r0 + 4 * q + (m >> 2)) * LD + place4((c0 >> 2) + (m & 3));
+    const v4h_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)p);
+    const v4h_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)(p + 16 * LD));
+    const u2t_t x = __builtin_bit_cast(u2t_t, a), y = __builtin_bit_cast(u2t_t, b);
+    return {u4t_t{x.x, x.y, y.x, y.y}};
+}
+template <int N, int LD> __device__ __forceinline__ void frags_rows(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = frag_rows<LD>(tile + i * plane, r0, c0);
+}
+template <int N, int LD> __device__ __forceinline__ void frags_cols(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = frag_cols<LD>(tile + i * plane, r0, c0);
+}
+
+// eight consecutive numbers from a column that is a multiple of 8 on, into a row of an LDS tile of N parts
+template <int N> __device__ __forceinline__ void put8(bf16_t *row, int plane, int col, const float (&x)[8])
+{
+    uint32_t p[4][N];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], x[2 * i + 1], p[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        *reinterpret_cast<u2t_t *>(row + i * plane + place4(col >> 2)) = u2t_t{p[0][i], p[1][i]};
+        *reinterpret_cast<u2t_t *>(row + i * plane + place4((col >> 2) + 1)) = u2t_t{p[2][i], p[3][i]};
+    }
+}
+// the same for eight numbers as stored
+template <typename T> __device__ __forceinline__ void put8_stored(bf16_t *row, int plane, int col, const Some<T, 8> &v)
+{
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u2t_t *>(row + place4(col >> 2)) = u2t_t{v.w[0], v.w[1]};
+        *reinterpret_cast<u2t_t *>(row + place4((col >> 2) + 1)) = u2t_t{v.w[2], v.w[3]};
+    } else {
+        float x[8];
+        v.get(x);
+        put8<PartsOf<T>::RAW>(row, plane, col, x);
+    }
+}
+
+// A tile of 64 rows of KP columns on its way from memory to LDS: held by THREADS lanes, of which each has every THREADS-th eight columns
+template <typename T, int KP, int THREADS> struct Rows {
+    static constexpr int PER_ROW = KP / 8, N = CHUNK * PER_ROW / THREADS;
+    static_assert(CHUNK * PER_ROW % THREADS == 0, "all lanes alike");
+    Some<T, 8> v[N];
+    // len rows of `width` columns are there
+    __device__ __forceinline__ void load(const T *p, long long stride, int len, int width)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, col = at % PER_ROW * 8;
+            v[i].load(p + row * stride + col, row < len ? width - col : 0);
+        }
+    }
+    template <int LD> __device__ __forceinline__ void put(bf16_t *tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, col = at % PER_ROW * 8;
+            put8_stored<T>(tile + row * LD, CHUNK * LD, col, v[i]);
+        }
+    }
+};
+
+// One of the first pass's matrices on its way to LDS: parts of 64 x 64, stored in the order of the LDS tiles
+template <int N, int THREADS> struct Matrix {
+    static constexpr int PER = N * CHUNK * CHUNK / 8 / THREADS;
+    u4t_t v[PER];
+    __device__ __forceinline__ void load(const char *p)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = reinterpret_cast<const u4t_t *>(p)[threadIdx.x + i * THREADS];
+    }
+    __device__ __forceinline__ void put(bf16_t *tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = at / (CHUNK / 8);      // rows of all parts, one after the other
+            *reinterpret_cast<u4t_t *>(tile + row * LDM + at % (CHUNK / 8) * 8) = v[i];
+        }
+    }
+};
+
+// Vectors of a chunk and head that the first pass leaves, 64 floats each
+enum { VEC_READ = 0,     // exp(G) rk: what a row of k^T S is multiplied by
+       VEC_BETA = 1,
+       VEC_WRITE = 2,    // exp(G_end - G) rk: what a token's write is multiplied by at the chunk's end
+       VEC_ASK = 3,      // scale exp(G) rq
+       VEC_RQ = 4, VEC_RK = 5,
+       VEC_G = 6,        // the sum of the decays' logarithms from the chunk's start, 64 doubles
+       VEC_ONE = 8,      // [0] exp(G_end); [1] as int: the first token whose k, a or b is not finite, 64 if there is none
+       VECS = 9 };
+
+// ---- chunks of packed sequences ----
+// Sequence s has its chunks at floor(starts[s] / 64) + s and the places behind it: no two sequences share one, and none has to be counted.
+struct ChunkAt { int first, len, seq, place; };      // the first token, how many (0: nothing here), the sequence, the chunk's number in it
+__device__ __forceinline__ int gd_start(const GdArgs &g, int s)
+{
+    if (!g.starts) return s * g.length;
+    const int v = g.starts[s];
+    return v < 0 ? 0 : v > g.T ? g.T : v;
+}
+__device__ __forceinline__ int gd_base(const GdArgs &g, int s)
+{
+    return g.starts ? gd_start(g, s) / CHUNK + s : s * cdiv(g.length > 0 ? g.length : 1, CHUNK);
+}
+__device__ __forceinline__ ChunkAt gd_chunk(const GdArgs &g, int id)
+{
+    int lo = 0, hi = g.sequences;
+    if (!g.starts) lo = min(id / cdiv(g.length > 0 ? g.length : 1, CHUNK), g.sequences - 1);
+    else while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (gd_base(g, mid) <= id) lo = mid;
+        else hi = mid;
+    }
+    const int place = id - gd_base(g, lo), start = gd_start(g, lo), end = gd_start(g, lo + 1);
+    const long long first = start + (long long)place * CHUNK;
+    if (place < 0 || first >= end) return {0, 0, lo, place};
+    return {(int)first, (int)min((long long)CHUNK, end - first), lo, place};
+}
+
+}  // namespace
+
+}  // namespace dwc

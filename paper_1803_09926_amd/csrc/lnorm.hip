@@ -8,67 +8,12 @@
 //
 // The weight's gradient is a sum over rows: each lane keeps the sums of its own channels over all rows that its team walks, the teams of a block add
 // theirs in LDS one after the other, and the blocks' partials meet in seq_sum.hip.
-#include "seq_common.hpp"
+#include "seq_rows.hpp"
 #include <initializer_list>
 
 namespace dwc {
 
 namespace {
-
-// The sum over a team of two values at a time, in every lane.  `lds` holds 2 floats a wavefront and is free again after the caller's next barrier.
-template <int TEAM> __device__ __forceinline__ void team_sum2(float &a, float &b, float *lds)
-{
-    a = lanes_sum(a);
-    b = lanes_sum(b);
-    if constexpr (TEAM > 64) {
-        constexpr int WAVES = TEAM / 64;
-        const int wv = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) { lds[2 * wv] = a; lds[2 * wv + 1] = b; }
-        __syncthreads();
-        a = b = 0.f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) { a += lds[2 * i]; b += lds[2 * i + 1]; }
-    }
-}
-template <int TEAM> __device__ __forceinline__ float team_sum(float a, float *lds)
-{
-    a = lanes_sum(a);
-    if constexpr (TEAM > 64) {
-        constexpr int WAVES = TEAM / 64;
-        const int wv = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) lds[wv] = a;
-        __syncthreads();
-        a = 0.f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) a += lds[i];
-    }
-    return a;
-}
-
-// V channels of a row from channel c on.  WHOLE: C is a multiple of V and rows are aligned: loads and stores through a view of the row, in which what lies
-// behind its end reads zero and is not written, without a branch.  Otherwise each vector is looked at.
-template <typename T, int V, bool WHOLE> struct Part;
-template <typename T, int V> struct Part<T, V, true> {
-    Ahead<T, V, true> v;
-    __device__ __forceinline__ void load(const T *row, int C, int c) { v.load(BufView(row, (uint32_t)C * (uint32_t)sizeof(T)), (uint32_t)c * (uint32_t)sizeof(T), 1); }
-    __device__ __forceinline__ float at(int i) const { return v.at(i); }
-    static __device__ __forceinline__ void store(T *row, int C, int c, const float (&r)[V])
-    {
-        // (past the end of the last 16 bytes of a vector that starts inside there is nothing: a whole vector is inside or outside)
-        store_late<T, V, true>(BufView(row, (uint32_t)C * (uint32_t)sizeof(T)), (uint32_t)c * (uint32_t)sizeof(T), 1, r);
-    }
-};
-template <typename T, int V> struct Part<T, V, false> {
-    Some<T, V> v;
-    __device__ __forceinline__ void load(const T *row, int C, int c) { v.load(row + c, C - c); }
-    __device__ __forceinline__ float at(int i) const { return v.at(i); }
-    static __device__ __forceinline__ void store(T *row, int C, int c, const float (&r)[V])
-    {
-        Some<T, V> p;
-        p.set(r);
-        p.store(row + c, C - c);
-    }
-};
 
 template <typename T, int TEAM, int V, int NV, int BLOCK, bool WHOLE>
 __global__ __launch_bounds__(BLOCK) void k_lnorm_fwd(int rows, int C, float eps, float inv_c, const T *__restrict__ x, const T *__restrict__ residual,
@@ -250,7 +195,6 @@ int validate(const lnorm_desc *d)
 // How many lanes share a row, and how many of its channels a lane has.  A wavefront alone needs no barrier; 16 channels a lane (8 in the backward pass, which
 // holds seven values a channel) leave enough wavefronts on a compute unit: 2048 channels of bf16 by 64, 128, 256 lanes forward 26.0, 26.0, 29.1 us (16384
 // rows); backward 67, 50, 47 us.  1536 channels of fp32 forward 27.7, 26.5, 25.4 us (9999 rows), backward 60, 41, 40 us.
-struct Team { int lanes, channels; };
 Team fwd_team(int C)
 {
     if (C <= 512) return {64, 8};
@@ -272,7 +216,6 @@ Team bwd_team(int C, int T)
     if (C <= 8192) return {1024, 8};
     return {1024, 16};
 }
-constexpr int block_of(int lanes) { return lanes == 64 ? 256 : lanes; }
 
 // Blocks of the backward pass: two on each of the 256 compute units (one of 1024 lanes), fewer where there are fewer rows.  Each leaves partials that are read again:
 // 256, 512, 1024 blocks take 63, 42, 46 us at 9999 x 1536 in fp32, and 61, 47, 57 at 32768 x 1024 in bf16.
@@ -289,15 +232,6 @@ bool whole_rows(const lnorm_desc *d, std::initializer_list<const void *> rows)
     if (d->C % (d->dtype == DWCONV_F32 ? 4 : 8)) return false;
     for (const void *p : rows)
         if (unaligned16(p)) return false;
-    return true;
-}
-
-// f(lanes, vectors a lane) with the numbers as types
-template <int LANES, int NV> struct Shape { static constexpr int TEAM = LANES, VECTORS = NV, BLOCK = block_of(LANES); };
-template <int V, int LANES, int CHANNELS, typename F> bool shape_is(const Team &t, F f)
-{
-    if (t.lanes != LANES || t.channels != CHANNELS) return false;
-    f(Shape<LANES, CHANNELS / V>());
     return true;
 }
 

@@ -1,13 +1,13 @@
-// The calls of sequence.py in native code, as binding.cpp has those of the convolutions: what is checked of plain device tensors, and the library call.
+// The calls of sequence.py and delta.py in native code, as binding.cpp has those of the convolutions: what is checked of plain device tensors, and the library call.
 // Every function takes the descriptor, the operands in the order of its entry below (None where one is left out), the workspace where there is one, and the
 // stream; it returns the library's status, or None where an argument is anything but what it takes for granted.
 #include "binding.hpp"
 
-#include "../../include/seqops.h"
+#include "../../include/deltaops.h"
 
 namespace {
 
-enum Op { LNORM, CCONV, SSCAN };
+enum Op { LNORM, CCONV, SSCAN, GDELTA, HNORM, RNORM, OPS };
 enum Type { STORED, F32, I32, BYTES };
 // Sizes of a descriptor that operands refer to: rows of a width and a stride, or a number of elements (BYTES: at least)
 struct Sizes { int64_t T; int64_t width[6], stride[6]; int64_t flat[6]; at::ScalarType stored; };
@@ -20,6 +20,9 @@ struct Entry { const char *symbol; Op op; bool workspace; Field fields[24]; };
 #define L(F, ...) {AT(lnorm_tensors, F), __VA_ARGS__}
 #define K(F, ...) {AT(cconv_tensors, F), __VA_ARGS__}
 #define S(F, ...) {AT(sscan_tensors, F), __VA_ARGS__}
+#define G(F, ...) {AT(gdelta_tensors, F), __VA_ARGS__}
+#define H(F, ...) {AT(hnorm_tensors, F), __VA_ARGS__}
+#define R(F, ...) {AT(rnorm_tensors, F), __VA_ARGS__}
 #define STOP {END, STORED, false, 0}
 const Entry ENTRIES[] = {
     {"lnorm_fwd", LNORM, false, {L(x, STORED, true, 0), L(residual, STORED, true, 0), L(w, STORED, false, 0), L(b, STORED, false, 0), L(y, STORED, true, 0),
@@ -42,10 +45,31 @@ const Entry ENTRIES[] = {
     {"sscan_step", SSCAN, false, {S(x, STORED, true, 0), S(dt, STORED, true, 1), S(A, F32, false, 0), S(B, STORED, true, 3), S(C, STORED, true, 4),
                                   S(D, F32, false, 1), S(z, STORED, true, 2), S(dt_bias, F32, false, 1), S(slots, I32, false, 4), S(state, F32, false, 3),
                                   S(y, STORED, true, 5), STOP}},
+    {"gdelta_fwd", GDELTA, true, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
+                                  G(A, F32, false, 0), G(a_bias, F32, false, 0), G(starts, I32, false, 2), G(init, F32, false, 3), G(y, STORED, true, 5),
+                                  G(final, F32, false, 3), G(kept, BYTES, false, 5), STOP}},
+    {"gdelta_bwd", GDELTA, true, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
+                                  G(A, F32, false, 0), G(a_bias, F32, false, 0), G(starts, I32, false, 2), G(kept, BYTES, false, 5), G(dy, STORED, true, 5),
+                                  G(dq, STORED, true, 0), G(dk, STORED, true, 1), G(dv, STORED, true, 2), G(da, STORED, true, 3), G(db, STORED, true, 4),
+                                  G(dA, F32, false, 0), G(da_bias, F32, false, 0), STOP}},
+    {"gdelta_step", GDELTA, false, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
+                                    G(A, F32, false, 0), G(a_bias, F32, false, 0), G(slots, I32, false, 4), G(state, F32, false, 3), G(y, STORED, true, 5),
+                                    STOP}},
+    {"hnorm_fwd", HNORM, false, {H(x, STORED, true, 0), H(z, STORED, true, 1), H(w, STORED, false, 0), H(y, STORED, true, 2), H(rstd, F32, false, 1), STOP}},
+    {"hnorm_bwd", HNORM, true, {H(x, STORED, true, 0), H(z, STORED, true, 1), H(w, STORED, false, 0), H(rstd, F32, false, 1), H(dy, STORED, true, 2),
+                                H(dx, STORED, true, 0), H(dz, STORED, true, 1), H(dw, F32, false, 0), STOP}},
+    {"rnorm_fwd", RNORM, false, {R(x, STORED, true, 0), R(z, STORED, true, 1), R(residual, STORED, true, 2), R(w1, STORED, false, 0),
+                                 R(scale, STORED, false, 0), R(w2, STORED, false, 0), R(total, STORED, true, 2), R(y, STORED, true, 2),
+                                 R(rstd1, F32, false, 1), R(rstd2, F32, false, 1), STOP}},
+    {"rnorm_bwd", RNORM, true, {R(x, STORED, true, 0), R(z, STORED, true, 1), R(w1, STORED, false, 0), R(scale, STORED, false, 0), R(w2, STORED, false, 0),
+                                R(total, STORED, true, 2), R(rstd1, F32, false, 1), R(rstd2, F32, false, 1), R(dy, STORED, true, 2),
+                                R(dtotal, STORED, true, 2), R(dx, STORED, true, 0), R(dz, STORED, true, 1), R(dresidual, STORED, true, 2),
+                                R(dw1, F32, false, 0), R(dscale, F32, false, 0), R(dw2, F32, false, 0), STOP}},
 };
 constexpr int NENTRIES = sizeof ENTRIES / sizeof ENTRIES[0];
 constexpr size_t SLOTS = sizeof(sscan_tensors) / sizeof(void *);     // the largest struct of tensors
-static_assert(SLOTS * sizeof(void *) >= sizeof(cconv_tensors) && SLOTS * sizeof(void *) >= sizeof(lnorm_tensors), "the largest struct");
+static_assert(SLOTS * sizeof(void *) >= sizeof(cconv_tensors) && SLOTS * sizeof(void *) >= sizeof(lnorm_tensors) && SLOTS * sizeof(void *) >= sizeof(gdelta_tensors) &&
+              SLOTS * sizeof(void *) >= sizeof(hnorm_tensors) && SLOTS * sizeof(void *) >= sizeof(rnorm_tensors), "the largest struct");
 
 typedef int (*call_fn)(const void *, const void *, void *);
 typedef int (*call_ws_fn)(const void *, const void *, void *, size_t, void *);
@@ -53,11 +77,12 @@ typedef size_t (*bytes_fn)(const void *);
 
 // set once by bind(), under the interpreter's lock
 void *entry_points[NENTRIES];
-bytes_fn kept_bytes;
-PyObject *desc_type[3];
-constexpr size_t DESC_SIZE[3] = {sizeof(lnorm_desc), sizeof(cconv_desc), sizeof(sscan_desc)};
+constexpr const char *KEPT[2] = {"sscan_kept_bytes", "gdelta_kept_bytes"};
+bytes_fn kept_bytes[2];
+PyObject *desc_type[OPS];
+constexpr size_t DESC_SIZE[OPS] = {sizeof(lnorm_desc), sizeof(cconv_desc), sizeof(sscan_desc), sizeof(gdelta_desc), sizeof(hnorm_desc), sizeof(rnorm_desc)};
 
-union Desc { lnorm_desc l; cconv_desc k; sscan_desc s; };
+union Desc { lnorm_desc l; cconv_desc k; sscan_desc s; gdelta_desc g; hnorm_desc h; rnorm_desc r; };
 
 // false: left to the checks of the library by way of Python
 bool sizes_of(Op op, const Desc &d, Sizes *s)
@@ -73,12 +98,31 @@ bool sizes_of(Op op, const Desc &d, Sizes *s)
         *s = {c.T, {c.C, c.C}, {c.x_stride, c.y_stride},
               {(int64_t)c.K * c.C, c.C, (int64_t)c.sequences + 1, (int64_t)c.sequences * (c.K - 1) * c.C, c.T}, at::kFloat};
         dtype = c.dtype;
+    } else if (op == GDELTA) {
+        const gdelta_desc &c = d.g;
+        if (c.T < 0 || c.H < 1 || c.K < 1 || c.K > GDELTA_MAX_K || c.V < 1 || c.V > GDELTA_MAX_V || c.key_heads < 1 || c.sequences < 1) return false;
+        const int64_t keys = (int64_t)c.key_heads * c.K, values = (int64_t)c.H * c.V;
+        *s = {c.T, {keys, keys, values, c.H, c.H, values}, {c.q_stride, c.k_stride, c.v_stride, c.a_stride, c.b_stride, c.y_stride},
+              {c.H, 0, (int64_t)c.sequences + 1, 0, c.T, (int64_t)kept_bytes[1](&c)}, at::kFloat};
+        if (__builtin_mul_overflow((int64_t)c.sequences * c.H, (int64_t)c.K * c.V, &s->flat[3])) return false;
+        dtype = c.dtype;
+    } else if (op == HNORM) {
+        const hnorm_desc &c = d.h;
+        if (c.T < 0 || c.H < 1 || c.D < 1 || c.D > HNORM_MAX_D) return false;
+        const int64_t width = (int64_t)c.H * c.D;
+        *s = {c.T, {width, width, width}, {c.x_stride, c.z_stride, c.y_stride}, {c.D, (int64_t)c.T * c.H}, at::kFloat};
+        dtype = c.dtype;
+    } else if (op == RNORM) {
+        const rnorm_desc &c = d.r;
+        if (c.T < 0 || c.C < 1) return false;
+        *s = {c.T, {c.C, c.C, c.C}, {c.x_stride, c.z_stride, c.C}, {c.C, c.T}, at::kFloat};
+        dtype = c.dtype;
     } else {
         const sscan_desc &c = d.s;
         if (c.T < 0 || c.C < 1 || c.N < 1 || c.N > SSCAN_MAX_N || c.groups < 1 || c.sequences < 1) return false;
         const int64_t shared = (int64_t)c.groups * c.N;
         *s = {c.T, {c.C, c.C, c.C, shared, shared, c.C}, {c.x_stride, c.dt_stride, c.z_stride, c.b_stride, c.c_stride, c.y_stride},
-              {(int64_t)c.C * c.N, c.C, (int64_t)c.sequences + 1, 0, c.T, (int64_t)kept_bytes(&c)}, at::kFloat};
+              {(int64_t)c.C * c.N, c.C, (int64_t)c.sequences + 1, 0, c.T, (int64_t)kept_bytes[0](&c)}, at::kFloat};
         if (__builtin_mul_overflow((int64_t)c.sequences * c.C, (int64_t)c.N, &s->flat[3])) return false;
         dtype = c.dtype;
     }
@@ -166,30 +210,35 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// bind(lookup, LnormDesc, CconvDesc, SscanDesc, Tensor, Parameter): lookup(symbol) gives the address of one of the library's functions
+// bind(lookup, the descriptors' types in the order of Op, Tensor, Parameter): lookup(symbol) gives the address of one of the library's functions
 PyObject *bind(PyObject *, PyObject *args)
 {
-    PyObject *lookup, *type[5];
-    if (!PyArg_ParseTuple(args, "OOOOOO", &lookup, &type[0], &type[1], &type[2], &type[3], &type[4])) return nullptr;
-    void *found[NENTRIES + 1];
-    for (int i = 0; i < NENTRIES + 1; ++i) {
-        PyObject *a = PyObject_CallFunction(lookup, "s", i < NENTRIES ? ENTRIES[i].symbol : "sscan_kept_bytes");
+    if (PyTuple_GET_SIZE(args) != 1 + OPS + 2) {
+        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+        return nullptr;
+    }
+    void *found[NENTRIES + 2];
+    for (int i = 0; i < NENTRIES + 2; ++i) {
+        PyObject *a = PyObject_CallFunction(PyTuple_GET_ITEM(args, 0), "s", i < NENTRIES ? ENTRIES[i].symbol : KEPT[i - NENTRIES]);
         found[i] = a ? PyLong_AsVoidPtr(a) : nullptr;
         Py_XDECREF(a);
         if (PyErr_Occurred()) return nullptr;
         if (!found[i]) { PyErr_SetString(PyExc_RuntimeError, "no such function"); return nullptr; }
     }
     for (int i = 0; i < NENTRIES; ++i) entry_points[i] = found[i];
-    kept_bytes = (bytes_fn)found[NENTRIES];
-    for (PyObject *t : type) Py_INCREF(t);   // (kept until the process ends)
-    for (int i = 0; i < 3; ++i) desc_type[i] = type[i];
-    tensor_type = type[3]; parameter_type = type[4];
+    for (int i = 0; i < 2; ++i) kept_bytes[i] = (bytes_fn)found[NENTRIES + i];
+    for (int i = 1; i < 1 + OPS + 2; ++i) Py_INCREF(PyTuple_GET_ITEM(args, i));   // (kept until the process ends)
+    for (int i = 0; i < OPS; ++i) desc_type[i] = PyTuple_GET_ITEM(args, 1 + i);
+    tensor_type = PyTuple_GET_ITEM(args, 1 + OPS);
+    parameter_type = PyTuple_GET_ITEM(args, 2 + OPS);
     Py_RETURN_NONE;
 }
 
 #define CALL(E) {ENTRIES[E].symbol, (PyCFunction)(void (*)(void))call<E>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CALL(0), CALL(1), CALL(2), CALL(3), CALL(4), CALL(5), CALL(6), CALL(7),
+PyMethodDef methods[] = {CALL(0), CALL(1), CALL(2), CALL(3), CALL(4), CALL(5), CALL(6), CALL(7), CALL(8), CALL(9), CALL(10), CALL(11),
+                         CALL(12), CALL(13), CALL(14),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+static_assert(NENTRIES == 15, "one method each");
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_seq_binding", "checks and library calls of the sequence operators", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -18,6 +18,8 @@ MAX_STATES = 64
 SEQ_EXPORTS = ("lnorm_fwd", "lnorm_bwd_workspace_bytes", "lnorm_bwd", "cconv_fwd", "cconv_bwd_workspace_bytes", "cconv_bwd", "cconv_step",
                "sscan_kept_bytes", "sscan_fwd_workspace_bytes", "sscan_bwd_workspace_bytes", "sscan_fwd", "sscan_bwd", "sscan_step")
 
+_EXPORTS = SEQ_EXPORTS                       # and those of delta.py, whose calls are checked here too
+
 
 class LnormDesc(ctypes.Structure):
     """Mirror of struct lnorm_desc."""
@@ -79,7 +81,7 @@ def _lib():
     if _library is None:
         lib = load()
         VP, SZ = ctypes.c_void_p, ctypes.c_size_t
-        for name in SEQ_EXPORTS:
+        for name in _EXPORTS:
             f = getattr(lib, name)
             if name.endswith("_bytes"):
                 f.argtypes, f.restype = [VP], SZ
@@ -98,8 +100,7 @@ def _bind():
     except ImportError as e:
         raise RuntimeError("the binding's native part is not built: run `python -m paper_1803_09926_amd.build` (or "
                            "__graft_entry__.build()) first") from e
-    native.bind(lambda symbol: ctypes.cast(getattr(lib, symbol), ctypes.c_void_p).value, LnormDesc, CconvDesc, SscanDesc, torch.Tensor,
-                torch.nn.Parameter)
+    native.bind(lambda symbol: ctypes.cast(getattr(lib, symbol), ctypes.c_void_p).value, *(_STRUCT[op][1] for op in _STRUCT), torch.Tensor, torch.nn.Parameter)
     _native = native
     return native
 
@@ -161,7 +162,7 @@ def _pointer(op, name, t, d):
     if not getattr(t, "is_cuda", False):
         raise ValueError("%s must be a device tensor" % name)
     if name == "kept":
-        need = sscan_kept_bytes(d)
+        need = _bytes(op + "_kept_bytes", d)
         if not t.is_contiguous() or t.numel() * t.element_size() < need:
             raise ValueError("kept must be contiguous with at least %d bytes" % need)
         return t.data_ptr()

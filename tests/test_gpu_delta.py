@@ -1,0 +1,368 @@
+"""GPU parity of the gated delta rule with its oracle in 64 bits: forward, backward and single tokens, at the sizes where a kernel changes its tile or its path, with packed and
+carried sequences, shared key heads, strides and odd alignment.
+
+Tolerances (relative, in the max norm and the 2-norm).  What is stored in bf16 is rounded once, by at most 2^-9 of itself: 1e-2 leaves room for the largest value's neighbours.  fp32 tensors:
+products hold all 24 bits of their factors but terms of 2^-24 (three of them of a pair, 2^-22), and a number passes four products a chunk (K S, T, K^T U, Q S) with sums of at most 256 terms in
+fp32, whose roundings add up to sqrt(256) * 2^-24 = 1e-6 each where they do not all go one way; four chunks: 4 * 4 * 1e-6 = 1.6e-5, gradients as much again, as they
+go the way back over what the way forward left: 4e-5.  fp32 outputs of bf16 tensors: factors that the kernels compute are held to 2^-17 = 8e-6, four products a chunk over four chunks
+and back, of which again the square root adds up: sqrt(32) * 8e-6 = 4.5e-5, and the gradients of A are differences of terms some times their size: 2e-4."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1803_09926_amd as dw
+from oracle import delta as od
+
+import gpu_util as gu
+from test_gpu_sequence import Made, _close, _space, _starts
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"f32": 4e-5, "bf16": 1e-2}
+TOL_WIDE = {"f32": 4e-5, "bf16": 2e-4}        # fp32 outputs
+DTYPE = {"f32": dw.F32, "bf16": dw.BF16}
+RAGGED = [0, 0, 1, 3, 64, 64, 129, 200]
+NAMES = ("q", "k", "v", "a", "b")
+
+
+def host_inputs(m, T, Hk, H, K, V, gates=1.0):
+    x = {"q": m.host((T, Hk, K)), "k": m.host((T, Hk, K)), "v": m.host((T, H, V)), "a": m.host((T, H), 0.7 * gates), "b": m.host((T, H))}
+    par = {"A": -np.exp(m.host((H,), stored=False)), "a_bias": m.host((H,), 0.5, -1.0, stored=False)}
+    return x, par
+
+
+class Call:
+    """Device tensors of one call; rows `more` elements apart beyond their width."""
+
+    def __init__(self, m, x, par, bounds, more=0, even=False, **desc):
+        self.m, self.more = m, more
+        T, Hk, K = x["q"].shape
+        H, V = x["v"].shape[1:]
+        self.widths = {"q": Hk * K, "k": Hk * K, "v": H * V, "a": H, "b": H, "y": H * V}
+        self.d = dw.gdelta_desc(T, H, K, V, Hk, len(bounds) - 1, DTYPE[m.dtype], **{k + "_stride": w + more for k, w in self.widths.items()}, **desc)
+        self.t = {k: m.dev(x[k].reshape(T, self.widths[k]), rows=self.widths[k] + more) for k in NAMES}
+        self.par = {k: None if v is None else m.dev(v, stored=False) for k, v in par.items()}
+        self.starts = None if even else _starts(bounds)
+        self.states = (len(bounds) - 1, H, K, V)
+        self.T = T
+
+    def rows(self, k):
+        return self.m.out((self.T, self.widths[k]), rows=self.widths[k] + self.more)
+
+    def forward(self, init=None, keep=True):
+        m = self.m
+        y, final = self.rows("y"), m.out(self.states, False)
+        self.kept = _space(dw.gdelta_kept_bytes(self.d)) if keep else None
+        dw.gdelta_fwd(self.d, *(self.t[k] for k in NAMES), y, _space(dw.gdelta_fwd_workspace_bytes(self.d)), **self.par, starts=self.starts,
+                      init=None if init is None else m.dev(init, stored=False), final=final, kept=self.kept)
+        return y, final
+
+    def backward(self, dy):
+        m, H = self.m, self.d.H
+        g = {"d" + k: self.rows(k) for k in NAMES}
+        more = {"dA": m.out((H,), False), "da_bias": m.out((H,), False)}
+        dw.gdelta_bwd(self.d, *(self.t[k] for k in NAMES), self.kept, m.dev(dy.reshape(self.T, self.widths["y"]), rows=self.widths["y"] + self.more),
+                      *(g["d" + k] for k in NAMES), _space(dw.gdelta_bwd_workspace_bytes(self.d)), **self.par, starts=self.starts, **more)
+        return g | more
+
+
+def check(m, x, par, bounds, init=None, more=0, even=False, backward=True, **options):
+    K = x["q"].shape[2]
+    call = Call(m, x, par, bounds, more, even, **options)
+    y, final = call.forward(init, keep=backward)
+    rule = od.Rule(**x, **par, bounds=bounds, init=init, **options)
+    _close(y, rule.y, TOL[m.dtype], "y")
+    _close(final, rule.final, TOL_WIDE[m.dtype], "final")
+    if backward:
+        dy = m.host(x["v"].shape)
+        g, want = call.backward(dy), rule.backward(dy)
+        for k, v in g.items():
+            if K == 1 and k in ("dq", "dk") and options.get("norm", True):
+                # q / sqrt(q^2 + eps) is a sign: of d = r dy the gradient is d - d q^2 / (q^2 + eps) = d eps / (q^2 + eps), a difference of numbers that are alike in all
+                # but their last bits, whose rounding, 2^-24 d each, is all that is left of it for eps = 1e-6
+                continue
+            if k in ("dA", "da_bias"):
+                # a sum of 200 tokens' terms of either sign: its rounding is that of the terms, not of what is left of them
+                terms = np.abs(rule.log_terms if k == "dA" else want["da"]).sum(0)
+                assert np.isfinite(gu.to_host(v)).all() and (np.abs(gu.to_host(v) - want[k]) <= TOL_WIDE[m.dtype] * terms).all(), k
+                continue
+            _close(v, want[k], TOL[m.dtype], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hk,H,K,V,more,shift,carry", [
+    (1, 1, 1, 1, 0, 0, False), (2, 2, 5, 3, 3, 1, True), (1, 2, 16, 16, 0, 0, False), (2, 4, 32, 33, 0, 1, True), (1, 1, 33, 64, 8, 0, False),
+    (2, 2, 64, 65, 0, 0, True), (1, 3, 65, 100, 1, 1, False), (1, 2, 128, 128, 16, 0, True), (1, 1, 129, 40, 0, 0, False), (1, 2, 200, 130, 5, 1, True),
+    (1, 1, 256, 256, 0, 0, True)])
+def test_rule(gpu_lib, dtype, Hk, H, K, V, more, shift, carry):
+    print("rule", dtype, Hk, H, K, V, more, shift, flush=True)
+    m = Made(K * 1000 + V, dtype, shift)
+    x, par = host_inputs(m, 200, Hk, H, K, V)
+    check(m, x, par, RAGGED, m.host((7, H, K, V), 0.3, stored=False) if carry else None, more)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,S", [(1, 1), (2, 2), (63, 1), (64, 1), (65, 1), (130, 2), (192, 3), (257, 1)])
+def test_equal_lengths(gpu_lib, dtype, T, S):
+    print("equal lengths", dtype, T, S, flush=True)
+    m = Made(T, dtype)
+    x, par = host_inputs(m, T, 1, 2, 24, 40)
+    bounds = [T // S * i for i in range(S + 1)]
+    check(m, x, par, bounds, even=True)
+    check(m, x, par, bounds, m.host((S, 2, 24, 40), 0.3, stored=False))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("options,params", [({"norm": False}, True), ({"softplus": False}, True), ({"sigmoid": False}, True), ({"scale": -1.5, "eps": 0.5}, True),
+                                            ({"norm": False, "softplus": False, "sigmoid": False}, False), ({}, False)])
+def test_options(gpu_lib, dtype, options, params):
+    print("options", dtype, options, params, flush=True)
+    m = Made(17, dtype)
+    x, par = host_inputs(m, 200, 2, 4, 32, 32)
+    if not options.get("norm", True):           # keys of length one or less, as callers that do not ask for the norm bring them
+        x["k"] = m.host(x["k"].shape, 0.15)
+    if not options.get("softplus", True):       # logarithms of decays up to the sign
+        x["a"] = np.abs(x["a"])
+        par["a_bias"] = np.abs(par["a_bias"])
+    if not options.get("sigmoid", True):
+        x["b"] = m.host(x["b"].shape, 0.2, 0.5)
+    check(m, x, par if params else {"A": None, "a_bias": None}, RAGGED, **options)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decays_of_any_size(gpu_lib, dtype):
+    """From nothing forgotten to everything, beside each other in a chunk; what is clamped has no gradient."""
+    m = Made(23, dtype)
+    x, par = host_inputs(m, 200, 1, 2, 32, 32)
+    x["a"][...] = np.float32(-30)                # decays of one
+    x["a"][[5, 70, 71, 130]] = np.float32(512)   # e^-512 A and less: zero
+    x["a"][[9, 90, 180]] = np.float32(8)
+    x["a"][150] = np.inf
+    par = {"A": np.array([-1.0, -4.0], np.float32), "a_bias": None}
+    call = Call(m, x, par, [0, 200])
+    y, final = call.forward()
+    rule = od.Rule(**x, **par, bounds=[0, 200])
+    _close(y, rule.y, TOL[dtype], "y")
+    _close(final, rule.final, TOL_WIDE[dtype], "final")
+    x["a"][150] = np.float32(512)                # (an infinity times a gradient of zero is no number to compare with)
+    rule, dy = od.Rule(**x, **par, bounds=[0, 200]), m.host(x["v"].shape)
+    call = Call(m, x, par, [0, 200])
+    call.forward()
+    g, want = call.backward(dy), rule.backward(dy)
+    for k in ("dq", "dk", "dv", "da", "db"):
+        _close(g[k], want[k], TOL[dtype], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hk,H,K,V,more,shift", [(1, 1, 1, 1, 0, 0), (2, 4, 33, 31, 3, 1), (2, 2, 64, 64, 0, 0), (1, 3, 128, 130, 8, 0), (1, 1, 256, 256, 0, 1)])
+@pytest.mark.parametrize("options", [{}, {"norm": False, "softplus": False, "sigmoid": False}])
+def test_step(gpu_lib, dtype, Hk, H, K, V, more, shift, options):
+    print("step", dtype, Hk, H, K, V, more, shift, options, flush=True)
+    m = Made(K + V, dtype, shift)
+    T, slots = 5, 9
+    x, par = host_inputs(m, T, Hk, H, K, V)
+    if options:
+        x["k"], x["a"] = x["k"] * np.float32(0.125), np.abs(x["a"])
+        par["a_bias"] = np.abs(par["a_bias"])
+    state = m.host((slots, H, K, V), 0.3, stored=False)
+    where = [7, -1, 0, 9, 3]                     # two rows of padding
+    call = Call(m, x, par, list(range(slots + 1)), more, **options)
+    st, y = m.dev(state, stored=False), call.rows("y")
+    dw.gdelta_step(call.d, *(call.t[k] for k in NAMES), st, y, **call.par, slots=torch.tensor(where, dtype=torch.int32, device="cuda"))
+    want, got = state.astype(np.float64), gu.to_host(y).reshape(T, H, V)
+    for t, s in enumerate(where):
+        if not 0 <= s < slots:
+            assert not got[t].any()
+            continue
+        one = {k: v[t:t + 1] for k, v in x.items()}
+        rule = od.Rule(**one, **par, bounds=[0, 1], init=state[s:s + 1], **options)
+        _close(torch.from_numpy(got[t]), rule.y[0], 1e-5 if dtype == "f32" else 1e-2, "y of row %d" % t)
+        want[s] = rule.final[0]
+    _close(st, want, 1e-5, "states")
+    untouched = [s for s in range(slots) if s not in where]
+    assert np.array_equal(gu.to_host(st)[untouched], state[untouched])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pieces_and_steps_continue_each_other(gpu_lib, dtype):
+    """A sequence read at once, in pieces, and its end token by token."""
+    m = Made(31, dtype)
+    x, par = host_inputs(m, 150, 1, 2, 40, 48)
+    rule = od.Rule(**x, **par, bounds=[0, 150])
+    state, ys = None, []
+    for lo, hi in ((0, 70), (70, 71), (71, 140)):
+        part = {k: v[lo:hi] for k, v in x.items()}
+        y, final = Call(m, part, par, [0, hi - lo]).forward(state, keep=False)
+        state = gu.to_host(final)
+        ys.append(gu.to_host(y))
+    st = m.dev(state, stored=False)
+    for t in range(140, 150):
+        call = Call(m, {k: v[t:t + 1] for k, v in x.items()}, par, [0, 1])
+        y = call.rows("y")
+        dw.gdelta_step(call.d, *(call.t[k] for k in NAMES), st, y, **call.par)
+        ys.append(gu.to_host(y))
+    _close(torch.from_numpy(np.concatenate(ys)), rule.y.reshape(150, -1), TOL[dtype], "y")
+    _close(st, rule.final, TOL_WIDE[dtype], "state")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name,value", [("v", np.nan), ("v", np.inf), ("k", np.nan), ("k", -np.inf), ("q", np.nan), ("a", np.nan), ("b", np.nan)])
+def test_what_is_not_finite_stays_behind(gpu_lib, dtype, name, value):
+    """Tokens before it, other heads and other sequences: the same bits."""
+    m = Made(41, dtype)
+    T, t0, bounds = 200, 100, [0, 30, 170, 200]
+    x, par = host_inputs(m, T, 2, 4, 40, 72)
+    clean = [gu.to_host(v) for v in Call(m, x, par, bounds).forward()]
+    x[name][t0].reshape(-1)[0] = value           # of head 0
+    y, final = (gu.to_host(v) for v in Call(m, x, par, bounds).forward())
+    y, was = y.reshape(T, 4, 72), clean[0].reshape(T, 4, 72)
+    heads = slice(2, 4) if name in "qk" else slice(1, 4)
+    rest = [t for t in range(T) if t < t0 or t >= 170]
+    assert np.array_equal(y[rest], was[rest]) and np.array_equal(y[:, heads], was[:, heads])
+    assert np.array_equal(final[[0, 2]], clean[1][[0, 2]]) and np.array_equal(final[:, heads], clean[1][:, heads])
+    assert not np.isfinite(y[t0, 0]).all()
+    if name == "v":                              # the other columns of the state do not know of it
+        assert np.array_equal(y[:, 0, 1:], was[:, 0, 1:]) and not np.isfinite(y[t0:170, 0, 0]).any()
+    if name == "q":
+        assert np.array_equal(final, clean[1]) and np.array_equal(np.delete(y, t0, 0), np.delete(was, t0, 0))
+    elif name != "v":
+        assert not np.isfinite(y[t0:170, 0]).any() and not np.isfinite(final[1, 0]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_other_sequences_stay_finite(gpu_lib, dtype):
+    m = Made(43, dtype)
+    T, bounds = 150, [0, 40, 110, 150]
+    x, par = host_inputs(m, T, 2, 4, 32, 40)
+    dy = m.host(x["v"].shape)
+    call = Call(m, x, par, bounds)
+    call.forward()
+    clean = {k: gu.to_host(v) for k, v in call.backward(dy).items()}
+    bad = dy.copy()
+    bad[60, 0, 3] = np.nan
+    call.forward()
+    g = {k: gu.to_host(v) for k, v in call.backward(bad).items()}
+    for k in NAMES:
+        got, was = g["d" + k], clean["d" + k]
+        out = np.r_[0:40, 110:150]
+        assert np.array_equal(got[out], was[out]), k
+        half = got.shape[1] // 2                 # the other key head, and its value heads
+        assert np.array_equal(got[:, half:], was[:, half:]), k
+    assert not np.isfinite(g["dv"][60]).all()
+
+
+def test_no_tokens(gpu_lib):
+    m = Made(3, "f32")
+    x, par = host_inputs(m, 0, 1, 2, 8, 8)
+    init = m.host((2, 2, 8, 8), stored=False)
+    call = Call(m, x, par, [0, 0, 0], even=True)
+    _, final = call.forward(init)
+    assert np.array_equal(gu.to_host(final), init)
+    g = call.backward(np.zeros((0, 2, 8), np.float32))
+    assert not g["dA"].any() and not g["da_bias"].any()
+
+
+def test_the_same_bits_every_time_and_on_other_streams(gpu_lib):
+    m = Made(53, "bf16")
+    x, par = host_inputs(m, 200, 2, 4, 64, 64)
+    dy = m.host(x["v"].shape)
+    call = Call(m, x, par, RAGGED)
+    want = list(call.forward()) + list(call.backward(dy).values())
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    calls = [Call(m, x, par, RAGGED) for _ in sides]
+    torch.cuda.synchronize()
+    got = []
+    for side, c in zip(sides, calls):            # at once, each with a workspace of its own
+        with torch.cuda.stream(side):
+            got.append(list(c.forward()) + list(c.backward(dy).values()))
+    torch.cuda.synchronize()
+    for g in got:
+        for a, b in zip(g, want):
+            assert torch.equal(a, b)
+
+
+def test_captured_and_replayed(gpu_lib):
+    """Both passes and a step in a graph, replayed on new inputs with eager work in between."""
+    m = Made(59, "bf16")
+    T, H, K, V = 200, 4, 64, 64
+    x, par = host_inputs(m, T, 2, H, K, V)
+    call = Call(m, x, par, RAGGED)
+    d, t = call.d, call.t
+    y, g = call.rows("y"), {"d" + k: call.rows(k) for k in NAMES}
+    dy, kept = m.dev(m.host((T, H * V))), _space(dw.gdelta_kept_bytes(d))
+    fs, bs = _space(dw.gdelta_fwd_workspace_bytes(d)), _space(dw.gdelta_bwd_workspace_bytes(d))
+    more = {"dA": m.out((H,), False), "da_bias": m.out((H,), False)}
+    sd = dw.gdelta_desc(3, H, K, V, 2, 3, dw.BF16)
+    state, sy = torch.zeros(3, H, K, V, device="cuda"), torch.empty(3, H * V, device="cuda", dtype=torch.bfloat16)
+
+    def run():
+        dw.gdelta_fwd(d, *(t[k] for k in NAMES), y, fs, **call.par, starts=call.starts, kept=kept)
+        dw.gdelta_bwd(d, *(t[k] for k in NAMES), kept, dy, *(g["d" + k] for k in NAMES), bs, **call.par, starts=call.starts, **more)
+        dw.gdelta_step(sd, *(t[k][:3] for k in NAMES), state, sy, **call.par)
+
+    outs = [y, *g.values(), *more.values(), state, sy]
+    run()
+    state.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(3):
+        for k in NAMES:
+            t[k].copy_(torch.randn_like(t[k], dtype=torch.float32))
+        state.zero_()
+        run()
+        want = [o.clone() for o in outs]
+        state.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits(gpu_lib):
+    """Rows 2^25 elements apart."""
+    m = Made(61, "bf16")
+    T, K, V, far = 70, 32, 32, 1 << 25
+    x, par = host_inputs(m, T, 1, 1, K, V)
+    space = torch.empty((T - 1) * far + 256, device="cuda", dtype=torch.bfloat16)
+    at = {k: space[o:].as_strided((T, w), (far, 1)) for k, o, w in (("q", 0, K), ("k", 32, K), ("v", 64, V), ("a", 96, 1), ("b", 97, 1), ("y", 98, V))}
+    for k in NAMES:
+        at[k].copy_(torch.from_numpy(x[k].reshape(T, -1)))
+    d = dw.gdelta_desc(T, 1, K, V, dtype=dw.BF16, **{k + "_stride": far for k in at})
+    par = {k: m.dev(v, stored=False) for k, v in par.items()}
+    kept = _space(dw.gdelta_kept_bytes(d))
+    dw.gdelta_fwd(d, *(at[k] for k in NAMES), at["y"], None, **par, kept=kept)
+    rule = od.Rule(**x, **{k: gu.to_host(v) for k, v in par.items()}, bounds=[0, T])
+    _close(at["y"], rule.y, 1e-2, "y")
+    dy = m.host((T, 1, V))
+    want = rule.backward(dy)
+    given = at["y"]
+    given.copy_(torch.from_numpy(dy.reshape(T, V)))
+    g = {"d" + k: space[128 + o:].as_strided((T, w), (far, 1)) for k, o, w in (("q", 2, K), ("k", 34, K), ("v", 66, V), ("a", 98, 1), ("b", 99, 1))}
+    dw.gdelta_bwd(d, *(at[k] for k in NAMES), kept, given, *(g["d" + k] for k in NAMES), _space(dw.gdelta_bwd_workspace_bytes(d)), **par)
+    for k in NAMES:
+        _close(g["d" + k], want["d" + k], 1e-2, k)
+
+
+def test_starts_that_are_no_starts(gpu_lib):
+    """Unspecified values, but nothing outside the tensors is written (and nothing is read there: the kernels clamp each start to the tokens)."""
+    m = Made(67, "bf16")
+    T, guard = 200, 4096
+    x, par = host_inputs(m, T, 2, 4, 32, 32)
+    for starts in ([5, 300, -7, 64, 2000000000, 0, 199, 200], [0, 0, 0, 0, 0, 0, 0, 0], [200, 150, 100, 50, 40, 30, 20, 10], [-2147483648] * 4 + [2147483647] * 4):
+        print("starts", starts, flush=True)
+        call = Call(m, x, par, RAGGED)
+        call.starts = _starts(starts)
+        space = torch.full((T * 128 + 2 * guard,), 7.0, device="cuda", dtype=torch.bfloat16)
+        y = space[guard:-guard].view(T, 128)
+        final = torch.full((7 * 4 * 32 * 32 + 2 * guard,), 7.0, device="cuda")
+        kept = _space(dw.gdelta_kept_bytes(call.d) + 2 * guard)
+        dw.gdelta_fwd(call.d, *(call.t[k] for k in NAMES), y, None, **call.par, starts=call.starts, kept=kept[guard:-guard],
+                      final=final[guard:-guard])
+        call.kept = kept[guard:-guard]
+        call.backward(m.host((T, 4, 32)))
+        torch.cuda.synchronize()
+        assert (space[:guard] == 7).all() and (space[-guard:] == 7).all() and (final[:guard] == 7).all() and (final[-guard:] == 7).all()
+        assert (kept[:guard] == 0xFF).all() and (kept[-guard:] == 0xFF).all()
