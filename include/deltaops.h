@@ -37,6 +37,7 @@ extern "C" {
 #define GDELTA_MAX_K 256
 #define GDELTA_MAX_V 256
 #define GDELTA_MAX_H 65535          /* value heads */
+#define GDELTA_MAX_STRIDE (1 << 22) /* elements from one row to the next */
 typedef struct gdelta_desc {
     int32_t T, H;               /* tokens >= 0, value heads >= 1                                            */
     int32_t K, V;               /* 1 <= K <= GDELTA_MAX_K, 1 <= V <= GDELTA_MAX_V                           */

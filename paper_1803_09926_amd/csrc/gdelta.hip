@@ -20,7 +20,7 @@ int validate(const gdelta_desc *d)
     const long long keys = (long long)d->key_heads * d->K, values = (long long)d->H * d->V;
     if (d->T > SEQOPS_MAX_T || d->sequences > SEQOPS_MAX_T || d->H > GDELTA_MAX_H) return DWCONV_ERR_TOO_LARGE;
     for (const int64_t s : {d->q_stride, d->k_stride, d->v_stride, d->a_stride, d->b_stride, d->y_stride})
-        if (s > SEQOPS_MAX_STRIDE) return DWCONV_ERR_TOO_LARGE;
+        if (s > GDELTA_MAX_STRIDE) return DWCONV_ERR_TOO_LARGE;
     if (d->T > 1 && (d->q_stride < keys || d->k_stride < keys || d->v_stride < values || d->a_stride < d->H || d->b_stride < d->H || d->y_stride < values))
         return DWCONV_ERR_BAD_DIM;
     // chunks are counted in 32 bits, bytes of all states in 64
@@ -37,6 +37,11 @@ GdArgs args_of(const gdelta_desc *d, const gdelta_tensors *t)
     GdArgs g = {d->T, d->H, d->K, d->V, d->key_heads, d->sequences, t->starts ? 0 : d->T / d->sequences, d->softplus, d->sigmoid, d->norm, d->scale, d->eps,
                 d->q_stride, d->k_stride, d->v_stride, d->a_stride, d->b_stride, d->y_stride, t->q, t->k, t->v, t->a, t->b, (const float *)t->A,
                 (const float *)t->a_bias, (const int32_t *)t->starts};
+    if (d->T < 2) {                               // the stride of a row alone says nothing
+        g.q_stride = g.k_stride = (long long)d->key_heads * d->K;
+        g.v_stride = g.y_stride = (long long)d->H * d->V;
+        g.a_stride = g.b_stride = d->H;
+    }
     return g;
 }
 

@@ -10,7 +10,7 @@ namespace dwc {
 
 namespace {
 
-template <typename T, int KP, int NT, bool SHARE>
+template <typename T, int KP, int NT, bool SHARE, bool WHOLE>
 __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, unsigned first,
                                                                   int blocks)
 {
@@ -24,7 +24,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
     const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
     const Columns<NT> cols((int)(bid % (unsigned)blocks));
     const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
-    const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
+    const int chunks = (int)min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const yp = dy + (long long)h * g.V;
 
     v4f_t S[KP / 16][NT];
@@ -33,42 +33,38 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
 
-    Rows<T, KP, THREADS> rows;
+    Rows<T, KP, THREADS, WHOLE> rows;
     Matrix<INNER, THREADS> matrix, second;
-    float o[4][4][NT];
-    auto load_keys = [&](long long c) {
-        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
-        const long long where = (base + c) * g.H + h;
+    Ahead<T, NT, WHOLE> o[4][4];
+    float vec_next, decay_next;
+    auto load_keys = [&](int c) {
+        const int at = start + c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = ((long long)base + c) * g.H + h;
         rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
         matrix.load(s.T + where * l.matrix);
         second.load(s.P + where * l.matrix);
+        const BufView view = rows_view(yp + at * g.y_stride, g.y_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(yp + (at + row_of(mt, r)) * g.y_stride, g.V, row_of(mt, r) < len, o[mt][r]);
+            for (int r = 0; r < 4; ++r) cols.load(o[mt][r], view, cols.at(row_of(mt, r), (int)g.y_stride, (int)sizeof(T)), g.V);
+        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+        vec_next = vec[threadIdx.x];
+        decay_next = vec[VEC_ONE * 64];
     };
     if (chunks > 0) load_keys(chunks - 1);
-    for (long long c = chunks - 1; c >= 0; --c) {
-        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
-        const long long where = (base + c) * g.H + h;
-        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+    for (int c = chunks - 1; c >= 0; --c) {
+        const int at = start + c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
         if (SHARE && c < chunks - 1) __syncthreads();
         rows.template put<LD>(kt);
         matrix.put(tm);
         second.put(pm);
-        vl[threadIdx.x] = vec[threadIdx.x];
+        vl[threadIdx.x] = vec_next;
+        const float decay = decay_next;
         rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
-        const float decay = vec[VEC_ONE * 64];
-#pragma unroll
-        for (int ct = 0; ct < KP / 16; ++ct)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
-                cols.store(s.dS + where * (l.state / 4) + (long long)row_of(ct, r) * l.VP, l.VP, true, x);
-            }
+        store_tiles<NT, KP / 16>(S, s.dS + where * (l.state / 4), l.VP, cols);
         __syncthreads();
         // dU
         v4f_t U[4][NT];
@@ -96,7 +92,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) d[mt][nt] = v4f_t{o[mt][0][nt], o[mt][1][nt], o[mt][2][nt], o[mt][3][nt]};
+                for (int nt = 0; nt < NT; ++nt) d[mt][nt] = v4f_t{o[mt][0].at(nt), o[mt][1].at(nt), o[mt][2].at(nt), o[mt][3].at(nt)};
             split_rows<RAW, NT>(d, b);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
@@ -127,24 +123,22 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(X[mt][nt], a, f[ks][nt]);
             }
         }
+        store_tiles<NT, 4>(X, s.X + where * (l.rows / 4), l.VP, cols);
+        const BufView out = rows_view(dv + at * g.v_stride + (long long)h * g.V, g.v_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 beta = four(vl + VEC_BETA * 64, mt), read = four(vl + VEC_READ * 64, mt);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x[NT], y[NT];
-                const int row = row_of(mt, r);
-                const float b = r == 0 ? beta.x : r == 1 ? beta.y : r == 2 ? beta.z : beta.w;
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = times(X[mt][nt], beta);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    x[nt] = X[mt][nt][r];
-                    y[nt] = x[nt] * b;
-                }
-                cols.store(s.X + where * (l.rows / 4) + (long long)row * l.VP, l.VP, true, x);
-                cols.store(dv + (at + row) * g.v_stride + (long long)h * g.V, g.V, row < len, y);
+            for (int r = 0; r < 4; ++r) {
+                float x[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) x[nt] = X[mt][nt][r];
+                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), (int)g.v_stride, (int)sizeof(T)), g.V, x);
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = -times(times(X[mt][nt], beta), read);
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = -times(X[mt][nt], read);
         }
         // dS
         split_rows<INNER, NT>(X, f);
@@ -164,7 +158,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
         for (int mt = 0; mt < 4; ++mt) {
             const float4 ask = four(vl + VEC_ASK * 64, mt);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = times(v4f_t{o[mt][0][nt], o[mt][1][nt], o[mt][2][nt], o[mt][3][nt]}, ask);
+            for (int nt = 0; nt < NT; ++nt) X[mt][nt] = times(v4f_t{o[mt][0].at(nt), o[mt][1].at(nt), o[mt][2].at(nt), o[mt][3].at(nt)}, ask);
         }
         split_rows<INNER, NT>(X, f);
         if constexpr (SHARE) __syncthreads();
@@ -188,7 +182,8 @@ template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const G
     constexpr bool SHARE = shares<T, KP>();
     constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    const auto kernel = k_gdelta_bwd_states<T, KP, NT, SHARE>;
+    const bool whole = whole_keys<T>(g) && pair_values<T>(g, dy, dv, g.y_stride, g.v_stride);
+    const auto kernel = whole ? k_gdelta_bwd_states<T, KP, NT, SHARE, true> : k_gdelta_bwd_states<T, KP, NT, SHARE, false>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT);
@@ -199,7 +194,7 @@ template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const G
 
 template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
 {
-    const bool wide = l.VP > 64;
+    const bool wide = two_tiles(g, l, sizeof(T) == 4);
     switch (l.KP) {
     case 32: return wide ? launch<T, 32, 2>(g, l, s, dy, dv, stream) : launch<T, 32, 1>(g, l, s, dy, dv, stream);
     case 64: return wide ? launch<T, 64, 2>(g, l, s, dy, dv, stream) : launch<T, 64, 1>(g, l, s, dy, dv, stream);

@@ -40,7 +40,7 @@ __device__ __forceinline__ float row_sum(float v)
     return v + lane_move<DPP_MIRROR>(v);
 }
 
-template <typename T, int KP>
+template <typename T, int KP, bool WHOLE>
 __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
@@ -66,7 +66,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     }
     const T *const kp = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K, *const qp = (const T *)g.q + at.first * g.q_stride + (long long)kh * g.K;
     auto put_tile = [&](const T *p, long long stride) {
-        Rows<T, KP, THREADS> rows;
+        Rows<T, KP, THREADS, WHOLE> rows;
         rows.load(p, stride, at.len, g.K);
         rows.template put<LD>(tile);
     };
@@ -175,7 +175,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                     put8<INNER>(ut + row * LDV, PLANE_V, col, x);
                     Some<T, 8> v;
                     v.load(yp + row * g.y_stride + v0 + col, row < at.len ? g.V - v0 - col : 0);
-                    put8_stored<T>(yt + row * LDV, PLANE_V, col, v);
+                    float o[8];
+                    v.get(o);
+                    put8<RAW>(yt + row * LDV, PLANE_V, col, o);
                 }
             }
             __syncthreads();
@@ -438,7 +440,7 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const vo
 {
     typedef Back<T, KP> C;
     static_assert(C::LDS <= 160 * 1024, "LDS of a compute unit");
-    const auto kernel = k_gdelta_bwd_rows<T, KP>;
+    const auto kernel = whole_keys<T>(g) ? k_gdelta_bwd_rows<T, KP, true> : k_gdelta_bwd_rows<T, KP, false>;
     const hipError_t e = gd_lds(kernel, C::LDS);
     if (e != hipSuccess) return e;
     return gd_launches(l.chunks, C::THREADS, [&](unsigned first, unsigned now) {

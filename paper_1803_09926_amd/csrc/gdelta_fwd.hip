@@ -11,7 +11,7 @@ namespace dwc {
 
 namespace {
 
-template <typename T, int KP, int NT, bool SHARE>
+template <typename T, int KP, int NT, bool SHARE, bool WHOLE>
 __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
                                                            float *__restrict__ final, unsigned first, int blocks)
 {
@@ -25,21 +25,18 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
     const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
     const Columns<NT> cols((int)(bid % (unsigned)blocks));
     const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
-    const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
+    const int chunks = (int)min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const vp = (const T *)g.v + (long long)h * g.V;
 
     v4f_t S[KP / 16][NT];
     const long long state = ((long long)seq * g.H + h) * g.K * g.V;
+    if (init) load_state<NT, KP / 16>(S, init + state, g.K, g.V, cols);
+    else {
 #pragma unroll
-    for (int ct = 0; ct < KP / 16; ++ct)
+        for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float x[NT];
-            const int row = row_of(ct, r);
-            cols.load(init + state + (long long)row * g.V, g.V, init && row < g.K, x);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[ct][nt][r] = x[nt];
-        }
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+    }
     Frag Sp[KP / 32][NT][INNER];
     auto split_state = [&] {
 #pragma unroll
@@ -49,62 +46,64 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
     };
     split_state();
 
-    Rows<T, KP, THREADS> rows;
+    Rows<T, KP, THREADS, WHOLE> rows;
     Matrix<INNER, THREADS> matrix;
-    float v[4][4][NT];
-    auto load_keys = [&](long long c) {
-        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
+    Ahead<T, NT, WHOLE> v[4][4];
+    float vec_next, decay_next;
+    int bad_next;
+    auto load_keys = [&](int c) {
+        const int at = start + c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = ((long long)base + c) * g.H + h;
         rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
-        matrix.load(s.T + ((base + c) * g.H + h) * l.matrix);
+        matrix.load(s.T + where * l.matrix);
+        const BufView view = rows_view(vp + at * g.v_stride, g.v_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(vp + (at + row_of(mt, r)) * g.v_stride, g.V, row_of(mt, r) < len, v[mt][r]);
+            for (int r = 0; r < 4; ++r) cols.load(v[mt][r], view, cols.at(row_of(mt, r), (int)g.v_stride, (int)sizeof(T)), g.V);
+        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+        vec_next = vec[threadIdx.x];
+        decay_next = vec[VEC_ONE * 64];
+        bad_next = reinterpret_cast<const int *>(vec + VEC_ONE * 64)[1];
     };
     if (chunks > 0) load_keys(0);
-    for (long long c = 0; c < chunks; ++c) {
-        const int at = start + (int)c * CHUNK, len = min(CHUNK, end - at);
-        const long long where = (base + c) * g.H + h;
-        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+    for (int c = 0; c < chunks; ++c) {
+        const int at = start + c * CHUNK, len = min(CHUNK, end - at);
+        const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
         if (SHARE && c) __syncthreads();
         rows.template put<LD>(kt);
         matrix.put(tm);
-        vl[threadIdx.x] = vec[threadIdx.x];
+        vl[threadIdx.x] = vec_next;
+        const float decay = decay_next;
+        const int bad = bad_next;
         rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
         matrix.load(s.P + where * l.matrix);
-        const float decay = vec[VEC_ONE * 64];
-        const int bad = reinterpret_cast<const int *>(vec + VEC_ONE * 64)[1];
         __syncthreads();
-        if (s.S) {
-#pragma unroll
-            for (int ct = 0; ct < KP / 16; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x[NT];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
-                    cols.store(s.S + where * (l.state / 4) + (long long)row_of(ct, r) * l.VP, l.VP, true, x);
-                }
-        }
+        if (s.S) store_tiles<NT, KP / 16>(S, s.S + where * (l.state / 4), l.VP, cols);
         // What is not finite in v, or the first key or gate that is not: from there on the column is, and before it nothing is of it.
+        float probe = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) probe = fmaf(v[mt][r].at(nt), 0.f, probe);
         int from[NT];
-        bool odd = bad < CHUNK;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            from[nt] = bad;
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (!finite(v[mt][r][nt])) { from[nt] = min(from[nt], row_of(mt, r)); odd = true; }
-        }
-        odd = __any(odd);
+        const bool odd = __any(bad < CHUNK || probe != 0.f);
         if (odd) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                from[nt] = min(from[nt], __shfl_xor(from[nt], 16, 64));
-                from[nt] = min(from[nt], __shfl_xor(from[nt], 32, 64));
+                from[nt] = bad;
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!finite(v[mt][r].at(nt))) from[nt] = min(from[nt], row_of(mt, r));
+                const int up = __shfl_xor(from[nt], 16, 64);
+                from[nt] = min(from[nt], up);
+                const int far = __shfl_xor(from[nt], 32, 64);
+                from[nt] = min(from[nt], far);
             }
         }
         v4f_t R[4][NT];
@@ -126,7 +125,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
             const float4 read = four(vl + VEC_READ * 64, mt), beta = four(vl + VEC_BETA * 64, mt);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const v4f_t x = {v[mt][0][nt], v[mt][1][nt], v[mt][2][nt], v[mt][3][nt]};
+                const v4f_t x = {v[mt][0].at(nt), v[mt][1].at(nt), v[mt][2].at(nt), v[mt][3].at(nt)};
                 R[mt][nt] = times(x - times(R[mt][nt], read), beta);
             }
         }
@@ -154,17 +153,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(U[mt][nt], a, f[ks][nt]);
             }
         }
-        if (s.U) {
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x[NT];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) x[nt] = U[mt][nt][r];
-                    cols.store(s.U + where * (l.rows / 4) + (long long)row_of(mt, r) * l.VP, l.VP, true, x);
-                }
-        }
+        if (s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
         v4f_t w[4][NT];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
@@ -232,6 +221,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                     if (from[nt] < CHUNK) S[ct][nt] = v4f_t{nan, nan, nan, nan};
             }
         }
+        const BufView out = rows_view(y + at * g.y_stride + (long long)h * g.V, g.y_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
@@ -239,22 +229,11 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                 float x[NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[nt] = O[mt][nt][r];
-                const int row = row_of(mt, r);
-                cols.store(y + (at + row) * g.y_stride + (long long)h * g.V, g.V, row < len, x);
+                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), (int)g.y_stride, (int)sizeof(T)), g.V, x);
             }
         split_state();
     }
-    if (!final) return;
-#pragma unroll
-    for (int ct = 0; ct < KP / 16; ++ct)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float x[NT];
-            const int row = row_of(ct, r);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
-            cols.store(final + state + (long long)row * g.V, g.V, row < g.K, x);
-        }
+    if (final) store_state<NT, KP / 16>(S, final + state, g.K, g.V, cols);
 }
 
 template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
@@ -262,7 +241,8 @@ template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const G
     constexpr bool SHARE = shares<T, KP>();
     constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    const auto kernel = k_gdelta_fwd<T, KP, NT, SHARE>;
+    const bool whole = whole_keys<T>(g) && pair_values<T>(g, g.v, y, g.v_stride, g.y_stride);
+    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, SHARE, true> : k_gdelta_fwd<T, KP, NT, SHARE, false>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT);
@@ -273,7 +253,7 @@ template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const G
 
 template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    const bool wide = l.VP > 64;
+    const bool wide = two_tiles(g, l, sizeof(T) == 4);
     switch (l.KP) {
     case 32: return wide ? launch<T, 32, 2>(g, l, s, init, y, final, stream) : launch<T, 32, 1>(g, l, s, init, y, final, stream);
     case 64: return wide ? launch<T, 64, 2>(g, l, s, init, y, final, stream) : launch<T, 64, 1>(g, l, s, init, y, final, stream);

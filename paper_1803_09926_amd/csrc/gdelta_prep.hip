@@ -66,7 +66,9 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
 #pragma unroll
             for (int j = 0; j < 8; ++j) bad |= !finite(v.at(j));
             if (bad) bads[row] = 1;
-            put8_stored<T>(kt + row * LD, PLANE, col, v);
+            float x[8];
+            v.get(x);
+            put8<RAW>(kt + row * LD, PLANE, col, x);
         }
     }
     __syncthreads();

@@ -9,28 +9,67 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 
-// The columns of a lane: NT neighbours, one in each of its NT result tiles, so that its numbers of a row lie beside each other
+// The columns of a lane: NT neighbours, one in each of its NT result tiles, so that its numbers of a row lie beside each other.  PAIRS: they are read and written
+// at once, aligned.  What is not there is asked for, and stored, outside the view: no branch.
 template <int NT> struct Columns {
     int c;                                        // the first
     __device__ __forceinline__ Columns(int block) : c((block * WAVES + (int)(threadIdx.x >> 6)) * 16 * NT + (int)(threadIdx.x & 15) * NT) {}
-    // NT numbers of a row, of which those below `width` are there
-    template <typename T> __device__ __forceinline__ void load(const T *row, int width, bool there, float (&x)[NT]) const
+    __device__ __forceinline__ uint32_t at(int row, int stride, int size) const { return (uint32_t)(row * stride + c) * (uint32_t)size; }
+    template <typename T, bool PAIRS> __device__ __forceinline__ void load(Ahead<T, NT, PAIRS> &x, const BufView &view, uint32_t off, int width) const
     {
-#pragma unroll
-        for (int i = 0; i < NT; ++i) x[i] = there && c + i < width ? ldf(row + c + i) : 0.f;
+        x.load(view, off, width - c);
     }
-    template <typename T> __device__ __forceinline__ void store(T *row, int width, bool there, const float (&x)[NT]) const
+    template <typename T, bool PAIRS> __device__ __forceinline__ void store(const BufView &view, uint32_t off, int width, const float (&x)[NT]) const
     {
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-            if (there && c + i < width) stf(row + c + i, x[i]);
+        store_late<T, NT, PAIRS>(view, off, width - c, x);
     }
 };
-
 // rows 16 mt + 4 q + r of a tile of tokens
 __device__ __forceinline__ int row_of(int mt, int r) { return mt * 16 + 4 * (int)((threadIdx.x & 63) >> 4) + r; }
 __device__ __forceinline__ float4 four(const float *v, int mt) { return *reinterpret_cast<const float4 *>(v + row_of(mt, 0)); }
 __device__ __forceinline__ v4f_t times(const v4f_t &a, const float4 &b) { return v4f_t{a[0] * b.x, a[1] * b.y, a[2] * b.z, a[3] * b.w}; }
+
+// the state of a sequence and head, [K][V], at a walk's ends
+template <int NT, int CT> __device__ __forceinline__ void load_state(v4f_t (&S)[CT][NT], const float *p, int K, int V, const Columns<NT> &cols)
+{
+    const BufView view(p, (uint32_t)(K * V) * 4u);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            Ahead<float, NT, false> x;
+            x.load(view, cols.at(row_of(ct, r), V, 4), row_of(ct, r) < K ? V - cols.c : 0);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt][r] = x.at(nt);
+        }
+}
+template <int NT, int CT> __device__ __forceinline__ void store_state(const v4f_t (&S)[CT][NT], float *p, int K, int V, const Columns<NT> &cols)
+{
+    const BufView view(p, (uint32_t)(K * V) * 4u);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float x[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) x[nt] = S[ct][nt][r];
+            store_late<float, NT, false>(view, cols.at(row_of(ct, r), V, 4), row_of(ct, r) < K ? V - cols.c : 0, x);
+        }
+}
+// what the passes hand to each other, [rows][VP]
+template <int NT, int MT> __device__ __forceinline__ void store_tiles(const v4f_t (&x)[MT][NT], float *p, int VP, const Columns<NT> &cols)
+{
+    const BufView view(p, (uint32_t)(MT * 16 * VP) * 4u);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float y[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) y[nt] = x[mt][nt][r];
+            store_late<float, NT, true>(view, cols.at(row_of(mt, r), VP, 4), VP - cols.c, y);
+        }
+}
 
 // result tiles of 64 rows as operands that are contracted over them
 template <int N, int NT> __device__ __forceinline__ void split_rows(const v4f_t (&x)[4][NT], Frag (&f)[2][NT][N])
@@ -48,6 +87,19 @@ template <typename T, int KP, bool SHARE> struct Walk {
 };
 // Whether the tiles of keys and queries share their place in LDS: where both do not fit
 template <typename T, int KP> constexpr bool shares() { return Walk<T, KP, false>::LDS > 160 * 1024; }
+
+// Whether a wavefront has 32 columns instead of 16: twice the products of what is read from LDS, where that still fills the card
+inline bool two_tiles(const GdArgs &g, const GdLayout &l, bool f32)
+{
+    return l.VP > 64 && (l.KP < 128 || !f32) && (long long)g.sequences * g.H * cdiv(l.VP, 128) >= 256;
+}
+
+// Whether two columns of the values are whole and aligned
+template <typename T> bool pair_values(const GdArgs &g, const void *p, const void *q, long long p_stride, long long q_stride)
+{
+    const uintptr_t pair = 2 * sizeof(T) - 1;
+    return g.V % 2 == 0 && !((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & pair) && (g.T < 2 || (p_stride % 2 == 0 && q_stride % 2 == 0));
+}
 
 }  // namespace
 

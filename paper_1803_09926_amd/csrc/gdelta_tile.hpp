@@ -128,39 +128,54 @@ template <int N> __device__ __forceinline__ void put8(bf16_t *row, int plane, in
         *reinterpret_cast<u2t_t *>(row + i * plane + place4((col >> 2) + 1)) = u2t_t{p[2][i], p[3][i]};
     }
 }
-// the same for eight numbers as stored
-template <typename T> __device__ __forceinline__ void put8_stored(bf16_t *row, int plane, int col, const Some<T, 8> &v)
+// the same for eight numbers as they came
+template <typename T, bool WHOLE> __device__ __forceinline__ void put8_ahead(bf16_t *row, int plane, int col, const Ahead<T, 8, WHOLE> &v)
 {
     if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u2t_t *>(row + place4(col >> 2)) = u2t_t{v.w[0], v.w[1]};
-        *reinterpret_cast<u2t_t *>(row + place4((col >> 2) + 1)) = u2t_t{v.w[2], v.w[3]};
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (WHOLE) w[i] = v.w[i];
+            else w[i] = v.w[2 * i] | v.w[2 * i + 1] << 16;
+        }
+        *reinterpret_cast<u2t_t *>(row + place4(col >> 2)) = u2t_t{w[0], w[1]};
+        *reinterpret_cast<u2t_t *>(row + place4((col >> 2) + 1)) = u2t_t{w[2], w[3]};
     } else {
         float x[8];
-        v.get(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = v.at(i);
         put8<PartsOf<T>::RAW>(row, plane, col, x);
     }
 }
 
-// A tile of 64 rows of KP columns on its way from memory to LDS: held by THREADS lanes, of which each has every THREADS-th eight columns
-template <typename T, int KP, int THREADS> struct Rows {
+// Rows of a chunk in memory: what lies behind the last row's `width` numbers is outside the view, and so is every row behind it
+template <typename T> __device__ __forceinline__ BufView rows_view(const T *p, long long stride, int len, int width)
+{
+    return BufView(p, (uint32_t)(((len - 1) * stride + width) * (long long)sizeof(T)));
+}
+
+// A tile of 64 rows of KP columns on its way from memory to LDS: held by THREADS lanes, of which each has every THREADS-th eight columns.  WHOLE: eight columns are
+// there or not, and aligned.  No branch: the loads are asked for early and used late.
+template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
     static constexpr int PER_ROW = KP / 8, N = CHUNK * PER_ROW / THREADS;
     static_assert(CHUNK * PER_ROW % THREADS == 0, "all lanes alike");
-    Some<T, 8> v[N];
+    Ahead<T, 8, WHOLE> v[N];
     // len rows of `width` columns are there
     __device__ __forceinline__ void load(const T *p, long long stride, int len, int width)
     {
+        const BufView view = rows_view(p, stride, len, width);
+        const int row = threadIdx.x / PER_ROW, col = threadIdx.x % PER_ROW * 8;
+        const uint32_t step = (uint32_t)(THREADS / PER_ROW * stride) * (uint32_t)sizeof(T);
+        uint32_t off = (uint32_t)(row * (int)stride + col) * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, col = at % PER_ROW * 8;
-            v[i].load(p + row * stride + col, row < len ? width - col : 0);
-        }
+        for (int i = 0; i < N; ++i, off += step) v[i].load(view, off, width - col);
     }
     template <int LD> __device__ __forceinline__ void put(bf16_t *tile) const
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, col = at % PER_ROW * 8;
-            put8_stored<T>(tile + row * LD, CHUNK * LD, col, v[i]);
+            const int at = threadIdx.x + i * THREADS;
+            put8_ahead<T, WHOLE>(tile + at / PER_ROW * LD, CHUNK * LD, at % PER_ROW * 8, v[i]);
         }
     }
 };
@@ -171,8 +186,9 @@ template <int N, int THREADS> struct Matrix {
     u4t_t v[PER];
     __device__ __forceinline__ void load(const char *p)
     {
+        const BufView view(p, N * CHUNK * CHUNK * 2);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] = reinterpret_cast<const u4t_t *>(p)[threadIdx.x + i * THREADS];
+        for (int i = 0; i < PER; ++i) v[i] = view.b128((threadIdx.x + i * THREADS) * 16, 0);
     }
     __device__ __forceinline__ void put(bf16_t *tile) const
     {
@@ -193,6 +209,13 @@ enum { VEC_READ = 0,     // exp(G) rk: what a row of k^T S is multiplied by
        VEC_G = 6,        // the sum of the decays' logarithms from the chunk's start, 64 doubles
        VEC_ONE = 8,      // [0] exp(G_end); [1] as int: the first token whose k, a or b is not finite, 64 if there is none
        VECS = 9 };
+
+// Whether eight columns of keys and queries are whole aligned vectors
+template <typename T> bool whole_keys(const GdArgs &g)
+{
+    const int v = 16 / (int)sizeof(T);
+    return g.K % 8 == 0 && !unaligned16(g.q) && !unaligned16(g.k) && (g.T < 2 || (g.q_stride % v == 0 && g.k_stride % v == 0));
+}
 
 // ---- chunks of packed sequences ----
 // Sequence s has its chunks at floor(starts[s] / 64) + s and the places behind it: no two sequences share one, and none has to be counted.

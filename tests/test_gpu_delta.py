@@ -322,9 +322,9 @@ def test_captured_and_replayed(gpu_lib):
 
 
 def test_offsets_beyond_32_bits(gpu_lib):
-    """Rows 2^25 elements apart."""
+    """Rows 2^22 elements apart."""
     m = Made(61, "bf16")
-    T, K, V, far = 70, 32, 32, 1 << 25
+    T, K, V, far = 530, 32, 32, 1 << 22
     x, par = host_inputs(m, T, 1, 1, K, V)
     space = torch.empty((T - 1) * far + 256, device="cuda", dtype=torch.bfloat16)
     at = {k: space[o:].as_strided((T, w), (far, 1)) for k, o, w in (("q", 0, K), ("k", 32, K), ("v", 64, V), ("a", 96, 1), ("b", 97, 1), ("y", 98, V))}
