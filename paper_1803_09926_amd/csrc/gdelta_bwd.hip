@@ -15,7 +15,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
                                                                   int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
-    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM;
+    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
 #pragma unroll
                 for (int ks = mt / 2; ks < 2; ++ks) {
                     Frag a[INNER];
-                    frags_cols<INNER, LDM>(a, pm, PLANE_M, ks * 32, mt * 16);
+                    frags_cols<INNER, CHUNK>(a, pm, PLANE_M, ks * 32, mt * 16);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma<INNER, RAW>(U[mt][nt], a, b[ks][nt]);
                 }
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
 #pragma unroll
             for (int ks = mt / 2; ks < 2; ++ks) {
                 Frag a[INNER];
-                frags_cols<INNER, LDM>(a, tm, PLANE_M, ks * 32, mt * 16);
+                frags_cols<INNER, CHUNK>(a, tm, PLANE_M, ks * 32, mt * 16);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(X[mt][nt], a, f[ks][nt]);
             }

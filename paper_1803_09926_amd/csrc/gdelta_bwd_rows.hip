@@ -16,18 +16,18 @@ namespace dwc {
 
 namespace {
 
-constexpr int VB = 32, LDV = VB + PAD;
+constexpr int VB = 32, LDV = VB;
 
 template <typename T, int KP> struct Back {
-    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP + PAD;
-    static constexpr int HALVES = KP > 128 ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
+    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP;
+    static constexpr int HALVES = KP > 128 || (KP == 128 && RAW == 1) ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
     static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
     static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
     static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
-    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * LDM * 2, SECOND = TILE + 2 * MATRIX;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * CHUNK * 2, SECOND = TILE + 2 * MATRIX;
     static constexpr size_t REGION = FIRST > SECOND ? FIRST : SECOND;
-    // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums
-    static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8, LDS = REGION + FLOATS * 4;
+    // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums; the chunk's vectors
+    static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8 + VECS * 64, LDS = REGION + FLOATS * 4;
 };
 
 constexpr int DPP_SHR1 = 0x111, DPP_SHR2 = 0x112, DPP_SHR4 = 0x114, DPP_SHR8 = 0x118;      // from the lane so many to the left, zero at a row's start
@@ -45,7 +45,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
     typedef Back<T, KP> C;
-    constexpr int RAW = C::RAW, INNER = C::INNER, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
+    constexpr int RAW = C::RAW, INNER = C::INNER, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
     constexpr int TILES = C::TILES, THREADS = C::THREADS, HALVES = C::HALVES;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const st = reinterpret_cast<bf16_t *>(lds), *const dst = C::TURNS ? st : st + INNER * PLANE_S;
@@ -53,11 +53,11 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     bf16_t *const tile = reinterpret_cast<bf16_t *>(lds), *const fm = tile + RAW * PLANE, *const mm = fm + INNER * PLANE_M;
     float *const row_m = reinterpret_cast<float *>(lds + C::REGION), *const xv = row_m + 64;
     float *const passing = xv + 64, *const dot_a = passing + 8 * 64, *const dot_b = dot_a + 2 * 64, *const dot_c = dot_b + 2 * 64;
-    float *const wave_sums = dot_c + 2 * 64;
+    float *const wave_sums = dot_c + 2 * 64, *const vec = wave_sums + 8;
 
     const unsigned id = first + blockIdx.x;
     const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
-    const int wv = threadIdx.x >> 6, mt = wv & 3, half = wv >> 2, col0 = half * C::KW;
+    const int wv = wave_number(), mt = wv & 3, half = wv >> 2, col0 = half * C::KW;
     const bool does_f = HALVES == 1 || half == 0, does_m = HALVES == 1 || half == 1;
     const ChunkAt at = gd_chunk(g, (int)id);
     if (at.len == 0) {
@@ -65,20 +65,12 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
         return;
     }
     const T *const kp = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K, *const qp = (const T *)g.q + at.first * g.q_stride + (long long)kh * g.K;
-    auto put_tile = [&](const T *p, long long stride) {
-        Rows<T, KP, THREADS, WHOLE> rows;
-        rows.load(p, stride, at.len, g.K);
-        rows.template put<LD>(tile);
-    };
-    auto tile_at = [&](int row, int col) {           // of a tile of keys or queries
-        float v = 0.f;
-#pragma unroll
-        for (int i = RAW - 1; i >= 0; --i) v += bf16_to_f32(tile[i * PLANE + row * LD + place(col)]);
-        return v;
-    };
-
-    // products of keys with keys and queries: rows 16 mt.., columns 16 n..
-    v4f_t kk[4], qk[4];
+    Rows<T, KP, THREADS, WHOLE> rows;                // a tile of keys or queries on its way
+    auto ask_keys = [&] { rows.load(kp, g.k_stride, at.len, g.K); };
+    auto ask_queries = [&] { rows.load(qp, g.q_stride, at.len, g.K); };
+    // Products of queries with keys, and of keys with keys: rows 16 mt.., columns 16 n...  Where two wavefronts share the rows each has one of them.
+    constexpr int BOTH = HALVES == 1 ? 2 : 1, AT_M = BOTH - 1;
+    v4f_t qk[BOTH][4];
     {
         Frag qa[KP / 32][RAW];
         const int row = mt * 16 + m;
@@ -96,11 +88,12 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
             for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
         }
-        put_tile(kp, g.k_stride);
+        ask_keys();
+        rows.template put<LD>(tile);
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            kk[n] = qk[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+            qk[0][n] = qk[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
             if (n > mt) continue;
 #pragma unroll
             for (int c = 0; c < KP / 32; ++c) {
@@ -108,9 +101,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 frags_rows<RAW, LD>(b, tile, PLANE, n * 16, c * 32);
                 if (does_m) {
                     frags_rows<RAW, LD>(a, tile, PLANE, mt * 16, c * 32);
-                    mma<RAW, RAW>(kk[n], a, b);
+                    mma<RAW, RAW>(qk[AT_M][n], a, b);
                 }
-                if (does_f) mma<RAW, RAW>(qk[n], qa[c], b);
+                if (does_f) mma<RAW, RAW>(qk[0][n], qa[c], b);
             }
         }
     }
@@ -122,64 +115,92 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     for (int hh = 0; hh < share; ++hh) {
         const int h = kh * share + hh;
         const long long where = (long long)id * g.H + h;
-        const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
         const float *const sp = s.S + where * (l.state / 4), *const dsp = s.dS + where * (l.state / 4);
         const float *const xp = s.X + where * (l.rows / 4), *const up = s.U + where * (l.rows / 4);
         const T *const yp = dy + at.first * g.y_stride + (long long)h * g.V, *const vp = (const T *)g.v + at.first * g.v_stride + (long long)h * g.V;
-        v4f_t ys[TILES], xs[TILES], us[TILES], yu[4], xu[4];
+        // what the next 32 columns of V take, on its way: 8 numbers a lane of each
+        constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
+        const int vrow = threadIdx.x % 256 / (VB / 8), vcol = threadIdx.x % (VB / 8) * 8;
+        const bool takes_x = HALVES == 1 || threadIdx.x < 256, takes_u = HALVES == 1 || threadIdx.x >= 256;
+        u4t_t sa[PER][2], sb[PER][2], xa8[2], ua8[2];
+        Some<T, 8> v8, y8;
+        auto ask = [&](int v0) {
+            const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state), view_x(xp, (uint32_t)l.rows), view_u(up, (uint32_t)l.rows);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int n = threadIdx.x + i * THREADS;
+                const uint32_t off = n < ALL ? (uint32_t)(n / (VB / 8) * l.VP + v0 + n % (VB / 8) * 8) * 4u : BufView::OUTSIDE;
+                sa[i][0] = view_s.b128(off, 0);
+                sa[i][1] = view_s.b128(off + 16, 0);
+                sb[i][0] = view_d.b128(off, 0);
+                sb[i][1] = view_d.b128(off + 16, 0);
+            }
+            const uint32_t off = (uint32_t)(vrow * l.VP + v0 + vcol) * 4u;
+            if (takes_x) {
+                xa8[0] = view_x.b128(off, 0);
+                xa8[1] = view_x.b128(off + 16, 0);
+                v8.load(vp + vrow * g.v_stride + v0 + vcol, vrow < at.len ? g.V - v0 - vcol : 0);
+            }
+            if (takes_u) {
+                ua8[0] = view_u.b128(off, 0);
+                ua8[1] = view_u.b128(off + 16, 0);
+                y8.load(yp + vrow * g.y_stride + v0 + vcol, vrow < at.len ? g.V - v0 - vcol : 0);
+            }
+        };
+        auto eight = [](const u4t_t (&w)[2], float (&x)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
+        };
+        ask(0);
+        v4f_t ys[TILES], xs[TILES], us[TILES], yu[BOTH][4];      // yu: dY U^T and X U^T
 #pragma unroll
         for (int t = 0; t < TILES; ++t) ys[t] = xs[t] = us[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) yu[n] = xu[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < 4; ++n) yu[0][n] = yu[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        float gate_a = 0.f, gate_b = 0.f;                // of the token that a lane of the first wavefront has in the end
+        if (wv == 0 && lane < at.len) {
+            gate_a = ldf((const T *)g.a + (at.first + lane) * g.a_stride + h);
+            gate_b = ldf((const T *)g.b + (at.first + lane) * g.b_stride + h);
+        }
         float ss = 0.f, xv_part = 0.f;                   // dS.S and X.V, this lane's share
 
         for (int v0 = 0; v0 < l.VP; v0 += VB) {
             __syncthreads();
-            constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
+            if (v0 == 0) {
+                const float *const p = reinterpret_cast<const float *>(s.vec + where * l.vectors);
+                for (int i = threadIdx.x; i < VECS * 64; i += THREADS) vec[i] = p[i];
+            }
             float keep[C::TURNS ? PER : 1][8];
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int n = threadIdx.x + i * THREADS, row = n / (VB / 8), col = n % (VB / 8) * 8;
                 if (ALL % THREADS && n >= ALL) break;
                 float a[8], b[8];
-                const float4 a0 = *reinterpret_cast<const float4 *>(sp + (long long)row * l.VP + v0 + col), a1 = *reinterpret_cast<const float4 *>(sp + (long long)row * l.VP + v0 + col + 4);
-                const float4 b0 = *reinterpret_cast<const float4 *>(dsp + (long long)row * l.VP + v0 + col), b1 = *reinterpret_cast<const float4 *>(dsp + (long long)row * l.VP + v0 + col + 4);
-                a[0] = a0.x; a[1] = a0.y; a[2] = a0.z; a[3] = a0.w; a[4] = a1.x; a[5] = a1.y; a[6] = a1.z; a[7] = a1.w;
-                b[0] = b0.x; b[1] = b0.y; b[2] = b0.z; b[3] = b0.w; b[4] = b1.x; b[5] = b1.y; b[6] = b1.z; b[7] = b1.w;
+                eight(sa[i], a);
+                eight(sb[i], b);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) ss += a[j] * b[j];
-                put8<INNER>(st + row * LDV, PLANE_S, col, a);
+                put8<INNER, LDV>(st, PLANE_S, row, col, a);
                 if constexpr (C::TURNS) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) keep[i][j] = b[j];
-                } else put8<INNER>(dst + row * LDV, PLANE_S, col, b);
+                } else put8<INNER, LDV>(dst, PLANE_S, row, col, b);
             }
-            {
-                const int n = threadIdx.x % 256, row = n / (VB / 8), col = n % (VB / 8) * 8;
-                auto eight = [&](const float *p, float (&x)[8]) {
-                    const float4 a = *reinterpret_cast<const float4 *>(p + (long long)row * l.VP + v0 + col), b = *reinterpret_cast<const float4 *>(p + (long long)row * l.VP + v0 + col + 4);
-                    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-                };
-                if (HALVES == 1 || threadIdx.x < 256) {
-                    float x[8];
-                    eight(xp, x);
-                    Some<T, 8> v;
-                    v.load(vp + row * g.v_stride + v0 + col, row < at.len ? g.V - v0 - col : 0);
+            if (takes_x) {
+                float x[8];
+                eight(xa8, x);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) xv_part += x[j] * v.at(j);
-                    put8<INNER>(xt + row * LDV, PLANE_V, col, x);
-                }
-                if (HALVES == 1 || threadIdx.x >= 256) {
-                    float x[8];
-                    eight(up, x);
-                    put8<INNER>(ut + row * LDV, PLANE_V, col, x);
-                    Some<T, 8> v;
-                    v.load(yp + row * g.y_stride + v0 + col, row < at.len ? g.V - v0 - col : 0);
-                    float o[8];
-                    v.get(o);
-                    put8<RAW>(yt + row * LDV, PLANE_V, col, o);
-                }
+                for (int j = 0; j < 8; ++j) xv_part += x[j] * v8.at(j);
+                put8<INNER, LDV>(xt, PLANE_V, vrow, vcol, x);
             }
+            if (takes_u) {
+                float x[8];
+                eight(ua8, x);
+                put8<INNER, LDV>(ut, PLANE_V, vrow, vcol, x);
+                y8.get(x);
+                put8<RAW, LDV>(yt, PLANE_V, vrow, vcol, x);
+            }
+            if (v0 + VB < l.VP) ask(v0 + VB);
             __syncthreads();
             Frag ya[RAW], xa[INNER], ua[INNER];
             frags_rows<RAW, LDV>(ya, yt, PLANE_V, mt * 16, 0);
@@ -190,8 +211,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 if (n > mt) continue;
                 Frag b[INNER];
                 frags_rows<INNER, LDV>(b, ut, PLANE_V, n * 16, 0);
-                if (does_f) mma<RAW, INNER>(yu[n], ya, b);
-                if (does_m) mma<INNER, INNER>(xu[n], xa, b);
+                if (does_f) mma<RAW, INNER>(yu[0][n], ya, b);
+                if (does_m) mma<INNER, INNER>(yu[AT_M][n], xa, b);
             }
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
@@ -205,7 +226,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     const int n = threadIdx.x + i * THREADS;
-                    put8<INNER>(dst + n / (VB / 8) * LDV, PLANE_S, n % (VB / 8) * 8, keep[i]);
+                    put8<INNER, LDV>(dst, PLANE_S, n / (VB / 8), n % (VB / 8) * 8, keep[i]);
                 }
                 __syncthreads();
             }
@@ -216,6 +237,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 mma<INNER, INNER>(us[t], ua, b);
             }
         }
+        ask_queries();
         __syncthreads();                                 // the first region is free
         ss = lanes_sum(ss);
         if (lane == 0) wave_sums[wv] = ss;
@@ -238,25 +260,25 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = mt * 16 + 4 * q4 + r;
-                    const float e = i >= j ? expf((float)(G[i] - gj)) * kj : 0.f;
+                    const float e = i >= j ? exp2_fast((float)(G[i] - gj) * LOG2E) * kj : 0.f;
                     float x = 0.f;
                     uint32_t p[INNER];
                     if (does_f) {
-                        const float f = i >= j ? g.scale * vec[VEC_RQ * 64 + i] * e * yu[n][r] : 0.f;
-                        x += f * qk[n][r];
+                        const float f = i >= j ? g.scale * vec[VEC_RQ * 64 + i] * e * yu[0][n][r] : 0.f;
+                        x += f * qk[0][n][r];
                         split2<INNER>(f, 0.f, p);
 #pragma unroll
-                        for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + i * LDM + place(j)] = (bf16_t)p[k];
+                        for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
                     }
                     if (does_m && i >= j) {
-                        const float b = i > j ? -vec[VEC_RK * 64 + i] * e * xu[n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
-                        rm[r] += b * kk[n][r];
-                        x += f * kk[n][r];
+                        const float b = i > j ? -vec[VEC_RK * 64 + i] * e * yu[AT_M][n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
+                        rm[r] += b * qk[AT_M][n][r];
+                        x += f * qk[AT_M][n][r];
                         split2<INNER>(f, 0.f, p);
 #pragma unroll
                         for (int k = 0; k < INNER; ++k) {
-                            mm[k * PLANE_M + i * LDM + place(j)] = (bf16_t)p[k];
-                            mm[k * PLANE_M + j * LDM + place(i)] = (bf16_t)p[k];
+                            mm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
+                            mm[k * PLANE_M + place<CHUNK>(j, i)] = (bf16_t)p[k];
                         }
                     }
                     // the sum over the columns before j, of the rows from j on
@@ -280,7 +302,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 }
             }
         }
-        put_tile(qp, g.q_stride);
+        rows.template put<LD>(tile);
+        ask_keys();
         __syncthreads();
         {
             float dot[4];
@@ -288,12 +311,12 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             for (int r = 0; r < 4; ++r) dot[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
+                const v4f_t q = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = mt * 16 + 4 * q4 + r;
-                    const float x = ys[t][r] * vec[VEC_ASK * 64 + i];
+                    const float x = ys[t][r] * vec[VEC_ASK * 64 + mt * 16 + 4 * q4 + r];
                     gq[t][r] += x;
-                    dot[r] += x * tile_at(i, col0 + t * 16 + m);
+                    dot[r] += x * q[r];
                 }
             }
 #pragma unroll
@@ -302,7 +325,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             for (int ks = 0; ks < 2; ++ks) {
                 if (ks < mt / 2) continue;
                 Frag a[INNER];
-                frags_cols<INNER, LDM>(a, fm, PLANE_M, ks * 32, mt * 16);
+                frags_cols<INNER, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
@@ -312,7 +335,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             }
         }
         __syncthreads();
-        put_tile(kp, g.k_stride);
+        rows.template put<LD>(tile);
+        if (hh + 1 == share) ask_queries();
         __syncthreads();
         {
             float db_[4], dc_[4];
@@ -320,14 +344,14 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             for (int r = 0; r < 4; ++r) db_[r] = dc_[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
+                const v4f_t k = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = mt * 16 + 4 * q4 + r;
-                    const float k = tile_at(i, col0 + t * 16 + m);
                     const float x = xs[t][r] * vec[VEC_READ * 64 + i], u = us[t][r] * vec[VEC_WRITE * 64 + i];
                     gk[t][r] += u - vec[VEC_BETA * 64 + i] * x;
-                    db_[r] += x * k;
-                    dc_[r] += u * k;
+                    db_[r] += x * k[r];
+                    dc_[r] += u * k[r];
                 }
             }
 #pragma unroll
@@ -342,8 +366,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 Frag a[INNER], b2[INNER];
-                frags_rows<INNER, LDM>(a, fm, PLANE_M, mt * 16, ks * 32);
-                frags_rows<INNER, LDM>(b2, mm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, CHUNK>(a, fm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, CHUNK>(b2, mm, PLANE_M, mt * 16, ks * 32);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
@@ -365,22 +389,22 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 sum += wave_sums[i];
             }
             // what is read from the token on, and what was written before it
-            const float left = __shfl_up(c, 1, 64);      // (by all lanes: one that is not here hands out nothing)
-            double d = (double)(a - beta * b), w = lane ? (double)left : 0.0;
+            float d = a - beta * b, w = __shfl_up(c, 1, 64);
+            if (lane == 0) w = 0.f;
 #pragma unroll
             for (int off = 1; off < 64; off *= 2) {
-                const double down = __shfl_down(d, off, 64), up = __shfl_up(w, off, 64);
+                const float down = __shfl_down(d, off, 64), up = __shfl_up(w, off, 64);
                 if (lane + off < 64) d += down;
                 if (lane >= off) w += up;
             }
             const float dbeta = xv[lane] - b + row_m[lane];
-            float dg = (float)(d + w + (double)(pass + vec[VEC_ONE * 64] * sum)), for_a = 0.f, for_A = 0.f;
+            float dg = d + w + (pass + vec[VEC_ONE * 64] * sum), for_a = 0.f, for_A = 0.f;
             if (lane < at.len) {
-                const float raw = gd_raw(g, ldf((const T *)g.a + (at.first + lane) * g.a_stride + h), h), soft = gd_soft(g, raw), A = g.A ? g.A[h] : -1.f;
+                const float raw = gd_raw(g, gate_a, h), soft = gd_soft(g, raw), A = g.A ? g.A[h] : -1.f;
                 if (A * soft < GD_LEAST) dg = 0.f;
                 for_A = dg * soft;
                 for_a = dg * A * (g.softplus ? 1.f / (1.f + expf(-raw)) : 1.f);
-                const float rate = gd_rate(g, ldf((const T *)g.b + (at.first + lane) * g.b_stride + h));
+                const float rate = gd_rate(g, gate_b);
                 stf(da + (at.first + lane) * g.a_stride + h, for_a);
                 stf(db + (at.first + lane) * g.b_stride + h, g.sigmoid ? dbeta * rate * (1.f - rate) : dbeta);
             }
@@ -394,16 +418,17 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     }
 
     // The lengths: of n = r x the gradient r (dn - n (n.dn)), where the factor r is in already.  The tile holds the keys.
-    const float *const vec = reinterpret_cast<const float *>(s.vec + ((long long)id * g.H + kh * share) * l.vectors);
     auto finish = [&](v4f_t (&grad)[TILES], int which, T *out, long long stride) {
-        float dot[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) dot[r] = 0.f;
         if (g.norm) {
+            float dot[4];
 #pragma unroll
-            for (int t = 0; t < TILES; ++t)
+            for (int r = 0; r < 4; ++r) dot[r] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dot[r] += grad[t][r] * tile_at(mt * 16 + 4 * q4 + r, col0 + t * 16 + m);
+            for (int t = 0; t < TILES; ++t) {
+                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dot[r] += grad[t][r] * n[r];
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) dot[r] = row_sum(dot[r]);
             if constexpr (HALVES == 2) {
@@ -415,22 +440,32 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
                 for (int r = 0; r < 4; ++r) dot[r] = dot_a[mt * 16 + 4 * q4 + r] + dot_a[64 + mt * 16 + 4 * q4 + r];
             }
-        }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = mt * 16 + 4 * q4 + r;
-            const float inv = vec[which * 64 + i], f = g.norm ? inv * inv * dot[r] : 0.f;
-            if (i >= at.len) continue;
+            for (int r = 0; r < 4; ++r) {
+                const float inv = vec[which * 64 + mt * 16 + 4 * q4 + r];
+                dot[r] *= inv * inv;
+            }
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const int col = col0 + t * 16 + m;
-                if (col < g.K) stf(out + i * stride + col, g.norm ? grad[t][r] - f * tile_at(i, col) : grad[t][r]);
+                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) grad[t][r] -= dot[r] * n[r];
+            }
+        }
+        const BufView view = rows_view(out, stride, at.len, g.K);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            const int col = col0 + t * 16 + m;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float x[1] = {grad[t][r]};
+                store_late<T, 1, false>(view, (uint32_t)((mt * 16 + 4 * q4 + r) * (int)stride + col) * (uint32_t)sizeof(T), g.K - col, x);
             }
         }
     };
     finish(gk, VEC_RK, dk + at.first * g.k_stride + (long long)kh * g.K, g.k_stride);
     __syncthreads();
-    put_tile(qp, g.q_stride);
+    rows.template put<LD>(tile);
     __syncthreads();
     finish(gq, VEC_RQ, dq + at.first * g.q_stride + (long long)kh * g.K, g.q_stride);
 }

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                                                            float *__restrict__ final, unsigned first, int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
-    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * LDM;
+    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
 #pragma unroll
             for (int ks = 0; ks <= mt / 2; ++ks) {
                 Frag a[INNER];
-                frags_rows<INNER, LDM>(a, tm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, CHUNK>(a, tm, PLANE_M, mt * 16, ks * 32);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(U[mt][nt], a, f[ks][nt]);
             }
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
 #pragma unroll
             for (int ks = 0; ks <= mt / 2; ++ks) {
                 Frag a[INNER];
-                frags_rows<INNER, LDM>(a, pm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, CHUNK>(a, pm, PLANE_M, mt * 16, ks * 32);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(O[mt][nt], a, f[ks][nt]);
             }

@@ -16,7 +16,7 @@ namespace {
 constexpr int THREADS = 256, LDF = 68;            // floats of a row of an fp32 matrix in LDS
 
 template <typename T, int KP> struct Prep {
-    static constexpr int RAW = PartsOf<T>::RAW, LD = KP + PAD;
+    static constexpr int RAW = PartsOf<T>::RAW, LD = KP;
     static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, F32S = (size_t)CHUNK * LDF * 4;
     static constexpr size_t LDS = TILE + 2 * F32S + 64 * 8 + 5 * 64 * 4;
 };
@@ -26,12 +26,16 @@ template <int N> __device__ __forceinline__ void put_matrix(const float *f, char
 {
     const int row = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
     bf16_t *const p = reinterpret_cast<bf16_t *>(to) + row * CHUNK;
+    const float *const x = f + row * LDF + c;
+    // four numbers, and the four 16 columns on, are a piece: a lane has halves of four
 #pragma unroll
-    for (int j = 0; j < 16; j += 8) {
-        float x[8];
+    for (int j = 0; j < 4; ++j) {
+        uint32_t a[N], b[N];
+        split2<N>(x[4 * j], x[4 * j + 1], a);
+        split2<N>(x[4 * j + 2], x[4 * j + 3], b);
+        const int j4 = (c >> 2) + j;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = f[row * LDF + c + j + i];
-        put8<N>(p, CHUNK * CHUNK, c + j, x);
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u2t_t *>(p + i * CHUNK * CHUNK + piece_of(j4) * 8 + half_of(j4) * 4) = u2t_t{a[i], b[i]};
     }
 }
 
@@ -50,7 +54,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
     const unsigned id = first + blockIdx.x;
     const ChunkAt at = gd_chunk(g, (int)id);
     if (at.len == 0) return;
-    const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, m = lane & 15, q4 = lane >> 4;
+    const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, wv = wave_number(), m = lane & 15, q4 = lane >> 4;
 
     // keys into LDS; a token's key that is not finite counts as none, and the token is remembered
     if (threadIdx.x < 64) bads[threadIdx.x] = 0;
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             if (bad) bads[row] = 1;
             float x[8];
             v.get(x);
-            put8<RAW>(kt + row * LD, PLANE, col, x);
+            put8<RAW, LD>(kt, PLANE, row, col, x);
         }
     }
     __syncthreads();

@@ -13,7 +13,7 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 // at once, aligned.  What is not there is asked for, and stored, outside the view: no branch.
 template <int NT> struct Columns {
     int c;                                        // the first
-    __device__ __forceinline__ Columns(int block) : c((block * WAVES + (int)(threadIdx.x >> 6)) * 16 * NT + (int)(threadIdx.x & 15) * NT) {}
+    __device__ __forceinline__ Columns(int block) : c((block * WAVES + wave_number()) * 16 * NT + (int)(threadIdx.x & 15) * NT) {}
     __device__ __forceinline__ uint32_t at(int row, int stride, int size) const { return (uint32_t)(row * stride + c) * (uint32_t)size; }
     template <typename T, bool PAIRS> __device__ __forceinline__ void load(Ahead<T, NT, PAIRS> &x, const BufView &view, uint32_t off, int width) const
     {
@@ -81,8 +81,8 @@ template <int N, int NT> __device__ __forceinline__ void split_rows(const v4f_t 
 }
 
 template <typename T, int KP, bool SHARE> struct Walk {
-    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP + PAD;
-    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * LDM * 2;
+    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * CHUNK * 2;
     static constexpr size_t LDS = (SHARE ? 1 : 2) * TILE + 2 * MATRIX + 2 * 256 * 4;
 };
 // Whether the tiles of keys and queries share their place in LDS: where both do not fit

@@ -7,7 +7,8 @@
 //
 // Lanes: m = lane % 16, q = lane / 16.  A result tile has rows 4 q + r (r = 0..3) of column m in a lane.  Two result tiles below each other are an operand as they are: the
 // contraction runs over their 32 rows in the order 4 q + 0..3 of the first, 4 q + 0..3 of the second.  Tiles in LDS are stored so that 16 consecutive bytes of a row hold the
-// same order (within every 32 columns), and columns are read through the transposing reads of LDS.
+// same order (within every 32 columns), and columns are read through the transposing reads of LDS.  Which 16 bytes of its row a piece has depends on the row: the pieces
+// that an instruction reads, one of each of 16 rows, or four of each of four, then lie in all 64 banks (with padded rows instead the transposing reads met four to a bank).
 #pragma once
 #include "gdelta.hpp"
 
@@ -37,12 +38,14 @@ template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
 }
 
 constexpr int CHUNK = 64;
-constexpr int PAD = 8;                            // elements behind a row of an LDS tile: rows start at other banks
-constexpr int LDM = CHUNK + PAD;                  // of a tile of CHUNK columns
 
 template <typename T> struct PartsOf;
 template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1, INNER = 2; };
 template <> struct PartsOf<float> { static constexpr int RAW = 3, INNER = 3; };
+
+// The number of a lane's wavefront, as a scalar.  What is done by some wavefronts only has to be behind a scalar branch where it holds matrix instructions: those do not
+// look at which lanes are on.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
 struct Frag { u4t_t w; };
 
@@ -84,26 +87,47 @@ template <int N> __device__ __forceinline__ void split_tiles(const v4f_t &a, con
     for (int i = 0; i < N; ++i) f[i].w = u4t_t{p[0][i], p[1][i], p[2][i], p[3][i]};
 }
 
-// where in an LDS row the four columns from 4 * j4 on lie
-__device__ __forceinline__ constexpr int place4(int j4) { return (j4 >> 3) * 32 + (j4 & 3) * 8 + ((j4 >> 2) & 1) * 4; }
-__device__ __forceinline__ constexpr int place(int col) { return place4(col >> 2) + (col & 3); }
+// the piece of 16 bytes, of a row of LD columns in memory order, that holds the four columns from 4 * j4 on, and which half of it
+__device__ __forceinline__ constexpr int piece_of(int j4) { return (j4 >> 3) * 4 + (j4 & 3); }
+__device__ __forceinline__ constexpr int half_of(int j4) { return (j4 >> 2) & 1; }
+// where in LDS a row's piece lies
+template <int LD> __device__ __forceinline__ constexpr int turned(int row, int piece)
+{
+    return piece ^ (LD == 32 ? (row >> 2) & 3 : LD == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3));
+}
+template <int LD> __device__ __forceinline__ constexpr int place4(int row, int j4) { return row * LD + turned<LD>(row, piece_of(j4)) * 8 + half_of(j4) * 4; }
+template <int LD> __device__ __forceinline__ constexpr int place(int row, int col) { return place4<LD>(row, col >> 2) + (col & 3); }
 
 // Operands out of LDS tiles of leading dimension LD.  rows: 16 of them from r0, contracted over the 32 columns from c0 on.  cols: 16 of them from c0, contracted over
 // the 32 rows from r0 on.
 template <int LD> __device__ __forceinline__ Frag frag_rows(const bf16_t *tile, int r0, int c0)
 {
     const int lane = threadIdx.x & 63;
-    return {*reinterpret_cast<const u4t_t *>(tile + (r0 + (lane & 15)) * LD + c0 + (lane >> 4) * 8)};
+    // (r0 is a multiple of 16: the rows' turns are those of the lane)
+    return {*reinterpret_cast<const u4t_t *>(tile + (r0 + (lane & 15)) * LD + turned<LD>(lane & 15, c0 / 8 + (lane >> 4)) * 8)};
 }
 typedef __attribute__((address_space(3))) v4h_t *lds_v4h_t;
 template <int LD> __device__ __forceinline__ Frag frag_cols(const bf16_t *tile, int r0, int c0)
 {
     const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
-    const bf16_t *const p = tile + (r0 + 4 * q + (m >> 2)) * LD + place4((c0 >> 2) + (m & 3));
+    const bf16_t *const p = tile + r0 * LD + place4<LD>(4 * q + (m >> 2), (c0 >> 2) + (m & 3));
     const v4h_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)p);
     const v4h_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)(p + 16 * LD));
     const u2t_t x = __builtin_bit_cast(u2t_t, a), y = __builtin_bit_cast(u2t_t, b);
     return {u4t_t{x.x, x.y, y.x, y.y}};
+}
+// the numbers of a tile of N parts where a result tile has its own: rows r0 + 4 q + r of column c0 + m
+template <int N, int LD> __device__ __forceinline__ v4f_t tile_of(const bf16_t *tile, int plane, int r0, int c0)
+{
+    const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    v4f_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+        const bf16_t *const p = tile + i * plane + r0 * LD + place4<LD>(4 * q + (m >> 2), (c0 >> 2) + (m & 3));
+        const u2t_t w = __builtin_bit_cast(u2t_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)p));
+        v += v4f_t{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+    }
+    return v;
 }
 template <int N, int LD> __device__ __forceinline__ void frags_rows(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0)
 {
@@ -117,19 +141,19 @@ template <int N, int LD> __device__ __forceinline__ void frags_cols(Frag (&f)[N]
 }
 
 // eight consecutive numbers from a column that is a multiple of 8 on, into a row of an LDS tile of N parts
-template <int N> __device__ __forceinline__ void put8(bf16_t *row, int plane, int col, const float (&x)[8])
+template <int N, int LD> __device__ __forceinline__ void put8(bf16_t *tile, int plane, int row, int col, const float (&x)[8])
 {
     uint32_t p[4][N];
 #pragma unroll
     for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], x[2 * i + 1], p[i]);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        *reinterpret_cast<u2t_t *>(row + i * plane + place4(col >> 2)) = u2t_t{p[0][i], p[1][i]};
-        *reinterpret_cast<u2t_t *>(row + i * plane + place4((col >> 2) + 1)) = u2t_t{p[2][i], p[3][i]};
+        *reinterpret_cast<u2t_t *>(tile + i * plane + place4<LD>(row, col >> 2)) = u2t_t{p[0][i], p[1][i]};
+        *reinterpret_cast<u2t_t *>(tile + i * plane + place4<LD>(row, (col >> 2) + 1)) = u2t_t{p[2][i], p[3][i]};
     }
 }
 // the same for eight numbers as they came
-template <typename T, bool WHOLE> __device__ __forceinline__ void put8_ahead(bf16_t *row, int plane, int col, const Ahead<T, 8, WHOLE> &v)
+template <typename T, int LD, bool WHOLE> __device__ __forceinline__ void put8_ahead(bf16_t *tile, int plane, int row, int col, const Ahead<T, 8, WHOLE> &v)
 {
     if constexpr (sizeof(T) == 2) {
         uint32_t w[4];
@@ -138,13 +162,13 @@ template <typename T, bool WHOLE> __device__ __forceinline__ void put8_ahead(bf1
             if constexpr (WHOLE) w[i] = v.w[i];
             else w[i] = v.w[2 * i] | v.w[2 * i + 1] << 16;
         }
-        *reinterpret_cast<u2t_t *>(row + place4(col >> 2)) = u2t_t{w[0], w[1]};
-        *reinterpret_cast<u2t_t *>(row + place4((col >> 2) + 1)) = u2t_t{w[2], w[3]};
+        *reinterpret_cast<u2t_t *>(tile + place4<LD>(row, col >> 2)) = u2t_t{w[0], w[1]};
+        *reinterpret_cast<u2t_t *>(tile + place4<LD>(row, (col >> 2) + 1)) = u2t_t{w[2], w[3]};
     } else {
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = v.at(i);
-        put8<PartsOf<T>::RAW>(row, plane, col, x);
+        put8<PartsOf<T>::RAW, LD>(tile, plane, row, col, x);
     }
 }
 
@@ -175,12 +199,12 @@ template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = threadIdx.x + i * THREADS;
-            put8_ahead<T, WHOLE>(tile + at / PER_ROW * LD, CHUNK * LD, at % PER_ROW * 8, v[i]);
+            put8_ahead<T, LD, WHOLE>(tile, CHUNK * LD, at / PER_ROW, at % PER_ROW * 8, v[i]);
         }
     }
 };
 
-// One of the first pass's matrices on its way to LDS: parts of 64 x 64, stored in the order of the LDS tiles
+// One of the first pass's matrices on its way to LDS: parts of 64 x 64, stored in the LDS tiles' order of columns, not turned
 template <int N, int THREADS> struct Matrix {
     static constexpr int PER = N * CHUNK * CHUNK / 8 / THREADS;
     u4t_t v[PER];
@@ -195,7 +219,7 @@ template <int N, int THREADS> struct Matrix {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int at = threadIdx.x + i * THREADS, row = at / (CHUNK / 8);      // rows of all parts, one after the other
-            *reinterpret_cast<u4t_t *>(tile + row * LDM + at % (CHUNK / 8) * 8) = v[i];
+            *reinterpret_cast<u4t_t *>(tile + row * CHUNK + turned<CHUNK>(row, at % (CHUNK / 8)) * 8) = v[i];
         }
     }
 };
