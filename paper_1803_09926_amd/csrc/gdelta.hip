@@ -1,7 +1,9 @@
 // Entry points of the gated delta rule (include/deltaops.h): checks, sizes, and the order of its kernels.
 #include "gdelta_launch.hpp"
+#include "tune.hpp"
 #include <initializer_list>
 #include <math.h>
+#include <stdlib.h>
 
 namespace dwc {
 
@@ -45,19 +47,38 @@ GdArgs args_of(const gdelta_desc *d, const gdelta_tensors *t)
     return g;
 }
 
-size_t first_pass_bytes(const gdelta_desc *d, const GdLayout &l) { return (size_t)l.chunks * d->H * (size_t)(2 * l.matrix + l.vectors); }
-void place_first_pass(const gdelta_desc *d, const GdLayout &l, char *p, GdSpace *s)
+// bytes of what the forward pass writes for itself, and of what it keeps for the backward pass besides
+size_t forward_bytes(const gdelta_desc *d, const GdLayout &l)
+{
+    return (size_t)l.chunks * d->H * (size_t)(2 * l.matrix + l.vectors) + (size_t)l.pieces * d->H * (size_t)(l.state + l.map);
+}
+void place_forward(const gdelta_desc *d, const GdLayout &l, char *p, GdSpace *s)
 {
     s->T = p;
     s->P = s->T + l.chunks * d->H * l.matrix;
     s->vec = s->P + l.chunks * d->H * l.matrix;
+    s->ends = (float *)(s->vec + l.chunks * d->H * l.vectors);
+    s->maps = (float *)((char *)s->ends + l.pieces * d->H * l.state);
 }
 void place_kept(const gdelta_desc *d, const GdLayout &l, void *kept, GdSpace *s)
 {
-    place_first_pass(d, l, (char *)kept, s);
-    char *const p = (char *)kept + first_pass_bytes(d, l);
+    place_forward(d, l, (char *)kept, s);
+    char *const p = (char *)kept + forward_bytes(d, l);
     s->S = (float *)p;
     s->U = (float *)(p + l.chunks * d->H * l.state);
+}
+
+// How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole.  Of heads of 128 x 128 in bf16 a chunk of a walk takes 4.2 us, of a
+// piece and its map 7.5 together, both as long as there are no more blocks than compute units, and a piece in the join 3.7.  16384 tokens of 16 heads: 1035 us whole,
+// 308 in pieces; 8 sequences of 1024 tokens of 8 heads 85 and 113.
+int piece_of(const gdelta_desc *d, long long VP)
+{
+    const char *const forced = tune_env("DWCONV_TUNE_GDELTA_PIECE");
+    if (forced) return atoi(forced) > 0 ? atoi(forced) : 0;
+    const double chunks = ceil((double)d->T / ((double)d->sequences * TOKENS)), walks = (double)d->sequences * d->H * ((VP + 63) / 64), units = 256;
+    const double piece = ceil(fmax(4, fmax(chunks * walks / (2 * units), sqrt(chunks / 2)))), pieces = ceil(chunks / piece);
+    if (walks >= units || pieces < 2) return 0;
+    return 7.5 * piece * fmax(1, pieces * walks / units) + 3.7 * pieces + 10 < 0.8 * 4.2 * chunks ? (int)piece : 0;
 }
 
 }  // namespace
@@ -74,6 +95,10 @@ GdLayout gdelta_layout(const gdelta_desc *d, bool packed)
     l.vectors = 9 * TOKENS * 4;
     l.state = (long long)l.KP * l.VP * 4;
     l.rows = TOKENS * l.VP * 4;
+    l.piece = d->T == 0 ? 0 : piece_of(d, l.VP);
+    l.map = (long long)l.KP * l.KP * 4;
+    const long long unit = l.piece * TOKENS;
+    l.pieces = !l.piece ? 0 : packed ? d->T / unit + d->sequences : d->sequences * ((length + unit - 1) / unit);
     return l;
 }
 
@@ -87,20 +112,21 @@ size_t gdelta_kept_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
     const GdLayout l = gdelta_layout(desc, true);
-    return first_pass_bytes(desc, l) + (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows);
+    return forward_bytes(desc, l) + (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows);
 }
 
 size_t gdelta_fwd_workspace_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
-    return first_pass_bytes(desc, gdelta_layout(desc, true));
+    return forward_bytes(desc, gdelta_layout(desc, true));
 }
 
 size_t gdelta_bwd_workspace_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
     const GdLayout l = gdelta_layout(desc, true);
-    return (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows) + round16((size_t)l.chunks * desc->H * 2 * sizeof(float));
+    return (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows) + (size_t)l.pieces * desc->H * (size_t)l.state +
+           round16((size_t)l.chunks * desc->H * 2 * sizeof(float));
 }
 
 static int check_tensors(const gdelta_desc *d, const gdelta_tensors *t, std::initializer_list<const void *> stored, std::initializer_list<const void *> others)
@@ -130,9 +156,9 @@ int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
         if (unaligned16(t->kept)) return DWCONV_ERR_ALIGN;
         place_kept(desc, most, t->kept, &s);
     } else if (most.chunks) {
-        if (!workspace || workspace_bytes < first_pass_bytes(desc, most)) return DWCONV_ERR_WORKSPACE;
+        if (!workspace || workspace_bytes < forward_bytes(desc, most)) return DWCONV_ERR_WORKSPACE;
         if (unaligned16(workspace)) return DWCONV_ERR_ALIGN;
-        place_first_pass(desc, most, (char *)workspace, &s);
+        place_forward(desc, most, (char *)workspace, &s);
     }
     if (desc->T == 0 && !t->final) return DWCONV_OK;
     const GdArgs g = args_of(desc, t);
@@ -160,7 +186,8 @@ int gdelta_bwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
     place_kept(desc, most, t->kept, &s);
     s.dS = (float *)workspace;
     s.X = (float *)((char *)workspace + most.chunks * desc->H * most.state);
-    s.partials = (float *)((char *)s.X + most.chunks * desc->H * most.rows);
+    s.ends = (float *)((char *)s.X + most.chunks * desc->H * most.rows);
+    s.partials = (float *)((char *)s.ends + most.pieces * desc->H * most.state);
     const GdArgs g = args_of(desc, t);
     hipError_t e = hipSuccess;
     if (desc->T > 0) {

@@ -3,6 +3,7 @@
 // As the walk forward (gdelta_fwd.hip), with dS the gradient of the state behind a chunk:
 //   dU = P^T dY + (exp(G_end - G) * K) dS,  X = T^T dU,  dV = beta * X
 //   dS = exp(G_end) dS + (scale exp(G) * Q)^T dY - (exp(G) * K)^T dV
+// MAP: what a piece of a sequence makes of a gradient of zero (gdelta_launch.hpp); the map's matrix is the forward one's, transposed.
 // X and the dS behind the chunk are what the gradients of keys, queries and gates take (gdelta_bwd_rows.hip), for all chunks at once.
 #include "gdelta_states.hpp"
 
@@ -10,8 +11,8 @@ namespace dwc {
 
 namespace {
 
-template <typename T, int KP, int NT, bool SHARE, bool WHOLE>
-__global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, unsigned first,
+template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
+__global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, unsigned first,
                                                                   int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
@@ -21,17 +22,22 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
     float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
     const unsigned bid = first + blockIdx.x;
-    const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const int id = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const Stretch at_ = stretch_of(g, l, id);
+    const int start = at_.start, end = at_.end, base = at_.base, from = at_.from, last = at_.to - 1;
+    if (at_.place < 0 || (MAP && at_.place == 0)) return;       // (nothing comes before the first piece)
     const Columns<NT> cols((int)(bid % (unsigned)blocks));
-    const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
-    const int chunks = (int)min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const yp = dy + (long long)h * g.V;
 
     v4f_t S[KP / 16][NT];
+    const long long piece = (long long)id * g.H + h;
+    if (!MAP && at_.place < at_.pieces - 1) load_state<NT, KP / 16>(S, s.ends + piece * (l.state / 4), KP, l.VP, cols);
+    else {
 #pragma unroll
-    for (int ct = 0; ct < KP / 16; ++ct)
+        for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+    }
 
     Rows<T, KP, THREADS, WHOLE> rows;
     Matrix<INNER, THREADS> matrix, second;
@@ -43,28 +49,29 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
         rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
         matrix.load(s.T + where * l.matrix);
         second.load(s.P + where * l.matrix);
+        const int y_stride = fresh((int)g.y_stride);
         const BufView view = rows_view(yp + at * g.y_stride, g.y_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(o[mt][r], view, cols.at(row_of(mt, r), (int)g.y_stride, (int)sizeof(T)), g.V);
+            for (int r = 0; r < 4; ++r) cols.load(o[mt][r], view, cols.at(row_of(mt, r), y_stride, (int)sizeof(T)), g.V);
         const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
         vec_next = vec[threadIdx.x];
         decay_next = vec[VEC_ONE * 64];
     };
-    if (chunks > 0) load_keys(chunks - 1);
-    for (int c = chunks - 1; c >= 0; --c) {
+    if (from <= last) load_keys(last);
+    for (int c = last; c >= from; --c) {
         const int at = start + c * CHUNK, len = min(CHUNK, end - at);
         const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
-        if (SHARE && c < chunks - 1) __syncthreads();
+        if (SHARE && c < last) __syncthreads();
         rows.template put<LD>(kt);
         matrix.put(tm);
         second.put(pm);
         vl[threadIdx.x] = vec_next;
         const float decay = decay_next;
         rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
-        store_tiles<NT, KP / 16>(S, s.dS + where * (l.state / 4), l.VP, cols);
+        if (!MAP) store_tiles<NT, KP / 16>(S, s.dS + where * (l.state / 4), l.VP, cols);
         __syncthreads();
         // dU
         v4f_t U[4][NT];
@@ -123,7 +130,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(X[mt][nt], a, f[ks][nt]);
             }
         }
-        store_tiles<NT, 4>(X, s.X + where * (l.rows / 4), l.VP, cols);
+        if (!MAP) store_tiles<NT, 4>(X, s.X + where * (l.rows / 4), l.VP, cols);
+        const int v_stride = fresh((int)g.v_stride);
         const BufView out = rows_view(dv + at * g.v_stride + (long long)h * g.V, g.v_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
@@ -131,11 +139,11 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) X[mt][nt] = times(X[mt][nt], beta);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+            for (int r = 0; r < (MAP ? 0 : 4); ++r) {
                 float x[NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[nt] = X[mt][nt][r];
-                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), (int)g.v_stride, (int)sizeof(T)), g.V, x);
+                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), v_stride, (int)sizeof(T)), g.V, x);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) X[mt][nt] = -times(X[mt][nt], read);
@@ -163,7 +171,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
         split_rows<INNER, NT>(X, f);
         if constexpr (SHARE) __syncthreads();
         rows.template put<LD>(qt);
-        if (c > 0) load_keys(c - 1);
+        if (c > from) load_keys(c - 1);
         __syncthreads();
 #pragma unroll
         for (int ct = 0; ct < KP / 16; ++ct)
@@ -175,31 +183,46 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_bwd_states(GdArgs g, GdLa
                 for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
             }
     }
+    if constexpr (MAP) store_tiles<NT, KP / 16>(S, s.ends + piece * (l.state / 4), l.VP, cols);
 }
 
-template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+template <typename T, int KP, int NT, bool MAP>
+hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
 {
     constexpr bool SHARE = shares<T, KP>();
     constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    const bool whole = whole_keys<T>(g) && pair_values<T>(g, dy, dv, g.y_stride, g.v_stride);
-    const auto kernel = whole ? k_gdelta_bwd_states<T, KP, NT, SHARE, true> : k_gdelta_bwd_states<T, KP, NT, SHARE, false>;
+    const bool whole = whole_keys<T>(g) && (NT == 1 || pair_values<T>(g, dy, dv, g.y_stride, g.v_stride));
+    const auto kernel = whole ? k_gdelta_bwd_states<T, KP, NT, SHARE, true, MAP> : k_gdelta_bwd_states<T, KP, NT, SHARE, false, MAP>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT);
-    return gd_launches((long long)g.sequences * blocks, THREADS, [&](unsigned first, unsigned now) {
+    return gd_launches((l.piece ? l.pieces : (long long)g.sequences) * blocks, THREADS, [&](unsigned first, unsigned now) {
         hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, (const T *)dy, (T *)dv, first, blocks);
     });
 }
 
-template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+// As the walk forward: where sequences go in pieces what they make of zero first, and the gradients that they begin with
+template <typename T, int KP> hipError_t walk(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
 {
-    const bool wide = two_tiles(g, l, sizeof(T) == 4);
+    if (l.piece) {
+        hipError_t e = launch<T, KP, 1, true>(g, l, s, dy, dv, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, true, stream);
+        if (e != hipSuccess) return e;
+    }
+    if constexpr (KP < 256) {
+        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false>(g, l, s, dy, dv, stream);
+    }
+    return launch<T, KP, 1, false>(g, l, s, dy, dv, stream);
+}
+
+template <typename T> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
+{
     switch (l.KP) {
-    case 32: return wide ? launch<T, 32, 2>(g, l, s, dy, dv, stream) : launch<T, 32, 1>(g, l, s, dy, dv, stream);
-    case 64: return wide ? launch<T, 64, 2>(g, l, s, dy, dv, stream) : launch<T, 64, 1>(g, l, s, dy, dv, stream);
-    case 128: return wide ? launch<T, 128, 2>(g, l, s, dy, dv, stream) : launch<T, 128, 1>(g, l, s, dy, dv, stream);
-    default: return launch<T, 256, 1>(g, l, s, dy, dv, stream);
+    case 32: return walk<T, 32>(g, l, s, dy, dv, stream);
+    case 64: return walk<T, 64>(g, l, s, dy, dv, stream);
+    case 128: return walk<T, 128>(g, l, s, dy, dv, stream);
+    default: return walk<T, 256>(g, l, s, dy, dv, stream);
     }
 }
 
@@ -207,7 +230,7 @@ template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, c
 
 hipError_t launch_gdelta_bwd_states(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
 {
-    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, dy, dv, stream) : launch_of<bf16_t>(g, l, s, dy, dv, stream);
+    return dtype == DWCONV_F32 ? walk_of<float>(g, l, s, dy, dv, stream) : walk_of<bf16_t>(g, l, s, dy, dv, stream);
 }
 
 }  // namespace dwc

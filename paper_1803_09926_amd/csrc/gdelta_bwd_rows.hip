@@ -59,7 +59,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
     const int wv = wave_number(), mt = wv & 3, half = wv >> 2, col0 = half * C::KW;
     const bool does_f = HALVES == 1 || half == 0, does_m = HALVES == 1 || half == 1;
-    const ChunkAt at = gd_chunk(g, (int)id);
+    const ChunkAt at = gd_chunk(g, (int)id, CHUNK);
     if (at.len == 0) {
         for (int i = threadIdx.x; i < 2 * share; i += THREADS) s.partials[(long long)id * 2 * g.H + i / share * g.H + kh * share + i % share] = 0.f;
         return;

@@ -5,14 +5,17 @@
 //   U = T (beta * (V - exp(G) * K S)),  Y = scale exp(G) * Q S + P U,  S = exp(G_end) S + (exp(G_end - G) * K)^T U
 // all as products on the matrix cores: S, V, U and Y never leave the registers, as a result tile is an operand as it lies; K, Q, T and P go through LDS, and the next ones
 // are on their way from memory meanwhile.
+//
+// MAP: the map of a piece of a sequence instead (gdelta_launch.hpp).  What it makes of zero (of the state that the sequence begins with, in the first piece) is the walk without
+// answers, and its matrix is what the walk without values makes of the K unit vectors: K columns more.
 #include "gdelta_states.hpp"
 
 namespace dwc {
 
 namespace {
 
-template <typename T, int KP, int NT, bool SHARE, bool WHOLE>
-__global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
+template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
+__global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
                                                            float *__restrict__ final, unsigned first, int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
@@ -22,20 +25,28 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
     float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
     const unsigned bid = first + blockIdx.x;
-    const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
-    const Columns<NT> cols((int)(bid % (unsigned)blocks));
-    const int start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq);
-    const int chunks = (int)min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - base);
+    const int id = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const Stretch at_ = stretch_of(g, l, id);
+    const int seq = at_.seq, start = at_.start, end = at_.end, base = at_.base, chunks = at_.to;
+    // the last piece's map is not asked for, nor the first one's matrix
+    const int values = cdiv(l.VP, WAVES * 16 * NT);
+    const bool unit = MAP && (int)(bid % (unsigned)blocks) >= values;
+    if (at_.place < 0 || (MAP && (at_.place == at_.pieces - 1 || (unit && at_.place == 0)))) return;
+    const Columns<NT> cols((int)(bid % (unsigned)blocks) - (unit ? values : 0));
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const vp = (const T *)g.v + (long long)h * g.V;
 
     v4f_t S[KP / 16][NT];
     const long long state = ((long long)seq * g.H + h) * g.K * g.V;
-    if (init) load_state<NT, KP / 16>(S, init + state, g.K, g.V, cols);
+    const bool begins = at_.place == 0;
+    if (!MAP && !begins) load_state<NT, KP / 16>(S, s.ends + ((long long)id * g.H + h) * (l.state / 4), KP, l.VP, cols);
+    else if (init && begins) load_state<NT, KP / 16>(S, init + state, g.K, g.V, cols);
     else {
 #pragma unroll
         for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[ct][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[ct][nt][r] = unit && row_of(ct, r) == cols.c + nt ? 1.f : 0.f;
     }
     Frag Sp[KP / 32][NT][INNER];
     auto split_state = [&] {
@@ -51,36 +62,47 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
     Ahead<T, NT, WHOLE> v[4][4];
     float vec_next, decay_next;
     int bad_next;
-    auto load_keys = [&](int c) {
+    auto load_next = [&](int c) {
         const int at = start + c * CHUNK, len = min(CHUNK, end - at);
         const long long where = ((long long)base + c) * g.H + h;
         rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
         matrix.load(s.T + where * l.matrix);
-        const BufView view = rows_view(vp + at * g.v_stride, g.v_stride, len, g.V);
-#pragma unroll
-        for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(v[mt][r], view, cols.at(row_of(mt, r), (int)g.v_stride, (int)sizeof(T)), g.V);
         const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
         vec_next = vec[threadIdx.x];
         decay_next = vec[VEC_ONE * 64];
         bad_next = reinterpret_cast<const int *>(vec + VEC_ONE * 64)[1];
     };
-    if (chunks > 0) load_keys(0);
-    for (int c = 0; c < chunks; ++c) {
+    auto load_values = [&](int c) {
+        const int at = start + c * CHUNK, len = min(CHUNK, end - at);
+        const int v_stride = fresh((int)g.v_stride);
+        const BufView view = rows_view(vp + at * g.v_stride, g.v_stride, len, g.V);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) cols.load(v[mt][r], view, cols.at(row_of(mt, r), v_stride, (int)sizeof(T)), unit ? 0 : g.V);
+    };
+    if (at_.from < chunks) {
+        load_next(at_.from);
+        load_values(at_.from);
+    }
+    for (int c = at_.from; c < chunks; ++c) {
         const int at = start + c * CHUNK, len = min(CHUNK, end - at);
         const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
-        if (SHARE && c) __syncthreads();
+        if ((SHARE || MAP) && c > at_.from) __syncthreads();
         rows.template put<LD>(kt);
         matrix.put(tm);
         vl[threadIdx.x] = vec_next;
         const float decay = decay_next;
         const int bad = bad_next;
-        rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
-        matrix.load(s.P + where * l.matrix);
+        if constexpr (MAP) {
+            if (c + 1 < chunks) load_next(c + 1);
+        } else {
+            rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
+            matrix.load(s.P + where * l.matrix);
+        }
         __syncthreads();
-        if (s.S) store_tiles<NT, KP / 16>(S, s.S + where * (l.state / 4), l.VP, cols);
+        if (!MAP && s.S) store_tiles<NT, KP / 16>(S, s.S + where * (l.state / 4), l.VP, cols);
         // What is not finite in v, or the first key or gate that is not: from there on the column is, and before it nothing is of it.
         float probe = 0.f;
 #pragma unroll
@@ -153,7 +175,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                 for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(U[mt][nt], a, f[ks][nt]);
             }
         }
-        if (s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
+        if (!MAP && s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
         v4f_t w[4][NT];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
@@ -174,37 +196,44 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                 for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
             }
         }
-        if constexpr (SHARE) __syncthreads();
-        rows.template put<LD>(qt);
-        matrix.put(pm);
-        if (c + 1 < chunks) load_keys(c + 1);
-        __syncthreads();
-        split_rows<INNER, NT>(U, f);
         v4f_t O[4][NT];
+        if constexpr (MAP) {
+            if (c + 1 < chunks) load_values(c + 1);
+        } else {
+            if constexpr (SHARE) __syncthreads();
+            rows.template put<LD>(qt);
+            matrix.put(pm);
+            if (c + 1 < chunks) {
+                load_next(c + 1);
+                load_values(c + 1);
+            }
+            __syncthreads();
+            split_rows<INNER, NT>(U, f);
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt)
+            for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+                for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c0 = 0; c0 < KP / 32; ++c0)
+            for (int c0 = 0; c0 < KP / 32; ++c0)
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+                    Frag a[RAW];
+                    frags_rows<RAW, LD>(a, qt, PLANE, mt * 16, c0 * 32);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(O[mt][nt], a, Sp[c0][nt]);
+                }
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
-                Frag a[RAW];
-                frags_rows<RAW, LD>(a, qt, PLANE, mt * 16, c0 * 32);
+                const float4 ask = four(vl + VEC_ASK * 64, mt);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(O[mt][nt], a, Sp[c0][nt]);
-            }
+                for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
-            const float4 ask = four(vl + VEC_ASK * 64, mt);
+                for (int ks = 0; ks <= mt / 2; ++ks) {
+                    Frag a[INNER];
+                    frags_rows<INNER, CHUNK>(a, pm, PLANE_M, mt * 16, ks * 32);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
-#pragma unroll
-            for (int ks = 0; ks <= mt / 2; ++ks) {
-                Frag a[INNER];
-                frags_rows<INNER, CHUNK>(a, pm, PLANE_M, mt * 16, ks * 32);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(O[mt][nt], a, f[ks][nt]);
+                    for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(O[mt][nt], a, f[ks][nt]);
+                }
             }
         }
         if (odd) {
@@ -215,50 +244,72 @@ __global__ __launch_bounds__(THREADS, 1) void k_gdelta_fwd(GdArgs g, GdLayout l,
                 for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (row_of(mt, r) >= from[nt]) O[mt][nt][r] = nan;
+                        if (!MAP && row_of(mt, r) >= from[nt]) O[mt][nt][r] = nan;
 #pragma unroll
                 for (int ct = 0; ct < KP / 16; ++ct)
                     if (from[nt] < CHUNK) S[ct][nt] = v4f_t{nan, nan, nan, nan};
             }
         }
-        const BufView out = rows_view(y + at * g.y_stride + (long long)h * g.V, g.y_stride, len, g.V);
+        if constexpr (!MAP) {
+            const int y_stride = fresh((int)g.y_stride);
+            const BufView out = rows_view(y + at * g.y_stride + (long long)h * g.V, g.y_stride, len, g.V);
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt)
+            for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x[NT];
+                for (int r = 0; r < 4; ++r) {
+                    float x[NT];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) x[nt] = O[mt][nt][r];
-                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), (int)g.y_stride, (int)sizeof(T)), g.V, x);
-            }
+                    for (int nt = 0; nt < NT; ++nt) x[nt] = O[mt][nt][r];
+                    cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), y_stride, (int)sizeof(T)), g.V, x);
+                }
+        }
         split_state();
     }
-    if (final) store_state<NT, KP / 16>(S, final + state, g.K, g.V, cols);
+    if constexpr (MAP) {
+        const long long where = (long long)id * g.H + h;
+        if (unit) store_tiles<NT, KP / 16>(S, s.maps + where * (l.map / 4), KP, cols);
+        else store_tiles<NT, KP / 16>(S, s.ends + where * (l.state / 4), l.VP, cols);
+    } else if (final && at_.place == at_.pieces - 1) store_state<NT, KP / 16>(S, final + state, g.K, g.V, cols);
 }
 
-template <typename T, int KP, int NT> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+template <typename T, int KP, int NT, bool MAP>
+hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
     constexpr bool SHARE = shares<T, KP>();
     constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    const bool whole = whole_keys<T>(g) && pair_values<T>(g, g.v, y, g.v_stride, g.y_stride);
-    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, SHARE, true> : k_gdelta_fwd<T, KP, NT, SHARE, false>;
+    const bool whole = whole_keys<T>(g) && (NT == 1 || pair_values<T>(g, g.v, y, g.v_stride, g.y_stride));
+    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, SHARE, true, MAP> : k_gdelta_fwd<T, KP, NT, SHARE, false, MAP>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
-    const int blocks = cdiv(l.VP, WAVES * 16 * NT);
-    return gd_launches((long long)g.sequences * blocks, THREADS, [&](unsigned first, unsigned now) {
+    const int blocks = cdiv(l.VP, WAVES * 16 * NT) + (MAP ? cdiv(KP, WAVES * 16 * NT) : 0);
+    return gd_launches((l.piece ? l.pieces : (long long)g.sequences) * blocks, THREADS, [&](unsigned first, unsigned now) {
         hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, init, (T *)y, final, first, blocks);
     });
 }
 
-template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+// The walk; where sequences go in pieces their maps first, and the states that they begin with
+template <typename T, int KP>
+hipError_t walk(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    const bool wide = two_tiles(g, l, sizeof(T) == 4);
+    if (l.piece) {
+        hipError_t e = launch<T, KP, 1, true>(g, l, s, init, y, final, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, false, stream);
+        if (e != hipSuccess) return e;
+    }
+    if constexpr (KP < 256) {
+        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false>(g, l, s, init, y, final, stream);
+    }
+    return launch<T, KP, 1, false>(g, l, s, init, y, final, stream);
+}
+
+template <typename T> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+{
     switch (l.KP) {
-    case 32: return wide ? launch<T, 32, 2>(g, l, s, init, y, final, stream) : launch<T, 32, 1>(g, l, s, init, y, final, stream);
-    case 64: return wide ? launch<T, 64, 2>(g, l, s, init, y, final, stream) : launch<T, 64, 1>(g, l, s, init, y, final, stream);
-    case 128: return wide ? launch<T, 128, 2>(g, l, s, init, y, final, stream) : launch<T, 128, 1>(g, l, s, init, y, final, stream);
-    default: return launch<T, 256, 1>(g, l, s, init, y, final, stream);
+    case 32: return walk<T, 32>(g, l, s, init, y, final, stream);
+    case 64: return walk<T, 64>(g, l, s, init, y, final, stream);
+    case 128: return walk<T, 128>(g, l, s, init, y, final, stream);
+    default: return walk<T, 256>(g, l, s, init, y, final, stream);
     }
 }
 
@@ -266,7 +317,7 @@ template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, c
 
 hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, init, y, final, stream) : launch_of<bf16_t>(g, l, s, init, y, final, stream);
+    return dtype == DWCONV_F32 ? walk_of<float>(g, l, s, init, y, final, stream) : walk_of<bf16_t>(g, l, s, init, y, final, stream);
 }
 
 }  // namespace dwc

@@ -21,6 +21,35 @@ template <typename T, int KP> struct Prep {
     static constexpr size_t LDS = TILE + 2 * F32S + 64 * 8 + 5 * 64 * 4;
 };
 
+// the sum over N neighbouring lanes, 4 to 32, in every one of them
+template <int N> __device__ __forceinline__ float group_sum(float v)
+{
+    v += lane_move<DPP_XOR1>(v);
+    v += lane_move<DPP_XOR2>(v);
+    if constexpr (N >= 8) v += lane_move<DPP_HALF_MIRROR>(v);
+    if constexpr (N >= 16) v += lane_move<DPP_MIRROR>(v);
+    if constexpr (N >= 32) v = rows_join(v, v);
+    return v;
+}
+// the sum of a number over the lanes up to one's own, in 64 bits
+template <int CTRL, int ROWS> __device__ __forceinline__ double lane_move64(double v)
+{
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sum_up_to(float x)
+{
+    double v = x;
+    v += lane_move64<0x111, 0xf>(v);              // from 1, 2, 4 and 8 lanes to the left in a row of 16,
+    v += lane_move64<0x112, 0xf>(v);
+    v += lane_move64<0x114, 0xf>(v);
+    v += lane_move64<0x118, 0xf>(v);
+    v += lane_move64<0x142, 0xa>(v);              // the row before's last lane to the second and fourth row,
+    return v + lane_move64<0x143, 0xc>(v);        // the second row's to the upper half
+}
+
 // the parts of an fp32 matrix in LDS, into memory
 template <int N> __device__ __forceinline__ void put_matrix(const float *f, char *to)
 {
@@ -39,7 +68,7 @@ template <int N> __device__ __forceinline__ void put_matrix(const float *f, char
     }
 }
 
-template <typename T, int KP>
+template <typename T, int KP, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restrict__ t_out, char *__restrict__ p_out, char *__restrict__ vec_out, long long matrix,
                                                          long long vectors, unsigned first)
 {
@@ -52,84 +81,73 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
     float *const betas = reinterpret_cast<float *>(Gs + 64), *const rks = betas + 64, *const rqs = rks + 64;
     int *const bads = reinterpret_cast<int *>(rqs + 64);          // [64] tokens whose key is not finite
     const unsigned id = first + blockIdx.x;
-    const ChunkAt at = gd_chunk(g, (int)id);
+    const ChunkAt at = gd_chunk(g, (int)id, CHUNK);
     if (at.len == 0) return;
     const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, wv = wave_number(), m = lane & 15, q4 = lane >> 4;
 
-    // keys into LDS; a token's key that is not finite counts as none, and the token is remembered
-    if (threadIdx.x < 64) bads[threadIdx.x] = 0;
-    __syncthreads();
+    // all that comes from memory is asked for at once: keys, queries (each wavefront its 16 rows, in the order of the operands), the first head's gates
+    constexpr int PER_ROW = KP / 8, NROWS = CHUNK * PER_ROW / THREADS;
+    Rows<T, KP, THREADS, WHOLE> rows;
+    rows.load((const T *)g.k + at.first * g.k_stride + (long long)kh * g.K, g.k_stride, at.len, g.K);
+    Ahead<T, 4, WHOLE> qs[KP / 32][2];
     {
-        const T *const p = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K;
-        constexpr int PER_ROW = KP / 8;
-        for (int i = threadIdx.x; i < CHUNK * PER_ROW; i += THREADS) {
-            const int row = i / PER_ROW, col = i % PER_ROW * 8;
-            Some<T, 8> v;
-            v.load(p + row * g.k_stride + col, row < at.len ? g.K - col : 0);
-            bool bad = false;
+        const BufView view = rows_view((const T *)g.q + at.first * g.q_stride + (long long)kh * g.K, g.q_stride, at.len, g.K);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bad |= !finite(v.at(j));
-            if (bad) bads[row] = 1;
-            float x[8];
-            v.get(x);
-            put8<RAW, LD>(kt, PLANE, row, col, x);
-        }
-    }
-    __syncthreads();
-    // lengths: four lanes a key
-    {
-        const int row = threadIdx.x / 4;
-        const bool bad = bads[row] != 0;
-        float s = 0.f;
-        for (int c = threadIdx.x % 4 * 8; c < KP; c += 32) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float v = 0.f;
-#pragma unroll
-                for (int i = RAW - 1; i >= 0; --i) v += bf16_to_f32(kt[i * PLANE + row * LD + c + j]);
-                s += v * v;
-                if (bad) {
-#pragma unroll
-                    for (int i = 0; i < RAW; ++i) kt[i * PLANE + row * LD + c + j] = 0;
-                }
-            }
-        }
-        s += lane_move<DPP_XOR1>(s);
-        s += lane_move<DPP_XOR2>(s);
-        if (threadIdx.x % 4 == 0) {
-            const float rk = row >= at.len || bad ? 0.f : g.norm ? 1.f / sqrtf(s + g.eps) : 1.f;
-            if (!finite(rk)) bads[row] = 1;              // (a key of length zero without eps)
-            rks[row] = finite(rk) ? rk : 0.f;
-        }
-    }
-    // queries: each wavefront its 16 rows, straight from memory in the order of the operands
-    Frag qa[KP / 32][RAW];
-    {
-        const int row = wv * 16 + m;
-        const T *const p = (const T *)g.q + (at.first + row) * g.q_stride + (long long)kh * g.K;
-        float s = 0.f;
-#pragma unroll
-        for (int c = 0; c < KP / 32; ++c) {
-            Some<T, 4> v[2];
-            float x[8];
+        for (int c = 0; c < KP / 32; ++c)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int col = c * 32 + i * 16 + q4 * 4;
-                v[i].load(p + col, row < at.len ? g.K - col : 0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[4 * i + j] = v[i].at(j);
-                    s += x[4 * i + j] * x[4 * i + j];
-                }
+                qs[c][i].load(view, (uint32_t)((wv * 16 + m) * (int)g.q_stride + col) * (uint32_t)sizeof(T), g.K - col);
             }
+    }
+    const bool here = lane < at.len;
+    float gate_a, gate_b;
+    auto ask_gates = [&](int h) {
+        gate_a = here ? ldf((const T *)g.a + (at.first + lane) * g.a_stride + h) : 0.f;
+        gate_b = here ? ldf((const T *)g.b + (at.first + lane) * g.b_stride + h) : 0.f;
+    };
+    ask_gates(kh * share);
+    // keys into LDS, and their lengths; a key that is not finite counts as none, and its token is remembered
+#pragma unroll
+    for (int i = 0; i < NROWS; ++i) {
+        const int n = threadIdx.x + i * THREADS, row = n / PER_ROW, col = n % PER_ROW * 8;
+        float x[8], s = 0.f, probe = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = rows.v[i].at(j);
+            s += x[j] * x[j];
+            probe = fmaf(x[j], 0.f, probe);
+        }
+        s = group_sum<PER_ROW>(s);
+        const bool bad = !(group_sum<PER_ROW>(probe) == 0.f);
+        const float rk = row >= at.len || bad ? 0.f : g.norm ? 1.f / sqrtf(s + g.eps) : 1.f;
+        if (n % PER_ROW == 0) {
+            bads[row] = bad || !finite(rk);              // (or a key of length zero without eps)
+            rks[row] = finite(rk) ? rk : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = bad ? 0.f : x[j];
+        put8<RAW, LD>(kt, PLANE, row, col, x);
+    }
+    Frag qa[KP / 32][RAW];
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < KP / 32; ++c) {
             uint32_t w[4][RAW];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) split2<RAW>(x[2 * i], x[2 * i + 1], w[i]);
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s += qs[c][i].at(j) * qs[c][i].at(j);
+                split2<RAW>(qs[c][i].at(0), qs[c][i].at(1), w[2 * i]);
+                split2<RAW>(qs[c][i].at(2), qs[c][i].at(3), w[2 * i + 1]);
+            }
 #pragma unroll
             for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
         }
         s = rows_join(s, s);
         s = halves_join(s, s);
+        const int row = wv * 16 + m;
         if (q4 == 0) rqs[row] = row >= at.len ? 0.f : g.norm ? 1.f / sqrtf(s + g.eps) : 1.f;
     }
     __syncthreads();
@@ -153,21 +171,16 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
         const long long where = (long long)id * g.H + h;
         float *const vec = reinterpret_cast<float *>(vec_out + where * vectors);
         // gates, by each wavefront: a lane a token
-        const bool here = lane < at.len;
         float d = 0.f, beta = 0.f;
         if (here) {
-            d = gd_log_decay(g, gd_raw(g, ldf((const T *)g.a + (at.first + lane) * g.a_stride + h), h), h);
-            beta = gd_rate(g, ldf((const T *)g.b + (at.first + lane) * g.b_stride + h));
+            d = gd_log_decay(g, gd_raw(g, gate_a, h), h);
+            beta = gd_rate(g, gate_b);
         }
         const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
         const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
         if (lane >= bad_from) d = beta = 0.f;
-        double G = d;
-#pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const double up = __shfl_up(G, off, 64);
-            if (lane >= off) G += up;
-        }
+        const double G = sum_up_to(d);
+        if (hh + 1 < share) ask_gates(h + 1);
         const double end = __shfl(G, 63, 64);
         __syncthreads();                                 // the head before has been read
         if (wv == 0) {
@@ -204,7 +217,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = wv * 16 + 4 * q4 + r;
-                    const float e = i >= j ? expf((float)(gi[r] - gj)) * kj : 0.f;
+                    const float e = i >= j ? exp2_fast((float)(gi[r] - gj) * LOG2E) * kj : 0.f;
                     pv[n][r] = i >= j ? qi[r] * e * qk[n][r] : 0.f;
                     L[i * LDF + j] = i > j ? bi[r] * ki[r] * e * kk[n][r] : 0.f;
                 }
@@ -280,7 +293,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
 
 template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
 {
-    const auto kernel = k_gdelta_prep<T, KP>;
+    const auto kernel = whole_keys<T>(g) ? k_gdelta_prep<T, KP, true> : k_gdelta_prep<T, KP, false>;
     constexpr size_t lds = Prep<T, KP>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const hipError_t e = gd_lds(kernel, lds);

@@ -9,6 +9,13 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 
+// A uniform number that the compiler takes for a new one each time: what is formed with it is formed where it is used, and does not occupy registers over the whole walk
+__device__ __forceinline__ int fresh(int v)
+{
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
 // The columns of a lane: NT neighbours, one in each of its NT result tiles, so that its numbers of a row lie beside each other.  PAIRS: they are read and written
 // at once, aligned.  What is not there is asked for, and stored, outside the view: no branch.
 template <int NT> struct Columns {
@@ -60,6 +67,7 @@ template <int NT, int CT> __device__ __forceinline__ void store_state(const v4f_
 template <int NT, int MT> __device__ __forceinline__ void store_tiles(const v4f_t (&x)[MT][NT], float *p, int VP, const Columns<NT> &cols)
 {
     const BufView view(p, (uint32_t)(MT * 16 * VP) * 4u);
+    VP = fresh(VP);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -88,10 +96,40 @@ template <typename T, int KP, bool SHARE> struct Walk {
 // Whether the tiles of keys and queries share their place in LDS: where both do not fit
 template <typename T, int KP> constexpr bool shares() { return Walk<T, KP, false>::LDS > 160 * 1024; }
 
+// Which chunks a block of a walk has: those of a sequence, or of one of its pieces
+struct Stretch { int seq, start, end, base, from, to, place, pieces; };       // chunks from .. to - 1 of the sequence's; the piece's number, and how many there are
+__device__ __forceinline__ Stretch stretch_of(const GdArgs &g, const GdLayout &l, int id)
+{
+    Stretch s;
+    s.seq = id;
+    s.place = 0;
+    s.pieces = 1;
+    if (l.piece) {
+        const ChunkAt at = gd_chunk(g, id, l.piece * CHUNK);
+        s.seq = at.seq;
+        s.place = at.place;
+    }
+    s.start = gd_start(g, s.seq);
+    s.end = gd_start(g, s.seq + 1);
+    s.base = gd_base(g, s.seq, CHUNK);
+    const long long chunks = min((long long)(s.end > s.start ? cdiv(s.end - s.start, CHUNK) : 0), l.chunks - s.base);
+    s.from = 0;
+    s.to = (int)chunks;
+    if (l.piece) {
+        s.pieces = chunks > 0 ? cdiv((int)chunks, l.piece) : 1;
+        if (s.place < 0 || s.place >= s.pieces) s.place = s.pieces = -1;       // nothing here
+        else {
+            s.from = s.place * l.piece;
+            s.to = min(s.to, s.from + l.piece);
+        }
+    }
+    return s;
+}
+
 // Whether a wavefront has 32 columns instead of 16: twice the products of what is read from LDS, where that still fills the card
 inline bool two_tiles(const GdArgs &g, const GdLayout &l, bool f32)
 {
-    return l.VP > 64 && (l.KP < 128 || !f32) && (long long)g.sequences * g.H * cdiv(l.VP, 128) >= 256;
+    return l.VP > 64 && (l.KP < 128 || !f32) && !l.piece && (long long)g.sequences * g.H * cdiv(l.VP, 128) >= 256;
 }
 
 // Whether two columns of the values are whole and aligned

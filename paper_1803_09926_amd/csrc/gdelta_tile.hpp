@@ -250,23 +250,27 @@ __device__ __forceinline__ int gd_start(const GdArgs &g, int s)
     const int v = g.starts[s];
     return v < 0 ? 0 : v > g.T ? g.T : v;
 }
-__device__ __forceinline__ int gd_base(const GdArgs &g, int s)
+// The same holds for pieces of several chunks: unit is 64, or the tokens of a piece
+__device__ __forceinline__ int gd_base(const GdArgs &g, int s, int unit)
 {
-    return g.starts ? gd_start(g, s) / CHUNK + s : s * cdiv(g.length > 0 ? g.length : 1, CHUNK);
+    return g.starts ? gd_start(g, s) / unit + s : s * cdiv(g.length > 0 ? g.length : 1, unit);
 }
-__device__ __forceinline__ ChunkAt gd_chunk(const GdArgs &g, int id)
+// (id is the same in a wavefront's 64 lanes, all of which are here: one load for 64 sequences, two for 4096)
+__device__ __forceinline__ ChunkAt gd_chunk(const GdArgs &g, int id, int unit)
 {
     int lo = 0, hi = g.sequences;
-    if (!g.starts) lo = min(id / cdiv(g.length > 0 ? g.length : 1, CHUNK), g.sequences - 1);
+    if (!g.starts) lo = min(id / cdiv(g.length > 0 ? g.length : 1, unit), g.sequences - 1);
     else while (hi - lo > 1) {
-        const int mid = lo + (hi - lo) / 2;
-        if (gd_base(g, mid) <= id) lo = mid;
-        else hi = mid;
+        const int step = (hi - lo + 63) / 64;
+        const long long at = lo + (long long)step * ((threadIdx.x & 63) + 1);
+        lo += step * __popcll(__ballot(at < hi && gd_base(g, at < hi ? (int)at : lo, unit) <= id));
+        hi = hi - lo > step ? lo + step : hi;
     }
-    const int place = id - gd_base(g, lo), start = gd_start(g, lo), end = gd_start(g, lo + 1);
-    const long long first = start + (long long)place * CHUNK;
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int place = id - gd_base(g, lo, unit), start = gd_start(g, lo), end = gd_start(g, lo + 1);
+    const long long first = start + (long long)place * unit;
     if (place < 0 || first >= end) return {0, 0, lo, place};
-    return {(int)first, (int)min((long long)CHUNK, end - first), lo, place};
+    return {(int)first, (int)min((long long)unit, end - first), lo, place};
 }
 
 }  // namespace

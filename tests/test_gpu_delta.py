@@ -6,6 +6,8 @@ products hold all 24 bits of their factors but terms of 2^-24 (three of them of 
 fp32, whose roundings add up to sqrt(256) * 2^-24 = 1e-6 each where they do not all go one way; four chunks: 4 * 4 * 1e-6 = 1.6e-5, gradients as much again, as they
 go the way back over what the way forward left: 4e-5.  fp32 outputs of bf16 tensors: factors that the kernels compute are held to 2^-17 = 8e-6, four products a chunk over four chunks
 and back, of which again the square root adds up: sqrt(32) * 8e-6 = 4.5e-5, and the gradients of A are differences of terms some times their size: 2e-4."""
+import itertools
+
 import numpy as np
 import pytest
 import torch
@@ -130,6 +132,21 @@ def test_options(gpu_lib, dtype, options, params):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("piece", [1, 2, 3])
+@pytest.mark.parametrize("Hk,H,K,V,carry", [(1, 1, 24, 20, True), (1, 2, 64, 64, False), (2, 2, 100, 130, True), (1, 1, 256, 48, False)])
+def test_sequences_in_pieces(gpu_lib, dtype, piece, Hk, H, K, V, carry):
+    """Pieces of that many chunks: sequences of none, of one and of several, with whole last chunks and others.  (A state passes a product more a piece: the tolerances have
+    room for twice the chunks of these sequences.)"""
+    print("pieces", dtype, piece, Hk, H, K, V, carry, flush=True)
+    m = Made(K * 10 + piece, dtype)
+    x, par = host_inputs(m, 420, Hk, H, K, V, 0.3)
+    bounds = [0, 0, 250, 251, 251, 379, 420]
+    with dw.tuning_overrides({"DWCONV_TUNE_GDELTA_PIECE": piece}):
+        check(m, x, par, bounds, m.host((6, H, K, V), 0.3, stored=False) if carry else None)
+        check(m, x, par, [0, 210, 420], even=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_decays_of_any_size(gpu_lib, dtype):
     """From nothing forgotten to everything, beside each other in a chunk; what is clamped has no gradient."""
     m = Made(23, dtype)
@@ -207,8 +224,14 @@ def test_pieces_and_steps_continue_each_other(gpu_lib, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("name,value", [("v", np.nan), ("v", np.inf), ("k", np.nan), ("k", -np.inf), ("q", np.nan), ("a", np.nan), ("b", np.nan)])
-def test_what_is_not_finite_stays_behind(gpu_lib, dtype, name, value):
+@pytest.mark.parametrize("piece", [0, 1])
+def test_what_is_not_finite_stays_behind(gpu_lib, dtype, name, value, piece):
     """Tokens before it, other heads and other sequences: the same bits."""
+    with dw.tuning_overrides({"DWCONV_TUNE_GDELTA_PIECE": piece}):
+        _not_finite(dtype, name, value)
+
+
+def _not_finite(dtype, name, value):
     m = Made(41, dtype)
     T, t0, bounds = 200, 100, [0, 30, 170, 200]
     x, par = host_inputs(m, T, 2, 4, 40, 72)
@@ -351,18 +374,23 @@ def test_starts_that_are_no_starts(gpu_lib):
     m = Made(67, "bf16")
     T, guard = 200, 4096
     x, par = host_inputs(m, T, 2, 4, 32, 32)
-    for starts in ([5, 300, -7, 64, 2000000000, 0, 199, 200], [0, 0, 0, 0, 0, 0, 0, 0], [200, 150, 100, 50, 40, 30, 20, 10], [-2147483648] * 4 + [2147483647] * 4):
-        print("starts", starts, flush=True)
-        call = Call(m, x, par, RAGGED)
-        call.starts = _starts(starts)
-        space = torch.full((T * 128 + 2 * guard,), 7.0, device="cuda", dtype=torch.bfloat16)
-        y = space[guard:-guard].view(T, 128)
-        final = torch.full((7 * 4 * 32 * 32 + 2 * guard,), 7.0, device="cuda")
-        kept = _space(dw.gdelta_kept_bytes(call.d) + 2 * guard)
-        dw.gdelta_fwd(call.d, *(call.t[k] for k in NAMES), y, None, **call.par, starts=call.starts, kept=kept[guard:-guard],
-                      final=final[guard:-guard])
-        call.kept = kept[guard:-guard]
-        call.backward(m.host((T, 4, 32)))
-        torch.cuda.synchronize()
-        assert (space[:guard] == 7).all() and (space[-guard:] == 7).all() and (final[:guard] == 7).all() and (final[-guard:] == 7).all()
-        assert (kept[:guard] == 0xFF).all() and (kept[-guard:] == 0xFF).all()
+    for starts, piece in itertools.product(([5, 300, -7, 64, 2000000000, 0, 199, 200], [0, 0, 0, 0, 0, 0, 0, 0], [200, 150, 100, 50, 40, 30, 20, 10], [-2147483648] * 4 + [2147483647] * 4), (0, 1, 2)):
+        print("starts", starts, piece, flush=True)
+        with dw.tuning_overrides({"DWCONV_TUNE_GDELTA_PIECE": piece}):
+            _guarded(m, x, par, starts, T, guard)
+
+
+def _guarded(m, x, par, starts, T, guard):
+    call = Call(m, x, par, RAGGED)
+    call.starts = _starts(starts)
+    space = torch.full((T * 128 + 2 * guard,), 7.0, device="cuda", dtype=torch.bfloat16)
+    y = space[guard:-guard].view(T, 128)
+    final = torch.full((7 * 4 * 32 * 32 + 2 * guard,), 7.0, device="cuda")
+    kept = _space(dw.gdelta_kept_bytes(call.d) + 2 * guard)
+    dw.gdelta_fwd(call.d, *(call.t[k] for k in NAMES), y, None, **call.par, starts=call.starts, kept=kept[guard:-guard],
+                  final=final[guard:-guard])
+    call.kept = kept[guard:-guard]
+    call.backward(m.host((T, 4, 32)))
+    torch.cuda.synchronize()
+    assert (space[:guard] == 7).all() and (space[-guard:] == 7).all() and (final[:guard] == 7).all() and (final[-guard:] == 7).all()
+    assert (kept[:guard] == 0xFF).all() and (kept[-guard:] == 0xFF).all()
