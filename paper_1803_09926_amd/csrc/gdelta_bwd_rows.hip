@@ -40,8 +40,8 @@ __device__ __forceinline__ float row_sum(float v)
     return v + lane_move<DPP_MIRROR>(v);
 }
 
-template <typename T, int KP, bool WHOLE>
-__global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
+template <typename T, int KP, bool WHOLE, bool VALUES>
+__global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP <= 64 ? 2 : 1)) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
     typedef Back<T, KP> C;
@@ -56,7 +56,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     float *const wave_sums = dot_c + 2 * 64, *const vec = wave_sums + 8;
 
     const unsigned id = first + blockIdx.x;
-    const int kh = blockIdx.y, share = g.H / g.key_heads, lane = threadIdx.x & 63, m = lane & 15, q4 = lane >> 4;
+    const int kh = blockIdx.y, share = g.H / g.key_heads;
     const int wv = wave_number(), mt = wv & 3, half = wv >> 2, col0 = half * C::KW;
     const bool does_f = HALVES == 1 || half == 0, does_m = HALVES == 1 || half == 1;
     const ChunkAt at = gd_chunk(g, (int)id, CHUNK);
@@ -73,7 +73,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
     v4f_t qk[BOTH][4];
     {
         Frag qa[KP / 32][RAW];
-        const int row = mt * 16 + m;
+        const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4, row = mt * 16 + m;
 #pragma unroll
         for (int c = 0; c < KP / 32; ++c) {
             Some<T, 4> v[2];
@@ -98,9 +98,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
             for (int c = 0; c < KP / 32; ++c) {
                 Frag a[RAW], b[RAW];
-                frags_rows<RAW, LD>(b, tile, PLANE, n * 16, c * 32);
+                frags_rows<RAW, LD>(b, tile, PLANE, n * 16, c * 32, lane);
                 if (does_m) {
-                    frags_rows<RAW, LD>(a, tile, PLANE, mt * 16, c * 32);
+                    frags_rows<RAW, LD>(a, tile, PLANE, mt * 16, c * 32, lane);
                     mma<RAW, RAW>(qk[AT_M][n], a, b);
                 }
                 if (does_f) mma<RAW, RAW>(qk[0][n], qa[c], b);
@@ -121,11 +121,11 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
         // what the next 32 columns of V take, on its way: 8 numbers a lane of each
         constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
         const int vrow = threadIdx.x % 256 / (VB / 8), vcol = threadIdx.x % (VB / 8) * 8;
-        const bool takes_x = HALVES == 1 || threadIdx.x < 256, takes_u = HALVES == 1 || threadIdx.x >= 256;
-        u4t_t sa[PER][2], sb[PER][2], xa8[2], ua8[2];
-        Some<T, 8> v8, y8;
+        const bool takes_x = HALVES == 1 || wv < 4, takes_u = HALVES == 1 || wv >= 4;
+        u4t_t sa[PER][2], sb[PER][2], w8[BOTH][2];       // w8: X and U,
+        Ahead<T, 8, VALUES> t8[BOTH];                    // t8: V and dY, of both or one of each pair
         auto ask = [&](int v0) {
-            const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state), view_x(xp, (uint32_t)l.rows), view_u(up, (uint32_t)l.rows);
+            const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int n = threadIdx.x + i * THREADS;
@@ -137,14 +137,16 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             }
             const uint32_t off = (uint32_t)(vrow * l.VP + v0 + vcol) * 4u;
             if (takes_x) {
-                xa8[0] = view_x.b128(off, 0);
-                xa8[1] = view_x.b128(off + 16, 0);
-                v8.load(vp + vrow * g.v_stride + v0 + vcol, vrow < at.len ? g.V - v0 - vcol : 0);
+                const BufView view(xp, (uint32_t)l.rows), rows_v = rows_view(vp, g.v_stride, at.len, g.V);
+                w8[0][0] = view.b128(off, 0);
+                w8[0][1] = view.b128(off + 16, 0);
+                t8[0].load(rows_v, (uint32_t)(vrow * (int)g.v_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
             }
             if (takes_u) {
-                ua8[0] = view_u.b128(off, 0);
-                ua8[1] = view_u.b128(off + 16, 0);
-                y8.load(yp + vrow * g.y_stride + v0 + vcol, vrow < at.len ? g.V - v0 - vcol : 0);
+                const BufView view(up, (uint32_t)l.rows), rows_y = rows_view(yp, g.y_stride, at.len, g.V);
+                w8[AT_M][0] = view.b128(off, 0);
+                w8[AT_M][1] = view.b128(off + 16, 0);
+                t8[AT_M].load(rows_y, (uint32_t)(vrow * (int)g.y_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
             }
         };
         auto eight = [](const u4t_t (&w)[2], float (&x)[8]) {
@@ -158,7 +160,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
         for (int n = 0; n < 4; ++n) yu[0][n] = yu[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
         float gate_a = 0.f, gate_b = 0.f;                // of the token that a lane of the first wavefront has in the end
-        if (wv == 0 && lane < at.len) {
+        if (wv == 0 && (int)threadIdx.x < at.len) {
+            const int lane = threadIdx.x;
             gate_a = ldf((const T *)g.a + (at.first + lane) * g.a_stride + h);
             gate_b = ldf((const T *)g.b + (at.first + lane) * g.b_stride + h);
         }
@@ -188,36 +191,36 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             }
             if (takes_x) {
                 float x[8];
-                eight(xa8, x);
+                eight(w8[0], x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) xv_part += x[j] * v8.at(j);
+                for (int j = 0; j < 8; ++j) xv_part += x[j] * t8[0].at(j);
                 put8<INNER, LDV>(xt, PLANE_V, vrow, vcol, x);
             }
             if (takes_u) {
                 float x[8];
-                eight(ua8, x);
+                eight(w8[AT_M], x);
                 put8<INNER, LDV>(ut, PLANE_V, vrow, vcol, x);
-                y8.get(x);
-                put8<RAW, LDV>(yt, PLANE_V, vrow, vcol, x);
+                put8_ahead<T, LDV, VALUES>(yt, PLANE_V, vrow, vcol, t8[AT_M]);
             }
             if (v0 + VB < l.VP) ask(v0 + VB);
             __syncthreads();
+            const int lane = lane_anew();
             Frag ya[RAW], xa[INNER], ua[INNER];
-            frags_rows<RAW, LDV>(ya, yt, PLANE_V, mt * 16, 0);
-            frags_rows<INNER, LDV>(xa, xt, PLANE_V, mt * 16, 0);
-            frags_rows<INNER, LDV>(ua, ut, PLANE_V, mt * 16, 0);
+            frags_rows<RAW, LDV>(ya, yt, PLANE_V, mt * 16, 0, lane);
+            frags_rows<INNER, LDV>(xa, xt, PLANE_V, mt * 16, 0, lane);
+            frags_rows<INNER, LDV>(ua, ut, PLANE_V, mt * 16, 0, lane);
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 if (n > mt) continue;
                 Frag b[INNER];
-                frags_rows<INNER, LDV>(b, ut, PLANE_V, n * 16, 0);
+                frags_rows<INNER, LDV>(b, ut, PLANE_V, n * 16, 0, lane);
                 if (does_f) mma<RAW, INNER>(yu[0][n], ya, b);
                 if (does_m) mma<INNER, INNER>(yu[AT_M][n], xa, b);
             }
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 Frag b[INNER];
-                frags_rows<INNER, LDV>(b, st, PLANE_S, col0 + t * 16, 0);
+                frags_rows<INNER, LDV>(b, st, PLANE_S, col0 + t * 16, 0, lane);
                 mma<RAW, INNER>(ys[t], ya, b);
                 mma<INNER, INNER>(xs[t], xa, b);
             }
@@ -233,20 +236,21 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 Frag b[INNER];
-                frags_rows<INNER, LDV>(b, dst, PLANE_S, col0 + t * 16, 0);
+                frags_rows<INNER, LDV>(b, dst, PLANE_S, col0 + t * 16, 0, lane);
                 mma<INNER, INNER>(us[t], ua, b);
             }
         }
         ask_queries();
         __syncthreads();                                 // the first region is free
         ss = lanes_sum(ss);
-        if (lane == 0) wave_sums[wv] = ss;
+        if (threadIdx.x % 64 == 0) wave_sums[wv] = ss;
         xv_part += lane_move<DPP_XOR1>(xv_part);
         xv_part += lane_move<DPP_XOR2>(xv_part);
         if (threadIdx.x < 256 && threadIdx.x % 4 == 0) xv[threadIdx.x / 4] = xv_part;
 
         // F and M + M^T, and what of their products passes each token
         {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             const double *const G = reinterpret_cast<const double *>(vec + VEC_G * 64);
             float rm[4], before[4];                      // before: the sums of the tiles to the left
 #pragma unroll
@@ -293,6 +297,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
                 pass = rows_join(pass, pass);
                 pass = halves_join(pass, pass);
                 if (q4 == 0) passing[wv * 64 + j] = pass;
+                __builtin_amdgcn_sched_barrier(0);       // (one tile after the other: the numbers of four at once spill)
             }
             if (does_m) {
 #pragma unroll
@@ -306,12 +311,13 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
         ask_keys();
         __syncthreads();
         {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             float dot[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) dot[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const v4f_t q = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+                const v4f_t q = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float x = ys[t][r] * vec[VEC_ASK * 64 + mt * 16 + 4 * q4 + r];
@@ -325,11 +331,11 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             for (int ks = 0; ks < 2; ++ks) {
                 if (ks < mt / 2) continue;
                 Frag a[INNER];
-                frags_cols<INNER, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16);
+                frags_cols<INNER, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16, lane);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
-                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16);
+                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16, lane);
                     mma<INNER, RAW>(gk[t], a, b);
                 }
             }
@@ -339,12 +345,13 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
         if (hh + 1 == share) ask_queries();
         __syncthreads();
         {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             float db_[4], dc_[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) db_[r] = dc_[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const v4f_t k = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+                const v4f_t k = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = mt * 16 + 4 * q4 + r;
@@ -366,12 +373,12 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 Frag a[INNER], b2[INNER];
-                frags_rows<INNER, CHUNK>(a, fm, PLANE_M, mt * 16, ks * 32);
-                frags_rows<INNER, CHUNK>(b2, mm, PLANE_M, mt * 16, ks * 32);
+                frags_rows<INNER, CHUNK>(a, fm, PLANE_M, mt * 16, ks * 32, lane);
+                frags_rows<INNER, CHUNK>(b2, mm, PLANE_M, mt * 16, ks * 32, lane);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
-                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16);
+                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16, lane);
                     if (ks <= mt / 2) mma<INNER, RAW>(gq[t], a, b);
                     mma<INNER, RAW>(gk[t], b2, b);
                 }
@@ -379,6 +386,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
         }
         __syncthreads();
         if (wv == 0) {                                   // gates: a lane a token
+            const int lane = threadIdx.x;
             const float beta = vec[VEC_BETA * 64 + lane];
             float a = dot_a[lane], b = dot_b[lane], c = dot_c[lane];
             if constexpr (HALVES == 2) { a += dot_a[64 + lane]; b += dot_b[64 + lane]; c += dot_c[64 + lane]; }
@@ -419,13 +427,14 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
 
     // The lengths: of n = r x the gradient r (dn - n (n.dn)), where the factor r is in already.  The tile holds the keys.
     auto finish = [&](v4f_t (&grad)[TILES], int which, T *out, long long stride) {
+        const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
         if (g.norm) {
             float dot[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) dot[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) dot[r] += grad[t][r] * n[r];
             }
@@ -447,7 +456,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), 1) void k_gdelta_bwd_rows(G
             }
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16);
+                const v4f_t n = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) grad[t][r] -= dot[r] * n[r];
             }
@@ -475,7 +484,9 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const vo
 {
     typedef Back<T, KP> C;
     static_assert(C::LDS <= 160 * 1024, "LDS of a compute unit");
-    const auto kernel = whole_keys<T>(g) ? k_gdelta_bwd_rows<T, KP, true> : k_gdelta_bwd_rows<T, KP, false>;
+    const int v = 16 / (int)sizeof(T);
+    const bool values = g.V % 8 == 0 && !unaligned16(g.v) && !unaligned16(dy) && (g.T < 2 || (g.v_stride % v == 0 && g.y_stride % v == 0));
+    const auto kernel = whole_keys<T>(g) && values ? k_gdelta_bwd_rows<T, KP, true, true> : k_gdelta_bwd_rows<T, KP, false, false>;
     const hipError_t e = gd_lds(kernel, C::LDS);
     if (e != hipSuccess) return e;
     return gd_launches(l.chunks, C::THREADS, [&](unsigned first, unsigned now) {

@@ -47,6 +47,15 @@ template <> struct PartsOf<float> { static constexpr int RAW = 3, INNER = 3; };
 // look at which lanes are on.
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
+// A lane's number that the compiler takes for a new one each time: what is formed with it is formed where it is used, and does not occupy registers from one part of
+// a kernel to the next
+__device__ __forceinline__ int lane_anew()
+{
+    int v = threadIdx.x & 63;
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 struct Frag { u4t_t w; };
 
 __device__ __forceinline__ v4f_t mfma(const Frag &a, const Frag &b, v4f_t c)
@@ -100,16 +109,15 @@ template <int LD> __device__ __forceinline__ constexpr int place(int row, int co
 
 // Operands out of LDS tiles of leading dimension LD.  rows: 16 of them from r0, contracted over the 32 columns from c0 on.  cols: 16 of them from c0, contracted over
 // the 32 rows from r0 on.
-template <int LD> __device__ __forceinline__ Frag frag_rows(const bf16_t *tile, int r0, int c0)
+template <int LD> __device__ __forceinline__ Frag frag_rows(const bf16_t *tile, int r0, int c0, int lane)
 {
-    const int lane = threadIdx.x & 63;
     // (r0 is a multiple of 16: the rows' turns are those of the lane)
     return {*reinterpret_cast<const u4t_t *>(tile + (r0 + (lane & 15)) * LD + turned<LD>(lane & 15, c0 / 8 + (lane >> 4)) * 8)};
 }
 typedef __attribute__((address_space(3))) v4h_t *lds_v4h_t;
-template <int LD> __device__ __forceinline__ Frag frag_cols(const bf16_t *tile, int r0, int c0)
+template <int LD> __device__ __forceinline__ Frag frag_cols(const bf16_t *tile, int r0, int c0, int lane)
 {
-    const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    const int m = lane & 15, q = lane >> 4;
     const bf16_t *const p = tile + r0 * LD + place4<LD>(4 * q + (m >> 2), (c0 >> 2) + (m & 3));
     const v4h_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)p);
     const v4h_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4h_t)(p + 16 * LD));
@@ -117,9 +125,9 @@ template <int LD> __device__ __forceinline__ Frag frag_cols(const bf16_t *tile, 
     return {u4t_t{x.x, x.y, y.x, y.y}};
 }
 // the numbers of a tile of N parts where a result tile has its own: rows r0 + 4 q + r of column c0 + m
-template <int N, int LD> __device__ __forceinline__ v4f_t tile_of(const bf16_t *tile, int plane, int r0, int c0)
+template <int N, int LD> __device__ __forceinline__ v4f_t tile_of(const bf16_t *tile, int plane, int r0, int c0, int lane)
 {
-    const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    const int m = lane & 15, q = lane >> 4;
     v4f_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) {
@@ -129,15 +137,15 @@ template <int N, int LD> __device__ __forceinline__ v4f_t tile_of(const bf16_t *
     }
     return v;
 }
-template <int N, int LD> __device__ __forceinline__ void frags_rows(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0)
+template <int N, int LD> __device__ __forceinline__ void frags_rows(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0, int lane = threadIdx.x & 63)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = frag_rows<LD>(tile + i * plane, r0, c0);
+    for (int i = 0; i < N; ++i) f[i] = frag_rows<LD>(tile + i * plane, r0, c0, lane);
 }
-template <int N, int LD> __device__ __forceinline__ void frags_cols(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0)
+template <int N, int LD> __device__ __forceinline__ void frags_cols(Frag (&f)[N], const bf16_t *tile, int plane, int r0, int c0, int lane = threadIdx.x & 63)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = frag_cols<LD>(tile + i * plane, r0, c0);
+    for (int i = 0; i < N; ++i) f[i] = frag_cols<LD>(tile + i * plane, r0, c0, lane);
 }
 
 // eight consecutive numbers from a column that is a multiple of 8 on, into a row of an LDS tile of N parts
