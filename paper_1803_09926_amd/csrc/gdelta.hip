@@ -68,17 +68,26 @@ void place_kept(const gdelta_desc *d, const GdLayout &l, void *kept, GdSpace *s)
     s->U = (float *)(p + l.chunks * d->H * l.state);
 }
 
+size_t kept_bytes(const gdelta_desc *d, const GdLayout &l) { return forward_bytes(d, l) + (size_t)l.chunks * d->H * (size_t)(l.state + l.rows); }
+size_t backward_bytes(const gdelta_desc *d, const GdLayout &l)
+{
+    return (size_t)l.chunks * d->H * (size_t)(l.state + l.rows) + (size_t)l.pieces * d->H * (size_t)l.state + round16((size_t)l.chunks * d->H * 2 * sizeof(float));
+}
+
 // How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole.  Of heads of 128 x 128 in bf16 a chunk of a walk takes 4.2 us, of a
 // piece and its map 7.5 together, both as long as there are no more blocks than compute units, and a piece in the join 3.7.  16384 tokens of 16 heads: 1035 us whole,
 // 308 in pieces; 8 sequences of 1024 tokens of 8 heads 85 and 113.
-int piece_of(const gdelta_desc *d, long long VP)
+int piece_of(const gdelta_desc *d, long long VP, bool packed)
 {
     const char *const forced = tune_env("DWCONV_TUNE_GDELTA_PIECE");
     if (forced) return atoi(forced) > 0 ? atoi(forced) : 0;
     const double chunks = ceil((double)d->T / ((double)d->sequences * TOKENS)), walks = (double)d->sequences * d->H * ((VP + 63) / 64), units = 256;
     const double piece = ceil(fmax(4, fmax(chunks * walks / (2 * units), sqrt(chunks / 2)))), pieces = ceil(chunks / piece);
-    if (walks >= units || pieces < 2) return 0;
-    return 7.5 * piece * fmax(1, pieces * walks / units) + 3.7 * pieces + 10 < 0.8 * 4.2 * chunks ? (int)piece : 0;
+    if (walks < units && pieces >= 2 && 7.5 * piece * fmax(1, pieces * walks / units) + 3.7 * pieces + 10 < 0.8 * 4.2 * chunks) return (int)piece;
+    // Lengths that differ: what is longer than the mean goes in pieces of about that, so that no sequence is walked long after the others (24 prompts of 2 to 2000 tokens, 16 heads
+    // of 64 x 128: 326 us whole, in pieces of 8, 16, 32 chunks 251, 252, 315).
+    const double mean = ceil(1.25 * chunks);
+    return packed && d->sequences > 1 && chunks >= 8 && mean < d->T / (double)TOKENS ? (int)mean : 0;
 }
 
 }  // namespace
@@ -91,11 +100,11 @@ GdLayout gdelta_layout(const gdelta_desc *d, bool packed)
     l.KP = d->K <= 32 ? 32 : d->K <= 64 ? 64 : d->K <= 128 ? 128 : 256;
     l.VP = cdiv(d->V, 32) * 32;
     l.inner = d->dtype == DWCONV_F32 ? 3 : 2;
-    l.matrix = l.inner * TOKENS * TOKENS * 2;
+    l.matrix = l.inner * 384 * 16;                // (MATRIX_PIECES)
     l.vectors = 9 * TOKENS * 4;
     l.state = (long long)l.KP * l.VP * 4;
     l.rows = TOKENS * l.VP * 4;
-    l.piece = d->T == 0 ? 0 : piece_of(d, l.VP);
+    l.piece = d->T == 0 ? 0 : piece_of(d, l.VP, packed);
     l.map = (long long)l.KP * l.KP * 4;
     const long long unit = l.piece * TOKENS;
     l.pieces = !l.piece ? 0 : packed ? d->T / unit + d->sequences : d->sequences * ((length + unit - 1) / unit);
@@ -108,25 +117,26 @@ using namespace dwc;
 
 extern "C" {
 
+// (the layouts of sequences of equal and of other lengths differ)
 size_t gdelta_kept_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
-    const GdLayout l = gdelta_layout(desc, true);
-    return forward_bytes(desc, l) + (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows);
+    const size_t a = kept_bytes(desc, gdelta_layout(desc, false)), b = kept_bytes(desc, gdelta_layout(desc, true));
+    return a > b ? a : b;
 }
 
 size_t gdelta_fwd_workspace_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
-    return forward_bytes(desc, gdelta_layout(desc, true));
+    const size_t a = forward_bytes(desc, gdelta_layout(desc, false)), b = forward_bytes(desc, gdelta_layout(desc, true));
+    return a > b ? a : b;
 }
 
 size_t gdelta_bwd_workspace_bytes(const gdelta_desc *desc)
 {
     if (validate(desc) != DWCONV_OK) return 0;
-    const GdLayout l = gdelta_layout(desc, true);
-    return (size_t)l.chunks * desc->H * (size_t)(l.state + l.rows) + (size_t)l.pieces * desc->H * (size_t)l.state +
-           round16((size_t)l.chunks * desc->H * 2 * sizeof(float));
+    const size_t a = backward_bytes(desc, gdelta_layout(desc, false)), b = backward_bytes(desc, gdelta_layout(desc, true));
+    return a > b ? a : b;
 }
 
 static int check_tensors(const gdelta_desc *d, const gdelta_tensors *t, std::initializer_list<const void *> stored, std::initializer_list<const void *> others)
@@ -150,15 +160,15 @@ int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
     rc = check_tensors(desc, t, {t->q, t->k, t->v, t->a, t->b, t->y}, {t->A, t->a_bias, t->starts, t->init, t->final});
     if (rc != DWCONV_OK) return rc;
     if (!t->starts && desc->T % desc->sequences) return DWCONV_ERR_BAD_DIM;
-    const GdLayout l = gdelta_layout(desc, t->starts != nullptr), most = gdelta_layout(desc, true);
+    const GdLayout l = gdelta_layout(desc, t->starts != nullptr);
     GdSpace s = {};
     if (t->kept) {
         if (unaligned16(t->kept)) return DWCONV_ERR_ALIGN;
-        place_kept(desc, most, t->kept, &s);
-    } else if (most.chunks) {
-        if (!workspace || workspace_bytes < forward_bytes(desc, most)) return DWCONV_ERR_WORKSPACE;
+        place_kept(desc, l, t->kept, &s);
+    } else if (l.chunks) {
+        if (!workspace || workspace_bytes < gdelta_fwd_workspace_bytes(desc)) return DWCONV_ERR_WORKSPACE;
         if (unaligned16(workspace)) return DWCONV_ERR_ALIGN;
-        place_forward(desc, most, (char *)workspace, &s);
+        place_forward(desc, l, (char *)workspace, &s);
     }
     if (desc->T == 0 && !t->final) return DWCONV_OK;
     const GdArgs g = args_of(desc, t);
@@ -177,17 +187,17 @@ int gdelta_bwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
     if (rc != DWCONV_OK) return rc;
     if (desc->T > 0 && !t->kept) return DWCONV_ERR_NULL;
     if (!t->starts && desc->T % desc->sequences) return DWCONV_ERR_BAD_DIM;
-    const GdLayout l = gdelta_layout(desc, t->starts != nullptr), most = gdelta_layout(desc, true);
-    if (most.chunks) {
+    const GdLayout l = gdelta_layout(desc, t->starts != nullptr);
+    if (l.chunks) {
         if (!workspace || workspace_bytes < gdelta_bwd_workspace_bytes(desc)) return DWCONV_ERR_WORKSPACE;
         if (unaligned16(workspace) || unaligned16(t->kept)) return DWCONV_ERR_ALIGN;
     }
     GdSpace s = {};
-    place_kept(desc, most, t->kept, &s);
+    place_kept(desc, l, t->kept, &s);
     s.dS = (float *)workspace;
-    s.X = (float *)((char *)workspace + most.chunks * desc->H * most.state);
-    s.ends = (float *)((char *)s.X + most.chunks * desc->H * most.rows);
-    s.partials = (float *)((char *)s.ends + most.pieces * desc->H * most.state);
+    s.X = (float *)((char *)workspace + l.chunks * desc->H * l.state);
+    s.ends = (float *)((char *)s.X + l.chunks * desc->H * l.rows);
+    s.partials = (float *)((char *)s.ends + l.pieces * desc->H * l.state);
     const GdArgs g = args_of(desc, t);
     hipError_t e = hipSuccess;
     if (desc->T > 0) {

@@ -49,12 +49,12 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         rows.load(kp + at * g.k_stride, g.k_stride, len, g.K);
         matrix.load(s.T + where * l.matrix);
         second.load(s.P + where * l.matrix);
-        const int y_stride = fresh((int)g.y_stride);
+        const auto places = cols.template places<T>((int)g.y_stride, g.V);
         const BufView view = rows_view(yp + at * g.y_stride, g.y_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(o[mt][r], view, cols.at(row_of(mt, r), y_stride, (int)sizeof(T)), g.V);
+            for (int r = 0; r < 4; ++r) cols.load(o[mt][r], view, places, mt, r);
         const float *const vec = reinterpret_cast<const float *>(s.vec + where * l.vectors);
         vec_next = vec[threadIdx.x];
         decay_next = vec[VEC_ONE * 64];
@@ -80,58 +80,39 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        {
+            Frag p[KP / 32][NT][INNER];
 #pragma unroll
-        for (int c0 = 0; c0 < KP / 32; ++c0) {
-            Frag p[NT][INNER];
+            for (int c0 = 0; c0 < KP / 32; ++c0)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c0][nt], S[2 * c0 + 1][nt], p[nt]);
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt) {
-                Frag a[RAW];
-                frags_rows<RAW, LD>(a, kt, PLANE, mt * 16, c0 * 32);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(U[mt][nt], a, p[nt]);
-            }
+                for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c0][nt], S[2 * c0 + 1][nt], p[c0][nt]);
+            times_state<RAW, INNER, NT, KP>(U, kt, p);
         }
         {
             v4f_t d[4][NT];
             Frag b[2][NT][RAW];
 #pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) d[mt][nt] = v4f_t{o[mt][0].at(nt), o[mt][1].at(nt), o[mt][2].at(nt), o[mt][3].at(nt)};
-            split_rows<RAW, NT>(d, b);
-#pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
                 const float4 write = four(vl + VEC_WRITE * 64, mt);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) U[mt][nt] = times(U[mt][nt], write);
-#pragma unroll
-                for (int ks = mt / 2; ks < 2; ++ks) {
-                    Frag a[INNER];
-                    frags_cols<INNER, CHUNK>(a, pm, PLANE_M, ks * 32, mt * 16);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<INNER, RAW>(U[mt][nt], a, b[ks][nt]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    d[mt][nt] = v4f_t{o[mt][0].at(nt), o[mt][1].at(nt), o[mt][2].at(nt), o[mt][3].at(nt)};
+                    U[mt][nt] = times(U[mt][nt], write);
                 }
             }
+            split_rows<RAW, NT>(d, b);
+            times_triangle<INNER, RAW, true, NT>(U, pm, b);
         }
         // X
         split_rows<INNER, NT>(U, f);
         v4f_t X[4][NT];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) X[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = mt / 2; ks < 2; ++ks) {
-                Frag a[INNER];
-                frags_cols<INNER, CHUNK>(a, tm, PLANE_M, ks * 32, mt * 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(X[mt][nt], a, f[ks][nt]);
-            }
-        }
+        times_triangle<INNER, INNER, true, NT>(X, tm, f);
         if (!MAP) store_tiles<NT, 4>(X, s.X + where * (l.rows / 4), l.VP, cols);
-        const int v_stride = fresh((int)g.v_stride);
+        const auto places = cols.template places<T>((int)g.v_stride, g.V);
         const BufView out = rows_view(dv + at * g.v_stride + (long long)h * g.V, g.v_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
@@ -143,7 +124,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
                 float x[NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[nt] = X[mt][nt][r];
-                cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), v_stride, (int)sizeof(T)), g.V, x);
+                cols.template store<T, WHOLE>(out, places, mt, r, x);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) X[mt][nt] = -times(X[mt][nt], read);
@@ -151,17 +132,10 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         // dS
         split_rows<INNER, NT>(X, f);
 #pragma unroll
-        for (int ct = 0; ct < KP / 16; ++ct) {
+        for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                Frag a[RAW];
-                frags_cols<RAW, LD>(a, kt, PLANE, ks * 32, ct * 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
-            }
-        }
+        add_to_state<RAW, INNER, NT, KP>(S, kt, f);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 ask = four(vl + VEC_ASK * 64, mt);
@@ -173,15 +147,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         rows.template put<LD>(qt);
         if (c > from) load_keys(c - 1);
         __syncthreads();
-#pragma unroll
-        for (int ct = 0; ct < KP / 16; ++ct)
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                Frag a[RAW];
-                frags_cols<RAW, LD>(a, qt, PLANE, ks * 32, ct * 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
-            }
+        add_to_state<RAW, INNER, NT, KP>(S, qt, f);
     }
     if constexpr (MAP) store_tiles<NT, KP / 16>(S, s.ends + piece * (l.state / 4), l.VP, cols);
 }

@@ -20,7 +20,7 @@ constexpr int VB = 32, LDV = VB;
 
 template <typename T, int KP> struct Back {
     static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP;
-    static constexpr int HALVES = KP > 128 || (KP == 128 && RAW == 1) ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
+    static constexpr int HALVES = KP > 128 || (KP >= 64 && RAW == 1) ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
     static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
     static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
     static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
@@ -40,8 +40,32 @@ __device__ __forceinline__ float row_sum(float v)
     return v + lane_move<DPP_MIRROR>(v);
 }
 
+// the sum over the lanes to the left in a row of 16
+__device__ __forceinline__ float sum_before(float v)
+{
+    float s = lane_move<DPP_SHR1>(v);
+    s += lane_move<DPP_SHR1>(s);
+    s += lane_move<DPP_SHR2>(s);
+    s += lane_move<DPP_SHR4>(s);
+    return s + lane_move<DPP_SHR8>(s);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ float lane_move_rows(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+// the sum over the lanes up to one's own, of 64
+__device__ __forceinline__ float sum_up_to(float v)
+{
+    v += lane_move<DPP_SHR1>(v);
+    v += lane_move<DPP_SHR2>(v);
+    v += lane_move<DPP_SHR4>(v);
+    v += lane_move<DPP_SHR8>(v);
+    v += lane_move_rows<0x142, 0xa>(v);           // the row before's last lane to the second and fourth row,
+    return v + lane_move_rows<0x143, 0xc>(v);     // the second row's to the upper half
+}
+
 template <typename T, int KP, bool WHOLE, bool VALUES>
-__global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP <= 64 ? 2 : 1)) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
+__global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP <= 32 ? 2 : 1)) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
     typedef Back<T, KP> C;
@@ -68,8 +92,61 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
     Rows<T, KP, THREADS, WHOLE> rows;                // a tile of keys or queries on its way
     auto ask_keys = [&] { rows.load(kp, g.k_stride, at.len, g.K); };
     auto ask_queries = [&] { rows.load(qp, g.q_stride, at.len, g.K); };
+    constexpr int BOTH = HALVES == 1 ? 2 : 1, AT_M = BOTH - 1;       // places of what two wavefronts that share rows have one of each
+    const float *sp, *dsp, *xp, *up;                 // of the head in hand
+    const T *yp, *vp;
+    constexpr int VECS_PER = (VECS * 64 + THREADS - 1) / THREADS;
+    float vec_ahead[VECS_PER];
+    auto point_to = [&](int h) {
+        const long long where = (long long)id * g.H + h;
+        sp = s.S + where * (l.state / 4);
+        dsp = s.dS + where * (l.state / 4);
+        xp = s.X + where * (l.rows / 4);
+        up = s.U + where * (l.rows / 4);
+        yp = dy + at.first * g.y_stride + (long long)h * g.V;
+        vp = (const T *)g.v + at.first * g.v_stride + (long long)h * g.V;
+        const BufView view(s.vec + where * l.vectors, VECS * 64 * 4);
+#pragma unroll
+        for (int i = 0; i < VECS_PER; ++i) vec_ahead[i] = __uint_as_float(view.b32((threadIdx.x + i * THREADS) * 4, 0));
+    };
+    // what the next 32 columns of V take, on its way: 8 numbers a lane of each
+    constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
+    const int vrow = threadIdx.x % 256 / (VB / 8), vcol = threadIdx.x % (VB / 8) * 8;
+    const bool takes_x = HALVES == 1 || wv < 4, takes_u = HALVES == 1 || wv >= 4;
+    u4t_t sa[PER][2], sb[PER][2], w8[BOTH][2];       // w8: X and U,
+    Ahead<T, 8, VALUES> t8[BOTH];                    // t8: V and dY, of both or one of each pair
+    auto ask = [&](int v0) {
+        const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int n = threadIdx.x + i * THREADS;
+            const uint32_t off = n < ALL ? (uint32_t)(n / (VB / 8) * l.VP + v0 + n % (VB / 8) * 8) * 4u : BufView::OUTSIDE;
+            sa[i][0] = view_s.b128(off, 0);
+            sa[i][1] = view_s.b128(off + 16, 0);
+            sb[i][0] = view_d.b128(off, 0);
+            sb[i][1] = view_d.b128(off + 16, 0);
+        }
+        const uint32_t off = (uint32_t)(vrow * l.VP + v0 + vcol) * 4u;
+        if (takes_x) {
+            const BufView view(xp, (uint32_t)l.rows), rows_v = rows_view(vp, g.v_stride, at.len, g.V);
+            w8[0][0] = view.b128(off, 0);
+            w8[0][1] = view.b128(off + 16, 0);
+            t8[0].load(rows_v, (uint32_t)(vrow * (int)g.v_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
+        }
+        if (takes_u) {
+            const BufView view(up, (uint32_t)l.rows), rows_y = rows_view(yp, g.y_stride, at.len, g.V);
+            w8[AT_M][0] = view.b128(off, 0);
+            w8[AT_M][1] = view.b128(off + 16, 0);
+            t8[AT_M].load(rows_y, (uint32_t)(vrow * (int)g.y_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
+        }
+    };
+    auto eight = [](const u4t_t (&w)[2], float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
+    };
+    point_to(kh * share);
+    ask(0);
     // Products of queries with keys, and of keys with keys: rows 16 mt.., columns 16 n...  Where two wavefronts share the rows each has one of them.
-    constexpr int BOTH = HALVES == 1 ? 2 : 1, AT_M = BOTH - 1;
     v4f_t qk[BOTH][4];
     {
         Frag qa[KP / 32][RAW];
@@ -114,46 +191,10 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
 
     for (int hh = 0; hh < share; ++hh) {
         const int h = kh * share + hh;
-        const long long where = (long long)id * g.H + h;
-        const float *const sp = s.S + where * (l.state / 4), *const dsp = s.dS + where * (l.state / 4);
-        const float *const xp = s.X + where * (l.rows / 4), *const up = s.U + where * (l.rows / 4);
-        const T *const yp = dy + at.first * g.y_stride + (long long)h * g.V, *const vp = (const T *)g.v + at.first * g.v_stride + (long long)h * g.V;
-        // what the next 32 columns of V take, on its way: 8 numbers a lane of each
-        constexpr int ALL = KP * VB / 8, PER = (ALL + THREADS - 1) / THREADS;
-        const int vrow = threadIdx.x % 256 / (VB / 8), vcol = threadIdx.x % (VB / 8) * 8;
-        const bool takes_x = HALVES == 1 || wv < 4, takes_u = HALVES == 1 || wv >= 4;
-        u4t_t sa[PER][2], sb[PER][2], w8[BOTH][2];       // w8: X and U,
-        Ahead<T, 8, VALUES> t8[BOTH];                    // t8: V and dY, of both or one of each pair
-        auto ask = [&](int v0) {
-            const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int n = threadIdx.x + i * THREADS;
-                const uint32_t off = n < ALL ? (uint32_t)(n / (VB / 8) * l.VP + v0 + n % (VB / 8) * 8) * 4u : BufView::OUTSIDE;
-                sa[i][0] = view_s.b128(off, 0);
-                sa[i][1] = view_s.b128(off + 16, 0);
-                sb[i][0] = view_d.b128(off, 0);
-                sb[i][1] = view_d.b128(off + 16, 0);
-            }
-            const uint32_t off = (uint32_t)(vrow * l.VP + v0 + vcol) * 4u;
-            if (takes_x) {
-                const BufView view(xp, (uint32_t)l.rows), rows_v = rows_view(vp, g.v_stride, at.len, g.V);
-                w8[0][0] = view.b128(off, 0);
-                w8[0][1] = view.b128(off + 16, 0);
-                t8[0].load(rows_v, (uint32_t)(vrow * (int)g.v_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
-            }
-            if (takes_u) {
-                const BufView view(up, (uint32_t)l.rows), rows_y = rows_view(yp, g.y_stride, at.len, g.V);
-                w8[AT_M][0] = view.b128(off, 0);
-                w8[AT_M][1] = view.b128(off + 16, 0);
-                t8[AT_M].load(rows_y, (uint32_t)(vrow * (int)g.y_stride + v0 + vcol) * (uint32_t)sizeof(T), g.V - v0 - vcol);
-            }
-        };
-        auto eight = [](const u4t_t (&w)[2], float (&x)[8]) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
-        };
-        ask(0);
+        if (hh) {
+            point_to(h);
+            ask(0);
+        }
         v4f_t ys[TILES], xs[TILES], us[TILES], yu[BOTH][4];      // yu: dY U^T and X U^T
 #pragma unroll
         for (int t = 0; t < TILES; ++t) ys[t] = xs[t] = us[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
@@ -170,8 +211,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         for (int v0 = 0; v0 < l.VP; v0 += VB) {
             __syncthreads();
             if (v0 == 0) {
-                const float *const p = reinterpret_cast<const float *>(s.vec + where * l.vectors);
-                for (int i = threadIdx.x; i < VECS * 64; i += THREADS) vec[i] = p[i];
+#pragma unroll
+                for (int i = 0; i < VECS_PER; ++i)
+                    if (threadIdx.x + i * THREADS < VECS * 64) vec[threadIdx.x + i * THREADS] = vec_ahead[i];
             }
             float keep[C::TURNS ? PER : 1][8];
 #pragma unroll
@@ -252,50 +294,70 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         {
             const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             const double *const G = reinterpret_cast<const double *>(vec + VEC_G * 64);
-            float rm[4], before[4];                      // before: the sums of the tiles to the left
+            float rm[4], left[4], behind = 0.f;          // left: of a row in the tiles left of the diagonal's, this lane's columns; behind: those tiles' sums
 #pragma unroll
-            for (int r = 0; r < 4; ++r) rm[r] = before[r] = 0.f;
+            for (int r = 0; r < 4; ++r) rm[r] = left[r] = 0.f;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const int j = n * 16 + m;
-                const double gj = G[j];
-                const float kj = vec[VEC_RK * 64 + j];
                 float pass = 0.f;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = mt * 16 + 4 * q4 + r;
-                    const float e = i >= j ? exp2_fast((float)(G[i] - gj) * LOG2E) * kj : 0.f;
-                    float x = 0.f;
-                    uint32_t p[INNER];
+                if (n > mt) {                            // above the diagonal all is zero
                     if (does_f) {
-                        const float f = i >= j ? g.scale * vec[VEC_RQ * 64 + i] * e * yu[0][n][r] : 0.f;
-                        x += f * qk[0][n][r];
-                        split2<INNER>(f, 0.f, p);
 #pragma unroll
-                        for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(mt * 16 + 4 * q4 + r, j)] = 0;
                     }
-                    if (does_m && i >= j) {
-                        const float b = i > j ? -vec[VEC_RK * 64 + i] * e * yu[AT_M][n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
-                        rm[r] += b * qk[AT_M][n][r];
-                        x += f * qk[AT_M][n][r];
-                        split2<INNER>(f, 0.f, p);
+                } else {
+                    const double gj = G[j];
+                    const float kj = vec[VEC_RK * 64 + j];
+                    float x[4];
 #pragma unroll
-                        for (int k = 0; k < INNER; ++k) {
-                            mm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
-                            mm[k * PLANE_M + place<CHUNK>(j, i)] = (bf16_t)p[k];
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = mt * 16 + 4 * q4 + r;
+                        const float e = i >= j ? exp2_fast((float)(G[i] - gj) * LOG2E) * kj : 0.f;
+                        uint32_t p[INNER];
+                        x[r] = 0.f;
+                        if (does_f) {
+                            const float f = g.scale * vec[VEC_RQ * 64 + i] * e * yu[0][n][r];
+                            x[r] = f * qk[0][n][r];
+                            split2<INNER>(f, 0.f, p);
+#pragma unroll
+                            for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
+                        }
+                        if (does_m) {
+                            const float b = i > j ? -vec[VEC_RK * 64 + i] * e * yu[AT_M][n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
+                            rm[r] += b * qk[AT_M][n][r];
+                            x[r] += f * qk[AT_M][n][r];
+                            split2<INNER>(f, 0.f, p);
+                            if (i >= j) {
+#pragma unroll
+                                for (int k = 0; k < INNER; ++k) {
+                                    mm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
+                                    mm[k * PLANE_M + place<CHUNK>(j, i)] = (bf16_t)p[k];
+                                }
+                            }
                         }
                     }
-                    // the sum over the columns before j, of the rows from j on
-                    float left = lane_move<DPP_SHR1>(x);
-                    left += lane_move<DPP_SHR1>(left);
-                    left += lane_move<DPP_SHR2>(left);
-                    left += lane_move<DPP_SHR4>(left);
-                    left += lane_move<DPP_SHR8>(left);
-                    pass += i >= j ? left + before[r] : 0.f;
-                    before[r] += row_sum(x);
+                    // the sum over the columns before j, of the rows from j on: of tiles left of the diagonal's all rows, of that tile those from j on
+                    if (n < mt) {
+                        float c = (x[0] + x[1]) + (x[2] + x[3]);
+                        c = rows_join(c, c);
+                        c = halves_join(c, c);
+                        pass = sum_before(c) + behind;
+                        behind += row_sum(c);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) left[r] += x[r];
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float to = sum_before(x[r]) + row_sum(left[r]);
+                            pass += mt * 16 + 4 * q4 + r >= j ? to : 0.f;
+                        }
+                        pass = rows_join(pass, pass);
+                        pass = halves_join(pass, pass);
+                    }
                 }
-                pass = rows_join(pass, pass);
-                pass = halves_join(pass, pass);
                 if (q4 == 0) passing[wv * 64 + j] = pass;
                 __builtin_amdgcn_sched_barrier(0);       // (one tile after the other: the numbers of four at once spill)
             }
@@ -396,15 +458,10 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 pass += passing[i * 64 + lane];
                 sum += wave_sums[i];
             }
-            // what is read from the token on, and what was written before it
-            float d = a - beta * b, w = __shfl_up(c, 1, 64);
+            // what is read from the token on (summed with the lanes the other way round), and what was written before it
+            const float d = __shfl(sum_up_to(__shfl(a - beta * b, 63 - lane, 64)), 63 - lane, 64);
+            float w = __shfl_up(sum_up_to(c), 1, 64);
             if (lane == 0) w = 0.f;
-#pragma unroll
-            for (int off = 1; off < 64; off *= 2) {
-                const float down = __shfl_down(d, off, 64), up = __shfl_up(w, off, 64);
-                if (lane + off < 64) d += down;
-                if (lane >= off) w += up;
-            }
             const float dbeta = xv[lane] - b + row_m[lane];
             float dg = d + w + (pass + vec[VEC_ONE * 64] * sum), for_a = 0.f, for_A = 0.f;
             if (lane < at.len) {

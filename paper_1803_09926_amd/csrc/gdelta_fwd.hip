@@ -74,12 +74,12 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     };
     auto load_values = [&](int c) {
         const int at = start + c * CHUNK, len = min(CHUNK, end - at);
-        const int v_stride = fresh((int)g.v_stride);
+        const auto places = cols.template places<T>((int)g.v_stride, unit ? 0 : g.V);
         const BufView view = rows_view(vp + at * g.v_stride, g.v_stride, len, g.V);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) cols.load(v[mt][r], view, cols.at(row_of(mt, r), v_stride, (int)sizeof(T)), unit ? 0 : g.V);
+            for (int r = 0; r < 4; ++r) cols.load(v[mt][r], view, places, mt, r);
     };
     if (at_.from < chunks) {
         load_next(at_.from);
@@ -114,6 +114,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         int from[NT];
         const bool odd = __any(bad < CHUNK || probe != 0.f);
         if (odd) {
+            seldom();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 from[nt] = bad;
@@ -133,15 +134,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) R[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c0 = 0; c0 < KP / 32; ++c0)
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt) {
-                Frag a[RAW];
-                frags_rows<RAW, LD>(a, kt, PLANE, mt * 16, c0 * 32);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(R[mt][nt], a, Sp[c0][nt]);
-            }
+        times_state<RAW, INNER, NT, KP>(R, kt, Sp);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 read = four(vl + VEC_READ * 64, mt), beta = four(vl + VEC_BETA * 64, mt);
@@ -152,6 +145,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             }
         }
         if (odd) {
+            seldom();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -164,17 +158,10 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         split_rows<INNER, NT>(R, f);
         v4f_t U[4][NT];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks <= mt / 2; ++ks) {
-                Frag a[INNER];
-                frags_rows<INNER, CHUNK>(a, tm, PLANE_M, mt * 16, ks * 32);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(U[mt][nt], a, f[ks][nt]);
-            }
-        }
+        times_triangle<INNER, INNER, false, NT>(U, tm, f);
         if (!MAP && s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
         v4f_t w[4][NT];
 #pragma unroll
@@ -185,17 +172,10 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         }
         split_rows<INNER, NT>(w, f);
 #pragma unroll
-        for (int ct = 0; ct < KP / 16; ++ct) {
+        for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                Frag a[RAW];
-                frags_cols<RAW, LD>(a, kt, PLANE, ks * 32, ct * 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, f[ks][nt]);
-            }
-        }
+        add_to_state<RAW, INNER, NT, KP>(S, kt, f);
         v4f_t O[4][NT];
         if constexpr (MAP) {
             if (c + 1 < chunks) load_values(c + 1);
@@ -213,30 +193,17 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c0 = 0; c0 < KP / 32; ++c0)
-#pragma unroll
-                for (int mt = 0; mt < 4; ++mt) {
-                    Frag a[RAW];
-                    frags_rows<RAW, LD>(a, qt, PLANE, mt * 16, c0 * 32);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(O[mt][nt], a, Sp[c0][nt]);
-                }
+            times_state<RAW, INNER, NT, KP>(O, qt, Sp);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
                 const float4 ask = four(vl + VEC_ASK * 64, mt);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
-#pragma unroll
-                for (int ks = 0; ks <= mt / 2; ++ks) {
-                    Frag a[INNER];
-                    frags_rows<INNER, CHUNK>(a, pm, PLANE_M, mt * 16, ks * 32);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<INNER, INNER>(O[mt][nt], a, f[ks][nt]);
-                }
             }
+            times_triangle<INNER, INNER, false, NT>(O, pm, f);
         }
         if (odd) {
+            seldom();
             const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -251,7 +218,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             }
         }
         if constexpr (!MAP) {
-            const int y_stride = fresh((int)g.y_stride);
+            const auto places = cols.template places<T>((int)g.y_stride, g.V);
             const BufView out = rows_view(y + at * g.y_stride + (long long)h * g.V, g.y_stride, len, g.V);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt)
@@ -260,7 +227,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
                     float x[NT];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) x[nt] = O[mt][nt][r];
-                    cols.template store<T, WHOLE>(out, cols.at(row_of(mt, r), y_stride, (int)sizeof(T)), g.V, x);
+                    cols.template store<T, WHOLE>(out, places, mt, r, x);
                 }
         }
         split_state();

@@ -18,7 +18,8 @@ constexpr int THREADS = 256, LDF = 68;            // floats of a row of an fp32 
 template <typename T, int KP> struct Prep {
     static constexpr int RAW = PartsOf<T>::RAW, LD = KP;
     static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, F32S = (size_t)CHUNK * LDF * 4;
-    static constexpr size_t LDS = TILE + 2 * F32S + 64 * 8 + 5 * 64 * 4;
+    static constexpr size_t FIRST = TILE > F32S ? TILE : F32S;    // the keys, and when their products are taken the inverse
+    static constexpr size_t LDS = FIRST + F32S + 64 * 8 + 5 * 64 * 4;
 };
 
 // the sum over N neighbouring lanes, 4 to 32, in every one of them
@@ -54,8 +55,9 @@ __device__ __forceinline__ double sum_up_to(float x)
 template <int N> __device__ __forceinline__ void put_matrix(const float *f, char *to)
 {
     const int row = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
-    bf16_t *const p = reinterpret_cast<bf16_t *>(to) + row * CHUNK;
+    bf16_t *const p = reinterpret_cast<bf16_t *>(to);
     const float *const x = f + row * LDF + c;
+    if (row < 32 && c >= 32) return;              // (above the diagonal)
     // four numbers, and the four 16 columns on, are a piece: a lane has halves of four
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -64,7 +66,8 @@ template <int N> __device__ __forceinline__ void put_matrix(const float *f, char
         split2<N>(x[4 * j + 2], x[4 * j + 3], b);
         const int j4 = (c >> 2) + j;
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<u2t_t *>(p + i * CHUNK * CHUNK + piece_of(j4) * 8 + half_of(j4) * 4) = u2t_t{a[i], b[i]};
+        for (int i = 0; i < N; ++i)
+            *reinterpret_cast<u2t_t *>(p + (i * MATRIX_PIECES + matrix_piece(row, piece_of(j4))) * 8 + half_of(j4) * 4) = u2t_t{a[i], b[i]};
     }
 }
 
@@ -76,8 +79,8 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
     constexpr int RAW = C::RAW, INNER = PartsOf<T>::INNER, LD = C::LD, PLANE = CHUNK * LD;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds);
-    float *const L = reinterpret_cast<float *>(lds + C::TILE), *const X = L + CHUNK * LDF;      // L, then P; the inverse
-    double *const Gs = reinterpret_cast<double *>(X + CHUNK * LDF);
+    float *const X = reinterpret_cast<float *>(lds), *const L = reinterpret_cast<float *>(lds + C::FIRST);      // the inverse; L, then P
+    double *const Gs = reinterpret_cast<double *>(L + CHUNK * LDF);
     float *const betas = reinterpret_cast<float *>(Gs + 64), *const rks = betas + 64, *const rqs = rks + 64;
     int *const bads = reinterpret_cast<int *>(rqs + 64);          // [64] tokens whose key is not finite
     const unsigned id = first + blockIdx.x;

@@ -15,6 +15,8 @@ __device__ __forceinline__ int fresh(int v)
     asm volatile("" : "+s"(v));
     return v;
 }
+// In a branch that is hardly ever taken: it stays one, instead of selections that are always made
+__device__ __forceinline__ void seldom() { asm volatile(""); }
 
 // The columns of a lane: NT neighbours, one in each of its NT result tiles, so that its numbers of a row lie beside each other.  PAIRS: they are read and written
 // at once, aligned.  What is not there is asked for, and stored, outside the view: no branch.
@@ -22,15 +24,29 @@ template <int NT> struct Columns {
     int c;                                        // the first
     __device__ __forceinline__ Columns(int block) : c((block * WAVES + wave_number()) * 16 * NT + (int)(threadIdx.x & 15) * NT) {}
     __device__ __forceinline__ uint32_t at(int row, int stride, int size) const { return (uint32_t)(row * stride + c) * (uint32_t)size; }
-    template <typename T, bool PAIRS> __device__ __forceinline__ void load(Ahead<T, NT, PAIRS> &x, const BufView &view, uint32_t off, int width) const
+    // Rows 16 mt + 4 q + r, `stride` apart, of `width` columns: the part of their places that differs between lanes (outside the view where the columns are outside
+    // the row), and that which does not
+    template <typename T> struct Places {
+        uint32_t lane;
+        int row, there;
+        __device__ __forceinline__ uint32_t at(int mt, int r) const { return lane + (uint32_t)((16 * mt + r) * row); }
+    };
+    template <typename T> __device__ __forceinline__ Places<T> places(int stride, int width) const
     {
-        x.load(view, off, width - c);
+        stride = fresh(stride);
+        const uint32_t off = (uint32_t)(4 * (int)((threadIdx.x & 63) >> 4) * stride + c) * (uint32_t)sizeof(T);
+        return {c < width ? off : BufView::OUTSIDE, stride * (int)sizeof(T), width - c};
     }
-    template <typename T, bool PAIRS> __device__ __forceinline__ void store(const BufView &view, uint32_t off, int width, const float (&x)[NT]) const
+    template <typename T, bool PAIRS> __device__ __forceinline__ void load(Ahead<T, NT, PAIRS> &x, const BufView &view, const Places<T> &p, int mt, int r) const
     {
-        store_late<T, NT, PAIRS>(view, off, width - c, x);
+        x.load(view, p.at(mt, r), PAIRS || NT == 1 ? 1 : p.there);
+    }
+    template <typename T, bool PAIRS> __device__ __forceinline__ void store(const BufView &view, const Places<T> &p, int mt, int r, const float (&x)[NT]) const
+    {
+        store_late<T, NT, PAIRS>(view, p.at(mt, r), PAIRS || NT == 1 ? 1 : p.there, x);
     }
 };
+
 // rows 16 mt + 4 q + r of a tile of tokens
 __device__ __forceinline__ int row_of(int mt, int r) { return mt * 16 + 4 * (int)((threadIdx.x & 63) >> 4) + r; }
 __device__ __forceinline__ float4 four(const float *v, int mt) { return *reinterpret_cast<const float4 *>(v + row_of(mt, 0)); }
@@ -67,7 +83,7 @@ template <int NT, int CT> __device__ __forceinline__ void store_state(const v4f_
 template <int NT, int MT> __device__ __forceinline__ void store_tiles(const v4f_t (&x)[MT][NT], float *p, int VP, const Columns<NT> &cols)
 {
     const BufView view(p, (uint32_t)(MT * 16 * VP) * 4u);
-    VP = fresh(VP);
+    const auto places = cols.template places<float>(VP, VP);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -75,7 +91,7 @@ template <int NT, int MT> __device__ __forceinline__ void store_tiles(const v4f_
             float y[NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) y[nt] = x[mt][nt][r];
-            store_late<float, NT, true>(view, cols.at(row_of(mt, r), VP, 4), VP - cols.c, y);
+            cols.template store<float, true>(view, places, mt, r, y);
         }
 }
 
@@ -86,6 +102,49 @@ template <int N, int NT> __device__ __forceinline__ void split_rows(const v4f_t 
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) split_tiles<N>(x[2 * ks][nt], x[2 * ks + 1][nt], f[ks][nt]);
+}
+
+// Products with operands out of LDS.  (Operands read by eight and sixteen ahead of their use were no faster than what the compiler orders: the walks are bound by the reads
+// themselves and by vector instructions.)
+// c += A B: A the 64 rows of a tile of KP columns, B the state's operands
+template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void times_state(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[KP / 32][NT][INNER])
+{
+#pragma unroll
+    for (int c0 = 0; c0 < KP / 32; ++c0)
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+            Frag a[RAW];
+            frags_rows<RAW, KP>(a, tile, CHUNK * KP, mt * 16, c0 * 32);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(c[mt][nt], a, b[c0][nt]);
+        }
+}
+// S += A^T B: A as above, B the operands of 64 rows
+template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void add_to_state(v4f_t (&S)[KP / 16][NT], const bf16_t *tile, const Frag (&b)[2][NT][INNER])
+{
+#pragma unroll
+    for (int ct = 0; ct < KP / 16; ++ct)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            Frag a[RAW];
+            frags_cols<RAW, KP>(a, tile, CHUNK * KP, ks * 32, ct * 16);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, b[ks][nt]);
+        }
+}
+// c += A B: A one of the first pass's matrices, which are zero above the diagonal, or (BACK) its transpose
+template <int N, int PB, bool BACK, int NT> __device__ __forceinline__ void times_triangle(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[2][NT][PB])
+{
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+        for (int ks = BACK ? mt / 2 : 0; ks <= (BACK ? 1 : mt / 2); ++ks) {
+            Frag a[N];
+            if constexpr (BACK) frags_cols<N, CHUNK>(a, tile, CHUNK * CHUNK, ks * 32, mt * 16);
+            else frags_rows<N, CHUNK>(a, tile, CHUNK * CHUNK, mt * 16, ks * 32);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<N, PB>(c[mt][nt], a, b[ks][nt]);
+        }
 }
 
 template <typename T, int KP, bool SHARE> struct Walk {
@@ -108,10 +167,13 @@ __device__ __forceinline__ Stretch stretch_of(const GdArgs &g, const GdLayout &l
         const ChunkAt at = gd_chunk(g, id, l.piece * CHUNK);
         s.seq = at.seq;
         s.place = at.place;
+        s.start = at.start;
+        s.end = at.end;
+    } else {
+        s.start = gd_start(g, s.seq);
+        s.end = gd_start(g, s.seq + 1);
     }
-    s.start = gd_start(g, s.seq);
-    s.end = gd_start(g, s.seq + 1);
-    s.base = gd_base(g, s.seq, CHUNK);
+    s.base = g.starts ? s.start / CHUNK + s.seq : gd_base(g, s.seq, CHUNK);
     const long long chunks = min((long long)(s.end > s.start ? cdiv(s.end - s.start, CHUNK) : 0), l.chunks - s.base);
     s.from = 0;
     s.to = (int)chunks;

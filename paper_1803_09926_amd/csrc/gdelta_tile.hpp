@@ -212,13 +212,17 @@ template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
     }
 };
 
-// One of the first pass's matrices on its way to LDS: parts of 64 x 64, stored in the LDS tiles' order of columns, not turned
+// One of the first pass's matrices, of N parts: zero above the diagonal, and the 32 x 32 block there is neither stored nor read.  A part is 384 pieces of 16 bytes in the
+// LDS tiles' order of columns (not turned): four of each of the first 32 rows, eight of each of the others.
+constexpr int MATRIX_PIECES = 384;
+__device__ __forceinline__ constexpr int matrix_piece(int row, int piece) { return row < 32 ? row * 4 + piece : row * 8 + piece - 128; }
+// ... on its way to LDS
 template <int N, int THREADS> struct Matrix {
-    static constexpr int PER = N * CHUNK * CHUNK / 8 / THREADS;
+    static constexpr int ALL = N * MATRIX_PIECES, PER = (ALL + THREADS - 1) / THREADS;
     u4t_t v[PER];
     __device__ __forceinline__ void load(const char *p)
     {
-        const BufView view(p, N * CHUNK * CHUNK * 2);
+        const BufView view(p, ALL * 16);                 // (beyond it nothing is read)
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] = view.b128((threadIdx.x + i * THREADS) * 16, 0);
     }
@@ -226,8 +230,10 @@ template <int N, int THREADS> struct Matrix {
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = at / (CHUNK / 8);      // rows of all parts, one after the other
-            *reinterpret_cast<u4t_t *>(tile + row * CHUNK + turned<CHUNK>(row, at % (CHUNK / 8)) * 8) = v[i];
+            const int n = threadIdx.x + i * THREADS, part = n / MATRIX_PIECES, at = n % MATRIX_PIECES;
+            const int row = at < 128 ? at / 4 : at / 8 + 16, piece = at < 128 ? at % 4 : at % 8;
+            if (ALL % THREADS == 0 || n < ALL)
+                *reinterpret_cast<u4t_t *>(tile + part * CHUNK * CHUNK + row * CHUNK + turned<CHUNK>(row, piece) * 8) = v[i];
         }
     }
 };
@@ -251,7 +257,7 @@ template <typename T> bool whole_keys(const GdArgs &g)
 
 // ---- chunks of packed sequences ----
 // Sequence s has its chunks at floor(starts[s] / 64) + s and the places behind it: no two sequences share one, and none has to be counted.
-struct ChunkAt { int first, len, seq, place; };      // the first token, how many (0: nothing here), the sequence, the chunk's number in it
+struct ChunkAt { int first, len, seq, place, start, end; };   // the first token, how many (0: nothing here), the sequence, the chunk's number in it, its tokens
 __device__ __forceinline__ int gd_start(const GdArgs &g, int s)
 {
     if (!g.starts) return s * g.length;
@@ -263,22 +269,34 @@ __device__ __forceinline__ int gd_base(const GdArgs &g, int s, int unit)
 {
     return g.starts ? gd_start(g, s) / unit + s : s * cdiv(g.length > 0 ? g.length : 1, unit);
 }
-// (id is the same in a wavefront's 64 lanes, all of which are here: one load for 64 sequences, two for 4096)
+// (id is the same in a wavefront's 64 lanes, all of which are here: up to 63 sequences one load and no other after it, which counts where the memory is busy)
 __device__ __forceinline__ ChunkAt gd_chunk(const GdArgs &g, int id, int unit)
 {
-    int lo = 0, hi = g.sequences;
-    if (!g.starts) lo = min(id / cdiv(g.length > 0 ? g.length : 1, unit), g.sequences - 1);
-    else while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64;
-        const long long at = lo + (long long)step * ((threadIdx.x & 63) + 1);
-        lo += step * __popcll(__ballot(at < hi && gd_base(g, at < hi ? (int)at : lo, unit) <= id));
-        hi = hi - lo > step ? lo + step : hi;
+    int lo = 0, hi = g.sequences, base, start, end;
+    const int lane = threadIdx.x & 63;
+    if (g.starts && hi < 64) {
+        const int mine = gd_start(g, min(lane, hi));
+        lo = max(__popcll(__ballot(lane < hi && mine / unit + lane <= id)) - 1, 0);
+        start = __builtin_amdgcn_readlane(mine, lo);
+        end = __builtin_amdgcn_readlane(mine, lo + 1);
+        base = start / unit + lo;
+    } else {
+        if (!g.starts) lo = min(id / cdiv(g.length > 0 ? g.length : 1, unit), g.sequences - 1);
+        else while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64;
+            const long long at = lo + (long long)step * (lane + 1);
+            lo += step * __popcll(__ballot(at < hi && gd_base(g, at < hi ? (int)at : lo, unit) <= id));
+            hi = hi - lo > step ? lo + step : hi;
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        base = gd_base(g, lo, unit);
+        start = gd_start(g, lo);
+        end = gd_start(g, lo + 1);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    const int place = id - gd_base(g, lo, unit), start = gd_start(g, lo), end = gd_start(g, lo + 1);
+    const int place = id - base;
     const long long first = start + (long long)place * unit;
-    if (place < 0 || first >= end) return {0, 0, lo, place};
-    return {(int)first, (int)min((long long)unit, end - first), lo, place};
+    if (place < 0 || first >= end) return {0, 0, lo, place, start, end};
+    return {(int)first, (int)min((long long)unit, end - first), lo, place, start, end};
 }
 
 }  // namespace
