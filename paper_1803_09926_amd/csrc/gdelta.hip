@@ -74,20 +74,33 @@ size_t backward_bytes(const gdelta_desc *d, const GdLayout &l)
     return (size_t)l.chunks * d->H * (size_t)(l.state + l.rows) + (size_t)l.pieces * d->H * (size_t)l.state + round16((size_t)l.chunks * d->H * 2 * sizeof(float));
 }
 
-// How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole.  Of heads of 128 x 128 in bf16 a chunk of a walk takes 4.2 us, of a
-// piece and its map 7.5 together, both as long as there are no more blocks than compute units, and a piece in the join 3.7.  16384 tokens of 16 heads: 1035 us whole,
-// 308 in pieces; 8 sequences of 1024 tokens of 8 heads 85 and 113.
-int piece_of(const gdelta_desc *d, long long VP, bool packed)
+// How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole: the least of an estimated time, in us.  A chunk of a walk takes 3.8 us
+// and of a piece and its map 5.5 together, both where a compute unit has one block; each more takes 2 us a chunk of each pass; a piece in the join takes 2.7 of 128-wide keys.
+// Lengths that are not known here are taken to be those that points cut at random out of T: the longest is 0.6 + ln n times their mean, and nothing is left idle at the end of a round
+// of blocks.  Measured, whole and in pieces: 16384 tokens of 16 heads of 128 x 128 in one sequence 1035 us and 300, in four 311 and 289, of 4 heads 893 and 165; 24 prompts of 2 to
+// 2000 tokens, 16 heads of 64 x 128, 239 and 200; 8 sequences of 1024 tokens, 8 heads, 85 and 113, so whole; 64 prompts of 256 at the mean 180 and 204, so whole.
+int piece_of(const gdelta_desc *d, const GdLayout &l, bool packed)
 {
     const char *const forced = tune_env("DWCONV_TUNE_GDELTA_PIECE");
     if (forced) return atoi(forced) > 0 ? atoi(forced) : 0;
-    const double chunks = ceil((double)d->T / ((double)d->sequences * TOKENS)), walks = (double)d->sequences * d->H * ((VP + 63) / 64), units = 256;
-    const double piece = ceil(fmax(4, fmax(chunks * walks / (2 * units), sqrt(chunks / 2)))), pieces = ceil(chunks / piece);
-    if (walks < units && pieces >= 2 && 7.5 * piece * fmax(1, pieces * walks / units) + 3.7 * pieces + 10 < 0.8 * 4.2 * chunks) return (int)piece;
-    // Lengths that differ: what is longer than the mean goes in pieces of about that, so that no sequence is walked long after the others (24 prompts of 2 to 2000 tokens, 16 heads
-    // of 64 x 128: 326 us whole, in pieces of 8, 16, 32 chunks 251, 252, 315).
-    const double mean = ceil(1.25 * chunks);
-    return packed && d->sequences > 1 && chunks >= 8 && mean < d->T / (double)TOKENS ? (int)mean : 0;
+    const bool ragged = packed && d->sequences > 1;
+    const double n = d->sequences, chunks = ceil((double)d->T / (n * TOKENS)), longest = ragged ? chunks * (0.6 + log(n)) : chunks, units = 256;
+    const double columns = (double)((l.VP + 63) / 64), all = columns + (double)((l.KP + 63) / 64), join = 1.4 + 1.3 * l.KP / 128.0;
+    auto least = [&](double blocks, double each, double part) {      // us of a pass beyond those of a chunk alone
+        return ragged ? 1.3 * fmax(0, blocks * each * part / units - each) : 2 * each * (ceil(blocks / units) - 1);
+    };
+    double best = 0.92 * (3.8 * longest + least(n * d->H * columns * chunks / longest, longest, 1));
+    int piece = 0;
+    for (long long p = ragged ? 6 : 4; 2 * p <= longest; p = p < 16 ? p + 1 : p * 5 / 4) {
+        const double pieces = n * ceil(chunks / p), mapped = ragged ? (1 + p / chunks) * exp(-p / chunks) : 1;
+        const double blocks = (ragged ? n * chunks / p : pieces) * d->H;
+        const double us = 5.5 * (p + 1) + least(blocks * all, (double)p, mapped) + least(blocks * columns, (double)p, 1) + join * ceil(longest / p) + 4;
+        if (us < best) {
+            best = us;
+            piece = (int)p;
+        }
+    }
+    return piece;
 }
 
 }  // namespace
@@ -104,7 +117,7 @@ GdLayout gdelta_layout(const gdelta_desc *d, bool packed)
     l.vectors = 9 * TOKENS * 4;
     l.state = (long long)l.KP * l.VP * 4;
     l.rows = TOKENS * l.VP * 4;
-    l.piece = d->T == 0 ? 0 : piece_of(d, l.VP, packed);
+    l.piece = d->T == 0 ? 0 : piece_of(d, l, packed);
     l.map = (long long)l.KP * l.KP * 4;
     const long long unit = l.piece * TOKENS;
     l.pieces = !l.piece ? 0 : packed ? d->T / unit + d->sequences : d->sequences * ((length + unit - 1) / unit);

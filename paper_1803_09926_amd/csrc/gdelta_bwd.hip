@@ -12,7 +12,7 @@ namespace dwc {
 namespace {
 
 template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
-__global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, unsigned first,
+__global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, long long first,
                                                                   int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
@@ -21,12 +21,14 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
     float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
-    const unsigned bid = first + blockIdx.x;
-    const int id = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const int share = g.H / g.key_heads;
+    const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
+    if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
+    const int id = (int)(which.item / g.key_heads), kh = (int)(which.item - (long long)id * g.key_heads), h = kh * share + which.block / blocks;
     const Stretch at_ = stretch_of(g, l, id);
     const int start = at_.start, end = at_.end, base = at_.base, from = at_.from, last = at_.to - 1;
     if (at_.place < 0 || (MAP && at_.place == 0)) return;       // (nothing comes before the first piece)
-    const Columns<NT> cols((int)(bid % (unsigned)blocks));
+    const Columns<NT> cols(which.block % blocks);
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const yp = dy + (long long)h * g.V;
 
     v4f_t S[KP / 16][NT];
@@ -163,8 +165,9 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const vo
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT);
-    return gd_launches((l.piece ? l.pieces : (long long)g.sequences) * blocks, THREADS, [&](unsigned first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, (const T *)dy, (T *)dv, first, blocks);
+    const long long items = (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads;
+    return gd_launches(gd_shared_blocks(items, blocks * (g.H / g.key_heads)), THREADS, [&](long long first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now), dim3(THREADS), lds, stream, g, l, s, (const T *)dy, (T *)dv, first, blocks);
     });
 }
 

@@ -546,8 +546,8 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const vo
     const auto kernel = whole_keys<T>(g) && values ? k_gdelta_bwd_rows<T, KP, true, true> : k_gdelta_bwd_rows<T, KP, false, false>;
     const hipError_t e = gd_lds(kernel, C::LDS);
     if (e != hipSuccess) return e;
-    return gd_launches(l.chunks, C::THREADS, [&](unsigned first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(C::THREADS), C::LDS, stream, g, l, s, (const T *)dy, (T *)dq, (T *)dk, (T *)da, (T *)db, first);
+    return gd_launches(l.chunks, C::THREADS, [&](long long first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(C::THREADS), C::LDS, stream, g, l, s, (const T *)dy, (T *)dq, (T *)dk, (T *)da, (T *)db, (unsigned)first);
     });
 }
 

@@ -14,9 +14,20 @@ namespace dwc {
 
 namespace {
 
+// Whether the product of a stretch's decays is zero in fp32, and all of them are numbers
+__device__ __forceinline__ bool a_decay_is_zero(const GdArgs &g, const GdLayout &l, const GdSpace &s, const Stretch &at, int h)
+{
+    float p = 1.f;
+    for (int c = at.from + (int)(threadIdx.x & 63); c < at.to; c += 64)
+        p *= reinterpret_cast<const float *>(s.vec + (((long long)at.base + c) * g.H + h) * l.vectors)[VEC_ONE * 64];
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) p *= __shfl_xor(p, off, 64);
+    return p == 0.f;
+}
+
 template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
 __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
-                                                           float *__restrict__ final, unsigned first, int blocks)
+                                                           float *__restrict__ final, long long first, int blocks)
 {
     typedef Walk<T, KP, SHARE> W;
     constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK;
@@ -24,16 +35,26 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
     bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
     float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
-    const unsigned bid = first + blockIdx.x;
-    const int id = (int)(bid / (unsigned)blocks), h = blockIdx.y, kh = h / (g.H / g.key_heads);
+    const int share = g.H / g.key_heads;
+    const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
+    if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
+    const int id = (int)(which.item / g.key_heads), kh = (int)(which.item - (long long)id * g.key_heads), h = kh * share + which.block / blocks;
+    const int block = which.block % blocks;
     const Stretch at_ = stretch_of(g, l, id);
     const int seq = at_.seq, start = at_.start, end = at_.end, base = at_.base, chunks = at_.to;
     // the last piece's map is not asked for, nor the first one's matrix
     const int values = cdiv(l.VP, WAVES * 16 * NT);
-    const bool unit = MAP && (int)(bid % (unsigned)blocks) >= values;
+    const bool unit = MAP && block >= values;
     if (at_.place < 0 || (MAP && (at_.place == at_.pieces - 1 || (unit && at_.place == 0)))) return;
-    const Columns<NT> cols((int)(bid % (unsigned)blocks) - (unit ? values : 0));
+    const Columns<NT> cols(block - (unit ? values : 0));
     const T *const kp = (const T *)g.k + (long long)kh * g.K, *const qp = (const T *)g.q + (long long)kh * g.K, *const vp = (const T *)g.v + (long long)h * g.V;
+
+    if (unit && g.norm && g.sigmoid && a_decay_is_zero(g, l, s, at_, h)) {
+        // keys of length one and rates below one: no product of the piece's factors is larger than its decays, and those are zero
+        v4f_t none[KP / 16][NT] = {};
+        store_tiles<NT, KP / 16>(none, s.maps + ((long long)id * g.H + h) * (l.map / 4), KP, cols);
+        return;
+    }
 
     v4f_t S[KP / 16][NT];
     const long long state = ((long long)seq * g.H + h) * g.K * g.V;
@@ -250,8 +271,9 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const fl
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT) + (MAP ? cdiv(KP, WAVES * 16 * NT) : 0);
-    return gd_launches((l.piece ? l.pieces : (long long)g.sequences) * blocks, THREADS, [&](unsigned first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, init, (T *)y, final, first, blocks);
+    const long long items = (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads;
+    return gd_launches(gd_shared_blocks(items, blocks * (g.H / g.key_heads)), THREADS, [&](long long first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now), dim3(THREADS), lds, stream, g, l, s, init, (T *)y, final, first, blocks);
     });
 }
 

@@ -1,112 +1,112 @@
 // The gated delta rule, long sequences in pieces: the states that the pieces begin with (forward), or the gradients of those that they end with (backward).
 //
-// A piece makes M S + N of the state S before it; N lies in `ends`, M in `maps`.  A block has 64 columns of a sequence's head, 16 a wavefront, and goes from piece to
-// piece: S <- M S + N, each S put in the place of the N that it is added to.  Backward S <- M^T S + N from the last piece to the first.  The matrix goes through LDS by
-// 64 rows (backward 64 columns of them), the next ones on their way meanwhile.
-#include "gdelta_states.hpp"
+// A piece makes M S + N of the state S before it; N lies in `ends`, M in `maps`.  A block has 16 columns of a sequence's head and goes from piece to piece:
+// S <- M S + N, each S put in the place of the N that it is added to; backward S <- M^T S + N from the last piece to the first.  A wavefront has 32 rows: of the matrix
+// it reads its own straight into operands, the next piece's on their way meanwhile, and its rows of S it hands to the others through LDS as operands, which they are as they
+// lie.  Bound by the way round: 15 pieces of 128 x 128 in 16 heads 42 us, where blocks of 64 columns that staged the matrix in LDS took 54.
+#include "gdelta_tile.hpp"
+#include "gdelta_launch.hpp"
 
 namespace dwc {
 
 namespace {
 
 template <int KP, int N, bool BACK>
-__global__ __launch_bounds__(THREADS, 1) void k_gdelta_join(GdArgs g, GdLayout l, GdSpace s, unsigned first, int blocks)
+__global__ __launch_bounds__(2 * KP, 1) void k_gdelta_join(GdArgs g, GdLayout l, GdSpace s, long long first, int blocks)
 {
-    constexpr int ROWS = KP < 64 ? KP : 64;              // of the matrix, at a time
-    constexpr int PLANE = ROWS * KP, PER = ROWS * KP / 8 / THREADS > 0 ? ROWS * KP / 8 / THREADS : 1;
-    extern __shared__ __align__(16) char lds[];
-    bf16_t *const tile = reinterpret_cast<bf16_t *>(lds);
-    const unsigned bid = first + blockIdx.x;
-    const int seq = (int)(bid / (unsigned)blocks), h = blockIdx.y;
-    const Columns<1> cols((int)(bid % (unsigned)blocks));
+    constexpr int GROUPS = KP / 32;                      // of 32 rows: one a wavefront
+    __shared__ u4t_t handed[2][GROUPS][N][64];
+    const Shared which = gd_shared(first + blockIdx.x, (unsigned)blocks);
+    if (which.item >= (long long)g.sequences * g.H) return;
+    const int seq = (int)(which.item / g.H), h = (int)(which.item - (long long)seq * g.H), w = wave_number(), lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    const int col = which.block * 16 + m;
     const int unit = l.piece * CHUNK, start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq, unit);
     const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - gd_base(g, seq, CHUNK));
     const int pieces = (int)min((long long)(chunks > 0 ? cdiv((int)chunks, l.piece) : 0), l.pieces - base);
     if (pieces < 2) return;
-    auto ends = [&](int p) { return s.ends + (((long long)base + p) * g.H + h) * (l.state / 4); };
-    auto maps = [&](int p) { return s.maps + (((long long)base + p) * g.H + h) * (l.map / 4); };
-    // forward: the state behind piece p, p = 0 .. pieces - 2, is what piece p + 1 begins with; backward: the gradient before piece p, p = pieces - 1 .. 1, piece p - 1's
-    v4f_t S[KP / 16][1], next[KP / 16][1];
-    const int begin = BACK ? pieces - 1 : 0, stop = BACK ? 1 : pieces - 2, step = BACK ? -1 : 1;
-    load_state<1, KP / 16>(S, ends(begin), KP, l.VP, cols);
-    u4t_t ahead[PER][2];
-    // (the rows of M are contracted forward, its columns backward: rows of it in LDS either way)
-    auto ask = [&](int p, int r0) {
-        const BufView view(maps(p), (uint32_t)l.map);
+    auto ends = [&](int p) { return BufView(s.ends + (((long long)base + p) * g.H + h) * (l.state / 4), (uint32_t)l.state); };
+    v4f_t S[2], next[2];
+    auto load = [&](v4f_t (&x)[2], int p) {
+        const BufView view = ends(p);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int n = threadIdx.x + i * THREADS;
-            const uint32_t off = n < ROWS * KP / 8 ? (uint32_t)((r0 + n / (KP / 8)) * KP + n % (KP / 8) * 8) * 4u : BufView::OUTSIDE;
-            ahead[i][0] = view.b128(off, 0);
-            ahead[i][1] = view.b128(off + 16, 0);
-        }
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = __uint_as_float(view.b32((uint32_t)((w * 32 + t * 16 + 4 * q + r) * l.VP + col) * 4u, 0));
     };
+    auto store = [&](const v4f_t (&x)[2], int p) {
+        const BufView view = ends(p);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) view.st32<false>(__float_as_uint(x[t][r]), (uint32_t)((w * 32 + t * 16 + 4 * q + r) * l.VP + col) * 4u, 0);
+    };
+    // the wavefront's 32 rows of the matrix (backward: of its transpose), eight numbers of a row for each operand
+    v4f_t M[2][GROUPS][2];
+    auto ask = [&](int p) {
+        const BufView view(s.maps + (((long long)base + p) * g.H + h) * (l.map / 4), (uint32_t)l.map);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < GROUPS; ++c)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int row = w * 32 + t * 16 + m, k = c * 32 + i * 16 + 4 * q;
+                    if constexpr (!BACK) M[t][c][i] = __builtin_bit_cast(v4f_t, view.b128((uint32_t)(row * KP + k) * 4u, 0));
+                    else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) M[t][c][i][r] = __uint_as_float(view.b32((uint32_t)((k + r) * KP + row) * 4u, 0));
+                    }
+                }
+    };
+    // forward: the state behind piece p, p = 0 .. pieces - 2, is what piece p + 1 begins with; backward: the gradient before piece p, p = pieces - 1 .. 1, piece p - 1's
+    const int begin = BACK ? pieces - 1 : 0, stop = BACK ? 1 : pieces - 2, step = BACK ? -1 : 1;
+    load(S, begin);
     if (begin != stop) {
-        ask(begin + step, 0);
-        load_state<1, KP / 16>(next, ends(begin + step), KP, l.VP, cols);
+        ask(begin + step);
+        load(next, begin + step);
     }
-    for (int p = begin; p != stop; p += step) {
+    int turn = 0;
+    for (int p = begin; p != stop; p += step, turn ^= 1) {
         const int to = p + step;
-        store_tiles<1, KP / 16>(S, ends(to), l.VP, cols);
-        Frag f[KP / 32][N];
+        store(S, to);
+        Frag f[GROUPS][N];
+        split_tiles<N>(S[0], S[1], f[0]);
 #pragma unroll
-        for (int c = 0; c < KP / 32; ++c) split_tiles<N>(S[2 * c][0], S[2 * c + 1][0], f[c]);
+        for (int i = 0; i < N; ++i) handed[turn][w][i][lane] = f[0][i].w;
+        __syncthreads();                                 // (who writes to the other half next has read this one two barriers before)
 #pragma unroll
-        for (int r0 = 0; r0 < KP; r0 += ROWS) {
-            __syncthreads();
+        for (int c = 0; c < GROUPS; ++c)
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int n = threadIdx.x + i * THREADS;
-                float x[8];
+            for (int i = 0; i < N; ++i) f[c][i].w = handed[turn][c][i][lane];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(ahead[i][j / 4][j % 4]);
-                if (n < ROWS * KP / 8) put8<N, KP>(tile, PLANE, n / (KP / 8), n % (KP / 8) * 8, x);
-            }
-            if (r0 + ROWS < KP) ask(to, r0 + ROWS);
-            else if (to != stop) ask(to + step, 0);
-            __syncthreads();
-            if constexpr (!BACK) {
+        for (int t = 0; t < 2; ++t) {
+            S[t] = next[t];
 #pragma unroll
-                for (int c = 0; c < KP / 32; ++c)
-#pragma unroll
-                    for (int t = 0; t < ROWS / 16; ++t) {
-                        Frag a[N];
-                        frags_rows<N, KP>(a, tile, PLANE, t * 16, c * 32);
-                        mma<N, N>(next[r0 / 16 + t][0], a, f[c]);
-                    }
-            } else {
-#pragma unroll
-                for (int c = 0; c < ROWS / 32; ++c)
-#pragma unroll
-                    for (int t = 0; t < KP / 16; ++t) {
-                        Frag a[N];
-                        frags_cols<N, KP>(a, tile, PLANE, c * 32, t * 16);
-                        mma<N, N>(next[t][0], a, f[r0 / 32 + c]);
-                    }
+            for (int c = 0; c < GROUPS; ++c) {
+                Frag a[N];
+                split_tiles<N>(M[t][c][0], M[t][c][1], a);
+                mma<N, N>(S[t], a, f[c]);
             }
         }
-#pragma unroll
-        for (int t = 0; t < KP / 16; ++t) S[t][0] = next[t][0];
-        if (to != stop) load_state<1, KP / 16>(next, ends(to + step), KP, l.VP, cols);
+        if (to != stop) {
+            ask(to + step);
+            load(next, to + step);
+        }
     }
-    store_tiles<1, KP / 16>(S, ends(stop + step), l.VP, cols);
+    store(S, stop + step);
 }
 
-template <int KP, int N, bool BACK> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
+template <int KP, int N> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
 {
-    constexpr size_t lds = (size_t)N * (KP < 64 ? KP : 64) * KP * 2;
-    const auto kernel = k_gdelta_join<KP, N, BACK>;
-    const hipError_t e = gd_lds(kernel, lds);
-    if (e != hipSuccess) return e;
-    const int blocks = cdiv(l.VP, WAVES * 16);
-    return gd_launches((long long)g.sequences * blocks, THREADS, [&](unsigned first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.H), dim3(THREADS), lds, stream, g, l, s, first, blocks);
+    const int blocks = l.VP / 16;
+    return gd_launches(gd_shared_blocks((long long)g.sequences * g.H, blocks), 2 * KP, [&](long long first, unsigned now) {
+        if (backward) hipLaunchKernelGGL((k_gdelta_join<KP, N, true>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
+        else hipLaunchKernelGGL((k_gdelta_join<KP, N, false>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
     });
 }
 template <int KP> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
 {
-    if (l.inner == 2) return backward ? launch<KP, 2, true>(g, l, s, stream) : launch<KP, 2, false>(g, l, s, stream);
-    return backward ? launch<KP, 3, true>(g, l, s, stream) : launch<KP, 3, false>(g, l, s, stream);
+    return l.inner == 2 ? launch<KP, 2>(g, l, s, backward, stream) : launch<KP, 3>(g, l, s, backward, stream);
 }
 
 }  // namespace

@@ -301,8 +301,8 @@ template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout 
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
-    return gd_launches(l.chunks, THREADS, [&](unsigned first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(THREADS), lds, stream, g, s.T, s.P, s.vec, l.matrix, l.vectors, first);
+    return gd_launches(l.chunks, THREADS, [&](long long first, unsigned now) {
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(THREADS), lds, stream, g, s.T, s.P, s.vec, l.matrix, l.vectors, (unsigned)first);
     });
 }
 

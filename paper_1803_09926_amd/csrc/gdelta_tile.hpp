@@ -24,12 +24,21 @@ typedef uint32_t u2t_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 
-// `blocks` workgroups in launches that each have fewer than 2^32 lanes: f(the first, how many)
+// `blocks` workgroups in launches that each have fewer than 2^32 lanes: f(the first (64 bits), how many)
 template <typename F> hipError_t gd_launches(long long blocks, int threads, F f)
 {
     const long long most = most_blocks(threads);
-    for (long long first = 0; first < blocks; first += most) f((unsigned)first, (unsigned)(blocks - first < most ? blocks - first : most));
+    for (long long first = 0; first < blocks; first += most) f(first, (unsigned)(blocks - first < most ? blocks - first : most));
     return hipGetLastError();
+}
+// Blocks that read the same rows, `blocks` of each of `items`, lie on one of the eight XCDs, whose L2 they share, and run close in time: the dispatcher hands blocks to the
+// XCDs in turn.  The number of a launch's blocks; the item and the number in it of one of them (item may be behind the last one).
+inline long long gd_shared_blocks(long long items, int blocks) { return (items + 7) / 8 * 8 * blocks; }
+struct Shared { long long item; int block; };
+__device__ __forceinline__ Shared gd_shared(unsigned long long n, unsigned blocks)
+{
+    const unsigned long long group = n / (8 * blocks);
+    return {(long long)(group * 8 + n % 8), (int)((n - group * (8 * blocks)) / 8)};
 }
 // more LDS than a launch has without being told
 template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
