@@ -112,8 +112,7 @@ GdLayout gdelta_layout(const gdelta_desc *d, bool packed)
     l.chunks = d->T == 0 ? 0 : packed ? d->T / TOKENS + d->sequences : d->sequences * ((length + TOKENS - 1) / TOKENS);
     l.KP = d->K <= 32 ? 32 : d->K <= 64 ? 64 : d->K <= 128 ? 128 : 256;
     l.VP = cdiv(d->V, 32) * 32;
-    l.inner = d->dtype == DWCONV_F32 ? 3 : 2;
-    l.matrix = l.inner * 384 * 16;                // (MATRIX_PIECES)
+    l.matrix = 3 * 384 * 16;                      // (INNER * MATRIX_PIECES)
     l.vectors = 9 * TOKENS * 4;
     l.state = (long long)l.KP * l.VP * 4;
     l.rows = TOKENS * l.VP * 4;
@@ -186,7 +185,7 @@ int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
     if (desc->T == 0 && !t->final) return DWCONV_OK;
     const GdArgs g = args_of(desc, t);
     hipError_t e = hipSuccess;
-    if (desc->T > 0) e = launch_gdelta_prep(desc->dtype, g, l, s, (hipStream_t)stream);
+    if (desc->T > 0) e = launch_gdelta_prep(desc->dtype, g, l, s, (const float *)t->final, (hipStream_t)stream);
     if (e == hipSuccess) e = launch_gdelta_fwd(desc->dtype, g, l, s, (const float *)t->init, t->y, (float *)t->final, (hipStream_t)stream);
     return e == hipSuccess ? DWCONV_OK : DWCONV_ERR_LAUNCH;
 }

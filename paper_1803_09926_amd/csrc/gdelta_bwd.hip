@@ -11,16 +11,17 @@ namespace dwc {
 
 namespace {
 
-template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
+template <typename T, int KP, int NT, bool WHOLE, bool MAP>
 __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_bwd_states(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dv, long long first,
                                                                   int blocks)
 {
-    typedef Walk<T, KP, SHARE> W;
-    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK;
+    typedef Walk<T, KP, true, 2 * INNER> W;
+    constexpr int RAW = W::RAW;
+    constexpr bool SHARE = W::SHARE;
     extern __shared__ __align__(16) char lds[];
-    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
-    bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
-    float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * CHUNK * KP;
+    bf16_t *const tm = qt + RAW * CHUNK * KP, *const pm = tm + INNER * MATRIX_PLANE;
+    float *const vecs = reinterpret_cast<float *>(pm + INNER * MATRIX_PLANE);       // two chunks' worth, in turn
     const int share = g.H / g.key_heads;
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
     if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
         if (SHARE && c < last) __syncthreads();
-        rows.template put<LD>(kt);
+        rows.template put<KP>(kt);
         matrix.put(tm);
         second.put(pm);
         vl[threadIdx.x] = vec_next;
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             for (int c0 = 0; c0 < KP / 32; ++c0)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c0][nt], S[2 * c0 + 1][nt], p[c0][nt]);
-            times_state<RAW, INNER, NT, KP>(U, kt, p);
+            times_state<RAW, INNER, KP>(U, kt, p);
         }
         {
             v4f_t d[4][NT];
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
                 }
             }
             split_rows<RAW, NT>(d, b);
-            times_triangle<INNER, RAW, true, NT>(U, pm, b);
+            times_triangle<INNER, true>(U, pm, b);
         }
         // X
         split_rows<INNER, NT>(U, f);
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) X[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-        times_triangle<INNER, INNER, true, NT>(X, tm, f);
+        times_triangle<INNER, true>(X, tm, f);
         if (!MAP) store_tiles<NT, 4>(X, s.X + where * (l.rows / 4), l.VP, cols);
         const auto places = cols.template places<T>((int)g.v_stride, g.V);
         const BufView out = rows_view(dv + at * g.v_stride + (long long)h * g.V, g.v_stride, len, g.V);
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
-        add_to_state<RAW, INNER, NT, KP>(S, kt, f);
+        add_to_state<RAW, KP>(S, kt, f);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 ask = four(vl + VEC_ASK * 64, mt);
@@ -146,10 +147,10 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         }
         split_rows<INNER, NT>(X, f);
         if constexpr (SHARE) __syncthreads();
-        rows.template put<LD>(qt);
+        rows.template put<KP>(qt);
         if (c > from) load_keys(c - 1);
         __syncthreads();
-        add_to_state<RAW, INNER, NT, KP>(S, qt, f);
+        add_to_state<RAW, KP>(S, qt, f);
     }
     if constexpr (MAP) store_tiles<NT, KP / 16>(S, s.ends + piece * (l.state / 4), l.VP, cols);
 }
@@ -157,11 +158,10 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 template <typename T, int KP, int NT, bool MAP>
 hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream)
 {
-    constexpr bool SHARE = shares<T, KP>();
-    constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
+    constexpr size_t lds = Walk<T, KP, true, 2 * INNER>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const bool whole = whole_keys<T>(g) && (NT == 1 || pair_values<T>(g, dy, dv, g.y_stride, g.v_stride));
-    const auto kernel = whole ? k_gdelta_bwd_states<T, KP, NT, SHARE, true, MAP> : k_gdelta_bwd_states<T, KP, NT, SHARE, false, MAP>;
+    const auto kernel = whole ? k_gdelta_bwd_states<T, KP, NT, true, MAP> : k_gdelta_bwd_states<T, KP, NT, false, MAP>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT);
@@ -176,7 +176,7 @@ template <typename T, int KP> hipError_t walk(const GdArgs &g, const GdLayout &l
 {
     if (l.piece) {
         hipError_t e = launch<T, KP, 1, true>(g, l, s, dy, dv, stream);
-        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, true, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, INNER, true, stream);
         if (e != hipSuccess) return e;
     }
     if constexpr (KP < 256) {

@@ -6,6 +6,8 @@
 // all as products on the matrix cores: S, V, U and Y never leave the registers, as a result tile is an operand as it lies; K, Q, T and P go through LDS, and the next ones
 // are on their way from memory meanwhile.
 //
+// EXACT: what leaves the walk in fp32, the states behind sequences or what a backward pass takes, is made of three parts; where nothing does, of as many as the answers.
+//
 // MAP: the map of a piece of a sequence instead (gdelta_launch.hpp).  What it makes of zero (of the state that the sequence begins with, in the first piece) is the walk without
 // answers, and its matrix is what the walk without values makes of the K unit vectors: K columns more.
 #include "gdelta_states.hpp"
@@ -25,16 +27,19 @@ __device__ __forceinline__ bool a_decay_is_zero(const GdArgs &g, const GdLayout 
     return p == 0.f;
 }
 
-template <typename T, int KP, int NT, bool SHARE, bool WHOLE, bool MAP>
+template <typename T, int KP, bool MAP, bool EXACT> using WalkOf = Walk<T, KP, !MAP, (EXACT ? INNER : PartsOf<T>::LAST) + (MAP ? 0 : PartsOf<T>::LAST)>;
+
+template <typename T, int KP, int NT, bool WHOLE, bool MAP, bool EXACT>
 __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
                                                            float *__restrict__ final, long long first, int blocks)
 {
-    typedef Walk<T, KP, SHARE> W;
-    constexpr int RAW = W::RAW, INNER = W::INNER, LD = W::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK;
+    typedef WalkOf<T, KP, MAP, EXACT> W;
+    constexpr int RAW = W::RAW, LAST = PartsOf<T>::LAST, N = EXACT ? INNER : LAST;
+    constexpr bool SHARE = W::SHARE;
     extern __shared__ __align__(16) char lds[];
-    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE ? kt : kt + RAW * PLANE;
-    bf16_t *const tm = qt + RAW * PLANE, *const pm = tm + INNER * PLANE_M;
-    float *const vecs = reinterpret_cast<float *>(pm + INNER * PLANE_M);            // two chunks' worth, in turn
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE || MAP ? kt : kt + RAW * CHUNK * KP;
+    bf16_t *const tm = qt + RAW * CHUNK * KP, *const pm = tm + N * MATRIX_PLANE;
+    float *const vecs = reinterpret_cast<float *>(pm + (MAP ? 0 : LAST) * MATRIX_PLANE);     // two chunks' worth, in turn
     const int share = g.H / g.key_heads;
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
     if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
@@ -69,17 +74,18 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[ct][nt][r] = unit && row_of(ct, r) == cols.c + nt ? 1.f : 0.f;
     }
-    Frag Sp[KP / 32][NT][INNER];
+    Frag Sp[KP / 32][NT][N];
     auto split_state = [&] {
 #pragma unroll
         for (int c = 0; c < KP / 32; ++c)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) split_tiles<INNER>(S[2 * c][nt], S[2 * c + 1][nt], Sp[c][nt]);
+            for (int nt = 0; nt < NT; ++nt) split_tiles<N>(S[2 * c][nt], S[2 * c + 1][nt], Sp[c][nt]);
     };
     split_state();
 
     Rows<T, KP, THREADS, WHOLE> rows;
-    Matrix<INNER, THREADS> matrix;
+    Matrix<N, THREADS> matrix;
+    Matrix<LAST, THREADS> answers;
     Ahead<T, NT, WHOLE> v[4][4];
     float vec_next, decay_next;
     int bad_next;
@@ -111,7 +117,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         const long long where = ((long long)base + c) * g.H + h;
         float *const vl = vecs + (c & 1) * 256;
         if ((SHARE || MAP) && c > at_.from) __syncthreads();
-        rows.template put<LD>(kt);
+        rows.template put<KP>(kt);
         matrix.put(tm);
         vl[threadIdx.x] = vec_next;
         const float decay = decay_next;
@@ -120,7 +126,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             if (c + 1 < chunks) load_next(c + 1);
         } else {
             rows.load(qp + at * g.q_stride, g.q_stride, len, g.K);
-            matrix.load(s.P + where * l.matrix);
+            answers.load(s.P + where * l.matrix);
         }
         __syncthreads();
         if (!MAP && s.S) store_tiles<NT, KP / 16>(S, s.S + where * (l.state / 4), l.VP, cols);
@@ -155,7 +161,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) R[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-        times_state<RAW, INNER, NT, KP>(R, kt, Sp);
+        times_state<RAW, N, KP>(R, kt, Sp);
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 read = four(vl + VEC_READ * 64, mt), beta = four(vl + VEC_BETA * 64, mt);
@@ -175,14 +181,14 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
                     for (int r = 0; r < 4; ++r)
                         if (row_of(mt, r) >= from[nt]) R[mt][nt][r] = 0.f;
         }
-        Frag f[2][NT][INNER];
-        split_rows<INNER, NT>(R, f);
+        Frag f[2][NT][N];
+        split_rows<N, NT>(R, f);
         v4f_t U[4][NT];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-        times_triangle<INNER, INNER, false, NT>(U, tm, f);
+        times_triangle<N, false>(U, tm, f);
         if (!MAP && s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
         v4f_t w[4][NT];
 #pragma unroll
@@ -191,37 +197,38 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) w[mt][nt] = times(U[mt][nt], write);
         }
-        split_rows<INNER, NT>(w, f);
+        split_rows<N, NT>(w, f);
 #pragma unroll
         for (int ct = 0; ct < KP / 16; ++ct)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[ct][nt] *= decay;
-        add_to_state<RAW, INNER, NT, KP>(S, kt, f);
+        add_to_state<RAW, KP>(S, kt, f);
         v4f_t O[4][NT];
         if constexpr (MAP) {
             if (c + 1 < chunks) load_values(c + 1);
         } else {
             if constexpr (SHARE) __syncthreads();
-            rows.template put<LD>(qt);
-            matrix.put(pm);
+            rows.template put<KP>(qt);
+            answers.put(pm);
             if (c + 1 < chunks) {
                 load_next(c + 1);
                 load_values(c + 1);
             }
             __syncthreads();
-            split_rows<INNER, NT>(U, f);
+            Frag u[2][NT][LAST];
+            split_rows<LAST, NT>(U, u);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-            times_state<RAW, INNER, NT, KP>(O, qt, Sp);
+            times_state<RAW, LAST, KP>(O, qt, Sp);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
                 const float4 ask = four(vl + VEC_ASK * 64, mt);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
             }
-            times_triangle<INNER, INNER, false, NT>(O, pm, f);
+            times_triangle<LAST, false>(O, pm, u);
         }
         if (odd) {
             seldom();
@@ -260,14 +267,13 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     } else if (final && at_.place == at_.pieces - 1) store_state<NT, KP / 16>(S, final + state, g.K, g.V, cols);
 }
 
-template <typename T, int KP, int NT, bool MAP>
+template <typename T, int KP, int NT, bool MAP, bool EXACT>
 hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    constexpr bool SHARE = shares<T, KP>();
-    constexpr size_t lds = Walk<T, KP, SHARE>::LDS;
+    constexpr size_t lds = WalkOf<T, KP, MAP, EXACT>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const bool whole = whole_keys<T>(g) && (NT == 1 || pair_values<T>(g, g.v, y, g.v_stride, g.y_stride));
-    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, SHARE, true, MAP> : k_gdelta_fwd<T, KP, NT, SHARE, false, MAP>;
+    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, true, MAP, EXACT> : k_gdelta_fwd<T, KP, NT, false, MAP, EXACT>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT) + (MAP ? cdiv(KP, WAVES * 16 * NT) : 0);
@@ -278,27 +284,27 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const fl
 }
 
 // The walk; where sequences go in pieces their maps first, and the states that they begin with
-template <typename T, int KP>
+template <typename T, int KP, bool EXACT>
 hipError_t walk(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
     if (l.piece) {
-        hipError_t e = launch<T, KP, 1, true>(g, l, s, init, y, final, stream);
-        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, false, stream);
+        hipError_t e = launch<T, KP, 1, true, EXACT>(g, l, s, init, y, final, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, EXACT ? INNER : PartsOf<T>::LAST, false, stream);
         if (e != hipSuccess) return e;
     }
     if constexpr (KP < 256) {
-        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false>(g, l, s, init, y, final, stream);
+        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false, EXACT>(g, l, s, init, y, final, stream);
     }
-    return launch<T, KP, 1, false>(g, l, s, init, y, final, stream);
+    return launch<T, KP, 1, false, EXACT>(g, l, s, init, y, final, stream);
 }
 
-template <typename T> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+template <typename T, bool EXACT> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
     switch (l.KP) {
-    case 32: return walk<T, 32>(g, l, s, init, y, final, stream);
-    case 64: return walk<T, 64>(g, l, s, init, y, final, stream);
-    case 128: return walk<T, 128>(g, l, s, init, y, final, stream);
-    default: return walk<T, 256>(g, l, s, init, y, final, stream);
+    case 32: return walk<T, 32, EXACT>(g, l, s, init, y, final, stream);
+    case 64: return walk<T, 64, EXACT>(g, l, s, init, y, final, stream);
+    case 128: return walk<T, 128, EXACT>(g, l, s, init, y, final, stream);
+    default: return walk<T, 256, EXACT>(g, l, s, init, y, final, stream);
     }
 }
 
@@ -306,7 +312,8 @@ template <typename T> hipError_t walk_of(const GdArgs &g, const GdLayout &l, con
 
 hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    return dtype == DWCONV_F32 ? walk_of<float>(g, l, s, init, y, final, stream) : walk_of<bf16_t>(g, l, s, init, y, final, stream);
+    if (dtype == DWCONV_F32) return walk_of<float, true>(g, l, s, init, y, final, stream);
+    return gd_exact(s, final) ? walk_of<bf16_t, true>(g, l, s, init, y, final, stream) : walk_of<bf16_t, false>(g, l, s, init, y, final, stream);
 }
 
 }  // namespace dwc

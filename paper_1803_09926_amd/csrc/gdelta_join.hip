@@ -104,20 +104,21 @@ template <int KP, int N> hipError_t launch(const GdArgs &g, const GdLayout &l, c
         else hipLaunchKernelGGL((k_gdelta_join<KP, N, false>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
     });
 }
-template <int KP> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
+
+template <int KP> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream)
 {
-    return l.inner == 2 ? launch<KP, 2>(g, l, s, backward, stream) : launch<KP, 3>(g, l, s, backward, stream);
+    return parts == 2 ? launch<KP, 2>(g, l, s, backward, stream) : launch<KP, 3>(g, l, s, backward, stream);
 }
 
 }  // namespace
 
-hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
+hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream)
 {
     switch (l.KP) {
-    case 32: return launch_of<32>(g, l, s, backward, stream);
-    case 64: return launch_of<64>(g, l, s, backward, stream);
-    case 128: return launch_of<128>(g, l, s, backward, stream);
-    default: return launch_of<256>(g, l, s, backward, stream);
+    case 32: return launch_of<32>(g, l, s, parts, backward, stream);
+    case 64: return launch_of<64>(g, l, s, parts, backward, stream);
+    case 128: return launch_of<128>(g, l, s, parts, backward, stream);
+    default: return launch_of<256>(g, l, s, parts, backward, stream);
     }
 }
 

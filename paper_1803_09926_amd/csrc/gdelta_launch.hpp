@@ -10,7 +10,6 @@ namespace dwc {
 struct GdLayout {
     long long chunks;                            // that packed sequences may have at most; some may hold nothing
     int KP, VP;                                  // K up to a power of two of 32 and more, V up to a multiple of 32
-    int inner;                                   // parts that a number is split into (gdelta_tile.hpp)
     long long matrix, vectors, state, rows;      // T or P (all parts); vectors; [KP][VP] and [64][VP] of fp32
     // Where sequences and heads are too few to fill the card, a sequence is walked in pieces of `piece` chunks at once (0: it is not): what a piece makes of a state
     // is an affine map, found by a walk of its own, and the pieces' maps are joined in turn.  `pieces` is their number at most; the map's matrix is [KP][KP] of fp32.
@@ -27,10 +26,12 @@ struct GdSpace {
 };
 
 hipError_t launch_gdelta_step(int dtype, const GdArgs &g, const int32_t *slots, float *state, void *y, hipStream_t stream);
-hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream);
+// Whether the walk forward leaves anything in fp32
+inline bool gd_exact(const GdSpace &s, const float *final) { return s.S || final; }
+hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *final, hipStream_t stream);
 hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream);
 // the states that the pieces begin with, out of what they make of zero and of their matrices; backward: of the gradients, from the last piece to the first
-hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream);
+hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream);
 hipError_t launch_gdelta_bwd_states(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream);
 hipError_t launch_gdelta_bwd_rows(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dq, void *dk, void *da, void *db,
                                   hipStream_t stream);

@@ -107,7 +107,7 @@ template <int N, int NT> __device__ __forceinline__ void split_rows(const v4f_t 
 // Products with operands out of LDS.  (Operands read by eight and sixteen ahead of their use were no faster than what the compiler orders: the walks are bound by the reads
 // themselves and by vector instructions.)
 // c += A B: A the 64 rows of a tile of KP columns, B the state's operands
-template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void times_state(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[KP / 32][NT][INNER])
+template <int RAW, int PB, int KP, int NT, int NB> __device__ __forceinline__ void times_state(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[KP / 32][NT][NB])
 {
 #pragma unroll
     for (int c0 = 0; c0 < KP / 32; ++c0)
@@ -116,11 +116,11 @@ template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void ti
             Frag a[RAW];
             frags_rows<RAW, KP>(a, tile, CHUNK * KP, mt * 16, c0 * 32);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(c[mt][nt], a, b[c0][nt]);
+            for (int nt = 0; nt < NT; ++nt) mma<RAW, PB>(c[mt][nt], a, b[c0][nt]);
         }
 }
 // S += A^T B: A as above, B the operands of 64 rows
-template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void add_to_state(v4f_t (&S)[KP / 16][NT], const bf16_t *tile, const Frag (&b)[2][NT][INNER])
+template <int RAW, int KP, int NT, int NB> __device__ __forceinline__ void add_to_state(v4f_t (&S)[KP / 16][NT], const bf16_t *tile, const Frag (&b)[2][NT][NB])
 {
 #pragma unroll
     for (int ct = 0; ct < KP / 16; ++ct)
@@ -129,31 +129,31 @@ template <int RAW, int INNER, int NT, int KP> __device__ __forceinline__ void ad
             Frag a[RAW];
             frags_cols<RAW, KP>(a, tile, CHUNK * KP, ks * 32, ct * 16);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<RAW, INNER>(S[ct][nt], a, b[ks][nt]);
+            for (int nt = 0; nt < NT; ++nt) mma<RAW, NB>(S[ct][nt], a, b[ks][nt]);
         }
 }
 // c += A B: A one of the first pass's matrices, which are zero above the diagonal, or (BACK) its transpose
-template <int N, int PB, bool BACK, int NT> __device__ __forceinline__ void times_triangle(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[2][NT][PB])
+template <int N, bool BACK, int PB, int NT> __device__ __forceinline__ void times_triangle(v4f_t (&c)[4][NT], const bf16_t *tile, const Frag (&b)[2][NT][PB])
 {
 #pragma unroll
     for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
         for (int ks = BACK ? mt / 2 : 0; ks <= (BACK ? 1 : mt / 2); ++ks) {
             Frag a[N];
-            if constexpr (BACK) frags_cols<N, CHUNK>(a, tile, CHUNK * CHUNK, ks * 32, mt * 16);
-            else frags_rows<N, CHUNK>(a, tile, CHUNK * CHUNK, mt * 16, ks * 32);
+            if constexpr (BACK) matrix_cols(a, tile, ks * 32, mt * 16);
+            else matrix_rows(a, tile, mt * 16, ks * 32);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma<N, PB>(c[mt][nt], a, b[ks][nt]);
         }
 }
 
-template <typename T, int KP, bool SHARE> struct Walk {
-    static constexpr int RAW = PartsOf<T>::RAW, INNER = PartsOf<T>::INNER, LD = KP;
-    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * CHUNK * 2;
-    static constexpr size_t LDS = (SHARE ? 1 : 2) * TILE + 2 * MATRIX + 2 * 256 * 4;
+// What a walk has in LDS: the keys' tile and (OTHER) the queries', which shares its place where both do not fit; so many parts of T and of P; two chunks' vectors
+template <typename T, int KP, bool OTHER, int PARTS> struct Walk {
+    static constexpr int RAW = PartsOf<T>::RAW;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * KP * 2, REST = (size_t)PARTS * MATRIX_PLANE * 2 + 2 * 256 * 4;
+    static constexpr bool SHARE = OTHER && 2 * TILE + REST > 160 * 1024;
+    static constexpr size_t LDS = (OTHER && !SHARE ? 2 : 1) * TILE + REST;
 };
-// Whether the tiles of keys and queries share their place in LDS: where both do not fit
-template <typename T, int KP> constexpr bool shares() { return Walk<T, KP, false>::LDS > 160 * 1024; }
 
 // Which chunks a block of a walk has: those of a sequence, or of one of its pieces
 struct Stretch { int seq, start, end, base, from, to, place, pieces; };       // chunks from .. to - 1 of the sequence's; the piece's number, and how many there are

@@ -1,9 +1,10 @@
 // Tiles of the gated delta rule's matrix products.
 //
 // All products run on the bf16 matrix instruction of 16 x 16 x 32.  A number of 32 bits takes part as a sum of bf16 parts: what a bf16 tensor holds is one part; what
-// the kernels compute themselves (states, inverses, what tokens write) two parts of bf16 tensors' passes, 2^-17 of itself; and everything three parts of fp32
-// tensors' passes, which hold all of its 24 bits.  Of a product of parts those count whose order is below the larger number of parts (1 x 2: two instructions, 2 x 2:
-// three, 3 x 3: six).  All sums are fp32.
+// the kernels compute themselves (states, inverses, what tokens write) three parts, which hold all of its 24 bits, and so does all that an fp32 tensor holds.  Two parts,
+// 2^-17 of the number, are enough for what goes into nothing but a bf16 tensor of answers or gradients, which is rounded to 2^-9 at once.  Of a product of parts those
+// count whose order is below the larger number of parts (1 x 3: three instructions, 2 x 2: three, 3 x 3: six).  All sums are fp32.  (With two parts throughout the states behind
+// bf16 sequences and the sums over their tokens were 2e-6 to 5e-6 off, and are 2e-7 with three; 8192 tokens' training step took 300 us with two.)
 //
 // Lanes: m = lane % 16, q = lane / 16.  A result tile has rows 4 q + r (r = 0..3) of column m in a lane.  Two result tiles below each other are an operand as they are: the
 // contraction runs over their 32 rows in the order 4 q + 0..3 of the first, 4 q + 0..3 of the second.  Tiles in LDS are stored so that 16 consecutive bytes of a row hold the
@@ -48,9 +49,10 @@ template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
 
 constexpr int CHUNK = 64;
 
-template <typename T> struct PartsOf;
-template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1, INNER = 2; };
-template <> struct PartsOf<float> { static constexpr int RAW = 3, INNER = 3; };
+constexpr int INNER = 3;                          // parts of what the kernels compute themselves
+template <typename T> struct PartsOf;            // RAW: of what a tensor holds; LAST: of what goes into nothing but one
+template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1, LAST = 2; };
+template <> struct PartsOf<float> { static constexpr int RAW = 3, LAST = 3; };
 
 // The number of a lane's wavefront, as a scalar.  What is done by some wavefronts only has to be behind a scalar branch where it holds matrix instructions: those do not
 // look at which lanes are on.
@@ -71,8 +73,10 @@ __device__ __forceinline__ v4f_t mfma(const Frag &a, const Frag &b, v4f_t c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b_t, a.w), __builtin_bit_cast(v8b_t, b.w), c, 0, 0, 0);
 }
-template <int PA, int PB> __device__ __forceinline__ void mma(v4f_t &c, const Frag (&a)[PA], const Frag (&b)[PB])
+// c += a b, of the first PA and PB parts
+template <int PA, int PB, int NA, int NB> __device__ __forceinline__ void mma(v4f_t &c, const Frag (&a)[NA], const Frag (&b)[NB])
 {
+    static_assert(PA <= NA && PB <= NB, "parts that are there");
     constexpr int ORDER = PA > PB ? PA : PB;
 #pragma unroll
     for (int i = PA - 1; i >= 0; --i)             // the small ones first
@@ -222,8 +226,8 @@ template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
 };
 
 // One of the first pass's matrices, of N parts: zero above the diagonal, and the 32 x 32 block there is neither stored nor read.  A part is 384 pieces of 16 bytes in the
-// LDS tiles' order of columns (not turned): four of each of the first 32 rows, eight of each of the others.
-constexpr int MATRIX_PIECES = 384;
+// LDS tiles' order of columns (not turned): four of each of the first 32 rows, eight of each of the others.  So it is in LDS too: a tile of 32 columns, one of 64 behind it.
+constexpr int MATRIX_PIECES = 384, MATRIX_PLANE = MATRIX_PIECES * 8;
 __device__ __forceinline__ constexpr int matrix_piece(int row, int piece) { return row < 32 ? row * 4 + piece : row * 8 + piece - 128; }
 // ... on its way to LDS
 template <int N, int THREADS> struct Matrix {
@@ -240,12 +244,23 @@ template <int N, int THREADS> struct Matrix {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int n = threadIdx.x + i * THREADS, part = n / MATRIX_PIECES, at = n % MATRIX_PIECES;
-            const int row = at < 128 ? at / 4 : at / 8 + 16, piece = at < 128 ? at % 4 : at % 8;
-            if (ALL % THREADS == 0 || n < ALL)
-                *reinterpret_cast<u4t_t *>(tile + part * CHUNK * CHUNK + row * CHUNK + turned<CHUNK>(row, piece) * 8) = v[i];
+            const int to = at < 128 ? at / 4 * 4 + turned<32>(at / 4, at % 4) : at / 8 * 8 + turned<64>(at / 8, at % 8);
+            if (ALL % THREADS == 0 || n < ALL) *reinterpret_cast<u4t_t *>(tile + part * MATRIX_PLANE + to * 8) = v[i];
         }
     }
 };
+
+// operands out of it, as frags_rows and frags_cols; r0 and c0 are known when compiled
+template <int N> __device__ __forceinline__ void matrix_rows(Frag (&f)[N], const bf16_t *tile, int r0, int c0)
+{
+    if (r0 < 32) frags_rows<N, 32>(f, tile, MATRIX_PLANE, r0, c0);
+    else frags_rows<N, 64>(f, tile + 1024, MATRIX_PLANE, r0 - 32, c0);
+}
+template <int N> __device__ __forceinline__ void matrix_cols(Frag (&f)[N], const bf16_t *tile, int r0, int c0)
+{
+    if (r0 < 32) frags_cols<N, 32>(f, tile, MATRIX_PLANE, r0, c0);
+    else frags_cols<N, 64>(f, tile + 1024, MATRIX_PLANE, r0 - 32, c0);
+}
 
 // Vectors of a chunk and head that the first pass leaves, 64 floats each
 enum { VEC_READ = 0,     // exp(G) rk: what a row of k^T S is multiplied by
