@@ -51,23 +51,19 @@ __device__ __forceinline__ double sum_up_to(float x)
     return v + lane_move64<0x143, 0xc>(v);        // the second row's to the upper half
 }
 
-// the parts of an fp32 matrix in LDS, into memory
+// the parts of an fp32 matrix in LDS, into memory: a lane a piece of 16 bytes, four numbers and the four 16 columns on
 template <int N> __device__ __forceinline__ void put_matrix(const float *f, char *to)
 {
-    const int row = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
-    bf16_t *const p = reinterpret_cast<bf16_t *>(to);
-    const float *const x = f + row * LDF + c;
-    if (row < 32 && c >= 32) return;              // (above the diagonal)
-    // four numbers, and the four 16 columns on, are a piece: a lane has halves of four
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t a[N], b[N];
-        split2<N>(x[4 * j], x[4 * j + 1], a);
-        split2<N>(x[4 * j + 2], x[4 * j + 3], b);
-        const int j4 = (c >> 2) + j;
+    for (int i = 0; i < (MATRIX_PIECES + THREADS - 1) / THREADS; ++i) {
+        const int n = threadIdx.x + i * THREADS;
+        if (n >= MATRIX_PIECES) break;
+        const int row = n < 128 ? n / 4 : n / 8 + 16, piece = n < 128 ? n % 4 : n % 8;
+        const float *const x = f + row * LDF + (piece / 4 * 32 + piece % 4 * 4);
+        Frag w[N];
+        split_tiles<N>(*reinterpret_cast<const v4f_t *>(x), *reinterpret_cast<const v4f_t *>(x + 16), w);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            *reinterpret_cast<u2t_t *>(p + (i * MATRIX_PIECES + matrix_piece(row, piece_of(j4))) * 8 + half_of(j4) * 4) = u2t_t{a[i], b[i]};
+        for (int j = 0; j < N; ++j) reinterpret_cast<u4t_t *>(to)[j * MATRIX_PIECES + n] = w[j].w;
     }
 }
 
