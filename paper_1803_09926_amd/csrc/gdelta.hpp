@@ -22,9 +22,9 @@ __device__ __forceinline__ float gd_soft(const GdArgs &g, float raw)
     return !g.softplus || raw > 20.f ? raw : log1pf(expf(raw));
 }
 constexpr float GD_LEAST = -256.f;                  // e^-256 is zero in fp32, and sums of 64 such keep their parts in 64 bits
-__device__ __forceinline__ float gd_log_decay(const GdArgs &g, float raw, int h)
+__device__ __forceinline__ float gd_log_decay(const GdArgs &g, float raw, float A)
 {
-    const float d = (g.A ? g.A[h] : -1.f) * gd_soft(g, raw);
+    const float d = A * gd_soft(g, raw);
     return d < GD_LEAST ? GD_LEAST : d;
 }
 __device__ __forceinline__ float gd_rate(const GdArgs &g, float b) { return g.sigmoid ? 1.f / (1.f + expf(-b)) : b; }

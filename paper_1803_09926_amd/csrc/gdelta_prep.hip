@@ -100,10 +100,13 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             }
     }
     const bool here = lane < at.len;
-    float gate_a, gate_b;
+    Ahead<T, 1, false> gate_a, gate_b;
+    float A, bias;
     auto ask_gates = [&](int h) {
-        gate_a = here ? ldf((const T *)g.a + (at.first + lane) * g.a_stride + h) : 0.f;
-        gate_b = here ? ldf((const T *)g.b + (at.first + lane) * g.b_stride + h) : 0.f;
+        gate_a.load(rows_view((const T *)g.a + at.first * g.a_stride + h, g.a_stride, at.len, 1), (uint32_t)(lane * (int)g.a_stride) * (uint32_t)sizeof(T), 1);
+        gate_b.load(rows_view((const T *)g.b + at.first * g.b_stride + h, g.b_stride, at.len, 1), (uint32_t)(lane * (int)g.b_stride) * (uint32_t)sizeof(T), 1);
+        A = g.A ? g.A[h] : -1.f;
+        bias = g.a_bias ? g.a_bias[h] : 0.f;
     };
     ask_gates(kh * share);
     // keys into LDS, and their lengths; a key that is not finite counts as none, and its token is remembered
@@ -170,10 +173,12 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
         const long long where = (long long)id * g.H + h;
         float *const vec = reinterpret_cast<float *>(vec_out + where * vectors);
         // gates, by each wavefront: a lane a token
+        const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;      // (masks of lanes over all of the loop spill)
+        const bool here = lane < at.len;
         float d = 0.f, beta = 0.f;
         if (here) {
-            d = gd_log_decay(g, gd_raw(g, gate_a, h), h);
-            beta = gd_rate(g, gate_b);
+            d = gd_log_decay(g, gate_a.at(0) + bias, A);
+            beta = gd_rate(g, gate_b.at(0));
         }
         const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
         const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
@@ -185,22 +190,30 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
         if (wv == 0) {
             Gs[lane] = G;
             betas[lane] = beta;
-            const float rk = rks[lane], rq = rqs[lane], lam = expf((float)G);
+        }
+        __syncthreads();
+        // the vectors, by a wavefront each
+        if (wv == 0) {
+            const float rk = rks[lane], lam = expf((float)G);
             vec[VEC_READ * 64 + lane] = lam * rk;
+            vec[VEC_RK * 64 + lane] = rk;
+        } else if (wv == 1) {
+            vec[VEC_WRITE * 64 + lane] = expf((float)(end - G)) * rks[lane];
             vec[VEC_BETA * 64 + lane] = beta;
-            vec[VEC_WRITE * 64 + lane] = expf((float)(end - G)) * rk;
+        } else if (wv == 2) {
+            const float rq = rqs[lane], lam = expf((float)G);
             vec[VEC_ASK * 64 + lane] = g.scale * lam * rq;
             vec[VEC_RQ * 64 + lane] = rq;
-            vec[VEC_RK * 64 + lane] = rk;
+        } else {
             reinterpret_cast<double *>(vec + VEC_G * 64)[lane] = G;
             if (lane == 0) {
                 vec[VEC_ONE * 64] = expf((float)end);
                 reinterpret_cast<int *>(vec + VEC_ONE * 64)[1] = bad_from;
             }
         }
-        __syncthreads();
         v4f_t pv[4];
         {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             double gi[4];
             float bi[4], ki[4], qi[4];
 #pragma unroll
@@ -208,32 +221,41 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
                 const int i = wv * 16 + 4 * q4 + r;
                 gi[r] = Gs[i]; bi[r] = betas[i]; ki[r] = rks[i]; qi[r] = g.scale * rqs[i];
             }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
+            auto block = [&](int n, bool diagonal) {
                 const int j = n * 16 + m;
                 const double gj = Gs[j];
                 const float kj = rks[j];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = wv * 16 + 4 * q4 + r;
-                    const float e = i >= j ? exp2_fast((float)(gi[r] - gj) * LOG2E) * kj : 0.f;
-                    pv[n][r] = i >= j ? qi[r] * e * qk[n][r] : 0.f;
-                    L[i * LDF + j] = i > j ? bi[r] * ki[r] * e * kk[n][r] : 0.f;
+                    const float e = exp2_fast((float)(gi[r] - gj) * LOG2E) * kj, p = qi[r] * e * qk[n][r], x = bi[r] * ki[r] * e * kk[n][r];
+                    pv[n][r] = diagonal && i < j ? 0.f : p;
+                    L[i * LDF + j] = diagonal && i <= j ? 0.f : x;
                 }
+            };
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                pv[n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+                if (n < wv) block(n, false);
+                else if (n == wv) block(n, true);
             }
         }
         __syncthreads();
-        // the inverse of the diagonal block wv: lane m has its column m
+        // the inverse of the diagonal block wv: lane m has its column m; a row of the block comes from the lane that has read it (read from LDS by all lanes where it is
+        // needed, the substitution took three times as long)
         {
-            const float *const D = L + wv * 16 * LDF + wv * 16;
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             float x[16];
+            v4f_t D[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float s = i == m ? 1.f : 0.f;
+            for (int c = 0; c < 4; ++c) D[c] = *reinterpret_cast<const v4f_t *>(L + (wv * 16 + m) * LDF + wv * 16 + 4 * c);
 #pragma unroll
-                for (int j = 0; j < i; ++j) s -= D[i * LDF + j] * x[j];
-                x[i] = s;
-            }
+            for (int i = 0; i < 16; ++i) x[i] = i == m ? 1.f : 0.f;
+#pragma unroll
+            for (int j = 0; j < 15; ++j)
+#pragma unroll
+                for (int i = j + 1; i < 16; ++i)
+                    x[i] = fmaf(-__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(D[j / 4][j % 4]), i)), x[j], x[i]);
             if (q4 == 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) X[(wv * 16 + i) * LDF + wv * 16 + m] = x[i];
@@ -242,6 +264,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
         __syncthreads();
         // the blocks of column wv below the diagonal, and zeros above it
         {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             v4f_t col[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) col[0][r] = X[(wv * 16 + 4 * q4 + r) * LDF + wv * 16 + m];
@@ -249,15 +272,15 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             for (int n = 1; n < 4; ++n) {
                 const int i = wv + n;                    // block row
                 if (i > 3) break;
-                v4f_t s = {0.f, 0.f, 0.f, 0.f};
+                v4f_t sums[3];                           // (each on its own: what the last block of the column has no part in is not behind it)
 #pragma unroll
                 for (int k = 0; k < n; ++k) {
-                    const float4 a = *reinterpret_cast<const float4 *>(L + (i * 16 + m) * LDF + (wv + k) * 16 + 4 * q4);
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, col[k][0], s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, col[k][1], s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, col[k][2], s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, col[k][3], s, 0, 0, 0);
+                    const v4f_t a = *reinterpret_cast<const v4f_t *>(L + (i * 16 + m) * LDF + (wv + k) * 16 + 4 * q4);
+                    sums[k] = v4f_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sums[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], col[k][r], sums[k], 0, 0, 0);
                 }
+                const v4f_t s = n == 1 ? sums[0] : n == 2 ? sums[0] + sums[1] : sums[0] + sums[1] + sums[2];
                 const float4 a = *reinterpret_cast<const float4 *>(X + (i * 16 + m) * LDF + i * 16 + 4 * q4);
                 v4f_t c = {0.f, 0.f, 0.f, 0.f};
                 c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, -s[0], c, 0, 0, 0);

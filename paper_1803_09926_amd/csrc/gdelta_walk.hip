@@ -91,7 +91,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_step(GdArgs g, const int32_t
     }
     Some<T, WIDE> v;
     v.load((const T *)g.v + t * g.v_stride + (long long)h * g.V + c, there);
-    const float raw = gd_raw(g, ldf((const T *)g.a + t * g.a_stride + h), h), d = expf(gd_log_decay(g, raw, h));
+    const float raw = gd_raw(g, ldf((const T *)g.a + t * g.a_stride + h), h), d = expf(gd_log_decay(g, raw, g.A ? g.A[h] : -1.f));
     const float beta = gd_rate(g, ldf((const T *)g.b + t * g.b_stride + h));
     Round r;
     round_of<NK>(s, q, k, r, lds);
