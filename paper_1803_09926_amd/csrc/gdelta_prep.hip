@@ -5,7 +5,7 @@
 // and what they answer is exp(G) * Q S + P U with P[i,j] = scale exp(G[i] - G[j]) q[i].k[j] on and below it.  T and P are made here.
 //
 // One block of four wavefronts a chunk and key head; the products of q and k are taken once and serve all value heads.  T by blocks of 16: the four on the
-// diagonal by substitution, one a wavefront, and each column of blocks below by products with the fp32 matrix instruction, a wavefront each.
+// diagonal by substitution, and each column of blocks below by products with the fp32 matrix instruction, a wavefront each.
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 
@@ -172,43 +172,45 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
         const int h = kh * share + hh;
         const long long where = (long long)id * g.H + h;
         float *const vec = reinterpret_cast<float *>(vec_out + where * vectors);
-        // gates, by each wavefront: a lane a token
-        const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;      // (masks of lanes over all of the loop spill)
-        const bool here = lane < at.len;
-        float d = 0.f, beta = 0.f;
-        if (here) {
-            d = gd_log_decay(g, gate_a.at(0) + bias, A);
-            beta = gd_rate(g, gate_b.at(0));
-        }
-        const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
-        const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
-        if (lane >= bad_from) d = beta = 0.f;
-        const double G = sum_up_to(d);
-        if (hh + 1 < share) ask_gates(h + 1);
-        const double end = __shfl(G, 63, 64);
-        __syncthreads();                                 // the head before has been read
-        if (wv == 0) {
-            Gs[lane] = G;
+        // What one wavefront does alone another one does for the next chunk and head: each compute unit's four vector units have the same work.
+        const int turn = ((int)id + hh) & 3;
+        // gates: a lane a token
+        if (wv == turn) {
+            const int lane = lane_anew();                // (masks of lanes over all of the loop spill)
+            float d = 0.f, beta = 0.f;
+            if (lane < at.len) {
+                d = gd_log_decay(g, gate_a.at(0) + bias, A);
+                beta = gd_rate(g, gate_b.at(0));
+            }
+            const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
+            const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
+            if (lane >= bad_from) d = beta = 0.f;
+            const double G = sum_up_to(d);
+            Gs[lane] = G;                                // (who reads the head before's is behind two barriers)
             betas[lane] = beta;
-        }
-        __syncthreads();
-        // the vectors, by a wavefront each
-        if (wv == 0) {
-            const float rk = rks[lane], lam = expf((float)G);
-            vec[VEC_READ * 64 + lane] = lam * rk;
-            vec[VEC_RK * 64 + lane] = rk;
-        } else if (wv == 1) {
-            vec[VEC_WRITE * 64 + lane] = expf((float)(end - G)) * rks[lane];
-            vec[VEC_BETA * 64 + lane] = beta;
-        } else if (wv == 2) {
-            const float rq = rqs[lane], lam = expf((float)G);
-            vec[VEC_ASK * 64 + lane] = g.scale * lam * rq;
-            vec[VEC_RQ * 64 + lane] = rq;
-        } else {
             reinterpret_cast<double *>(vec + VEC_G * 64)[lane] = G;
-            if (lane == 0) {
-                vec[VEC_ONE * 64] = expf((float)end);
+            if (lane == 63) {
+                vec[VEC_ONE * 64] = expf((float)G);
                 reinterpret_cast<int *>(vec + VEC_ONE * 64)[1] = bad_from;
+            }
+        }
+        if (hh + 1 < share) ask_gates(h + 1);
+        __syncthreads();
+        // the vectors, by the others
+        if (wv != turn) {
+            const int lane = lane_anew(), which = (wv - turn) & 3;
+            const double G = Gs[lane];
+            if (which == 1) {
+                const float rk = rks[lane];
+                vec[VEC_READ * 64 + lane] = expf((float)G) * rk;
+                vec[VEC_RK * 64 + lane] = rk;
+            } else if (which == 2) {
+                vec[VEC_WRITE * 64 + lane] = expf((float)(Gs[63] - G)) * rks[lane];
+                vec[VEC_BETA * 64 + lane] = betas[lane];
+            } else {
+                const float rq = rqs[lane];
+                vec[VEC_ASK * 64 + lane] = g.scale * expf((float)G) * rq;
+                vec[VEC_RQ * 64 + lane] = rq;
             }
         }
         v4f_t pv[4];
@@ -241,24 +243,17 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             }
         }
         __syncthreads();
-        // the inverse of the diagonal block wv: lane m has its column m; a row of the block comes from the lane that has read it (read from LDS by all lanes where it is
-        // needed, the substitution took three times as long)
-        {
+        // the inverses of the four blocks on the diagonal: 16 lanes have one, a column each
+        if (wv == ((turn + 2) & 3)) {
             const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
+            const float *const D = L + q4 * 16 * (LDF + 1);
             float x[16];
-            v4f_t D[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) D[c] = *reinterpret_cast<const v4f_t *>(L + (wv * 16 + m) * LDF + wv * 16 + 4 * c);
+            for (int i = 0; i < 16; ++i) {
+                x[i] = i == m ? 1.f : 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = i == m ? 1.f : 0.f;
-#pragma unroll
-            for (int j = 0; j < 15; ++j)
-#pragma unroll
-                for (int i = j + 1; i < 16; ++i)
-                    x[i] = fmaf(-__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(D[j / 4][j % 4]), i)), x[j], x[i]);
-            if (q4 == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) X[(wv * 16 + i) * LDF + wv * 16 + m] = x[i];
+                for (int j = 0; j < i; ++j) x[i] = fmaf(-D[i * LDF + j], x[j], x[i]);
+                X[(q4 * 16 + i) * LDF + q4 * 16 + m] = x[i];
             }
         }
         __syncthreads();
