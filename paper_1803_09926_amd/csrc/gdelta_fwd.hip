@@ -43,7 +43,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     const int share = g.H / g.key_heads;
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
     if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
-    const int id = (int)(which.item / g.key_heads), kh = (int)(which.item - (long long)id * g.key_heads), h = kh * share + which.block / blocks;
+    const int id = uniform((int)quotient(which.item, (unsigned)g.key_heads)), kh = uniform((int)(which.item - (long long)id * g.key_heads)), h = uniform(kh * share + which.block / blocks);
     const int block = which.block % blocks;
     const Stretch at_ = stretch_of(g, l, id);
     const int seq = at_.seq, start = at_.start, end = at_.end, base = at_.base, chunks = at_.to;

@@ -18,7 +18,7 @@ __global__ __launch_bounds__(2 * KP, 1) void k_gdelta_join(GdArgs g, GdLayout l,
     __shared__ u4t_t handed[2][GROUPS][N][64];
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)blocks);
     if (which.item >= (long long)g.sequences * g.H) return;
-    const int seq = (int)(which.item / g.H), h = (int)(which.item - (long long)seq * g.H), w = wave_number(), lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
+    const int seq = uniform((int)quotient(which.item, (unsigned)g.H)), h = uniform((int)(which.item - (long long)seq * g.H)), w = wave_number(), lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
     const int col = which.block * 16 + m;
     const int unit = l.piece * CHUNK, start = gd_start(g, seq), end = gd_start(g, seq + 1), base = gd_base(g, seq, unit);
     const long long chunks = min((long long)(end > start ? cdiv(end - start, CHUNK) : 0), l.chunks - gd_base(g, seq, CHUNK));

@@ -170,10 +170,10 @@ __device__ __forceinline__ Stretch stretch_of(const GdArgs &g, const GdLayout &l
         s.start = at.start;
         s.end = at.end;
     } else {
-        s.start = gd_start(g, s.seq);
-        s.end = gd_start(g, s.seq + 1);
+        s.start = uniform(gd_start(g, s.seq));
+        s.end = uniform(gd_start(g, s.seq + 1));
     }
-    s.base = g.starts ? s.start / CHUNK + s.seq : gd_base(g, s.seq, CHUNK);
+    s.base = uniform(g.starts ? s.start / CHUNK + s.seq : gd_base(g, s.seq, CHUNK));
     const long long chunks = min((long long)(s.end > s.start ? cdiv(s.end - s.start, CHUNK) : 0), l.chunks - s.base);
     s.from = 0;
     s.to = (int)chunks;

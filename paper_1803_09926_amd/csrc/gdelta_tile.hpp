@@ -35,12 +35,16 @@ template <typename F> hipError_t gd_launches(long long blocks, int threads, F f)
 // Blocks that read the same rows, `blocks` of each of `items`, lie on one of the eight XCDs, whose L2 they share, and run close in time: the dispatcher hands blocks to the
 // XCDs in turn.  The number of a launch's blocks; the item and the number in it of one of them (item may be behind the last one).
 inline long long gd_shared_blocks(long long items, int blocks) { return (items + 7) / 8 * 8 * blocks; }
+// (quotients of what fits 32 bits are formed in 32: those of 64 take hundreds of instructions)
+__device__ __forceinline__ unsigned long long quotient(unsigned long long n, unsigned d) { return n >> 32 ? n / d : (unsigned)n / d; }
 struct Shared { long long item; int block; };
 __device__ __forceinline__ Shared gd_shared(unsigned long long n, unsigned blocks)
 {
-    const unsigned long long group = n / (8 * blocks);
+    const unsigned long long group = quotient(n, 8 * blocks);
     return {(long long)(group * 8 + n % 8), (int)((n - group * (8 * blocks)) / 8)};
 }
+// What is the same in all lanes, where the compiler does not see it: addresses are then formed once instead of in every lane
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // more LDS than a launch has without being told
 template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
 {
@@ -85,7 +89,8 @@ template <int PA, int PB, int NA, int NB> __device__ __forceinline__ void mma(v4
             if (i + j < ORDER) c = mfma(a[i], b[j], c);
 }
 
-// two numbers as N parts, each a pair of bf16: what is left after a part is taken is exact
+// two numbers as N parts, each a pair of bf16: what is left after a part is taken is exact.  (The dot product instruction takes
+// a part out in one instruction instead of two, and no walk was faster for it.)
 template <int N> __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[N])
 {
 #pragma unroll
@@ -229,9 +234,10 @@ template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
 // LDS tiles' order of columns (not turned): four of each of the first 32 rows, eight of each of the others.  So it is in LDS too: a tile of 32 columns, one of 64 behind it.
 constexpr int MATRIX_PIECES = 384, MATRIX_PLANE = MATRIX_PIECES * 8;
 __device__ __forceinline__ constexpr int matrix_piece(int row, int piece) { return row < 32 ? row * 4 + piece : row * 8 + piece - 128; }
-// ... on its way to LDS
+// ... on its way to LDS.  A wavefront has 64 pieces at a time, all of them of one of the two tiles: in LDS too they are those 64, in the order of the tile's turns.
 template <int N, int THREADS> struct Matrix {
     static constexpr int ALL = N * MATRIX_PIECES, PER = (ALL + THREADS - 1) / THREADS;
+    static_assert(THREADS % 64 == 0 && MATRIX_PIECES == 6 * 64, "64 at a time: two times of the first tile, four of the second");
     u4t_t v[PER];
     __device__ __forceinline__ void load(const char *p)
     {
@@ -241,15 +247,16 @@ template <int N, int THREADS> struct Matrix {
     }
     __device__ __forceinline__ void put(bf16_t *tile) const
     {
+        const int lane = threadIdx.x & 63, w = wave_number();
+        const int first = lane / 4 * 4 + turned<32>(lane / 4, lane % 4), second = lane / 8 * 8 + turned<64>(lane / 8, lane % 8);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int n = threadIdx.x + i * THREADS, part = n / MATRIX_PIECES, at = n % MATRIX_PIECES;
-            const int to = at < 128 ? at / 4 * 4 + turned<32>(at / 4, at % 4) : at / 8 * 8 + turned<64>(at / 8, at % 8);
-            if (ALL % THREADS == 0 || n < ALL) *reinterpret_cast<u4t_t *>(tile + part * MATRIX_PLANE + to * 8) = v[i];
+            const int n = i * (THREADS / 64) + w, at = n % 6;
+            // (eight rows on, turned<64> has its second bit the other way round)
+            if (ALL % THREADS == 0 || n < ALL / 64) *reinterpret_cast<u4t_t *>(tile + (n * 64 + (at < 2 ? first : at % 2 ? second ^ 2 : second)) * 8) = v[i];
         }
     }
 };
-
 // operands out of it, as frags_rows and frags_cols; r0 and c0 are known when compiled
 template <int N> __device__ __forceinline__ void matrix_rows(Frag (&f)[N], const bf16_t *tile, int r0, int c0)
 {
@@ -312,11 +319,15 @@ __device__ __forceinline__ ChunkAt gd_chunk(const GdArgs &g, int id, int unit)
             lo += step * __popcll(__ballot(at < hi && gd_base(g, at < hi ? (int)at : lo, unit) <= id));
             hi = hi - lo > step ? lo + step : hi;
         }
-        lo = __builtin_amdgcn_readfirstlane(lo);
+        lo = uniform(lo);
         base = gd_base(g, lo, unit);
         start = gd_start(g, lo);
         end = gd_start(g, lo + 1);
     }
+    lo = uniform(lo);
+    base = uniform(base);
+    start = uniform(start);
+    end = uniform(end);
     const int place = id - base;
     const long long first = start + (long long)place * unit;
     if (place < 0 || first >= end) return {0, 0, lo, place, start, end};
