@@ -33,7 +33,11 @@ extern "C" {
  * S before a sequence's first token is the sequence's row of `init` ([sequences,H,K,V]), or zero; `final` gets S after each sequence's last token (init's row, or
  * zero, where the sequence is empty).  init is a constant of the backward pass.  g is taken as -256 where it is less: its decay is zero in fp32 long before.
  * A number that is not finite leaves the outputs of its head before its token, of the other heads, and of other sequences as they were; which of the head's outputs from
- * its token on are not finite is not specified.  The same holds for the gradients of other sequences, and of heads of other key heads. */
+ * its token on are not finite is not specified.  The same holds for the gradients of other sequences, and of heads of other key heads.
+ *
+ * T / 64 + sequences must be less than 2^31.  With bf16 tensors a call that is asked for y alone holds what it computes between tokens to 2^-17 of itself, one that is
+ * asked for `final` or `kept` to 2^-24: y may differ in its last bit.  A backward pass takes `starts` where its forward pass did, with the same values, and the same
+ * value of DWCONV_TUNE_GDELTA_PIECE (the chunks of 64 tokens that a piece of a long sequence has, by default chosen from the sizes; kept's layout goes by it). */
 #define GDELTA_MAX_K 256
 #define GDELTA_MAX_V 256
 #define GDELTA_MAX_H 65535          /* value heads */
@@ -73,7 +77,7 @@ typedef struct gdelta_tensors {
 size_t gdelta_kept_bytes(const gdelta_desc *desc);
 size_t gdelta_fwd_workspace_bytes(const gdelta_desc *desc);
 size_t gdelta_bwd_workspace_bytes(const gdelta_desc *desc);
-/* q, k, v, a, b, A, a_bias, starts, init: read.  y, final, kept: written. */
+/* q, k, v, a, b, A, a_bias, starts, init: read.  y, final, kept: written.  Where kept is given no workspace is used (it may be NULL). */
 int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *tensors, void *workspace, size_t workspace_bytes, void *stream);
 /* What the forward pass read (init aside, whose part kept holds), kept and dy: read.  dq, dk, dv, da, db, dA, da_bias: written. */
 int gdelta_bwd(const gdelta_desc *desc, const gdelta_tensors *tensors, void *workspace, size_t workspace_bytes, void *stream);

@@ -122,7 +122,7 @@ _STEP = ("q", "k", "v", "a", "b", "A", "a_bias", "slots", "state", "y")
 def gdelta_fwd(d: GdeltaDesc, q, k, v, a, b, y, workspace, A=None, a_bias=None, starts=None, init=None, final=None, kept=None, stream=None):
     """Enqueue y = what the states answer to q while they learn v at k, with decays from a (A and a_bias: fp32 [H]) and rates from b.  `starts` (int32) packs
     sequences of any lengths; init and final (fp32 [sequences,H,K,V]) carry the states from call to call; kept (a device tensor of gdelta_kept_bytes(d) bytes) gets
-    what gdelta_bwd needs.  `workspace`: a device tensor of at least gdelta_fwd_workspace_bytes(d) bytes."""
+    what gdelta_bwd needs.  `workspace`: a device tensor of at least gdelta_fwd_workspace_bytes(d) bytes (None where there is kept)."""
     _call("gdelta_fwd", d, _FWD, (q, k, v, a, b, A, a_bias, starts, init, y, final, kept), workspace, stream)
     return y
 
