@@ -1,7 +1,8 @@
 // The RMS norm of each head with a gate, forward and backward.  The contract stands in include/deltaops.h.
 //
 // A run of D channels is held by a team of TL = 4 to 64 lanes of one wavefront, 16 bytes a vector and NV vectors a lane; its sum is taken inside the vector
-// registers, so that a run is read once and written once and nothing waits at a barrier.  Both passes are bound by memory.
+// registers, so that a run is read once and written once and nothing waits at a barrier.  Both passes are bound by memory: 9999 tokens of 12 runs of 100 in fp32 20.6 us (96 MB,
+// 4.7 TB/s), the gradients of 16384 tokens of 8 runs of 128 in bf16 with a gate 33 us (168 MB, 5.1 TB/s) and 4.6 for the sum of the partials.
 //
 // The weight's gradient is a sum over tokens and heads: each lane keeps the sums of its channels over all runs that its team walks, the teams of a wavefront add
 // theirs between lanes, the wavefronts of a block in LDS, and the blocks' partials meet in seq_sum.hip.
@@ -219,7 +220,8 @@ long long blocks_for(const hnorm_desc *d, long long most)
     const long long runs = (long long)d->T * d->H, need = (runs + teams - 1) / teams;
     return need < most ? need : most;
 }
-long long bwd_blocks(const hnorm_desc *d) { return blocks_for(d, 1024); }
+// Blocks of the backward pass; each leaves partials that are read again (16384 tokens of 8 runs of 128 in bf16, with their sum: 512 blocks 37.1 us, 1024 39.8, 2048 41.8).
+long long bwd_blocks(const hnorm_desc *d) { return blocks_for(d, 512); }
 
 HnormArgs args_of(const hnorm_desc *d)
 {
