@@ -179,8 +179,8 @@ template <typename T, int KP> hipError_t walk(const GdArgs &g, const GdLayout &l
         if (e == hipSuccess) e = launch_gdelta_join(g, l, s, INNER, true, stream);
         if (e != hipSuccess) return e;
     }
-    if constexpr (KP < 256) {
-        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false>(g, l, s, dy, dv, stream);
+    if constexpr (may_have_two_tiles<T, KP>) {
+        if (two_tiles(g, l)) return launch<T, KP, 2, false>(g, l, s, dy, dv, stream);
     }
     return launch<T, KP, 1, false>(g, l, s, dy, dv, stream);
 }

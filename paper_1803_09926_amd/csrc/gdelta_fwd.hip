@@ -292,8 +292,8 @@ hipError_t walk(const GdArgs &g, const GdLayout &l, const GdSpace &s, const floa
         if (e == hipSuccess) e = launch_gdelta_join(g, l, s, EXACT ? INNER : PartsOf<T>::LAST, false, stream);
         if (e != hipSuccess) return e;
     }
-    if constexpr (KP < 256) {
-        if (two_tiles(g, l, sizeof(T) == 4)) return launch<T, KP, 2, false, EXACT>(g, l, s, init, y, final, stream);
+    if constexpr (may_have_two_tiles<T, KP>) {
+        if (two_tiles(g, l)) return launch<T, KP, 2, false, EXACT>(g, l, s, init, y, final, stream);
     }
     return launch<T, KP, 1, false, EXACT>(g, l, s, init, y, final, stream);
 }

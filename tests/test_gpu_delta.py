@@ -152,6 +152,20 @@ def test_sequences_in_pieces(gpu_lib, dtype, piece, Hk, H, K, V, carry):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hk,H,K,V,more,shift", [(2, 2, 64, 80, 0, 0), (1, 2, 40, 131, 1, 1), (2, 2, 33, 256, 8, 0), (3, 3, 64, 66, 0, 1)])
+def test_many_sequences(gpu_lib, dtype, Hk, H, K, V, more, shift):
+    """As many as fill the card with blocks of 128 columns: empty ones, single tokens, and some of several chunks."""
+    print("many sequences", dtype, Hk, H, K, V, more, shift, flush=True)
+    m = Made(K + V, dtype, shift)
+    lengths = [0, 1, 2, 65, 0, 0, 130] + [1, 0, 3, 2] * 31
+    bounds = np.cumsum([0] + lengths).tolist()
+    x, par = host_inputs(m, bounds[-1], Hk, H, K, V)
+    check(m, x, par, bounds, m.host((len(lengths), H, K, V), 0.3, stored=False), more)
+    x, par = host_inputs(m, 393, Hk, H, K, V)
+    check(m, x, par, list(range(0, 394, 3)), None, more, even=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_decays_of_any_size(gpu_lib, dtype):
     """From nothing forgotten to everything, beside each other in a chunk; what is clamped has no gradient."""
     m = Made(23, dtype)
