@@ -8,7 +8,8 @@
 //   the gradient of the logarithm of token t's decay: the sum of what has passed it, exp(G_end) dS.S, all that tokens i >= t read of S, all that tokens j < t write for
 //           the chunk's end, and F * QK^T + M * KK^T over i >= t > j.  No term is in it that does not carry the decay: none cancel, however small it is.
 // One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens (of 256-wide keys 128 columns).  What is contracted over V
-// is read in blocks of 32 columns.
+// is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 138 us (with products of keys and queries
+// before it, and one tile for both, 146).
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 
@@ -24,7 +25,9 @@ template <typename T, int KP> struct Back {
     static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
     static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
     static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
-    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)LAST * CHUNK * CHUNK * 2, SECOND = TILE + 2 * MATRIX;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)LAST * CHUNK * CHUNK * 2;
+    static constexpr bool TWO = 2 * TILE + 2 * MATRIX <= 144 * 1024;    // keys and queries at once; else one after the other in the same place
+    static constexpr size_t SECOND = (TWO ? 2 : 1) * TILE + 2 * MATRIX;
     static constexpr size_t REGION = FIRST > SECOND ? FIRST : SECOND;
     // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums; the chunk's vectors
     static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8 + VECS * 64, LDS = REGION + FLOATS * 4;
@@ -74,7 +77,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
     extern __shared__ __align__(16) char lds[];
     bf16_t *const st = reinterpret_cast<bf16_t *>(lds), *const dst = C::TURNS ? st : st + INNER * PLANE_S;
     bf16_t *const xt = dst + INNER * PLANE_S, *const ut = xt + INNER * PLANE_V, *const yt = ut + INNER * PLANE_V;
-    bf16_t *const tile = reinterpret_cast<bf16_t *>(lds), *const fm = tile + RAW * PLANE, *const mm = fm + LAST * PLANE_M;
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = C::TWO ? kt + RAW * PLANE : kt, *const fm = qt + RAW * PLANE, *const mm = fm + LAST * PLANE_M;
     float *const row_m = reinterpret_cast<float *>(lds + C::REGION), *const xv = row_m + 64;
     float *const passing = xv + 64, *const dot_a = passing + 8 * 64, *const dot_b = dot_a + 2 * 64, *const dot_c = dot_b + 2 * 64;
     float *const wave_sums = dot_c + 2 * 64, *const vec = wave_sums + 8;
@@ -89,9 +92,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         return;
     }
     const T *const kp = (const T *)g.k + at.first * g.k_stride + (long long)kh * g.K, *const qp = (const T *)g.q + at.first * g.q_stride + (long long)kh * g.K;
-    Rows<T, KP, THREADS, WHOLE> rows;                // a tile of keys or queries on its way
+    Rows<T, KP, THREADS, WHOLE> rows, others;        // the tiles of keys and queries on their way (one after the other in `rows` where they have one place)
     auto ask_keys = [&] { rows.load(kp, g.k_stride, at.len, g.K); };
-    auto ask_queries = [&] { rows.load(qp, g.q_stride, at.len, g.K); };
+    auto ask_queries = [&] { (C::TWO ? others : rows).load(qp, g.q_stride, at.len, g.K); };
     constexpr int BOTH = HALVES == 1 ? 2 : 1, AT_M = BOTH - 1;       // places of what two wavefronts that share rows have one of each
     const float *sp, *dsp, *xp, *up;                 // of the head in hand
     const T *yp, *vp;
@@ -146,45 +149,6 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
     };
     point_to(kh * share);
     ask(0);
-    // Products of queries with keys, and of keys with keys: rows 16 mt.., columns 16 n...  Where two wavefronts share the rows each has one of them.
-    v4f_t qk[BOTH][4];
-    {
-        Frag qa[KP / 32][RAW];
-        const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4, row = mt * 16 + m;
-#pragma unroll
-        for (int c = 0; c < KP / 32; ++c) {
-            Some<T, 4> v[2];
-            uint32_t w[4][RAW];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int col = c * 32 + i * 16 + q4 * 4;
-                v[i].load(qp + row * g.q_stride + col, row < at.len ? g.K - col : 0);
-                split2<RAW>(v[i].at(0), v[i].at(1), w[2 * i]);
-                split2<RAW>(v[i].at(2), v[i].at(3), w[2 * i + 1]);
-            }
-#pragma unroll
-            for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
-        }
-        ask_keys();
-        rows.template put<LD>(tile);
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            qk[0][n] = qk[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
-            if (n > mt) continue;
-#pragma unroll
-            for (int c = 0; c < KP / 32; ++c) {
-                Frag a[RAW], b[RAW];
-                frags_rows<RAW, LD>(b, tile, PLANE, n * 16, c * 32, lane);
-                if (does_m) {
-                    frags_rows<RAW, LD>(a, tile, PLANE, mt * 16, c * 32, lane);
-                    mma<RAW, RAW>(qk[AT_M][n], a, b);
-                }
-                if (does_f) mma<RAW, RAW>(qk[0][n], qa[c], b);
-            }
-        }
-    }
-
     v4f_t gq[TILES], gk[TILES];                          // the gradients of q and k, their lengths taken for constants
 #pragma unroll
     for (int t = 0; t < TILES; ++t) gq[t] = gk[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
@@ -200,11 +164,11 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         for (int t = 0; t < TILES; ++t) ys[t] = xs[t] = us[t] = v4f_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < 4; ++n) yu[0][n] = yu[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
-        float gate_a = 0.f, gate_b = 0.f;                // of the token that a lane of the first wavefront has in the end
-        if (wv == 0 && (int)threadIdx.x < at.len) {
-            const int lane = threadIdx.x;
-            gate_a = ldf((const T *)g.a + (at.first + lane) * g.a_stride + h);
-            gate_b = ldf((const T *)g.b + (at.first + lane) * g.b_stride + h);
+        Ahead<T, 1, false> gate_a, gate_b;               // of the token that a lane of the first wavefront has in the end
+        if (wv == 0) {
+            const uint32_t lane = threadIdx.x;
+            gate_a.load(rows_view((const T *)g.a + at.first * g.a_stride + h, g.a_stride, at.len, 1), lane * (uint32_t)g.a_stride * (uint32_t)sizeof(T), 1);
+            gate_b.load(rows_view((const T *)g.b + at.first * g.b_stride + h, g.b_stride, at.len, 1), lane * (uint32_t)g.b_stride * (uint32_t)sizeof(T), 1);
         }
         float ss = 0.f, xv_part = 0.f;                   // dS.S and X.V, this lane's share
 
@@ -245,6 +209,10 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 put8_ahead<T, LDV, VALUES>(yt, PLANE_V, vrow, vcol, t8[AT_M]);
             }
             if (v0 + VB < l.VP) ask(v0 + VB);
+            else {
+                ask_keys();
+                if constexpr (C::TWO) ask_queries();
+            }
             __syncthreads();
             const int lane = lane_anew();
             Frag ya[RAW], xa[INNER], ua[INNER];
@@ -282,14 +250,60 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 mma<INNER, INNER>(us[t], ua, b);
             }
         }
-        ask_queries();
         __syncthreads();                                 // the first region is free
+        rows.template put<LD>(kt);
+        if constexpr (C::TWO) others.template put<LD>(qt);
+        else ask_queries();
         ss = lanes_sum(ss);
         if (threadIdx.x % 64 == 0) wave_sums[wv] = ss;
         xv_part += lane_move<DPP_XOR1>(xv_part);
         xv_part += lane_move<DPP_XOR2>(xv_part);
         if (threadIdx.x < 256 && threadIdx.x % 4 == 0) xv[threadIdx.x / 4] = xv_part;
 
+        __syncthreads();
+        // Products of queries with keys, and of keys with keys: rows 16 mt.., columns 16 n...  Where two wavefronts share the rows each has one of them.
+        v4f_t qk[BOTH][4];
+        {
+            const int lane = lane_anew();
+            Frag qa[C::TWO ? 1 : KP / 32][RAW];
+            if constexpr (!C::TWO) {
+                const int row = mt * 16 + (lane & 15);
+#pragma unroll
+                for (int c = 0; c < KP / 32; ++c) {
+                    Some<T, 4> v[2];
+                    uint32_t w[4][RAW];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int col = c * 32 + i * 16 + (lane >> 4) * 4;
+                        v[i].load(qp + row * g.q_stride + col, row < at.len ? g.K - col : 0);
+                        split2<RAW>(v[i].at(0), v[i].at(1), w[2 * i]);
+                        split2<RAW>(v[i].at(2), v[i].at(3), w[2 * i + 1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < RAW; ++i) qa[c][i].w = u4t_t{w[0][i], w[1][i], w[2][i], w[3][i]};
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                qk[0][n] = qk[AT_M][n] = v4f_t{0.f, 0.f, 0.f, 0.f};
+                if (n > mt) continue;
+#pragma unroll
+                for (int c = 0; c < KP / 32; ++c) {
+                    Frag a[RAW], b[RAW];
+                    frags_rows<RAW, LD>(b, kt, PLANE, n * 16, c * 32, lane);
+                    if (does_m) {
+                        frags_rows<RAW, LD>(a, kt, PLANE, mt * 16, c * 32, lane);
+                        mma<RAW, RAW>(qk[AT_M][n], a, b);
+                    }
+                    if (does_f) {
+                        if constexpr (C::TWO) {
+                            frags_rows<RAW, LD>(a, qt, PLANE, mt * 16, c * 32, lane);
+                            mma<RAW, RAW>(qk[0][n], a, b);
+                        } else mma<RAW, RAW>(qk[0][n], qa[c], b);
+                    }
+                }
+            }
+        }
         // F and M + M^T, and what of their products passes each token
         {
             const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
@@ -369,42 +383,6 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 }
             }
         }
-        rows.template put<LD>(tile);
-        ask_keys();
-        __syncthreads();
-        {
-            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
-            float dot[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dot[r] = 0.f;
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                const v4f_t q = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = ys[t][r] * vec[VEC_ASK * 64 + mt * 16 + 4 * q4 + r];
-                    gq[t][r] += x;
-                    dot[r] += x * q[r];
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { dot[r] = row_sum(dot[r]); if (m == 0) dot_a[half * 64 + mt * 16 + 4 * q4 + r] = dot[r]; }
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if (ks < mt / 2) continue;
-                Frag a[LAST];
-                frags_cols<LAST, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16, lane);
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    Frag b[RAW];
-                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16, lane);
-                    mma<LAST, RAW>(gk[t], a, b);
-                }
-            }
-        }
-        __syncthreads();
-        rows.template put<LD>(tile);
-        if (hh + 1 == share) ask_queries();
         __syncthreads();
         {
             const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
@@ -413,7 +391,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
             for (int r = 0; r < 4; ++r) db_[r] = dc_[r] = 0.f;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                const v4f_t k = tile_of<RAW, LD>(tile, PLANE, mt * 16, col0 + t * 16, lane);
+                const v4f_t k = tile_of<RAW, LD>(kt, PLANE, mt * 16, col0 + t * 16, lane);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = mt * 16 + 4 * q4 + r;
@@ -440,9 +418,47 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
-                    frags_cols<RAW, LD>(b, tile, PLANE, ks * 32, col0 + t * 16, lane);
-                    if (ks <= mt / 2) mma<LAST, RAW>(gq[t], a, b);
+                    frags_cols<RAW, LD>(b, kt, PLANE, ks * 32, col0 + t * 16, lane);
+                    // (F is zero above the diagonal.  With a branch that leaves those products out, the compiler of this version read results of fp32's 64-wide keys
+                    // two instructions behind the matrix instruction that forms them, over the branch, without the wait that they take.)
+                    mma<LAST, RAW>(gq[t], a, b);
                     mma<LAST, RAW>(gk[t], b2, b);
+                }
+            }
+        }
+        if constexpr (!C::TWO) {
+            __syncthreads();
+            rows.template put<LD>(qt);
+            if (hh + 1 == share) ask_keys();
+            __syncthreads();
+        }
+        {
+            const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
+            float dot[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot[r] = 0.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const v4f_t q = tile_of<RAW, LD>(qt, PLANE, mt * 16, col0 + t * 16, lane);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = ys[t][r] * vec[VEC_ASK * 64 + mt * 16 + 4 * q4 + r];
+                    gq[t][r] += x;
+                    dot[r] += x * q[r];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { dot[r] = row_sum(dot[r]); if (m == 0) dot_a[half * 64 + mt * 16 + 4 * q4 + r] = dot[r]; }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if (ks < mt / 2) continue;
+                Frag a[LAST];
+                frags_cols<LAST, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16, lane);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    Frag b[RAW];
+                    frags_cols<RAW, LD>(b, qt, PLANE, ks * 32, col0 + t * 16, lane);
+                    mma<LAST, RAW>(gk[t], a, b);
                 }
             }
         }
@@ -465,11 +481,11 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
             const float dbeta = xv[lane] - b + row_m[lane];
             float dg = d + w + (pass + vec[VEC_ONE * 64] * sum), for_a = 0.f, for_A = 0.f;
             if (lane < at.len) {
-                const float raw = gd_raw(g, gate_a, h), soft = gd_soft(g, raw), A = g.A ? g.A[h] : -1.f;
+                const float raw = gd_raw(g, gate_a.at(0), h), soft = gd_soft(g, raw), A = g.A ? g.A[h] : -1.f;
                 if (A * soft < GD_LEAST) dg = 0.f;
                 for_A = dg * soft;
                 for_a = dg * A * (g.softplus ? 1.f / (1.f + expf(-raw)) : 1.f);
-                const float rate = gd_rate(g, gate_b);
+                const float rate = gd_rate(g, gate_b.at(0));
                 stf(da + (at.first + lane) * g.a_stride + h, for_a);
                 stf(db + (at.first + lane) * g.b_stride + h, g.sigmoid ? dbeta * rate * (1.f - rate) : dbeta);
             }
@@ -482,8 +498,8 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         }
     }
 
-    // The lengths: of n = r x the gradient r (dn - n (n.dn)), where the factor r is in already.  The tile holds the keys.
-    auto finish = [&](v4f_t (&grad)[TILES], int which, T *out, long long stride) {
+    // The lengths: of n = r x the gradient r (dn - n (n.dn)), where the factor r is in already.
+    auto finish = [&](v4f_t (&grad)[TILES], const bf16_t *tile, int which, T *out, long long stride) {
         const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
         if (g.norm) {
             float dot[4];
@@ -529,11 +545,13 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
             }
         }
     };
-    finish(gk, VEC_RK, dk + at.first * g.k_stride + (long long)kh * g.K, g.k_stride);
-    __syncthreads();
-    rows.template put<LD>(tile);
-    __syncthreads();
-    finish(gq, VEC_RQ, dq + at.first * g.q_stride + (long long)kh * g.K, g.q_stride);
+    finish(gq, qt, VEC_RQ, dq + at.first * g.q_stride + (long long)kh * g.K, g.q_stride);
+    if constexpr (!C::TWO) {
+        __syncthreads();
+        rows.template put<LD>(kt);
+        __syncthreads();
+    }
+    finish(gk, kt, VEC_RK, dk + at.first * g.k_stride + (long long)kh * g.K, g.k_stride);
 }
 
 template <typename T, int KP>
