@@ -8,8 +8,8 @@
 //   the gradient of the logarithm of token t's decay: the sum of what has passed it, exp(G_end) dS.S, all that tokens i >= t read of S, all that tokens j < t write for
 //           the chunk's end, and F * QK^T + M * KK^T over i >= t > j.  No term is in it that does not carry the decay: none cancel, however small it is.
 // One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens (of 256-wide keys 128 columns).  What is contracted over V
-// is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 138 us (with products of keys and queries
-// before it, and one tile for both, 146).
+// is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 129 us (with products of keys and queries
+// before it, and one tile for both, 146; with blocks of columns in one place 138).
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 
@@ -28,9 +28,11 @@ template <typename T, int KP> struct Back {
     static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)LAST * CHUNK * CHUNK * 2;
     static constexpr bool TWO = 2 * TILE + 2 * MATRIX <= 144 * 1024;    // keys and queries at once; else one after the other in the same place
     static constexpr size_t SECOND = (TWO ? 2 : 1) * TILE + 2 * MATRIX;
-    static constexpr size_t REGION = FIRST > SECOND ? FIRST : SECOND;
     // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums; the chunk's vectors
-    static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8 + VECS * 64, LDS = REGION + FLOATS * 4;
+    static constexpr size_t FLOATS = 2 * 64 + 8 * 64 + 3 * 2 * 64 + 8 + VECS * 64;
+    // Blocks of columns in two places in turn, where that costs no block of a compute unit: one barrier a block, and wavefronts write the next one while others still take products
+    static constexpr bool DOUBLE = !TURNS && !(RAW == 1 && KP <= 32) && 2 * FIRST + FLOATS * 4 <= 160 * 1024;
+    static constexpr size_t BLOCKS = (DOUBLE ? 2 : 1) * FIRST, REGION = BLOCKS > SECOND ? BLOCKS : SECOND, LDS = REGION + FLOATS * 4;
 };
 
 constexpr int DPP_SHR1 = 0x111, DPP_SHR2 = 0x112, DPP_SHR4 = 0x114, DPP_SHR8 = 0x118;      // from the lane so many to the left, zero at a row's start
@@ -75,8 +77,6 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
     constexpr int RAW = C::RAW, LAST = C::LAST, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
     constexpr int TILES = C::TILES, THREADS = C::THREADS, HALVES = C::HALVES;
     extern __shared__ __align__(16) char lds[];
-    bf16_t *const st = reinterpret_cast<bf16_t *>(lds), *const dst = C::TURNS ? st : st + INNER * PLANE_S;
-    bf16_t *const xt = dst + INNER * PLANE_S, *const ut = xt + INNER * PLANE_V, *const yt = ut + INNER * PLANE_V;
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = C::TWO ? kt + RAW * PLANE : kt, *const fm = qt + RAW * PLANE, *const mm = fm + LAST * PLANE_M;
     float *const row_m = reinterpret_cast<float *>(lds + C::REGION), *const xv = row_m + 64;
     float *const passing = xv + 64, *const dot_a = passing + 8 * 64, *const dot_b = dot_a + 2 * 64, *const dot_c = dot_b + 2 * 64;
@@ -173,7 +173,9 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
         float ss = 0.f, xv_part = 0.f;                   // dS.S and X.V, this lane's share
 
         for (int v0 = 0; v0 < l.VP; v0 += VB) {
-            __syncthreads();
+            if (!C::DOUBLE || v0 == 0) __syncthreads();
+            bf16_t *const st = reinterpret_cast<bf16_t *>(lds + (C::DOUBLE && (v0 / VB) % 2 ? C::FIRST : 0)), *const dst = C::TURNS ? st : st + INNER * PLANE_S;
+            bf16_t *const xt = dst + INNER * PLANE_S, *const ut = xt + INNER * PLANE_V, *const yt = ut + INNER * PLANE_V;
             if (v0 == 0) {
 #pragma unroll
                 for (int i = 0; i < VECS_PER; ++i)
