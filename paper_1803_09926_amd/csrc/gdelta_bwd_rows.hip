@@ -21,7 +21,7 @@ constexpr int VB = 32, LDV = VB;
 
 template <typename T, int KP> struct Back {
     static constexpr int RAW = PartsOf<T>::RAW, LAST = PartsOf<T>::LAST, LD = KP;
-    static constexpr int HALVES = KP > 128 || (KP >= 64 && RAW == 1) ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
+    static constexpr int HALVES = KP >= 64 ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
     static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
     static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
     static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
