@@ -84,7 +84,7 @@ size_t backward_bytes(const gdelta_desc *d, const GdLayout &l)
 int piece_of(const gdelta_desc *d, const GdLayout &l, bool packed)
 {
     const char *const forced = tune_env("DWCONV_TUNE_GDELTA_PIECE");
-    if (forced) return atoi(forced) > 0 ? atoi(forced) : 0;
+    if (forced) return atoi(forced) > 0 ? (int)fmin(atoi(forced), 1 << 24) : 0;      // (a piece's tokens are counted in 32 bits)
     const bool ragged = packed && d->sequences > 1;
     const double n = d->sequences, chunks = ceil((double)d->T / (n * TOKENS)), longest = ragged ? chunks * (0.6 + log(n)) : chunks, units = 256;
     const double columns = (double)((l.VP + 63) / 64), all = columns + (double)((l.KP + 63) / 64), join = 0.3 + 2.4 * l.KP / 128.0;

@@ -16,15 +16,19 @@ namespace dwc {
 
 namespace {
 
-// Whether the product of a stretch's decays is zero in fp32, and all of them are numbers
+// Whether the product of a stretch's decays is zero in fp32, and all of them are numbers of at most one (a product in another order than the tokens' says nothing where some are larger)
 __device__ __forceinline__ bool a_decay_is_zero(const GdArgs &g, const GdLayout &l, const GdSpace &s, const Stretch &at, int h)
 {
     float p = 1.f;
-    for (int c = at.from + (int)(threadIdx.x & 63); c < at.to; c += 64)
-        p *= reinterpret_cast<const float *>(s.vec + (((long long)at.base + c) * g.H + h) * l.vectors)[VEC_ONE * 64];
+    bool grows = false;
+    for (int c = at.from + (int)(threadIdx.x & 63); c < at.to; c += 64) {
+        const float d = reinterpret_cast<const float *>(s.vec + (((long long)at.base + c) * g.H + h) * l.vectors)[VEC_ONE * 64];
+        grows |= !(d <= 1.f);
+        p *= d;
+    }
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) p *= __shfl_xor(p, off, 64);
-    return p == 0.f;
+    return !__any(grows) && p == 0.f;
 }
 
 template <typename T, int KP, bool MAP, bool EXACT> using WalkOf = Walk<T, KP, !MAP, (EXACT ? INNER : PartsOf<T>::LAST) + (MAP ? 0 : PartsOf<T>::LAST)>;

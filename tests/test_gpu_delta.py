@@ -165,6 +165,27 @@ def test_many_sequences(gpu_lib, dtype, Hk, H, K, V, more, shift):
     check(m, x, par, list(range(0, 394, 3)), None, more, even=True)
 
 
+def test_a_state_grows_and_decays_within_a_piece(gpu_lib):
+    """e^80 times as large over two chunks and e^-110 over two more: what is left of the state, e^-30 of it, is all that there is.  (Logarithms of 190 in all are rounded to
+    2^-24 of themselves: 1.1e-5 of the result.)"""
+    m = Made(29, "f32")
+    T = 12 * 64
+    x, par = host_inputs(m, T, 1, 1, 8, 8)
+    x["v"][...] = 0
+    x["b"][...] = -20                            # (next to nothing is taken off)
+    x["a"][...] = 0
+    for c, log in ((4, 40), (5, 40), (6, -55), (7, -55)):
+        x["a"][64 * c:64 * c + 64] = -log / 64
+    par = {"A": np.array([-1.0], np.float32), "a_bias": None}
+    init = m.host((1, 1, 8, 8), stored=False)
+    want = od.Rule(**x, **par, bounds=[0, T], init=init, softplus=False)
+    for piece in (0, 1, 4):
+        with dw.tuning_overrides({"DWCONV_TUNE_GDELTA_PIECE": piece}):
+            y, final = Call(m, x, par, [0, T], softplus=False).forward(init)
+        _close(final, want.final, 4e-5, "final")
+        _close(y, want.y, 4e-5, "y")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_decays_of_any_size(gpu_lib, dtype):
     """From nothing forgotten to everything, beside each other in a chunk; what is clamped has no gradient."""
