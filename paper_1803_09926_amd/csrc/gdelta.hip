@@ -76,9 +76,9 @@ size_t backward_bytes(const gdelta_desc *d, const GdLayout &l)
 
 // How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole: the least of an estimated time, in us.  Of 128-wide keys in bf16 a chunk
 // of a walk takes 3.8 us and of a piece and its map 5.5 together, both where a compute unit has one block; each more takes 2 us a chunk of each pass; the two passes begin with
-// another chunk's time and 4 us; a piece in the join takes 2.7.  Narrower keys take less of it, by 64 the share of 0.78, wider ones and fp32 more (1.45, 1.75).
+// another chunk's time and 4 us; a piece in the join takes 2.7.  Narrower keys take less of it, by 64 the share of 0.78, wider ones and fp32 more (1.45; 1.75, of wide keys, which spill, 3).
 // Lengths that are not known here are taken to be those that points cut at random out of T: the longest is 0.6 + ln n times their mean, and nothing is left idle at the end of a round
-// of blocks.  Measured, whole and in pieces: 16384 tokens of 16 heads of 128 x 128 in one sequence 951 us and 283, of 4 heads 893 and 165, 1000 tokens of 8 heads 67 and 48;
+// of blocks.  Measured, whole and in pieces: 16384 tokens of 16 heads of 128 x 128 in one sequence 951 us and 283, of 4 heads 893 and 165, 1000 tokens of 8 heads 67 and 48, in fp32 of 4 heads of 256 x 256 322 and 157;
 // 24 prompts of 2 to 2000 tokens, 16 heads of 64 x 128, 226 and 190; forward and backward of 5 prompts in 1501 tokens, 6 heads of 40 x 56 in fp32, 190 and 135.  Whole, as it should
 // be: 8 sequences of 1024 tokens, 8 heads, forward and backward 344 and 361; 64 prompts of 256 tokens at the mean 163 and 183; 301 tokens 24 and 26.
 int piece_of(const gdelta_desc *d, const GdLayout &l, bool packed)
@@ -88,7 +88,7 @@ int piece_of(const gdelta_desc *d, const GdLayout &l, bool packed)
     const bool ragged = packed && d->sequences > 1;
     const double n = d->sequences, chunks = ceil((double)d->T / (n * TOKENS)), longest = ragged ? chunks * (0.6 + log(n)) : chunks, units = 256;
     const double columns = (double)((l.VP + 63) / 64), all = columns + (double)((l.KP + 63) / 64), join = 0.3 + 2.4 * l.KP / 128.0;
-    const double work = (0.55 + 0.45 * l.KP / 128.0) * (d->dtype == DWCONV_F32 ? 1.75 : 1);
+    const double work = (0.55 + 0.45 * l.KP / 128.0) * (d->dtype != DWCONV_F32 ? 1 : l.KP > 128 ? 3 : 1.75);
     auto more = [&](double blocks, double each, double part) {       // chunks' times of a pass beyond those of a block alone
         return ragged ? 1.3 * fmax(0, blocks * each * part / units - each) : 2 * each * (ceil(blocks / units) - 1);
     };
