@@ -233,7 +233,6 @@ template <typename T, int KP, int THREADS, bool WHOLE> struct Rows {
 // One of the first pass's matrices, of N parts: zero above the diagonal, and the 32 x 32 block there is neither stored nor read.  A part is 384 pieces of 16 bytes in the
 // LDS tiles' order of columns (not turned): four of each of the first 32 rows, eight of each of the others.  So it is in LDS too: a tile of 32 columns, one of 64 behind it.
 constexpr int MATRIX_PIECES = 384, MATRIX_PLANE = MATRIX_PIECES * 8;
-__device__ __forceinline__ constexpr int matrix_piece(int row, int piece) { return row < 32 ? row * 4 + piece : row * 8 + piece - 128; }
 // ... on its way to LDS.  A wavefront has 64 pieces at a time, all of them of one of the two tiles: in LDS too they are those 64, in the order of the tile's turns.
 template <int N, int THREADS> struct Matrix {
     static constexpr int ALL = N * MATRIX_PIECES, PER = (ALL + THREADS - 1) / THREADS;
