@@ -35,9 +35,9 @@ extern "C" {
  * A number that is not finite leaves the outputs of its head before its token, of the other heads, and of other sequences as they were; which of the head's outputs from
  * its token on are not finite is not specified.  The same holds for the gradients of other sequences, and of heads of other key heads.
  *
- * T / 64 + sequences must be less than 2^31.  With bf16 tensors a call that is asked for y alone holds what it computes between tokens to 2^-17 of itself, one that is
- * asked for `final` or `kept` to 2^-24: y may differ in its last bit.  A backward pass takes `starts` where its forward pass did, with the same values, and the same
- * value of DWCONV_TUNE_GDELTA_PIECE (the chunks of 64 tokens that a piece of a long sequence has, by default chosen from the sizes; kept's layout goes by it). */
+ * T / 64 + sequences must be less than 2^31.  What is computed between tokens holds 24 bits with bf16 tensors too, and y has the same bits whatever else a call is
+ * asked for.  A backward pass takes `starts` where its forward pass did, with the same values, and the same value of DWCONV_TUNE_GDELTA_PIECE (the chunks of 64 tokens
+ * that a piece of a long sequence has, by default chosen from the sizes; kept's layout goes by it). */
 #define GDELTA_MAX_K 256
 #define GDELTA_MAX_V 256
 #define GDELTA_MAX_H 65535          /* value heads */

@@ -187,7 +187,7 @@ int gdelta_fwd(const gdelta_desc *desc, const gdelta_tensors *t, void *workspace
     if (desc->T == 0 && !t->final) return DWCONV_OK;
     const GdArgs g = args_of(desc, t);
     hipError_t e = hipSuccess;
-    if (desc->T > 0) e = launch_gdelta_prep(desc->dtype, g, l, s, (const float *)t->final, (hipStream_t)stream);
+    if (desc->T > 0) e = launch_gdelta_prep(desc->dtype, g, l, s, (hipStream_t)stream);
     if (e == hipSuccess) e = launch_gdelta_fwd(desc->dtype, g, l, s, (const float *)t->init, t->y, (float *)t->final, (hipStream_t)stream);
     return e == hipSuccess ? DWCONV_OK : DWCONV_ERR_LAUNCH;
 }

@@ -177,7 +177,7 @@ template <typename T, int KP> hipError_t walk(const GdArgs &g, const GdLayout &l
 {
     if (l.piece) {
         hipError_t e = launch<T, KP, 1, true>(g, l, s, dy, dv, stream);
-        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, INNER, true, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, true, stream);
         if (e != hipSuccess) return e;
     }
     if constexpr (may_have_two_tiles<T, KP>) {

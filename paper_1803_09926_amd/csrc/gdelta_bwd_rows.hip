@@ -20,12 +20,12 @@ namespace {
 constexpr int VB = 32, LDV = VB;
 
 template <typename T, int KP> struct Back {
-    static constexpr int RAW = PartsOf<T>::RAW, LAST = PartsOf<T>::LAST, LD = KP;
+    static constexpr int RAW = PartsOf<T>::RAW, LD = KP;
     static constexpr int HALVES = KP >= 64 ? 2 : 1, THREADS = 256 * HALVES, KW = KP / HALVES, TILES = KW / 16;
     static constexpr bool TURNS = RAW == 3 && KP > 128;           // S and dS one after the other in the same place
     static constexpr size_t STATE = (size_t)INNER * KP * LDV * 2, COLS = (size_t)INNER * CHUNK * LDV * 2, DY = (size_t)RAW * CHUNK * LDV * 2;
     static constexpr size_t FIRST = (TURNS ? 1 : 2) * STATE + 2 * COLS + DY;
-    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)LAST * CHUNK * CHUNK * 2;
+    static constexpr size_t TILE = (size_t)RAW * CHUNK * LD * 2, MATRIX = (size_t)INNER * CHUNK * CHUNK * 2;
     static constexpr bool TWO = 2 * TILE + 2 * MATRIX <= 144 * 1024;    // keys and queries at once; else one after the other in the same place
     static constexpr size_t SECOND = (TWO ? 2 : 1) * TILE + 2 * MATRIX;
     // behind it: [64] row sums of M KK^T / beta, X.V; [8][64] what of F QK^T and M KK^T passes a token, by wavefront; [HALVES][64] three products of rows; 8 sums; the chunk's vectors
@@ -74,10 +74,10 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
     typedef Back<T, KP> C;
-    constexpr int RAW = C::RAW, LAST = C::LAST, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
+    constexpr int RAW = C::RAW, LD = C::LD, PLANE = CHUNK * LD, PLANE_M = CHUNK * CHUNK, PLANE_S = KP * LDV, PLANE_V = CHUNK * LDV;
     constexpr int TILES = C::TILES, THREADS = C::THREADS, HALVES = C::HALVES;
     extern __shared__ __align__(16) char lds[];
-    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = C::TWO ? kt + RAW * PLANE : kt, *const fm = qt + RAW * PLANE, *const mm = fm + LAST * PLANE_M;
+    bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = C::TWO ? kt + RAW * PLANE : kt, *const fm = qt + RAW * PLANE, *const mm = fm + INNER * PLANE_M;
     float *const row_m = reinterpret_cast<float *>(lds + C::REGION), *const xv = row_m + 64;
     float *const passing = xv + 64, *const dot_a = passing + 8 * 64, *const dot_b = dot_a + 2 * 64, *const dot_c = dot_b + 2 * 64;
     float *const wave_sums = dot_c + 2 * 64, *const vec = wave_sums + 8;
@@ -322,7 +322,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
 #pragma unroll
-                            for (int k = 0; k < LAST; ++k) fm[k * PLANE_M + place<CHUNK>(mt * 16 + 4 * q4 + r, j)] = 0;
+                            for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(mt * 16 + 4 * q4 + r, j)] = 0;
                     }
                 } else {
                     const double gj = G[j];
@@ -332,23 +332,23 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                     for (int r = 0; r < 4; ++r) {
                         const int i = mt * 16 + 4 * q4 + r;
                         const float e = i >= j ? exp2_fast((float)(G[i] - gj) * LOG2E) * kj : 0.f;
-                        uint32_t p[LAST];
+                        uint32_t p[INNER];
                         x[r] = 0.f;
                         if (does_f) {
                             const float f = g.scale * vec[VEC_RQ * 64 + i] * e * yu[0][n][r];
                             x[r] = f * qk[0][n][r];
-                            split2<LAST>(f, 0.f, p);
+                            split2<INNER>(f, 0.f, p);
 #pragma unroll
-                            for (int k = 0; k < LAST; ++k) fm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
+                            for (int k = 0; k < INNER; ++k) fm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
                         }
                         if (does_m) {
                             const float b = i > j ? -vec[VEC_RK * 64 + i] * e * yu[AT_M][n][r] : 0.f, f = vec[VEC_BETA * 64 + i] * b;
                             rm[r] += b * qk[AT_M][n][r];
                             x[r] += f * qk[AT_M][n][r];
-                            split2<LAST>(f, 0.f, p);
+                            split2<INNER>(f, 0.f, p);
                             if (i >= j) {
 #pragma unroll
-                                for (int k = 0; k < LAST; ++k) {
+                                for (int k = 0; k < INNER; ++k) {
                                     mm[k * PLANE_M + place<CHUNK>(i, j)] = (bf16_t)p[k];
                                     mm[k * PLANE_M + place<CHUNK>(j, i)] = (bf16_t)p[k];
                                 }
@@ -414,17 +414,17 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
             }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                Frag a[LAST], b2[LAST];
-                frags_rows<LAST, CHUNK>(a, fm, PLANE_M, mt * 16, ks * 32, lane);
-                frags_rows<LAST, CHUNK>(b2, mm, PLANE_M, mt * 16, ks * 32, lane);
+                Frag a[INNER], b2[INNER];
+                frags_rows<INNER, CHUNK>(a, fm, PLANE_M, mt * 16, ks * 32, lane);
+                frags_rows<INNER, CHUNK>(b2, mm, PLANE_M, mt * 16, ks * 32, lane);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
                     frags_cols<RAW, LD>(b, kt, PLANE, ks * 32, col0 + t * 16, lane);
                     // (F is zero above the diagonal.  With a branch that leaves those products out, the compiler of this version read results of fp32's 64-wide keys
                     // two instructions behind the matrix instruction that forms them, over the branch, without the wait that they take.)
-                    mma<LAST, RAW>(gq[t], a, b);
-                    mma<LAST, RAW>(gk[t], b2, b);
+                    mma<INNER, RAW>(gq[t], a, b);
+                    mma<INNER, RAW>(gk[t], b2, b);
                 }
             }
         }
@@ -454,13 +454,13 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 if (ks < mt / 2) continue;
-                Frag a[LAST];
-                frags_cols<LAST, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16, lane);
+                Frag a[INNER];
+                frags_cols<INNER, CHUNK>(a, fm, PLANE_M, ks * 32, mt * 16, lane);
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
                     frags_cols<RAW, LD>(b, qt, PLANE, ks * 32, col0 + t * 16, lane);
-                    mma<LAST, RAW>(gk[t], a, b);
+                    mma<INNER, RAW>(gk[t], a, b);
                 }
             }
         }

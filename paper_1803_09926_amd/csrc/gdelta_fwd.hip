@@ -7,8 +7,6 @@
 // are on their way from memory meanwhile.  Bound by the way through a chunk, K S, T, K^T U, each of whose results is split and handed on: 128 x 128 in bf16 5.8 us a chunk where a
 // compute unit has one block, 4.1 where it has two; 8 x 1024 tokens of 8 heads 94 us.  (K S and Q S at once, behind one pair of barriers, 105 us.)
 //
-// EXACT: what leaves the walk in fp32, the states behind sequences or what a backward pass takes, is made of three parts; where nothing does, of as many as the answers.
-//
 // MAP: the map of a piece of a sequence instead (gdelta_launch.hpp).  What it makes of zero (of the state that the sequence begins with, in the first piece) is the walk without
 // answers, and its matrix is what the walk without values makes of the K unit vectors: K columns more.
 #include "gdelta_states.hpp"
@@ -32,19 +30,19 @@ __device__ __forceinline__ bool a_decay_is_zero(const GdArgs &g, const GdLayout 
     return !__any(grows) && p == 0.f;
 }
 
-template <typename T, int KP, bool MAP, bool EXACT> using WalkOf = Walk<T, KP, !MAP, (EXACT ? INNER : PartsOf<T>::LAST) + (MAP ? 0 : PartsOf<T>::LAST)>;
+template <typename T, int KP, bool MAP> using WalkOf = Walk<T, KP, !MAP, (MAP ? 1 : 2) * INNER>;
 
-template <typename T, int KP, int NT, bool WHOLE, bool MAP, bool EXACT>
+template <typename T, int KP, int NT, bool WHOLE, bool MAP>
 __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && PartsOf<T>::RAW == 1 ? 2 : 1)) void k_gdelta_fwd(GdArgs g, GdLayout l, GdSpace s, const float *__restrict__ init, T *__restrict__ y,
                                                            float *__restrict__ final, long long first, int blocks)
 {
-    typedef WalkOf<T, KP, MAP, EXACT> W;
-    constexpr int RAW = W::RAW, LAST = PartsOf<T>::LAST, N = EXACT ? INNER : LAST;
+    typedef WalkOf<T, KP, MAP> W;
+    constexpr int RAW = W::RAW, N = INNER;
     constexpr bool SHARE = W::SHARE;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds), *const qt = SHARE || MAP ? kt : kt + RAW * CHUNK * KP;
     bf16_t *const tm = qt + RAW * CHUNK * KP, *const pm = tm + N * MATRIX_PLANE;
-    float *const vecs = reinterpret_cast<float *>(pm + (MAP ? 0 : LAST) * MATRIX_PLANE);     // two chunks' worth, in turn
+    float *const vecs = reinterpret_cast<float *>(pm + (MAP ? 0 : N) * MATRIX_PLANE);     // two chunks' worth, in turn
     const int share = g.H / g.key_heads;
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)(blocks * share));      // of a key head: its value heads' blocks of columns
     if (which.item >= (l.piece ? l.pieces : (long long)g.sequences) * g.key_heads) return;
@@ -89,8 +87,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     split_state();
 
     Rows<T, KP, THREADS, WHOLE> rows;
-    Matrix<N, THREADS> matrix;
-    Matrix<LAST, THREADS> answers;
+    Matrix<N, THREADS> matrix, answers;
     Ahead<T, NT, WHOLE> v[4][4];
     float vec_next, decay_next;
     int bad_next;
@@ -167,6 +164,11 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) R[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
         times_state<RAW, N, KP>(R, kt, Sp);
+        // (here, not behind the state's sums: their registers and those of T's products do not fit beside it.  All wavefronts have read the chunk before's.)
+        if constexpr (!MAP) {
+            answers.put(pm);
+            if constexpr (!SHARE) rows.template put<KP>(qt);
+        }
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             const float4 read = four(vl + VEC_READ * 64, mt), beta = four(vl + VEC_BETA * 64, mt);
@@ -212,28 +214,29 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         if constexpr (MAP) {
             if (c + 1 < chunks) load_values(c + 1);
         } else {
-            if constexpr (SHARE) __syncthreads();
-            rows.template put<KP>(qt);
-            answers.put(pm);
+            if constexpr (SHARE) {
+                __syncthreads();
+                rows.template put<KP>(qt);
+            }
             if (c + 1 < chunks) {
                 load_next(c + 1);
                 load_values(c + 1);
             }
             __syncthreads();
-            Frag u[2][NT][LAST];
-            split_rows<LAST, NT>(U, u);
+            Frag u[2][NT][N];
+            split_rows<N, NT>(U, u);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
-            times_state<RAW, LAST, KP>(O, qt, Sp);
+            times_state<RAW, N, KP>(O, qt, Sp);
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
                 const float4 ask = four(vl + VEC_ASK * 64, mt);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[mt][nt] = times(O[mt][nt], ask);
             }
-            times_triangle<LAST, false>(O, pm, u);
+            times_triangle<N, false>(O, pm, u);
         }
         if (odd) {
             seldom();
@@ -272,13 +275,13 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
     } else if (final && at_.place == at_.pieces - 1) store_state<NT, KP / 16>(S, final + state, g.K, g.V, cols);
 }
 
-template <typename T, int KP, int NT, bool MAP, bool EXACT>
+template <typename T, int KP, int NT, bool MAP>
 hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    constexpr size_t lds = WalkOf<T, KP, MAP, EXACT>::LDS;
+    constexpr size_t lds = WalkOf<T, KP, MAP>::LDS;
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const bool whole = whole_keys<T>(g) && (NT == 1 || pair_values<T>(g, g.v, y, g.v_stride, g.y_stride));
-    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, true, MAP, EXACT> : k_gdelta_fwd<T, KP, NT, false, MAP, EXACT>;
+    const auto kernel = whole ? k_gdelta_fwd<T, KP, NT, true, MAP> : k_gdelta_fwd<T, KP, NT, false, MAP>;
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     const int blocks = cdiv(l.VP, WAVES * 16 * NT) + (MAP ? cdiv(KP, WAVES * 16 * NT) : 0);
@@ -289,27 +292,27 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const fl
 }
 
 // The walk; where sequences go in pieces their maps first, and the states that they begin with
-template <typename T, int KP, bool EXACT>
+template <typename T, int KP>
 hipError_t walk(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
     if (l.piece) {
-        hipError_t e = launch<T, KP, 1, true, EXACT>(g, l, s, init, y, final, stream);
-        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, EXACT ? INNER : PartsOf<T>::LAST, false, stream);
+        hipError_t e = launch<T, KP, 1, true>(g, l, s, init, y, final, stream);
+        if (e == hipSuccess) e = launch_gdelta_join(g, l, s, false, stream);
         if (e != hipSuccess) return e;
     }
     if constexpr (may_have_two_tiles<T, KP>) {
-        if (two_tiles(g, l)) return launch<T, KP, 2, false, EXACT>(g, l, s, init, y, final, stream);
+        if (two_tiles(g, l)) return launch<T, KP, 2, false>(g, l, s, init, y, final, stream);
     }
-    return launch<T, KP, 1, false, EXACT>(g, l, s, init, y, final, stream);
+    return launch<T, KP, 1, false>(g, l, s, init, y, final, stream);
 }
 
-template <typename T, bool EXACT> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
+template <typename T> hipError_t walk_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
     switch (l.KP) {
-    case 32: return walk<T, 32, EXACT>(g, l, s, init, y, final, stream);
-    case 64: return walk<T, 64, EXACT>(g, l, s, init, y, final, stream);
-    case 128: return walk<T, 128, EXACT>(g, l, s, init, y, final, stream);
-    default: return walk<T, 256, EXACT>(g, l, s, init, y, final, stream);
+    case 32: return walk<T, 32>(g, l, s, init, y, final, stream);
+    case 64: return walk<T, 64>(g, l, s, init, y, final, stream);
+    case 128: return walk<T, 128>(g, l, s, init, y, final, stream);
+    default: return walk<T, 256>(g, l, s, init, y, final, stream);
     }
 }
 
@@ -317,8 +320,7 @@ template <typename T, bool EXACT> hipError_t walk_of(const GdArgs &g, const GdLa
 
 hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream)
 {
-    if (dtype == DWCONV_F32) return walk_of<float, true>(g, l, s, init, y, final, stream);
-    return gd_exact(s, final) ? walk_of<bf16_t, true>(g, l, s, init, y, final, stream) : walk_of<bf16_t, false>(g, l, s, init, y, final, stream);
+    return dtype == DWCONV_F32 ? walk_of<float>(g, l, s, init, y, final, stream) : walk_of<bf16_t>(g, l, s, init, y, final, stream);
 }
 
 }  // namespace dwc

@@ -12,10 +12,10 @@ namespace dwc {
 
 namespace {
 
-template <int KP, int N, bool BACK>
+template <int KP, bool BACK>
 __global__ __launch_bounds__(2 * KP, 1) void k_gdelta_join(GdArgs g, GdLayout l, GdSpace s, long long first, int blocks)
 {
-    constexpr int GROUPS = KP / 32;                      // of 32 rows: one a wavefront
+    constexpr int GROUPS = KP / 32, N = INNER;           // of 32 rows: one a wavefront
     __shared__ u4t_t handed[2][GROUPS][N][64];
     const Shared which = gd_shared(first + blockIdx.x, (unsigned)blocks);
     if (which.item >= (long long)g.sequences * g.H) return;
@@ -97,29 +97,24 @@ __global__ __launch_bounds__(2 * KP, 1) void k_gdelta_join(GdArgs g, GdLayout l,
     store(S, stop + step);
 }
 
-template <int KP, int N> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
+template <int KP> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
 {
     const int blocks = l.VP / 16;
     return gd_launches(gd_shared_blocks((long long)g.sequences * g.H, blocks), 2 * KP, [&](long long first, unsigned now) {
-        if (backward) hipLaunchKernelGGL((k_gdelta_join<KP, N, true>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
-        else hipLaunchKernelGGL((k_gdelta_join<KP, N, false>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
+        if (backward) hipLaunchKernelGGL((k_gdelta_join<KP, true>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
+        else hipLaunchKernelGGL((k_gdelta_join<KP, false>), dim3(now), dim3(2 * KP), 0, stream, g, l, s, first, blocks);
     });
-}
-
-template <int KP> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream)
-{
-    return parts == 2 ? launch<KP, 2>(g, l, s, backward, stream) : launch<KP, 3>(g, l, s, backward, stream);
 }
 
 }  // namespace
 
-hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream)
+hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream)
 {
     switch (l.KP) {
-    case 32: return launch_of<32>(g, l, s, parts, backward, stream);
-    case 64: return launch_of<64>(g, l, s, parts, backward, stream);
-    case 128: return launch_of<128>(g, l, s, parts, backward, stream);
-    default: return launch_of<256>(g, l, s, parts, backward, stream);
+    case 32: return launch<32>(g, l, s, backward, stream);
+    case 64: return launch<64>(g, l, s, backward, stream);
+    case 128: return launch<128>(g, l, s, backward, stream);
+    default: return launch<256>(g, l, s, backward, stream);
     }
 }
 

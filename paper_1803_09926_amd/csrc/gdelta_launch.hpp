@@ -26,12 +26,10 @@ struct GdSpace {
 };
 
 hipError_t launch_gdelta_step(int dtype, const GdArgs &g, const int32_t *slots, float *state, void *y, hipStream_t stream);
-// Whether the walk forward leaves anything in fp32
-inline bool gd_exact(const GdSpace &s, const float *final) { return s.S || final; }
-hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *final, hipStream_t stream);
+hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream);
 hipError_t launch_gdelta_fwd(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *init, void *y, float *final, hipStream_t stream);
 // the states that the pieces begin with, out of what they make of zero and of their matrices; backward: of the gradients, from the last piece to the first
-hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, int parts, bool backward, hipStream_t stream);
+hipError_t launch_gdelta_join(const GdArgs &g, const GdLayout &l, const GdSpace &s, bool backward, hipStream_t stream);
 hipError_t launch_gdelta_bwd_states(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dv, hipStream_t stream);
 hipError_t launch_gdelta_bwd_rows(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const void *dy, void *dq, void *dk, void *da, void *db,
                                   hipStream_t stream);

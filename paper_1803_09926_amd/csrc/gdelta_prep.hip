@@ -53,7 +53,7 @@ __device__ __forceinline__ double sum_up_to(float x)
 }
 
 // the parts of an fp32 matrix in LDS, into memory: a lane a piece of 16 bytes, four numbers and the four 16 columns on
-template <int N> __device__ __forceinline__ void put_matrix(const float *f, char *to)
+__device__ __forceinline__ void put_matrix(const float *f, char *to)
 {
 #pragma unroll
     for (int i = 0; i < (MATRIX_PIECES + THREADS - 1) / THREADS; ++i) {
@@ -61,19 +61,19 @@ template <int N> __device__ __forceinline__ void put_matrix(const float *f, char
         if (n >= MATRIX_PIECES) break;
         const int row = n < 128 ? n / 4 : n / 8 + 16, piece = n < 128 ? n % 4 : n % 8;
         const float *const x = f + row * LDF + (piece / 4 * 32 + piece % 4 * 4);
-        Frag w[N];
-        split_tiles<N>(*reinterpret_cast<const v4f_t *>(x), *reinterpret_cast<const v4f_t *>(x + 16), w);
+        Frag w[INNER];
+        split_tiles<INNER>(*reinterpret_cast<const v4f_t *>(x), *reinterpret_cast<const v4f_t *>(x + 16), w);
 #pragma unroll
-        for (int j = 0; j < N; ++j) reinterpret_cast<u4t_t *>(to)[j * MATRIX_PIECES + n] = w[j].w;
+        for (int j = 0; j < INNER; ++j) reinterpret_cast<u4t_t *>(to)[j * MATRIX_PIECES + n] = w[j].w;
     }
 }
 
 template <typename T, int KP, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restrict__ t_out, char *__restrict__ p_out, char *__restrict__ vec_out, long long matrix,
-                                                         long long vectors, int t_parts, int p_parts, unsigned first)
+                                                         long long vectors, unsigned first)
 {
     typedef Prep<T, KP> C;
-    constexpr int RAW = C::RAW, LAST = PartsOf<T>::LAST, LD = C::LD, PLANE = CHUNK * LD;
+    constexpr int RAW = C::RAW, LD = C::LD, PLANE = CHUNK * LD;
     extern __shared__ __align__(16) char lds[];
     bf16_t *const kt = reinterpret_cast<bf16_t *>(lds);
     float *const X = reinterpret_cast<float *>(lds), *const L = reinterpret_cast<float *>(lds + C::FIRST);      // the inverse; L, then P
@@ -299,19 +299,17 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             }
         }
         __syncthreads();
-        if (LAST == INNER || t_parts == INNER) put_matrix<INNER>(X, t_out + where * matrix);
-        else put_matrix<LAST>(X, t_out + where * matrix);
+        put_matrix(X, t_out + where * matrix);
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) L[(wv * 16 + 4 * q4 + r) * LDF + n * 16 + m] = pv[n][r];
         __syncthreads();
-        if (LAST == INNER || p_parts == INNER) put_matrix<INNER>(L, p_out + where * matrix);
-        else put_matrix<LAST>(L, p_out + where * matrix);
+        put_matrix(L, p_out + where * matrix);
     }
 }
 
-template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *final, hipStream_t stream)
+template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
 {
     const auto kernel = whole_keys<T>(g) ? k_gdelta_prep<T, KP, true> : k_gdelta_prep<T, KP, false>;
     constexpr size_t lds = Prep<T, KP>::LDS;
@@ -319,25 +317,26 @@ template <typename T, int KP> hipError_t launch(const GdArgs &g, const GdLayout 
     const hipError_t e = gd_lds(kernel, lds);
     if (e != hipSuccess) return e;
     return gd_launches(l.chunks, THREADS, [&](long long first, unsigned now) {
-        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(THREADS), lds, stream, g, s.T, s.P, s.vec, l.matrix, l.vectors, gd_exact(s, final) ? INNER : PartsOf<T>::LAST, s.S ? INNER : PartsOf<T>::LAST, (unsigned)first);
+        hipLaunchKernelGGL(kernel, dim3(now, (unsigned)g.key_heads), dim3(THREADS), lds, stream, g, s.T, s.P, s.vec, l.matrix, l.vectors,
+                           (unsigned)first);
     });
 }
 
-template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *final, hipStream_t stream)
+template <typename T> hipError_t launch_of(const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
 {
     switch (l.KP) {
-    case 32: return launch<T, 32>(g, l, s, final, stream);
-    case 64: return launch<T, 64>(g, l, s, final, stream);
-    case 128: return launch<T, 128>(g, l, s, final, stream);
-    default: return launch<T, 256>(g, l, s, final, stream);
+    case 32: return launch<T, 32>(g, l, s, stream);
+    case 64: return launch<T, 64>(g, l, s, stream);
+    case 128: return launch<T, 128>(g, l, s, stream);
+    default: return launch<T, 256>(g, l, s, stream);
     }
 }
 
 }  // namespace
 
-hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, const float *final, hipStream_t stream)
+hipError_t launch_gdelta_prep(int dtype, const GdArgs &g, const GdLayout &l, const GdSpace &s, hipStream_t stream)
 {
-    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, final, stream) : launch_of<bf16_t>(g, l, s, final, stream);
+    return dtype == DWCONV_F32 ? launch_of<float>(g, l, s, stream) : launch_of<bf16_t>(g, l, s, stream);
 }
 
 }  // namespace dwc

@@ -1,10 +1,9 @@
 // Tiles of the gated delta rule's matrix products.
 //
 // All products run on the bf16 matrix instruction of 16 x 16 x 32.  A number of 32 bits takes part as a sum of bf16 parts: what a bf16 tensor holds is one part; what
-// the kernels compute themselves (states, inverses, what tokens write) three parts, which hold all of its 24 bits, and so does all that an fp32 tensor holds.  Two parts,
-// 2^-17 of the number, are enough for what goes into nothing but a bf16 tensor of answers or gradients, which is rounded to 2^-9 at once.  Of a product of parts those
-// count whose order is below the larger number of parts (1 x 3: three instructions, 2 x 2: three, 3 x 3: six).  All sums are fp32.  (With two parts throughout the states behind
-// bf16 sequences and the sums over their tokens were 2e-6 to 5e-6 off, and are 2e-7 with three; 8192 tokens' training step took 300 us with two.)
+// the kernels compute themselves (states, inverses, what tokens write and answer) three parts, which hold all of its 24 bits, and so does all that an fp32 tensor holds.
+// Of a product of parts those count whose order is below the larger number of parts (1 x 3: three instructions, 3 x 3: six).  All sums are fp32, and what a call is asked
+// for does not change a bit of its other outputs.  (With two parts, 2^-17 of a number, the states behind bf16 sequences were 2e-6 to 5e-6 off, and are 2e-7 with three.)
 //
 // Lanes: m = lane % 16, q = lane / 16.  A result tile has rows 4 q + r (r = 0..3) of column m in a lane.  Two result tiles below each other are an operand as they are: the
 // contraction runs over their 32 rows in the order 4 q + 0..3 of the first, 4 q + 0..3 of the second.  Tiles in LDS are stored so that 16 consecutive bytes of a row hold the
@@ -54,9 +53,9 @@ template <typename K> hipError_t gd_lds(K kernel, size_t bytes)
 constexpr int CHUNK = 64;
 
 constexpr int INNER = 3;                          // parts of what the kernels compute themselves
-template <typename T> struct PartsOf;            // RAW: of what a tensor holds; LAST: of what goes into nothing but one
-template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1, LAST = 2; };
-template <> struct PartsOf<float> { static constexpr int RAW = 3, LAST = 3; };
+template <typename T> struct PartsOf;            // RAW: of what a tensor holds
+template <> struct PartsOf<bf16_t> { static constexpr int RAW = 1; };
+template <> struct PartsOf<float> { static constexpr int RAW = 3; };
 
 // The number of a lane's wavefront, as a scalar.  What is done by some wavefronts only has to be behind a scalar branch where it holds matrix instructions: those do not
 // look at which lanes are on.
@@ -240,9 +239,9 @@ template <int N, int THREADS> struct Matrix {
     u4t_t v[PER];
     __device__ __forceinline__ void load(const char *p)
     {
-        const BufView view(p, ALL * 16);                 // (beyond it nothing is read)
+        // (beyond the matrix nothing is read; a view for each time: all have one offset)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] = view.b128((threadIdx.x + i * THREADS) * 16, 0);
+        for (int i = 0; i < PER; ++i) v[i] = BufView(p + i * THREADS * 16, (ALL - i * THREADS) * 16).b128(threadIdx.x * 16, 0);
     }
     __device__ __forceinline__ void put(bf16_t *tile) const
     {
