@@ -152,6 +152,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         if (c > from) load_keys(c - 1);
         __syncthreads();
         add_to_state<RAW, KP>(S, qt, f);
+        settled();
     }
     if constexpr (MAP) store_tiles<NT, KP / 16>(S, s.ends + piece * (l.state / 4), l.VP, cols);
 }

@@ -252,6 +252,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 mma<INNER, INNER>(us[t], ua, b);
             }
         }
+        settled();
         __syncthreads();                                 // the first region is free
         rows.template put<LD>(kt);
         if constexpr (C::TWO) others.template put<LD>(qt);
@@ -307,6 +308,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
             }
         }
         // F and M + M^T, and what of their products passes each token
+        settled();
         {
             const int lane = lane_anew(), m = lane & 15, q4 = lane >> 4;
             const double *const G = reinterpret_cast<const double *>(vec + VEC_G * 64);
@@ -421,8 +423,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 for (int t = 0; t < TILES; ++t) {
                     Frag b[RAW];
                     frags_cols<RAW, LD>(b, kt, PLANE, ks * 32, col0 + t * 16, lane);
-                    // (F is zero above the diagonal.  With a branch that leaves those products out, the compiler of this version read results of fp32's 64-wide keys
-                    // two instructions behind the matrix instruction that forms them, over the branch, without the wait that they take.)
+                    // (F is zero above the diagonal: of those products nothing comes, but they go without a branch)
                     mma<INNER, RAW>(gq[t], a, b);
                     mma<INNER, RAW>(gk[t], b2, b);
                 }
@@ -463,6 +464,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                     mma<INNER, RAW>(gk[t], a, b);
                 }
             }
+            settled();
         }
         __syncthreads();
         if (wv == 0) {                                   // gates: a lane a token

@@ -196,6 +196,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
         times_triangle<N, false>(U, tm, f);
+        if constexpr (!MAP) settled();
         if (!MAP && s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
         v4f_t w[4][NT];
 #pragma unroll
@@ -238,6 +239,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             }
             times_triangle<N, false>(O, pm, u);
         }
+        settled();                                       // (the answers; of a map the state)
         if (odd) {
             seldom();
             const float nan = __uint_as_float(0x7fc00000u);

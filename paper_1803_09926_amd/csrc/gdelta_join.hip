@@ -93,6 +93,7 @@ __global__ __launch_bounds__(2 * KP, 1) void k_gdelta_join(GdArgs g, GdLayout l,
             ask(to + step);
             load(next, to + step);
         }
+        settled();
     }
     store(S, stop + step);
 }

@@ -168,6 +168,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             mma<RAW, RAW>(qk[n], qa[c], b);
         }
     }
+    settled();
 
     for (int hh = 0; hh < share; ++hh) {
         const int h = kh * share + hh;
@@ -284,6 +285,7 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
                 c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, -s[2], c, 0, 0, 0);
                 c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, -s[3], c, 0, 0, 0);
                 col[n] = c;
+                settled();                               // (a factor of the next block's, and behind the loop's end)
             }
             // (the diagonal blocks that others read are not written here)
 #pragma unroll

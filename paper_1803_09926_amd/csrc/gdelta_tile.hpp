@@ -88,6 +88,16 @@ template <int PA, int PB, int NA, int NB> __device__ __forceinline__ void mma(v4
             if (i + j < ORDER) c = mfma(a[i], b[j], c);
 }
 
+// The hardware does not hold back what reads a matrix instruction's result, or writes over it, before it is there: 8 steps behind one of bf16, 10 behind one of fp32.  The compiler keeps
+// them within straight code, but has left some out where branches lay between (and tests/test_matrix_waits.py counts them in what it made).  So where a branch lies between such an
+// instruction and the first use of its result, the steps are waited for here, by all that comes behind.
+__device__ __forceinline__ void settled()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 9");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // two numbers as N parts, each a pair of bf16: what is left after a part is taken is exact.  (The dot product instruction takes
 // a part out in one instruction instead of two, and no walk was faster for it.)
 template <int N> __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[N])
