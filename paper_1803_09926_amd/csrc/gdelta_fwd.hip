@@ -132,32 +132,6 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
         }
         __syncthreads();
         if (!MAP && s.S) store_tiles<NT, KP / 16>(S, s.S + where * (l.state / 4), l.VP, cols);
-        // What is not finite in v, or the first key or gate that is not: from there on the column is, and before it nothing is of it.
-        float probe = 0.f;
-#pragma unroll
-        for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) probe = fmaf(v[mt][r].at(nt), 0.f, probe);
-        int from[NT];
-        const bool odd = __any(bad < CHUNK || probe != 0.f);
-        if (odd) {
-            seldom();
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                from[nt] = bad;
-#pragma unroll
-                for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (!finite(v[mt][r].at(nt))) from[nt] = min(from[nt], row_of(mt, r));
-                const int up = __shfl_xor(from[nt], 16, 64);
-                from[nt] = min(from[nt], up);
-                const int far = __shfl_xor(from[nt], 32, 64);
-                from[nt] = min(from[nt], far);
-            }
-        }
         v4f_t R[4][NT];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
@@ -178,15 +152,15 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
                 R[mt][nt] = times(x - times(R[mt][nt], read), beta);
             }
         }
+        // The first key or gate that is not finite, or the first number here that is not (of a value, or of a state that has grown): from there on the column is, and before it
+        // nothing is of it.
+        int from[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) from[nt] = bad;
+        const bool odd = __any(bad < CHUNK || not_finite(R));
         if (odd) {
             seldom();
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (row_of(mt, r) >= from[nt]) R[mt][nt][r] = 0.f;
+            rows_before(R, from);
         }
         Frag f[2][NT][N];
         split_rows<N, NT>(R, f);
@@ -196,8 +170,16 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) U[mt][nt] = v4f_t{0.f, 0.f, 0.f, 0.f};
         times_triangle<N, false>(U, tm, f);
-        if constexpr (!MAP) settled();
-        if (!MAP && s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
+        bool over = odd;
+        if constexpr (!MAP) {
+            settled();
+            if (s.U) store_tiles<NT, 4>(U, s.U + where * (l.rows / 4), l.VP, cols);
+            if (__any(not_finite(U))) {
+                seldom();
+                over = true;
+                rows_before(U, from);
+            }
+        }
         v4f_t w[4][NT];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
@@ -240,7 +222,7 @@ __global__ __launch_bounds__(THREADS, (NT == 1 && KP <= (WHOLE ? 128 : 64) && Pa
             times_triangle<N, false>(O, pm, u);
         }
         settled();                                       // (the answers; of a map the state)
-        if (odd) {
+        if (over) {
             seldom();
             const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll

@@ -52,6 +52,23 @@ __device__ __forceinline__ double sum_up_to(float x)
     return v + lane_move64<0x143, 0xc>(v);        // the second row's to the upper half
 }
 
+// Where decays grow: the first token at which neighbouring ones' logarithms, up to its own, add up to so much that the exponential passes fp32, alone or times the inverse of a
+// key's or query's length (`inverse`; the largest counts).  It counts as not finite: an infinity in the chunk's matrices would reach the tokens before it.
+__device__ __forceinline__ int grown_from(double G, float inverse)
+{
+    asm volatile("");                                    // (hardly ever taken: it stays a branch)
+    const int lane = threadIdx.x & 63;
+    double least = __shfl_up(G, 1, 64);                  // of the sums before the token
+    if (lane == 0) least = 0.0;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        least = fmin(least, __shfl_up(least, off, 64));  // (below `off` lanes one's own)
+        inverse = fmaxf(inverse, __shfl_xor(inverse, off, 64));
+    }
+    const uint64_t grown = __ballot(G - least > 88.0 - (double)logf(fmaxf(inverse, 1.f)));
+    return grown ? __ffsll((unsigned long long)grown) - 1 : 64;
+}
+
 // the parts of an fp32 matrix in LDS, into memory: a lane a piece of 16 bytes, four numbers and the four 16 columns on
 __device__ __forceinline__ void put_matrix(const float *f, char *to)
 {
@@ -185,9 +202,14 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
                 beta = gd_rate(g, gate_b.at(0));
             }
             const uint64_t bad = __ballot(!finite(d) || !finite(beta) || bads[lane] != 0);
-            const int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
+            int bad_from = bad ? __ffsll((unsigned long long)bad) - 1 : 64;
             if (lane >= bad_from) d = beta = 0.f;
-            const double G = sum_up_to(d);
+            double G = sum_up_to(d);
+            if (__any(d > 0.f)) {
+                bad_from = min(bad_from, grown_from(G, fmaxf(rks[lane], fabsf(g.scale) * rqs[lane])));
+                if (lane >= bad_from) d = beta = 0.f;
+                G = sum_up_to(d);
+            }
             Gs[lane] = G;                                // (who reads the head before's is behind two barriers)
             betas[lane] = beta;
             reinterpret_cast<double *>(vec + VEC_G * 64)[lane] = G;
@@ -232,7 +254,8 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = wv * 16 + 4 * q4 + r;
-                    const float e = exp2_fast((float)(gi[r] - gj) * LOG2E) * kj, p = qi[r] * e * qk[n][r], x = bi[r] * ki[r] * e * kk[n][r];
+                    // (first what the lengths make of the products: of short keys and queries they are small)
+                    const float e = exp2_fast((float)(gi[r] - gj) * LOG2E) * kj, p = qi[r] * qk[n][r] * e, x = bi[r] * ki[r] * kk[n][r] * e;
                     pv[n][r] = diagonal && i < j ? 0.f : p;
                     L[i * LDF + j] = diagonal && i <= j ? 0.f : x;
                 }

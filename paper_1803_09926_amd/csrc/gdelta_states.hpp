@@ -104,6 +104,40 @@ template <int N, int NT> __device__ __forceinline__ void split_rows(const v4f_t 
         for (int nt = 0; nt < NT; ++nt) split_tiles<N>(x[2 * ks][nt], x[2 * ks + 1][nt], f[ks][nt]);
 }
 
+// Whether some of a lane's numbers are not finite
+template <int NT> __device__ __forceinline__ bool not_finite(const v4f_t (&x)[4][NT])
+{
+    float probe = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) probe = fmaf(x[mt][nt][r], 0.f, probe);
+    return !(probe == 0.f);
+}
+// Zeros from a column's first row on that is not finite, or from `from` on where that comes before; `from` becomes the one of the two
+template <int NT> __device__ __forceinline__ void rows_before(v4f_t (&x)[4][NT], int (&from)[NT])
+{
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!finite(x[mt][nt][r])) from[nt] = min(from[nt], row_of(mt, r));
+        const int up = __shfl_xor(from[nt], 16, 64);
+        from[nt] = min(from[nt], up);
+        const int far = __shfl_xor(from[nt], 32, 64);
+        from[nt] = min(from[nt], far);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (row_of(mt, r) >= from[nt]) x[mt][nt][r] = 0.f;
+    }
+}
+
 // Products with operands out of LDS.  (Operands read by eight and sixteen ahead of their use were no faster than what the compiler orders: the walks are bound by the reads
 // themselves and by vector instructions.)
 // c += A B: A the 64 rows of a tile of KP columns, B the state's operands
