@@ -7,7 +7,7 @@
 //   dbeta[i] = X[i].V[i] - exp(G[i]) k[i].(S X[i]) - sum_j E (X U^T)[i,j] k[i].k[j]
 //   the gradient of the logarithm of token t's decay: the sum of what has passed it, exp(G_end) dS.S, all that tokens i >= t read of S, all that tokens j < t write for
 //           the chunk's end, and F * QK^T + M * KK^T over i >= t > j.  No term is in it that does not carry the decay: none cancel, however small it is.
-// One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens (of 256-wide keys 128 columns).  What is contracted over V
+// One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens, of keys wider than 32 half of the columns.  What is contracted over V
 // is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 129 us (with products of keys and queries
 // before it, and one tile for both, 146; with blocks of columns in one place 138).
 #include "gdelta_tile.hpp"
@@ -69,7 +69,8 @@ __device__ __forceinline__ float sum_up_to(float v)
     return v + lane_move_rows<0x143, 0xc>(v);     // the second row's to the upper half
 }
 
-template <typename T, int KP, bool WHOLE, bool VALUES>
+// WHOLE: eight columns of keys, queries, values and answers are there or not, and aligned
+template <typename T, int KP, bool WHOLE>
 __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP <= 32 ? 2 : 1)) void k_gdelta_bwd_rows(GdArgs g, GdLayout l, GdSpace s, const T *__restrict__ dy, T *__restrict__ dq,
                                                                              T *__restrict__ dk, T *__restrict__ da, T *__restrict__ db, unsigned first)
 {
@@ -117,7 +118,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
     const int vrow = threadIdx.x % 256 / (VB / 8), vcol = threadIdx.x % (VB / 8) * 8;
     const bool takes_x = HALVES == 1 || wv < 4, takes_u = HALVES == 1 || wv >= 4;
     u4t_t sa[PER][2], sb[PER][2], w8[BOTH][2];       // w8: X and U,
-    Ahead<T, 8, VALUES> t8[BOTH];                    // t8: V and dY, of both or one of each pair
+    Ahead<T, 8, WHOLE> t8[BOTH];                    // t8: V and dY, of both or one of each pair
     auto ask = [&](int v0) {
         const BufView view_s(sp, (uint32_t)l.state), view_d(dsp, (uint32_t)l.state);
 #pragma unroll
@@ -208,7 +209,7 @@ __global__ __launch_bounds__((Back<T, KP>::THREADS), (PartsOf<T>::RAW == 1 && KP
                 float x[8];
                 eight(w8[AT_M], x);
                 put8<INNER, LDV>(ut, PLANE_V, vrow, vcol, x);
-                put8_ahead<T, LDV, VALUES>(yt, PLANE_V, vrow, vcol, t8[AT_M]);
+                put8_ahead<T, LDV, WHOLE>(yt, PLANE_V, vrow, vcol, t8[AT_M]);
             }
             if (v0 + VB < l.VP) ask(v0 + VB);
             else {
@@ -565,7 +566,7 @@ hipError_t launch(const GdArgs &g, const GdLayout &l, const GdSpace &s, const vo
     static_assert(C::LDS <= 160 * 1024, "LDS of a compute unit");
     const int v = 16 / (int)sizeof(T);
     const bool values = g.V % 8 == 0 && !unaligned16(g.v) && !unaligned16(dy) && (g.T < 2 || (g.v_stride % v == 0 && g.y_stride % v == 0));
-    const auto kernel = whole_keys<T>(g) && values ? k_gdelta_bwd_rows<T, KP, true, true> : k_gdelta_bwd_rows<T, KP, false, false>;
+    const auto kernel = whole_keys<T>(g) && values ? k_gdelta_bwd_rows<T, KP, true> : k_gdelta_bwd_rows<T, KP, false>;
     const hipError_t e = gd_lds(kernel, C::LDS);
     if (e != hipSuccess) return e;
     return gd_launches(l.chunks, C::THREADS, [&](long long first, unsigned now) {
