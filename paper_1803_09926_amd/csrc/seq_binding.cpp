@@ -9,8 +9,8 @@ namespace {
 
 enum Op { LNORM, CCONV, SSCAN, GDELTA, HNORM, RNORM, OPS };
 enum Type { STORED, F32, I32, BYTES };
-// Sizes of a descriptor that operands refer to: rows of a width and a stride, or a number of elements (BYTES: at least)
-struct Sizes { int64_t T; int64_t width[6], stride[6]; int64_t flat[6]; at::ScalarType stored; };
+// Sizes of a descriptor that operands refer to: rows of a width and a stride, or a number of elements (BYTES: what the library says that `kept` needs)
+struct Sizes { int64_t T; int64_t width[6], stride[6]; int64_t flat[5]; at::ScalarType stored; };
 struct Field { int at; Type type; bool rows; int size; };   // its place in the struct of tensors; size: an index into width and stride, or into flat
 
 #define AT(S, F) (int)(offsetof(S, F) / sizeof(void *))
@@ -37,19 +37,19 @@ const Entry ENTRIES[] = {
                                   K(y, STORED, true, 1), STOP}},
     {"sscan_fwd", SSCAN, true, {S(x, STORED, true, 0), S(dt, STORED, true, 1), S(A, F32, false, 0), S(B, STORED, true, 3), S(C, STORED, true, 4),
                                 S(D, F32, false, 1), S(z, STORED, true, 2), S(dt_bias, F32, false, 1), S(starts, I32, false, 2), S(init, F32, false, 3),
-                                S(y, STORED, true, 5), S(final, F32, false, 3), S(kept, BYTES, false, 5), STOP}},
+                                S(y, STORED, true, 5), S(final, F32, false, 3), S(kept, BYTES, false, 0), STOP}},
     {"sscan_bwd", SSCAN, true, {S(x, STORED, true, 0), S(dt, STORED, true, 1), S(A, F32, false, 0), S(B, STORED, true, 3), S(C, STORED, true, 4),
                                 S(D, F32, false, 1), S(z, STORED, true, 2), S(dt_bias, F32, false, 1), S(starts, I32, false, 2), S(init, F32, false, 3),
-                                S(kept, BYTES, false, 5), S(dy, STORED, true, 5), S(dx, STORED, true, 0), S(ddt, STORED, true, 1), S(dA, F32, false, 0),
+                                S(kept, BYTES, false, 0), S(dy, STORED, true, 5), S(dx, STORED, true, 0), S(ddt, STORED, true, 1), S(dA, F32, false, 0),
                                 S(dB, STORED, true, 3), S(dC, STORED, true, 4), S(dD, F32, false, 1), S(dz, STORED, true, 2), S(ddt_bias, F32, false, 1), STOP}},
     {"sscan_step", SSCAN, false, {S(x, STORED, true, 0), S(dt, STORED, true, 1), S(A, F32, false, 0), S(B, STORED, true, 3), S(C, STORED, true, 4),
                                   S(D, F32, false, 1), S(z, STORED, true, 2), S(dt_bias, F32, false, 1), S(slots, I32, false, 4), S(state, F32, false, 3),
                                   S(y, STORED, true, 5), STOP}},
     {"gdelta_fwd", GDELTA, true, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
                                   G(A, F32, false, 0), G(a_bias, F32, false, 0), G(starts, I32, false, 2), G(init, F32, false, 3), G(y, STORED, true, 5),
-                                  G(final, F32, false, 3), G(kept, BYTES, false, 5), STOP}},
+                                  G(final, F32, false, 3), G(kept, BYTES, false, 0), STOP}},
     {"gdelta_bwd", GDELTA, true, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
-                                  G(A, F32, false, 0), G(a_bias, F32, false, 0), G(starts, I32, false, 2), G(kept, BYTES, false, 5), G(dy, STORED, true, 5),
+                                  G(A, F32, false, 0), G(a_bias, F32, false, 0), G(starts, I32, false, 2), G(kept, BYTES, false, 0), G(dy, STORED, true, 5),
                                   G(dq, STORED, true, 0), G(dk, STORED, true, 1), G(dv, STORED, true, 2), G(da, STORED, true, 3), G(db, STORED, true, 4),
                                   G(dA, F32, false, 0), G(da_bias, F32, false, 0), STOP}},
     {"gdelta_step", GDELTA, false, {G(q, STORED, true, 0), G(k, STORED, true, 1), G(v, STORED, true, 2), G(a, STORED, true, 3), G(b, STORED, true, 4),
@@ -77,7 +77,7 @@ typedef size_t (*bytes_fn)(const void *);
 
 // set once by bind(), under the interpreter's lock
 void *entry_points[NENTRIES];
-constexpr const char *KEPT[2] = {"sscan_kept_bytes", "gdelta_kept_bytes"};
+constexpr const char *KEPT[2] = {"sscan_kept_bytes", "gdelta_kept_bytes"};   // of the operators that have a `kept`, the second one's GDELTA
 bytes_fn kept_bytes[2];
 PyObject *desc_type[OPS];
 constexpr size_t DESC_SIZE[OPS] = {sizeof(lnorm_desc), sizeof(cconv_desc), sizeof(sscan_desc), sizeof(gdelta_desc), sizeof(hnorm_desc), sizeof(rnorm_desc)};
@@ -103,7 +103,7 @@ bool sizes_of(Op op, const Desc &d, Sizes *s)
         if (c.T < 0 || c.H < 1 || c.K < 1 || c.K > GDELTA_MAX_K || c.V < 1 || c.V > GDELTA_MAX_V || c.key_heads < 1 || c.sequences < 1) return false;
         const int64_t keys = (int64_t)c.key_heads * c.K, values = (int64_t)c.H * c.V;
         *s = {c.T, {keys, keys, values, c.H, c.H, values}, {c.q_stride, c.k_stride, c.v_stride, c.a_stride, c.b_stride, c.y_stride},
-              {c.H, 0, (int64_t)c.sequences + 1, 0, c.T, (int64_t)kept_bytes[1](&c)}, at::kFloat};
+              {c.H, 0, (int64_t)c.sequences + 1, 0, c.T}, at::kFloat};
         if (__builtin_mul_overflow((int64_t)c.sequences * c.H, (int64_t)c.K * c.V, &s->flat[3])) return false;
         dtype = c.dtype;
     } else if (op == HNORM) {
@@ -122,7 +122,7 @@ bool sizes_of(Op op, const Desc &d, Sizes *s)
         if (c.T < 0 || c.C < 1 || c.N < 1 || c.N > SSCAN_MAX_N || c.groups < 1 || c.sequences < 1) return false;
         const int64_t shared = (int64_t)c.groups * c.N;
         *s = {c.T, {c.C, c.C, c.C, shared, shared, c.C}, {c.x_stride, c.dt_stride, c.z_stride, c.b_stride, c.c_stride, c.y_stride},
-              {(int64_t)c.C * c.N, c.C, (int64_t)c.sequences + 1, 0, c.T, (int64_t)kept_bytes[0](&c)}, at::kFloat};
+              {(int64_t)c.C * c.N, c.C, (int64_t)c.sequences + 1, 0, c.T}, at::kFloat};
         if (__builtin_mul_overflow((int64_t)c.sequences * c.C, (int64_t)c.N, &s->flat[3])) return false;
         dtype = c.dtype;
     }
@@ -179,7 +179,8 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const at::Tensor *t = plain(args[1 + i]);
         if (!t) Py_RETURN_NONE;
         if (f.type == BYTES) {
-            if (!t->is_contiguous() || (int64_t)(t->numel() * t->itemsize()) < s.flat[f.size]) Py_RETURN_NONE;
+            // (asked for here: the library works it out anew, and calls without it do not need it)
+            if (!t->is_contiguous() || (size_t)t->numel() * t->itemsize() < kept_bytes[e.op == GDELTA](&d)) Py_RETURN_NONE;
         } else {
             if (t->scalar_type() != (f.type == F32 ? at::kFloat : f.type == I32 ? at::kInt : s.stored)) Py_RETURN_NONE;
             if (f.rows ? !is_rows(*t, s.T, s.width[f.size], s.stride[f.size]) : t->numel() != s.flat[f.size] || !t->is_contiguous()) Py_RETURN_NONE;
