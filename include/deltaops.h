@@ -11,7 +11,8 @@
  * from run to run.  A workspace is scratch of one call: calls that may run at the same time, and graphs that may be replayed at the same time, need one each.
  *
  * dtype F32: all tensors are fp32.  dtype BF16: tensors marked "stored" hold bf16, everything else is fp32 (int32 for `starts` and `slots`).
- * Sums, statistics and states are held in fp32 or wider; a stored output is rounded once, to nearest-even.
+ * Sums, statistics and states are held in fp32 or wider; a stored output is rounded once, to nearest-even.  Sums of squares are fp32: where one passes its range (numbers
+ * of 1e19 and more in a row) what is divided by its root is not specified.
  */
 #ifndef DELTAOPS_H
 #define DELTAOPS_H
