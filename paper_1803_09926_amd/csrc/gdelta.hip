@@ -74,13 +74,14 @@ size_t backward_bytes(const gdelta_desc *d, const GdLayout &l)
     return (size_t)l.chunks * d->H * (size_t)(l.state + l.rows) + (size_t)l.pieces * d->H * (size_t)l.state + round16((size_t)l.chunks * d->H * 2 * sizeof(float));
 }
 
-// How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole: the least of an estimated time, in us.  Of 128-wide keys in bf16 a chunk
-// of a walk takes 3.8 us and of a piece and its map 5.5 together, both where a compute unit has one block; each more takes 2 us a chunk of each pass; the two passes begin with
-// another chunk's time and 4 us; a piece in the join takes 2.7.  Narrower keys take less of it, by 64 the share of 0.78, wider ones and fp32 more (1.45; 1.75, of wide keys, which spill, 3).
+// How many chunks a piece of a sequence has that is walked beside others, 0 where sequences are walked whole: the least of an estimated time.  The estimate's unit is such that a chunk of a
+// walk of 128-wide keys in bf16 takes 3.8 (5.5 us measured), of a piece and its map 5.5 together, both where a compute unit has one block; each more takes 2 a chunk of each pass; the two passes
+// begin with another chunk's time and 4; a piece in the join takes 2.7.  Narrower keys take less of it, by 64 the share of 0.78, wider ones and fp32 more (1.45; 1.75, of wide keys, which spill, 3).
 // Lengths that are not known here are taken to be those that points cut at random out of T: the longest is 0.6 + ln n times their mean, and nothing is left idle at the end of a round
-// of blocks.  Measured, whole and in pieces: 16384 tokens of 16 heads of 128 x 128 in one sequence 951 us and 283, of 4 heads 893 and 165, 1000 tokens of 8 heads 67 and 48, in fp32 of 4 heads of 256 x 256 322 and 157;
-// 24 prompts of 2 to 2000 tokens, 16 heads of 64 x 128, 226 and 190; forward and backward of 5 prompts in 1501 tokens, 6 heads of 40 x 56 in fp32, 190 and 135.  Whole, as it should
-// be: 8 sequences of 1024 tokens, 8 heads, forward and backward 344 and 361; 64 prompts of 256 tokens at the mean 163 and 183; 301 tokens 24 and 26.
+// of blocks.  Measured, us, whole and in pieces: 16384 tokens of 16 heads of 128 x 128 in one sequence 1400 and 375, of 4 heads 1275 and 200, 1000 tokens of 8 heads 92 and 58, in fp32 of 4 heads of
+// 256 x 256 335 and 158; 24 prompts of 2 to 2000 tokens, 16 heads of 64 x 128, 253 and 250; forward and backward of 5 prompts in 1501 tokens, 6 heads of 40 x 56 in fp32, 189 and 133.  Whole, as it
+// should be: 8 sequences of 1024 tokens, 8 heads, forward and backward 345 and 361; 64 prompts of 256 tokens at the mean 185 and 204.  Of 29 sizes of both types the choice took 5 % more than the
+// best of 17 lengths in the geometric mean, and where it is furthest off, 900 tokens in 3 sequences of 6 heads of 64 x 64, 57 for 38.
 int piece_of(const gdelta_desc *d, const GdLayout &l, bool packed)
 {
     const char *const forced = tune_env("DWCONV_TUNE_GDELTA_PIECE");

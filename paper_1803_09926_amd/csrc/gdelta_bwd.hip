@@ -5,7 +5,7 @@
 //   dS = exp(G_end) dS + (scale exp(G) * Q)^T dY - (exp(G) * K)^T dV
 // MAP: what a piece of a sequence makes of a gradient of zero (gdelta_launch.hpp); the map's matrix is the forward one's, transposed.
 // X and the dS behind the chunk are what the gradients of keys, queries and gates take (gdelta_bwd_rows.hip), for all chunks at once.
-// Bound as the walk forward is: 8 x 1024 tokens of 8 heads of 128 x 128 in bf16 98 us.
+// Bound as the walk forward is: 8 x 1024 tokens of 8 heads of 128 x 128 in bf16 96 us.
 #include "gdelta_states.hpp"
 
 namespace dwc {

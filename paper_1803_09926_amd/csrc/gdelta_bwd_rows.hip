@@ -8,8 +8,8 @@
 //   the gradient of the logarithm of token t's decay: the sum of what has passed it, exp(G_end) dS.S, all that tokens i >= t read of S, all that tokens j < t write for
 //           the chunk's end, and F * QK^T + M * KK^T over i >= t > j.  No term is in it that does not carry the decay: none cancel, however small it is.
 // One block a chunk and key head: the value heads that share it are added up in registers, in turn.  A wavefront has 16 tokens, of keys wider than 32 half of the columns.  What is contracted over V
-// is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 129 us (with products of keys and queries
-// before it, and one tile for both, 146; with blocks of columns in one place 138).
+// is read in blocks of 32 columns, keys and queries behind it, asked for in its last block.  8192 tokens of 8 heads of 128 x 128 in bf16: 131 us (with products of keys and queries
+// before it, and one tile for both, 17 more; with blocks of columns in one place 9 more).
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 

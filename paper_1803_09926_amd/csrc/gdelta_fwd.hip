@@ -4,8 +4,8 @@
 // Of each chunk, with the first pass's T and P and the state S before it,
 //   U = T (beta * (V - exp(G) * K S)),  Y = scale exp(G) * Q S + P U,  S = exp(G_end) S + (exp(G_end - G) * K)^T U
 // all as products on the matrix cores: S, V, U and Y never leave the registers, as a result tile is an operand as it lies; K, Q, T and P go through LDS, and the next ones
-// are on their way from memory meanwhile.  Bound by the way through a chunk, K S, T, K^T U, each of whose results is split and handed on: 128 x 128 in bf16 5.8 us a chunk where a
-// compute unit has one block, 4.1 where it has two; 8 x 1024 tokens of 8 heads 94 us.  (K S and Q S at once, behind one pair of barriers, 105 us.)
+// are on their way from memory meanwhile.  Bound by the way through a chunk, K S, T, K^T U, each of whose results is split and handed on: 128 x 128 in bf16 6.2 us a chunk where a
+// compute unit has one block, 4.6 where it has two; 8 x 1024 tokens of 8 heads 100 us.  (K S and Q S at once, behind one pair of barriers, took 12 % more.)
 //
 // MAP: the map of a piece of a sequence instead (gdelta_launch.hpp).  What it makes of zero (of the state that the sequence begins with, in the first piece) is the walk without
 // answers, and its matrix is what the walk without values makes of the K unit vectors: K columns more.

@@ -3,8 +3,8 @@
 // A piece makes M S + N of the state S before it; N lies in `ends`, M in `maps`.  A block has 16 columns of a sequence's head and goes from piece to piece:
 // S <- M S + N, each S put in the place of the N that it is added to; backward S <- M^T S + N from the last piece to the first.  A wavefront has 32 rows: of the matrix
 // it reads its own straight into operands, the next piece's on their way meanwhile, and its rows of S it hands to the others through LDS as operands, which they are as they
-// lie.  Bound by the way round: 15 pieces of 128 x 128 in 16 heads 42 us, where blocks of 64 columns that staged the matrix in LDS took 54.
-// (Two pieces' matrices on their way instead of one: 54.)
+// lie.  Bound by the way round: 15 pieces of 128 x 128 in 16 heads 45 us, where blocks of 64 columns that staged the matrix in LDS took
+// 54.  (Two pieces' matrices on their way instead of one: 54.)
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 

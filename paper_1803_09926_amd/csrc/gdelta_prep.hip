@@ -6,7 +6,7 @@
 //
 // One block of four wavefronts a chunk and key head; the products of q and k are taken once and serve all value heads.  T by blocks of 16: the four on the
 // diagonal by substitution, and each column of blocks below by products with the fp32 matrix instruction, a wavefront each.  Bound by vector instructions, then by what it writes:
-// 16384 tokens of 16 heads of 128 wide keys in bf16 52 us (135 MB written), 16383 tokens of 16 heads with keys of their own of 64 51 us.
+// 16384 tokens of 16 heads of 128 wide keys in bf16 54 us (160 MB written), 16383 tokens of 16 heads with keys of their own of 64 58 us.
 #include "gdelta_tile.hpp"
 #include "gdelta_launch.hpp"
 

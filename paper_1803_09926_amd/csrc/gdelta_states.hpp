@@ -223,8 +223,8 @@ __device__ __forceinline__ Stretch stretch_of(const GdArgs &g, const GdLayout &l
 }
 
 // Whether a wavefront has 32 columns instead of 16: twice the products of what is read from LDS.  In fp32 with keys of up to 64, where that still fills the card (8192 tokens of 32
-// sequences, 16 heads of 64 x 128: 118 us, with 16 columns 136; forward and backward of half of them 271 and 285).  In bf16, whose tiles have a part instead of three, more
-// blocks are worth as much or more (16384 tokens of 64 sequences, 16 heads of 128 x 128: 223 and 201; of 64 x 128 122 both), and so they are with keys of up to 32 (88 and 82);
+// sequences, 16 heads of 64 x 128: 120 us, with 16 columns 136; forward and backward of half of them 266 and 285).  In bf16, whose tiles have a part instead of three, more
+// blocks are worth as much or more (16384 tokens of 32 sequences, 16 heads of 128 x 128: 221 and 202; of 64 x 128 171 and 159), and so they are with keys of up to 32 (fp32 97 and 90);
 // wider ones have no registers for it.
 template <typename T, int KP> constexpr bool may_have_two_tiles = sizeof(T) == 4 && KP == 64;
 inline bool two_tiles(const GdArgs &g, const GdLayout &l) { return l.VP > 64 && !l.piece && (long long)g.sequences * g.H * cdiv(l.VP, 128) >= 256; }
