@@ -35,10 +35,11 @@ extern "C" {
  * zero, where the sequence is empty).  init is a constant of the backward pass.  g is taken as -256 where it is less: its decay is zero in fp32 long before.
  * A number that is not finite leaves the outputs of its head before its token, of the other heads, and of other sequences as they were; which of the head's outputs from
  * its token on are not finite is not specified.  The same holds for the gradients of other sequences, and of heads of other key heads.
- * Decays may grow (with A > 0, or without softplus): over any run of neighbouring tokens of a sequence g may add up to 87 - ln(max(r, 1000)), which is 80, or less where keys are
- * very short: r is the largest of 1 / |k| and |scale| / (|q| |k|), with |x| = sqrt(sum x^2 + eps) (without norm r is 1).  Where it adds up to more, the head's answers from that run's
- * end on, the sequence's `final` and its gradients may be NaN though the formula's numbers are finite.  Answers before that, or before the first number that passes fp32, other heads
- * and other sequences keep their bits.  What decays by more than e^-87 over a run of tokens may count as nothing, however large it was.  gdelta_step has neither bound.
+ * Decays may grow (with A > 0, or without softplus): over any run of neighbouring tokens of a sequence g may add up to 87 - ln(max(r, 1000)), which is 80, or less where r is over
+ * 1000: with norm the largest of 1 / |k| and |scale| / (|q| |k|), where |x| = sqrt(sum x^2 + eps), without it the largest of |scale|, |scale| |q| |k| and |beta| |k|^2.  Where it adds up
+ * to more, the head's answers from that run's end on, the sequence's `final` and its gradients may be NaN though the formula's numbers are finite.  Answers before that, or before the
+ * first number that passes fp32, other heads and other sequences keep their bits.  What decays by more than e^-87 over a run of tokens may count as nothing, however large it was.
+ * gdelta_step has neither bound.
  *
  * T / 64 + sequences must be less than 2^31.  What is computed between tokens holds 24 bits with bf16 tensors too, and y has the same bits whatever else a call is
  * asked for.  A backward pass takes `starts` where its forward pass did, with the same values, and the same value of DWCONV_TUNE_GDELTA_PIECE (the chunks of 64 tokens
