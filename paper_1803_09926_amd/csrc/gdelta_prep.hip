@@ -206,7 +206,8 @@ __global__ __launch_bounds__(THREADS) void k_gdelta_prep(GdArgs g, char *__restr
             if (lane >= bad_from) d = beta = 0.f;
             double G = sum_up_to(d);
             if (__any(d > 0.f)) {
-                bad_from = min(bad_from, grown_from(G, fmaxf(rks[lane], fabsf(g.scale) * rqs[lane])));
+                const float ask = fabsf(g.scale) * rqs[lane];        // (infinite where a query has no length: then its own answer alone is not finite)
+                bad_from = min(bad_from, grown_from(G, fmaxf(rks[lane], finite(ask) ? ask : 0.f)));
                 if (lane >= bad_from) d = beta = 0.f;
                 G = sum_up_to(d);
             }

@@ -3,8 +3,8 @@
 // A block of 256 lanes holds 32 columns of one head's state in registers: eight lanes of four columns by 32 lanes of every 32nd row.  All that a token asks of the
 // state is taken in one round: q^T S and k^T S of each column, and q.k, q.q, k.k, so that
 //   u = beta (v - d rk k^T S),  y = scale rq (d q^T S + rk (q.k) u),  S = d S + rk k u^T        (d: the decay, rq and rk: one over the lengths)
-// and the state is read once and written once.  Bound by its way through memory: 64 rows of 8 heads of 128 x 128 in bf16 15.7 us, 67 MB, 4.3 TB/s, in fp32 14.2 us, 4.7 TB/s, with three sets of
-// states in turn (with one, which stays in the cache, 13.4 and 12.3); 128 rows of 16 heads of 64 x 64 16.7 and 16.3.  (Held to 64 registers a lane it spills.)
+// and the state is read once and written once.  Bound by its way through memory: 64 rows of 8 heads of 128 x 128 in bf16 15.7 us, 67 MB, 4.3 TB/s, in fp32 14.5 us, 4.6 TB/s, with three sets of
+// states in turn (with one, which stays in the cache, 13.4 and 12.5); 128 rows of 16 heads of 64 x 64 16.8 and 16.4.  (Held to 64 registers a lane it spills.)
 #include "gdelta.hpp"
 #include "gdelta_launch.hpp"
 #include <type_traits>

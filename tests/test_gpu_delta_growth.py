@@ -94,6 +94,28 @@ def test_what_is_behind_the_bound_does_not_reach_what_was_before(gpu_lib, dtype,
         assert np.array_equal(g[out], c[out])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [0.0, np.nan, np.inf])
+def test_a_query_ends_nothing_but_its_own_answer(gpu_lib, dtype, value):
+    """Without eps a query of zeros has no length: where decays grow too, its token's answer alone is not finite."""
+    m = Made(77, dtype)
+    logs = np.full(T, -0.25, np.float32)
+    logs[[40, 41, 100, 180]] = 2.0
+    x, par = _inputs(m, logs)
+    init = m.host((3, H, K, V), 0.3, stored=False)
+
+    def run():
+        y, final = Call(m, x, par, BOUNDS, softplus=False, eps=0.0).forward(init)
+        return gu.to_host(y).reshape(T, H, V), gu.to_host(final)
+
+    was, states = run()
+    assert np.isfinite(was).all() and np.isfinite(states).all()
+    x["q"][101] = value
+    y, final = run()
+    assert np.isnan(y[101]).all() and np.array_equal(final, states)
+    assert np.array_equal(np.delete(y, 101, 0), np.delete(was, 101, 0))
+
+
 def test_single_tokens_have_no_bound(gpu_lib):
     m = Made(5, "f32")
     logs = np.zeros(T, np.float32)
